@@ -93,7 +93,8 @@ def _quantise(x, dtype):
     """x [..., dh] float32 -> codes, scales: one scale per vector."""
     amax = x.abs().amax(-1).clamp_min(MIN_AMAX)
     scale = amax / QMAX[dtype]
-    y = x * (QMAX[dtype] / amax).unsqueeze(-1)
+    # (a number over a tensor would be torch's reciprocal times the number: two roundings)
+    y = x * torch.full_like(amax, QMAX[dtype]).div(amax).unsqueeze(-1)
     if dtype == "int8":
         y = y.round().clamp(-127, 127)
     else:
