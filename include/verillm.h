@@ -80,7 +80,9 @@ enum {
 enum {
     VERILLM_DEV_OK = 0,
     VERILLM_DEV_TOKEN_RANGE = 1, /* token id outside [0, vocab): clamped */
-    VERILLM_DEV_WAIT_TIMEOUT = 2 /* a pipeline wait inside a kernel gave up; results are invalid */
+    VERILLM_DEV_WAIT_TIMEOUT = 2, /* a pipeline wait inside a kernel gave up; results are invalid */
+    VERILLM_DEV_PAGE_RANGE = 3,   /* a page number outside the pool: not written, read as zeros / as some other page */
+    VERILLM_DEV_ROWS_RANGE = 4    /* cu_rows or kv_len outside what the buffers hold: bounded, or the sequence skipped */
 };
 
 enum { VERILLM_BF16 = 0, VERILLM_F32 = 1 };
@@ -284,6 +286,73 @@ int verillm_op_rmsnorm(const float *x, const void *gain, void *y, int32_t m, int
  * out: bf16 [M][n_heads*head_dim]. */
 int verillm_op_attention(const void *qkv, const int32_t *cu_seqlens, int32_t batch, int32_t max_seqlen, int32_t m,
                          int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, void *out, void *cuda_stream);
+
+/* ------------------------------------------------------------------ paged key/value cache
+ * The cache of a served model, one layer of it: pages of page_size positions in a pool, found through a table
+ * per sequence.  verillm_kv_write stores new keys and values (quantising them for the 8-bit pools), verillm_kv_read
+ * brings positions back as numbers, verillm_op_attention_paged attends from new tokens to everything a sequence has
+ * cached: a decode step (one row per sequence), drafted tokens, a chunk of a prompt, or a mixture.  A step writes
+ * its rows first and attends then.
+ *
+ * 8-bit pools hold, per (position, kv head) and separately for keys and values, the codes round(x_d * (Q / a)) (to
+ * nearest, ties to even) and the float32 scale a / Q, a = max(max_d |x_d|, 2^-110), Q = 448 (e4m3, finite codes
+ * only) or 127 (int8): they stand for code * scale.  A vector with an infinite or NaN entry gets the scale NaN and
+ * codes 0 and so stands for NaN.  Pools filled by other means hold no e4m3 NaN codes (0x7F, 0xFF) and no int8 -128. */
+enum { VERILLM_KV_BF16 = 0, VERILLM_KV_E4M3 = 1, VERILLM_KV_INT8 = 2 };
+
+typedef struct {
+    void *k, *v;               /* DEVICE [n_pages][n_kv_heads][page_size][head_dim], bf16 or 8-bit; 16-byte aligned */
+    float *k_scale, *v_scale;  /* DEVICE [n_pages][n_kv_heads][page_size]; 8-bit pools only, else NULL */
+    int32_t n_pages;
+    int32_t page_size;         /* 16, 32, 64, 128 or 256 */
+    int32_t n_kv_heads, head_dim; /* head_dim 64 or 128 */
+    int32_t dtype;             /* VERILLM_KV_* */
+} verillm_kv_cache;
+
+/* The rows of a call.  Sequence b owns the packed rows cu_rows[b] .. cu_rows[b+1]-1 (n_b of them, possibly none);
+ * row i of them is position kv_len[b] - n_b + i, i.e. the rows are the last n_b of the kv_len[b] positions that the
+ * sequence has (after this call's write).  Position p lies in row p % page_size of page
+ * page_table[b * table_width + p / page_size].  A row whose position is negative does not exist: it is not
+ * written, reads as zeros, and attends to nothing.  Rows behind the last sequence (padding of a captured batch)
+ * are left as they are.  The arrays are DEVICE memory and are read when the kernels run, so a captured graph sees
+ * their current contents; entries of the table behind a sequence's last page are never used.
+ * Pages may be shared between sequences; a position that one call writes must belong to one row only. */
+typedef struct {
+    const int32_t *page_table; /* [batch][table_width] */
+    const int32_t *cu_rows;    /* [batch + 1] */
+    const int32_t *kv_len;     /* [batch] */
+    int32_t table_width, batch;
+    int32_t n_rows;            /* rows that the packed buffers of the call hold; 0: the call does nothing */
+    int32_t max_rows;          /* at least every n_b; a sequence with more is skipped (VERILLM_DEV_ROWS_RANGE) */
+} verillm_kv_rows;
+
+/* k, v: DEVICE bf16, one row per packed row: n_kv_heads * head_dim entries, `row_stride` entries from one row to the
+ * next (e.g. the k and v columns of a fused projection); keys already rotated.  Pointers 16-byte aligned, strides
+ * multiples of 8 entries (E_SHAPE).
+ * status (all three calls): optional DEVICE word; raised from 0 to the first VERILLM_DEV_* problem met, never
+ * cleared by the call.  All three allocate nothing and are safe under stream capture. */
+int verillm_kv_write(const verillm_kv_cache *cache, const verillm_kv_rows *rows, const void *k, const void *v,
+                     int64_t row_stride, int32_t *status, void *cuda_stream);
+
+/* The mirror image: k_out, v_out receive the rows' positions as numbers, in out_dtype (VERILLM_BF16 / VERILLM_F32). */
+int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, void *k_out, void *v_out,
+                    int64_t row_stride, int32_t out_dtype, int32_t *status, void *cuda_stream);
+
+/* Causal grouped-query attention of the rows over the cache: row at position p attends to positions 0 .. p of its
+ * sequence; conventions as verillm_op_attention (scale 1/sqrt(head_dim), query head g reads kv head
+ * g * n_kv_heads / n_heads).
+ *  q         DEVICE bf16, n_heads * head_dim entries per row, q_stride entries from row to row, already rotated
+ *  out       DEVICE bf16, same form with out_stride; a row that attends to nothing receives zeros
+ *  lse       optional DEVICE float32 [n_rows][n_heads]: log of the sum of exp(scores), -inf for such a row
+ *  workspace DEVICE, 16-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code).
+ *            It holds nothing between calls, but calls that may overlap (other streams, graphs replayed side by side)
+ *            need one each.
+ * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 32 per kv head; workspace too
+ * small), E_ARCH, E_CUDA. */
+int64_t verillm_op_attention_paged_workspace(const verillm_kv_cache *cache, const verillm_kv_rows *rows, int32_t n_heads);
+int verillm_op_attention_paged(const verillm_kv_cache *cache, const verillm_kv_rows *rows, const void *q,
+                               int64_t q_stride, int32_t n_heads, void *out, int64_t out_stride, float *lse,
+                               void *workspace, int64_t workspace_bytes, int32_t *status, void *cuda_stream);
 
 /* Per-kernel timing of verify_prefill, for the roofline report (measurement aid, not part of the method).
  * While enabled, every verify_prefill call records one CUDA event after each launch on the caller's

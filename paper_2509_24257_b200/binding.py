@@ -23,7 +23,8 @@ STAT_NAMES = (
 BF16, F32 = 0, 1
 TOL_BIT_AWARE = 1
 E_INVAL, E_SHAPE, E_RANGE, E_NOMEM, E_CUDA, E_ARCH = -1, -2, -3, -4, -5, -6
-DEV_TOKEN_RANGE, DEV_WAIT_TIMEOUT = 1, 2
+DEV_TOKEN_RANGE, DEV_WAIT_TIMEOUT, DEV_PAGE_RANGE, DEV_ROWS_RANGE = 1, 2, 3, 4
+KV_BF16, KV_E4M3, KV_INT8 = 0, 1, 2
 
 EXPORTS = (
     "verillm_default_tol", "verillm_load_weights", "verillm_load_layer", "verillm_load_globals",
@@ -31,7 +32,8 @@ EXPORTS = (
     "verillm_op_rmsnorm", "verillm_op_attention", "verillm_free", "verillm_strerror",
     "verillm_last_launch_count", "verillm_profile_enable", "verillm_profile_read",
     "verillm_load_lm_head", "verillm_token_match", "verillm_verify_segment", "verillm_spot_check", "verillm_merkle_roots",
-    "verillm_threshold_sweep", "verillm_selftest_wait_timeout",
+    "verillm_threshold_sweep", "verillm_selftest_wait_timeout", "verillm_kv_write", "verillm_kv_read",
+    "verillm_op_attention_paged", "verillm_op_attention_paged_workspace",
 )
 PROF_CLASSES = ("setup", "rmsnorm", "gemm_qkv_rope", "attention", "gemm_o_resid", "gemm_gate_up_swiglu",
                 "gemm_down_resid_compare", "verdict")
@@ -70,6 +72,16 @@ class Tol(C.Structure):
 
 class ReportC(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("stats", "pos_ok", "first_bad_layer", "seq_ok", "seq_score", "hidden_out", "status")]
+
+
+class KVCacheC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [
+        (n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class KVRowsC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("page_table", "cu_rows", "kv_len")] + [
+        (n, C.c_int32) for n in ("table_width", "batch", "n_rows", "max_rows")]
 
 
 _lib: Optional[C.CDLL] = None
@@ -131,6 +143,16 @@ def lib() -> C.CDLL:
         L.verillm_op_gemm.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
         L.verillm_op_rmsnorm.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_void_p]
         L.verillm_op_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
+        cache_p, rows_p = C.POINTER(KVCacheC), C.POINTER(KVRowsC)
+        L.verillm_kv_write.argtypes = [cache_p, rows_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.verillm_kv_write.restype = C.c_int
+        L.verillm_kv_read.argtypes = [cache_p, rows_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]
+        L.verillm_kv_read.restype = C.c_int
+        L.verillm_op_attention_paged_workspace.argtypes = [cache_p, rows_p, C.c_int32]
+        L.verillm_op_attention_paged_workspace.restype = C.c_int64
+        L.verillm_op_attention_paged.argtypes = [cache_p, rows_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
+                                                 C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.verillm_op_attention_paged.restype = C.c_int
         L.verillm_profile_enable.argtypes = [C.c_void_p, C.c_int32]
         L.verillm_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_int32)]
         L.verillm_profile_enable.restype = C.c_int
@@ -490,3 +512,177 @@ def op_attention(qkv: torch.Tensor, cu_seqlens: Sequence[int], n_heads: int, n_k
         _check(lib().verillm_op_attention(qkv.data_ptr(), cu_dev.data_ptr(), len(cu) - 1, max_len, M, n_heads, n_kv_heads,
                                           head_dim, out.data_ptr(), _stream_ptr(None)), "verillm_op_attention")
     return out
+
+
+# --------------------------------------------------------------------------- paged key/value cache
+
+_KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_E4M3, torch.int8: KV_INT8}
+
+
+class KVCache:
+    """The paged cache of one layer: pools k, v [n_pages][n_kv_heads][page_size][head_dim] (bf16, float8_e4m3fn or int8)
+    and, for 8-bit pools, float32 scales [n_pages][n_kv_heads][page_size].  Wraps the caller's tensors; `alloc` makes
+    zeroed ones."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        dtype = _KV_DTYPES.get(k.dtype)
+        if dtype is None or k.dim() != 4 or v.dtype != k.dtype or v.shape != k.shape:
+            raise ValueError("k and v pools must be [n_pages][n_kv_heads][page_size][head_dim] of one type: bf16, float8_e4m3fn or int8")
+        tensors = [k, v]
+        if dtype != KV_BF16:
+            if k_scale is None or v_scale is None:
+                raise ValueError("8-bit pools need k_scale and v_scale")
+            if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
+                raise ValueError("scales must be float32 [n_pages][n_kv_heads][page_size]")
+            tensors += [k_scale, v_scale]
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("bf16 pools have no scales")
+        if not k.is_cuda or any(t.device != k.device or not t.is_contiguous() for t in tensors):
+            raise ValueError("pools and scales must be contiguous and on one CUDA device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device = k.device
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.c_struct = KVCacheC(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), self.n_pages, self.page_size,
+                                 self.n_kv_heads, self.head_dim, dtype)
+
+    @classmethod
+    def alloc(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16,
+              device: str | torch.device = "cuda:0") -> "KVCache":
+        pools = [torch.zeros(n_pages, n_kv_heads, page_size, head_dim, dtype=dtype, device=device) for _ in range(2)]
+        scales = [None, None]
+        if dtype != torch.bfloat16:
+            scales = [torch.zeros(n_pages, n_kv_heads, page_size, dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(*pools, *scales)
+
+
+class PagedRows:
+    """The rows of a paged call: int32 device tensors page_table [batch][width], cu_rows [batch+1], kv_len [batch] and
+    max_rows, at least every sequence's number of rows.  Row i of sequence b is position kv_len[b] - n_b + i of it.
+    Pass `status` (int32 [1], zeroed) to have problems that only the device can see reported there; `check` reads it."""
+
+    def __init__(self, page_table: torch.Tensor, cu_rows: torch.Tensor, kv_len: torch.Tensor, max_rows: int,
+                 status: Optional[torch.Tensor] = None):
+        for t in (page_table, cu_rows, kv_len) if status is None else (page_table, cu_rows, kv_len, status):
+            if t.dtype != torch.int32 or not t.is_cuda or t.device != page_table.device or not t.is_contiguous():
+                raise ValueError("page_table, cu_rows, kv_len and status must be contiguous int32 tensors on one CUDA device")
+        batch = kv_len.shape[0]
+        if page_table.dim() != 2 or page_table.shape[0] != batch or tuple(cu_rows.shape) != (batch + 1,) or kv_len.dim() != 1:
+            raise ValueError("page_table is [batch][width], cu_rows [batch + 1], kv_len [batch]")
+        self.page_table, self.cu_rows, self.kv_len, self.max_rows, self.status = page_table, cu_rows, kv_len, int(max_rows), status
+        self.device = page_table.device
+
+    def c_struct(self, n_rows: int) -> KVRowsC:
+        return KVRowsC(self.page_table.data_ptr(), self.cu_rows.data_ptr(), self.kv_len.data_ptr(), self.page_table.shape[1],
+                       self.kv_len.shape[0], n_rows, self.max_rows)
+
+    def check(self) -> None:
+        """Waits for the device and raises if a call reported a problem."""
+        if self.status is not None and int(self.status.item()) != 0:
+            raise RuntimeError(f"paged cache: device status {int(self.status.item())}")
+
+
+def _packed_rows(t: torch.Tensor, what: str, width: int, device: torch.device, dtypes=(torch.bfloat16,)) -> int:
+    """Row stride of a [rows][width] or [rows][heads][head_dim] tensor whose rows are contiguous."""
+    if t.dtype not in dtypes or t.device != device or t.dim() not in (2, 3):
+        raise ValueError(f"{what} must be a 2- or 3-dimensional {' / '.join(str(d) for d in dtypes)} tensor on {device}")
+    inner = t.shape[1] if t.dim() == 2 else t.shape[1] * t.shape[2]
+    packed = t.stride(-1) == 1 and (t.dim() == 2 or t.shape[1] == 1 or t.stride(1) == t.shape[2])
+    if inner != width or not packed:
+        raise ValueError(f"{what} must have {width} consecutive entries per row")
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+def _on_stream(stream: Optional[torch.cuda.Stream], device: torch.device):
+    """Makes `device`, and `stream` if one is given, current: what a call allocates then belongs to the stream it runs on."""
+    if stream is None:
+        return torch.cuda.device(device)
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the cache on {device}")
+    return torch.cuda.stream(stream)
+
+
+def kv_write(cache: KVCache, rows: PagedRows, k: torch.Tensor, v: torch.Tensor,
+             stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Stores the rows' keys and values (bf16 [n_rows][n_kv_heads * head_dim], e.g. column slices of a fused
+    projection; keys already rotated) at their positions, quantised to the cache's type."""
+    width = cache.n_kv_heads * cache.head_dim
+    stride = _packed_rows(k, "k", width, cache.device)
+    if _packed_rows(v, "v", width, cache.device) != stride or v.shape[0] != k.shape[0]:
+        raise ValueError("k and v must have the same rows and row stride")
+    if rows.device != cache.device:
+        raise ValueError("rows and cache must be on one device")
+    rc = rows.c_struct(k.shape[0])
+    with _on_stream(stream, cache.device):
+        _check(lib().verillm_kv_write(C.byref(cache.c_struct), C.byref(rc), k.data_ptr(), v.data_ptr(), stride, _ptr(rows.status),
+                                      _stream_ptr(stream)), "verillm_kv_write")
+
+
+def kv_read(cache: KVCache, rows: PagedRows, n_rows: int, dtype: torch.dtype = torch.bfloat16, out=None,
+            stream: Optional[torch.cuda.Stream] = None):
+    """(k, v) [n_rows][n_kv_heads][head_dim] in bf16 or float32: the rows' positions as numbers.  Rows behind the last
+    sequence keep what `out` (a pair of such tensors) holds; without `out` they are not defined."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be bf16 or float32")
+    if rows.device != cache.device:
+        raise ValueError("rows and cache must be on one device")
+    width = cache.n_kv_heads * cache.head_dim
+    with _on_stream(stream, cache.device):
+        if out is None:
+            out = tuple(torch.empty(n_rows, cache.n_kv_heads, cache.head_dim, dtype=dtype, device=cache.device) for _ in range(2))
+        k, v = out
+        stride = _packed_rows(k, "k", width, cache.device, (dtype,))
+        if _packed_rows(v, "v", width, cache.device, (dtype,)) != stride or k.shape[0] != n_rows or v.shape[0] != n_rows:
+            raise ValueError("out must be two tensors of n_rows rows with the same row stride")
+        rc = rows.c_struct(n_rows)
+        _check(lib().verillm_kv_read(C.byref(cache.c_struct), C.byref(rc), k.data_ptr(), v.data_ptr(), stride,
+                                     F32 if dtype == torch.float32 else BF16, _ptr(rows.status), _stream_ptr(stream)), "verillm_kv_read")
+    return k, v
+
+
+def op_attention_paged(q: torch.Tensor, cache: KVCache, rows: PagedRows, out: Optional[torch.Tensor] = None,
+                       lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Causal grouped-query attention of the rows' queries (bf16 [n_rows][n_heads * head_dim], already rotated) over
+    the cache -> bf16 [n_rows][n_heads * head_dim].  lse: optional float32 [n_rows][n_heads] that receives the log of
+    the sum of exp(scores).  workspace: optional uint8 tensor of `attention_paged_workspace` bytes to use instead of
+    allocating one for the call."""
+    n_rows = q.shape[0]
+    width = q.shape[1] if q.dim() == 2 else q.shape[1] * q.shape[-1]
+    if width == 0 or width % cache.head_dim:
+        raise ValueError("q must have n_heads * head_dim entries per row")
+    n_heads = width // cache.head_dim
+    q_stride = _packed_rows(q, "q", width, cache.device)
+    if rows.device != cache.device:
+        raise ValueError("rows and cache must be on one device")
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (n_rows, n_heads) or not lse.is_contiguous() or lse.device != cache.device):
+        raise ValueError("lse must be a contiguous float32 [n_rows][n_heads] tensor on the cache's device")
+    rc = rows.c_struct(n_rows)
+    L = lib()
+    with _on_stream(stream, cache.device):
+        if out is None:
+            out = torch.empty(n_rows, width, dtype=torch.bfloat16, device=cache.device)
+        out_stride = _packed_rows(out, "out", width, cache.device)
+        if out.shape[0] != n_rows:
+            raise ValueError("out must have as many rows as q")
+        if workspace is None:
+            need = L.verillm_op_attention_paged_workspace(C.byref(cache.c_struct), C.byref(rc), n_heads)
+            if need < 0:
+                raise VerillmError(int(need), "verillm_op_attention_paged_workspace")
+            workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+        elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != cache.device:
+            raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
+        _check(L.verillm_op_attention_paged(C.byref(cache.c_struct), C.byref(rc), q.data_ptr(), q_stride, n_heads, out.data_ptr(),
+                                            out_stride, _ptr(lse), workspace.data_ptr(), workspace.numel(), _ptr(rows.status),
+                                            _stream_ptr(stream)), "verillm_op_attention_paged")
+    return out
+
+
+def attention_paged_workspace(cache: KVCache, rows: PagedRows, n_rows: int, n_heads: int) -> int:
+    """Bytes of workspace that op_attention_paged needs for calls of up to n_rows rows."""
+    rc = rows.c_struct(n_rows)
+    with torch.cuda.device(cache.device):
+        need = lib().verillm_op_attention_paged_workspace(C.byref(cache.c_struct), C.byref(rc), n_heads)
+    if need < 0:
+        raise VerillmError(int(need), "verillm_op_attention_paged_workspace")
+    return int(need)

@@ -84,6 +84,44 @@ cudaError_t launch_attention_tc(const CUtensorMap& tmap_q, const CUtensorMap& tm
                                 int* status, int num_sms, int overlap_prologue, cudaStream_t stream);
 cudaError_t attention_tc_init();
 
+// ------------------------------------------------------------------ paged key/value cache
+// Device views of verillm_kv_cache / verillm_kv_rows (checked by the host driver).
+struct PagedCacheDev {
+    void *k, *v;               // [n_pages][n_kv_heads][page_size][head_dim]
+    float *k_scale, *v_scale;  // [n_pages][n_kv_heads][page_size], 8-bit pools only
+    int n_pages, page_shift, n_kv_heads, head_dim, dtype;
+};
+struct PagedRowsDev {
+    const int* page_table;  // [batch][table_width]
+    const int* cu_rows;     // [batch + 1]
+    const int* kv_len;      // [batch]
+    int table_width, batch, n_rows, max_rows;
+};
+cudaError_t launch_kv_write(const PagedCacheDev& c, const PagedRowsDev& r, const void* k, const void* v, long long row_stride,
+                            int* status, int num_sms, cudaStream_t stream);
+cudaError_t launch_kv_read(const PagedCacheDev& c, const PagedRowsDev& r, void* k, void* v, long long row_stride, int out_f32,
+                           int* status, int num_sms, cudaStream_t stream);
+
+struct PagedAttnParams {
+    PagedCacheDev c;
+    PagedRowsDev r;
+    const void* q;  // bf16 [n_rows][n_heads * head_dim], row stride q_stride
+    long long q_stride;
+    void* out;  // bf16, row stride out_stride
+    long long out_stride;
+    float* lse;  // optional [n_rows][n_heads]
+    int n_heads, group;
+    int tb_log;   // tokens per block, log2
+    int4* hdr;    // [grid]
+    float* part;  // [2 grid][rows][head_dim + 2]
+    int* status;
+};
+constexpr int kPagedMaxGroup = 32;  // query heads per kv head
+// Bytes of partial results and headers a launch needs; what the rule on sizes picks.
+size_t paged_attention_workspace(int head_dim, int group, int max_rows, int num_sms);
+cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_sms, cudaStream_t stream);
+cudaError_t paged_attention_init();
+
 // ------------------------------------------------------------------ small kernels
 cudaError_t launch_token_maps(const int* cu_seqlens_dev, int batch, int n_tokens, int* pos_of_token,
                               int* seq_of_token, cudaStream_t stream);

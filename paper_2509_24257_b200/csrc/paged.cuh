@@ -1,0 +1,243 @@
+// Paged key/value cache: what its kernels share.  Sequence description with its device-side checks, the walk
+// over the attention work of a batch, and the layout of the partial results of split work.
+//
+// Work of a batch: rows are packed per kv head ((token, query head of the group), token-major); a block is `tb`
+// tokens (a power of two) of one (sequence, kv head), and walks the key tiles of kTile positions up to the last
+// position one of its rows may see.  All tiles of all blocks form one line, ordered (sequence, kv head, block,
+// tile); CTA c takes tiles [c per, (c + 1) per) of that line, whatever the lengths are, which balances a batch of
+// very different lengths and splits a single long sequence over the whole GPU.  A block whose tiles lie in
+// several CTAs leaves fp32 partial results (maximum, sum, unnormalised output), at most one block that began
+// in an earlier CTA ("head" slot) and one that continues in the next ("tail" slot) per CTA; a second kernel joins
+// them in the order of the tiles, so that results do not depend on timing.
+#pragma once
+
+#include "common.cuh"
+#include "kernels.h"
+
+namespace vl {
+
+constexpr int kTile = 64;  // key positions per tile
+
+// One sequence as the device sees it: its packed rows [row0, row0 + n) and its cached positions.
+struct SeqView {
+    int row0, n, len;
+};
+
+__device__ __forceinline__ void raise_status(int* status, int code) {
+    if (status) atomicCAS(status, 0, code);
+}
+
+// Reads a sequence's description and bounds it to what the buffers hold; anything out of bounds is reported.
+__device__ __forceinline__ SeqView load_seq(const PagedRowsDev& r, int page_shift, int b, int* status) {
+    const int c0 = __ldg(r.cu_rows + b), c1 = __ldg(r.cu_rows + b + 1), len = __ldg(r.kv_len + b);
+    SeqView s;
+    s.row0 = min(max(c0, 0), r.n_rows);
+    s.n = min(max(c1, s.row0), r.n_rows) - s.row0;
+    const long long cap = static_cast<long long>(r.table_width) << page_shift;
+    s.len = len < 0 ? 0 : static_cast<int>(min(static_cast<long long>(len), cap));
+    if (c0 < 0 || c1 < c0 || c1 > r.n_rows || s.n > r.max_rows || s.len != len) raise_status(status, VERILLM_DEV_ROWS_RANGE);
+    if (s.n > r.max_rows) s.n = 0;
+    return s;
+}
+
+// Page of the sequence's position `pos`; a page outside the pool is reported and read as page 0.
+__device__ __forceinline__ int load_page(const PagedRowsDev& r, int page_shift, int n_pages, int b, int pos, int* status) {
+    const int page = __ldg(r.page_table + static_cast<size_t>(b) * r.table_width + (pos >> page_shift));
+    if (static_cast<unsigned>(page) < static_cast<unsigned>(n_pages)) return page;
+    raise_status(status, VERILLM_DEV_PAGE_RANGE);
+    return 0;
+}
+
+// sum_{y=1..z} ceil(y / 2^s)
+__host__ __device__ __forceinline__ long long sum_ceil(long long z, int s) {
+    const long long m = z >> s;
+    return ((m * (m + 1)) >> 1) * (1LL << s) + (z - (m << s)) * (m + 1);
+}
+
+// Tiles of the first m blocks of one (sequence, kv head), none of them its last: block i (from 1) ends at position
+// ctx + tb i and takes max(1, ceil((ctx + tb i) / kTile)) tiles.  With tb <= kTile, ceil((ctx + tb i) / kTile) =
+// ceil(z_i / p), p = kTile / tb, z_i = ceil(ctx / tb) + i: a sum over consecutive integers; with tb a multiple of
+// kTile the terms are an arithmetic series.
+__host__ __device__ __forceinline__ long long tiles_before(int ctx, int tb_log, long long m) {
+    constexpr int kTileLog = 6;
+    static_assert(kTile == 1 << kTileLog, "");
+    if (m <= 0) return 0;
+    if (tb_log <= kTileLog) {
+        const long long z0 = (static_cast<long long>(ctx) + (1 << tb_log) - 1) >> tb_log;  // ceil(ctx / tb)
+        if (z0 + m <= 0) return m;
+        const long long lo = z0 + 1 > 1 ? z0 + 1 : 1;  // first positive z
+        return (lo - (z0 + 1)) + sum_ceil(z0 + m, kTileLog - tb_log) - sum_ceil(lo - 1, kTileLog - tb_log);
+    }
+    const int q = 1 << (tb_log - kTileLog);
+    const long long c0 = (static_cast<long long>(ctx) + kTile - 1) >> kTileLog;
+    long long ones = c0 >= 1 ? 0 : (-c0) / q;  // i <= ones: c0 + q i <= 0, one tile each
+    if (ones > m) ones = m;
+    const long long k = m - ones;
+    return ones + k * c0 + q * ((m * (m + 1) - ones * (ones + 1)) >> 1);
+}
+
+__host__ __device__ __forceinline__ int block_count(int n, int tb_log) { return (n + (1 << tb_log) - 1) >> tb_log; }
+// Tiles of the block that ends before position `end`
+__host__ __device__ __forceinline__ int tiles_of_end(int end) { return end > kTile ? (end + kTile - 1) / kTile : 1; }
+// End position (exclusive) of block j
+__host__ __device__ __forceinline__ int block_end(const SeqView& s, int tb_log, int j) {
+    const int toks = ((j + 1) << tb_log) < s.n ? (j + 1) << tb_log : s.n;
+    return s.len - s.n + toks;
+}
+// All tiles of one (sequence, kv head)
+__host__ __device__ __forceinline__ long long tiles_of_head(const SeqView& s, int tb_log) {
+    if (s.n == 0) return 0;
+    return tiles_before(s.len - s.n, tb_log, block_count(s.n, tb_log) - 1) + tiles_of_end(s.len);
+}
+
+// The CTA's share of the line of tiles.
+struct WorkShare {
+    long long begin, end, total, per;
+    int seq;           // sequence that holds `begin`
+    long long offset;  // begin's distance from that sequence's first tile
+};
+
+// Finds the CTA's share; to be called by all `nthreads` threads (a multiple of 32, at most 1024) of the block.
+// scratch: 34 long longs + 2 in shared memory.  Ends with a barrier.
+struct ShareScratch {
+    long long warp_sum[32];
+    long long offset;
+    int seq;
+};
+__device__ __forceinline__ void find_share(const PagedRowsDev& r, int page_shift, int n_kv_heads, int tb_log, int nthreads,
+                                           int min_per, ShareScratch* sc, WorkShare& w, int* status) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps = nthreads >> 5;
+    int* st0 = blockIdx.x == 0 ? status : nullptr;  // one CTA reports
+    auto tiles = [&](int b) -> long long {
+        return b < r.batch ? tiles_of_head(load_seq(r, page_shift, b, st0), tb_log) * n_kv_heads : 0;
+    };
+    // inclusive scan over the block of one value per thread; returns the block's total
+    long long mine = 0, incl = 0;
+    auto scan = [&](long long v) -> long long {
+        incl = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long u = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += u;
+        }
+        __syncthreads();  // the previous use of warp_sum is over
+        if (lane == 31) sc->warp_sum[warp] = incl;
+        __syncthreads();
+        long long before = 0, total = 0;
+        for (int i = 0; i < nwarps; ++i) {
+            const long long s = sc->warp_sum[i];
+            before += i < warp ? s : 0;
+            total += s;
+        }
+        incl += before;
+        return total;
+    };
+    const bool one_pass = r.batch <= nthreads;
+    long long total = 0;
+    if (one_pass) {
+        mine = tiles(tid);
+        total = scan(mine);
+    } else {
+        long long v = 0;
+        for (int b = tid; b < r.batch; b += nthreads) v += tiles(b);
+        total = scan(v);
+    }
+    w.total = total;
+    long long per = (total + gridDim.x - 1) / gridDim.x;
+    if (per < min_per) per = min_per;
+    w.per = per;
+    w.begin = min(per * blockIdx.x, total);
+    w.end = min(w.begin + per, total);
+    if (w.begin < w.end) {
+        if (one_pass) {
+            if (incl - mine <= w.begin && w.begin < incl) {
+                sc->seq = tid;
+                sc->offset = w.begin - (incl - mine);
+            }
+        } else {
+            long long base = 0;
+            for (int b0 = 0; b0 < r.batch && base <= w.begin; b0 += nthreads) {
+                mine = tiles(b0 + tid);
+                const long long sum = scan(mine);
+                const long long first = base + incl - mine;
+                if (first <= w.begin && w.begin < first + mine) {
+                    sc->seq = b0 + tid;
+                    sc->offset = w.begin - first;
+                }
+                base += sum;
+            }
+        }
+    }
+    __syncthreads();
+    w.seq = sc->seq;
+    w.offset = sc->offset;
+}
+
+// Walk over the blocks of a share.  cur: the block's sequence, kv head, block number, its tiles and the part
+// [t0, t1) of them that belongs to this CTA.
+struct BlockWalk {
+    SeqView s;
+    int seq, kvh, j, tiles, t0, t1;
+    long long at;  // line position of the block's tile 0
+};
+
+// Positions the walk on the first block of a (non-empty) share.
+__device__ __forceinline__ void walk_begin(const PagedRowsDev& r, int page_shift, int tb_log, const WorkShare& w, BlockWalk& k) {
+    k.seq = w.seq;
+    k.s = load_seq(r, page_shift, k.seq, nullptr);
+    const long long per_head = tiles_of_head(k.s, tb_log);
+    k.kvh = static_cast<int>(w.offset / per_head);
+    const long long x = w.offset - per_head * k.kvh;
+    const int ctx = k.s.len - k.s.n;
+    int lo = 0, hi = block_count(k.s.n, tb_log) - 1;  // the last block that begins at or before x
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (tiles_before(ctx, tb_log, mid) <= x) lo = mid;
+        else hi = mid - 1;
+    }
+    k.j = lo;
+    k.tiles = tiles_of_end(block_end(k.s, tb_log, lo));
+    k.at = w.begin - (x - tiles_before(ctx, tb_log, lo));
+    k.t0 = static_cast<int>(w.begin - k.at);
+    k.t1 = static_cast<int>(min(static_cast<long long>(k.tiles), w.end - k.at));
+}
+
+// Moves to the next block; false at the end of the share.
+__device__ __forceinline__ bool walk_next(const PagedRowsDev& r, int page_shift, int n_kv_heads, int tb_log, const WorkShare& w,
+                                          BlockWalk& k) {
+    k.at += k.tiles;
+    if (k.at >= w.end) return false;
+    if (++k.j == block_count(k.s.n, tb_log)) {
+        k.j = 0;
+        if (++k.kvh == n_kv_heads) {
+            k.kvh = 0;
+            do {
+                k.s = load_seq(r, page_shift, ++k.seq, nullptr);
+            } while (k.s.n == 0);  // a later sequence has tiles: the share does not end here
+        }
+    }
+    k.tiles = tiles_of_end(block_end(k.s, tb_log, k.j));
+    k.t0 = 0;
+    k.t1 = static_cast<int>(min(static_cast<long long>(k.tiles), w.end - k.at));
+    return true;
+}
+
+// Partial results.  hdr[c]: {pieces, sequence, kv head, block} of the block whose first tiles CTA c holds and whose
+// last it does not (pieces 0: none).  Slot 2 c: the block that began before CTA c; slot 2 c + 1: hdr[c]'s block.
+// A slot holds `rows` maxima (log2 units, -inf: no key yet), `rows` sums, and `rows` x head_dim outputs.
+__device__ __forceinline__ float* part_slot(float* part, int slot, int rows, int dh) {
+    return part + static_cast<size_t>(slot) * rows * (dh + 2);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// weight of a partial result with maximum m in one with maximum mx >= m (both may be -inf: nothing to weigh)
+__device__ __forceinline__ float part_weight(float m, float mx) { return m == -INFINITY ? 0.f : exp2_fast(m - mx); }
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+}  // namespace vl

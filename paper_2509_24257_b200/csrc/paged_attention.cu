@@ -1,0 +1,612 @@
+// Causal grouped-query attention of new tokens over a paged cache, few rows per sequence (decode steps, drafted
+// tokens): out_r = sum_j p_j v_j scale^v_j, p = softmax_j(q_r . k_j scale^k_j / sqrt(dh)), j up to r's position.
+//
+// The work is one pass over the sequences' keys and values, bound by HBM: a cached (position, kv head) costs 4 dh
+// bytes in bf16, 2 dh + 8 in 8 bits, and meets only the few rows of its group.  So the kernel is built around
+// loads, and the products run on the warp-level tensor instructions, whose tiles fit few rows: S^T = K Q^T and
+// O^T = V^T P^T, where 16 keys (or 16 head_dim columns) fill the instruction's rows and NT blocks of 8 query rows its
+// columns.  (A 128-row tcgen05 tile would idle in 96 - 124 of its rows here and needs operands staged in shared
+// memory.)  Keys and values go from global memory straight into the operand registers, 16 bytes a lane: a lane's
+// 16 bytes are consecutive head_dim entries, and because both products sum over (or tile) head_dim in any order,
+// the order in which the fragments name them is chosen to fit the loads (Q is laid out once to match).  Each of the
+// CTA's four warps takes 16 of a tile's 64 keys and keeps its own running maximum, sum and output; they are joined
+// once per block.  8-bit codes are widened exactly to bf16 in registers (both code types fit bf16's 8 significant
+// bits); key scales multiply the scores and value scales the probabilities, both in fp32.
+//
+// The running maximum is a reference that is only raised when a score exceeds it by 2^8, as in the packed
+// attention kernel: probabilities stay below 256 and the sum divides the stale reference out.  Probabilities are
+// rounded to bf16 for the second product, everything else is fp32.
+#include "paged.cuh"
+
+namespace vl {
+
+namespace {
+
+constexpr int PR_THREADS = 128;
+constexpr int PR_WARPS = 4;
+constexpr float PR_RAISE_LOG2 = 8.f;
+
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 8 x 8 transpose of 16-bit values over the warp
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// Four codes in a word -> bf16 pairs of bytes (0, 2) and (1, 3), exactly.
+// e4m3 s eeee mmm: the 7 low bits moved to the bottom of a bf16's exponent and the top of its mantissa are the value
+// times 2^-120 (subnormal codes included), and a product with 2^120 is exact.
+// int8: 0x4300 | low 7 bits = 128 + (x & 127), and 0x4300 | sign bit = 128 or 256: their difference is x.
+template <int DTYPE>
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& even, uint32_t& odd) {
+    if (DTYPE == VERILLM_KV_E4M3) {
+        const uint32_t e = ((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u);
+        const uint32_t o = ((w >> 4) & 0x07F007F0u) | (w & 0x80008000u);
+        even = mul_bf16x2(e, 0x7B807B80u);  // 2^120
+        odd = mul_bf16x2(o, 0x7B807B80u);
+    } else {
+        const uint32_t h = w >> 8;
+        even = sub_bf16x2((w & 0x007F007Fu) | 0x43004300u, (w & 0x00800080u) | 0x43004300u);
+        odd = sub_bf16x2((h & 0x007F007Fu) | 0x43004300u, (h & 0x00800080u) | 0x43004300u);
+    }
+}
+
+// Whether one of 8 packed bf16 values is infinite or NaN, and the 8 values with those replaced by 0.
+__device__ __forceinline__ bool not_finite8(const uint4& x) {
+    const uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7F807F80u, x.y & 0x7F807F80u), __vmaxu2(x.z & 0x7F807F80u, x.w & 0x7F807F80u));
+    return (m >> 16) == 0x7F80u || (m & 0xFFFFu) == 0x7F80u;
+}
+__device__ __forceinline__ uint32_t finite2(uint32_t w) {
+    if ((w & 0x7F80u) == 0x7F80u) w &= 0xFFFF0000u;
+    if ((w & 0x7F800000u) == 0x7F800000u) w &= 0x0000FFFFu;
+    return w;
+}
+__device__ __forceinline__ uint4 finite8(const uint4& x) { return make_uint4(finite2(x.x), finite2(x.y), finite2(x.z), finite2(x.w)); }
+
+// How a warp holds 16 keys and 16 values (lane = 4 g + t).
+// Keys: lane loads 16 bytes of rows g and g + 8 per chunk; a chunk is 4 lanes x 16 bytes = 32 (bf16) or 64 (8-bit) entries.
+// Values: lane loads VB bytes of rows 2t, 2t + 1, 2t + 8, 2t + 9; the 8 lanes g cover VB * 8 bytes of a row.
+template <int DH, int DTYPE>
+struct Layout {
+    static constexpr bool BF16 = DTYPE == VERILLM_KV_BF16;
+    static constexpr int ROW_BYTES = DH * (BF16 ? 2 : 1);
+    static constexpr int KCHUNKS = ROW_BYTES / 64;
+    static constexpr int KSTEPS = DH / 16;
+    static constexpr int VPIECES = ROW_BYTES >= 128 ? ROW_BYTES / 128 : 1;  // 16-byte pieces per lane and row
+    static constexpr int VWORDS = ROW_BYTES >= 128 ? 4 : 2;                 // words per piece (8-byte pieces: 64 8-bit entries)
+    static constexpr int MT = DH / 16;                                      // m tiles of O^T
+    // the two head_dim columns a lane holds of m tile i, and i + 1 follows on in the same 16 bytes
+    static __device__ __forceinline__ int col(int i, int g) {
+        if (!BF16 && DH == 128) return 16 * g + 2 * i;
+        return (i >> 2) * 64 + 8 * g + 2 * (i & 3);
+    }
+};
+
+template <int DH, int DTYPE, int NT>
+__global__ void __launch_bounds__(PR_THREADS)
+paged_rows_kernel(const PagedAttnParams p) {
+    using L = Layout<DH, DTYPE>;
+    constexpr int RB = 8 * NT;
+    constexpr int OLD = DH + 4;  // row stride of the joined outputs in shared memory
+    extern __shared__ __align__(16) float pr_smem[];
+    float* sm_m = pr_smem;                              // [PR_WARPS][RB]
+    float* sm_l = sm_m + PR_WARPS * RB;                 // [PR_WARPS][RB]
+    float* sm_o = sm_l + PR_WARPS * RB;                 // [PR_WARPS][RB][OLD]
+    uint2* sm_q = reinterpret_cast<uint2*>(sm_o + PR_WARPS * RB * OLD);  // [NT][KSTEPS][32]
+    __shared__ ShareScratch sm_share;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const PagedCacheDev& c = p.c;
+    const int G = p.group, shift = c.page_shift, ps_mask = (1 << shift) - 1;
+
+    WorkShare share;
+    find_share(p.r, shift, c.n_kv_heads, p.tb_log, PR_THREADS, 1, &sm_share, share, p.status);
+    pdl_launch_dependents();
+    if (share.begin >= share.end) {
+        if (tid == 0) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+        return;
+    }
+    BlockWalk k;
+    walk_begin(p.r, shift, p.tb_log, share, k);
+    const float sl2 = rsqrtf(static_cast<float>(DH)) * kLog2e;
+    int4 header = make_int4(0, 0, 0, 0);
+
+    do {
+        const SeqView s = k.s;
+        const int tok0 = k.j << p.tb_log, toks = min(1 << p.tb_log, s.n - tok0);
+        const int rows = toks * G;  // <= RB
+        const int ctx = s.len - s.n;
+        const int first_pos = ctx + tok0;         // position of the block's first token
+        const int end = ctx + tok0 + toks;        // keys [0, end) are visible to some row
+        // ---- Q into fragment order: b registers of k step ks, rows 8 nt + g
+        __syncthreads();  // the previous block's rows have been read
+        for (int i = tid; i < NT * L::KSTEPS * 32; i += PR_THREADS) {
+            const int ln = i & 31, ks = (i >> 5) % L::KSTEPS, nt = i / (32 * L::KSTEPS);
+            const int r = 8 * nt + (ln >> 2), lt = ln & 3;
+            uint2 b = make_uint2(0u, 0u);
+            if (r < rows) {
+                const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.q) +
+                                           static_cast<size_t>(s.row0 + tok0 + r / G) * p.q_stride +
+                                           static_cast<size_t>(k.kvh * G + r % G) * DH;
+                if (L::BF16) {  // chunk of 32 entries = 2 steps; lane's entries 8 lt .. 8 lt + 7
+                    b = __ldg(reinterpret_cast<const uint2*>(src + (ks >> 1) * 32 + 8 * lt + 4 * (ks & 1)));
+                } else {  // chunk of 64 entries = 4 steps; lane's entries 16 lt + 4 step .. + 3, even ones first
+                    const uint2 x = __ldg(reinterpret_cast<const uint2*>(src + (ks >> 2) * 64 + 16 * lt + 4 * (ks & 3)));
+                    b = make_uint2(__byte_perm(x.x, x.y, 0x5410), __byte_perm(x.x, x.y, 0x7632));
+                }
+            }
+            sm_q[i] = b;
+        }
+        __syncthreads();
+
+        float o[NT][L::MT][4], m_ref[NT][2], l_run[NT][2];
+        int pos[NT][2];  // last visible key of this lane's rows, -1: none
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < L::MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = 8 * nt + 2 * t + h;
+                pos[nt][h] = r < rows ? first_pos + r / G : -1;
+                m_ref[nt][h] = -INFINITY;
+                l_run[nt][h] = 0.f;
+            }
+        }
+
+        uint4 ka[L::KCHUNKS], kb[L::KCHUNKS], v[L::VPIECES][4];
+        float ks0 = 1.f, ks1 = 1.f, vs0 = 1.f, vs1 = 1.f, vs0n = 1.f, vs1n = 1.f;
+        auto token_of = [&](int tile) { return tile * kTile + warp * 16; };
+        // index of (page, kv head, row in page) in units of vectors
+        auto vec_of = [&](int key) -> size_t {
+            const int page = load_page(p.r, shift, c.n_pages, k.seq, key, p.status);
+            return ((static_cast<size_t>(page) * c.n_kv_heads + k.kvh) << shift) + (key & ps_mask);
+        };
+        auto load_keys = [&](size_t vec) {
+            const char* base = reinterpret_cast<const char*>(c.k) + (vec + g) * L::ROW_BYTES + t * 16;
+#pragma unroll
+            for (int i = 0; i < L::KCHUNKS; ++i) {
+                ka[i] = __ldg(reinterpret_cast<const uint4*>(base + i * 64));
+                kb[i] = __ldg(reinterpret_cast<const uint4*>(base + 8 * L::ROW_BYTES + i * 64));
+            }
+            if (!L::BF16) {
+                ks0 = __ldg(c.k_scale + vec + g);
+                ks1 = __ldg(c.k_scale + vec + 8 + g);
+                vs0n = __ldg(c.v_scale + vec + g);
+                vs1n = __ldg(c.v_scale + vec + 8 + g);
+            }
+        };
+        auto load_values = [&](size_t vec) {
+            const char* base = reinterpret_cast<const char*>(c.v) + (vec + 2 * t) * L::ROW_BYTES + g * (4 * L::VWORDS);
+#pragma unroll
+            for (int i = 0; i < L::VPIECES; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const char* src = base + ((e & 1) + 8 * (e >> 1)) * L::ROW_BYTES + i * 128;
+                    if (L::VWORDS == 4) {
+                        v[i][e] = __ldg(reinterpret_cast<const uint4*>(src));
+                    } else {
+                        const uint2 x = __ldg(reinterpret_cast<const uint2*>(src));
+                        v[i][e] = make_uint4(x.x, x.y, 0u, 0u);
+                    }
+                }
+            }
+        };
+
+        int tile = k.t0;
+        size_t vec = 0;
+        if (token_of(tile) < end) {
+            vec = vec_of(token_of(tile));
+            load_keys(vec);
+            load_values(vec);
+        }
+        for (; tile < k.t1; ++tile) {
+            const int key0 = token_of(tile);
+            if (key0 >= end) break;  // the same for every later tile
+            const bool more = tile + 1 < k.t1 && key0 + kTile < end;
+            size_t vec_next = 0;
+            if (more) vec_next = vec_of(key0 + kTile);
+            // ---- S^T = K Q^T: 16 keys x 8 NT rows
+            float sc[NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+#pragma unroll
+            for (int i = 0; i < L::KCHUNKS; ++i) {
+                const uint32_t wa[4] = {ka[i].x, ka[i].y, ka[i].z, ka[i].w}, wb[4] = {kb[i].x, kb[i].y, kb[i].z, kb[i].w};
+                if (L::BF16) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint2 b = sm_q[(nt * L::KSTEPS + 2 * i + h) * 32 + lane];
+                            mma_bf16(sc[nt], wa[2 * h], wb[2 * h], wa[2 * h + 1], wb[2 * h + 1], b.x, b.y);
+                        }
+                } else {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        uint32_t a0, a1, a2, a3;
+                        widen4<DTYPE>(wa[w], a0, a2);
+                        widen4<DTYPE>(wb[w], a1, a3);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint2 b = sm_q[(nt * L::KSTEPS + 4 * i + w) * 32 + lane];
+                            mma_bf16(sc[nt], a0, a1, a2, a3, b.x, b.y);
+                        }
+                    }
+                }
+            }
+            const float f0 = L::BF16 ? sl2 : sl2 * ks0, f1 = L::BF16 ? sl2 : sl2 * ks1;
+            vs0 = vs0n;
+            vs1 = vs1n;
+            if (more) load_keys(vec_next);
+            // ---- mask, running maximum, probabilities
+            const bool masked = key0 + 15 > first_pos;  // some row may not see some key of the 16
+            bool raise = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                sc[nt][0] *= f0;
+                sc[nt][1] *= f0;
+                sc[nt][2] *= f1;
+                sc[nt][3] *= f1;
+                if (masked) {  // (rows past the block's last hold zeros and are not written)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (key0 + g > pos[nt][h]) sc[nt][h] = -INFINITY;
+                        if (key0 + 8 + g > pos[nt][h]) sc[nt][2 + h] = -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) raise |= fmaxf(sc[nt][h], sc[nt][2 + h]) > m_ref[nt][h] + PR_RAISE_LOG2;
+            }
+            if (__any_sync(0xFFFFFFFFu, raise)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float f[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float mx = fmaxf(sc[nt][h], sc[nt][2 + h]);
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
+                        f[h] = 1.f;
+                        if (mx > m_ref[nt][h] + PR_RAISE_LOG2) {
+                            f[h] = exp2_fast(m_ref[nt][h] - mx);  // 0 for the first keys
+                            m_ref[nt][h] = mx;
+                        }
+                        l_run[nt][h] *= f[h];
+                    }
+#pragma unroll
+                    for (int i = 0; i < L::MT; ++i) {
+                        o[nt][i][0] *= f[0];
+                        o[nt][i][1] *= f[1];
+                        o[nt][i][2] *= f[0];
+                        o[nt][i][3] *= f[1];
+                    }
+                }
+            }
+            // values behind the last visible key are whatever the page holds: make them 0
+            if (key0 + 16 > end) {
+#pragma unroll
+                for (int i = 0; i < L::VPIECES; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key0 + 2 * t + (e & 1) + 8 * (e >> 1) >= end) v[i][e] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            // An infinite or NaN value must not reach the rows that may not see its token (their probability 0 times it
+            // would be NaN): such entries are taken out of the product and added row by row.  8-bit pools carry a
+            // non-finite vector in its scale, which is masked with the probability.
+            bool stray = false;
+            if (L::BF16 && masked) {
+                bool bad = false;
+#pragma unroll
+                for (int i = 0; i < L::VPIECES; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) bad |= not_finite8(v[i][e]);
+                stray = __any_sync(0xFFFFFFFFu, bad);
+            }
+            auto add_stray = [&](int nt, const float (&e)[4]) {
+#pragma unroll 1
+                for (int kk = 0; kk < 16; ++kk) {
+                    const int src = ((kk & 7) << 2) | t;
+                    const float e0 = __shfl_sync(0xFFFFFFFFu, kk < 8 ? e[0] : e[2], src), e1 = __shfl_sync(0xFFFFFFFFu, kk < 8 ? e[1] : e[3], src);
+                    if (key0 + kk >= end) continue;  // uniform
+                    const char* base = reinterpret_cast<const char*>(c.v) + (vec + kk) * L::ROW_BYTES + g * 16;
+#pragma unroll
+                    for (int i = 0; i < L::VPIECES; ++i) {
+                        const uint4 x = __ldg(reinterpret_cast<const uint4*>(base + i * 128));
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int m = 0; m < 4; ++m)
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                const float y = half ? bf16_hi(w[m]) : bf16_lo(w[m]);
+                                if (isfinite(y)) continue;
+                                if (key0 + kk <= pos[nt][0]) o[nt][(4 * i + m) % L::MT][2 * half] += e0 * y;
+                                if (key0 + kk <= pos[nt][1]) o[nt][(4 * i + m) % L::MT][2 * half + 1] += e1 * y;
+                            }
+                    }
+                }
+            };
+            uint32_t pb[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float e[4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float ref = m_ref[nt][h] == -INFINITY ? 0.f : m_ref[nt][h];
+                    e[h] = exp2_fast(sc[nt][h] - ref);
+                    e[2 + h] = exp2_fast(sc[nt][2 + h] - ref);
+                    l_run[nt][h] += e[h] + e[2 + h];
+                }
+                if (!L::BF16) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {  // a masked key's scale may be anything: 0 stays 0
+                        e[h] = masked && key0 + g > pos[nt][h] ? 0.f : e[h] * vs0;
+                        e[2 + h] = masked && key0 + 8 + g > pos[nt][h] ? 0.f : e[2 + h] * vs1;
+                    }
+                } else if (stray) {
+                    add_stray(nt, e);
+                }
+                pb[nt][0] = transpose8(pack_bf16(e[0], e[1]));
+                pb[nt][1] = transpose8(pack_bf16(e[2], e[3]));
+            }
+            if (L::BF16 && stray) {
+#pragma unroll
+                for (int i = 0; i < L::VPIECES; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[i][e] = finite8(v[i][e]);
+            }
+            // ---- O^T += V^T P^T
+#pragma unroll
+            for (int i = 0; i < L::VPIECES; ++i) {
+                const uint32_t w0[4] = {v[i][0].x, v[i][0].y, v[i][0].z, v[i][0].w}, w1[4] = {v[i][1].x, v[i][1].y, v[i][1].z, v[i][1].w};
+                const uint32_t w2[4] = {v[i][2].x, v[i][2].y, v[i][2].z, v[i][2].w}, w3[4] = {v[i][3].x, v[i][3].y, v[i][3].z, v[i][3].w};
+#pragma unroll
+                for (int w = 0; w < L::VWORDS; ++w) {
+                    if (L::BF16) {  // a word holds two columns: one m tile
+                        const uint32_t a0 = __byte_perm(w0[w], w1[w], 0x5410), a1 = __byte_perm(w0[w], w1[w], 0x7632);
+                        const uint32_t a2 = __byte_perm(w2[w], w3[w], 0x5410), a3 = __byte_perm(w2[w], w3[w], 0x7632);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][4 * i + w], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                    } else {  // four columns: two m tiles
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t a0, a1, a2, a3;
+                            widen4<DTYPE>(__byte_perm(w0[w], w1[w], h ? 0x7632 : 0x5410), a0, a1);
+                            widen4<DTYPE>(__byte_perm(w2[w], w3[w], h ? 0x7632 : 0x5410), a2, a3);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][2 * w + h], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                        }
+                    }
+                }
+            }
+            if (more) load_values(vec_next);
+            vec = vec_next;
+        }
+
+        // ---- join the four warps: maxima and sums first, then outputs on the common reference
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l_run[nt][h] += __shfl_xor_sync(0xFFFFFFFFu, l_run[nt][h], x);
+                if (g == 0) {
+                    sm_m[warp * RB + 8 * nt + 2 * t + h] = m_ref[nt][h];
+                    sm_l[warp * RB + 8 * nt + 2 * t + h] = l_run[nt][h];
+                }
+            }
+        __syncthreads();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float f[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = 8 * nt + 2 * t + h;
+                const float mx = fmaxf(fmaxf(sm_m[r], sm_m[RB + r]), fmaxf(sm_m[2 * RB + r], sm_m[3 * RB + r]));
+                f[h] = part_weight(m_ref[nt][h], mx);
+            }
+#pragma unroll
+            for (int i = 0; i < L::MT; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *reinterpret_cast<float2*>(sm_o + (warp * RB + 8 * nt + 2 * t + h) * OLD + L::col(i, g)) =
+                        f[h] == 0.f ? make_float2(0.f, 0.f) : make_float2(o[nt][i][h] * f[h], o[nt][i][2 + h] * f[h]);
+        }
+        __syncthreads();
+
+        const bool whole = k.t0 == 0 && k.t1 == k.tiles;
+        const int slot = 2 * blockIdx.x + (k.t0 == 0 ? 1 : 0);
+        float* part = part_slot(p.part, slot, RB, DH);
+        if (!whole && k.t0 == 0)
+            header = make_int4(static_cast<int>((k.at + k.tiles - 1) / share.per) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
+        constexpr int LPR = DH / 8;  // lanes per row, 8 columns each
+        for (int r = tid / LPR; r < rows; r += PR_THREADS / LPR) {
+            const int cx = (tid % LPR) * 8;
+            float mx = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < PR_WARPS; ++w) mx = fmaxf(mx, sm_m[w * RB + r]);
+#pragma unroll
+            for (int w = 0; w < PR_WARPS; ++w) l += sm_l[w * RB + r] * part_weight(sm_m[w * RB + r], mx);
+            float acc[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < PR_WARPS; ++w)
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const float4 x = *reinterpret_cast<const float4*>(sm_o + (w * RB + r) * OLD + cx + i);
+                    acc[i] += x.x;
+                    acc[i + 1] += x.y;
+                    acc[i + 2] += x.z;
+                    acc[i + 3] += x.w;
+                }
+            if (whole) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;  // no visible key: 0
+                const int row = s.row0 + tok0 + r / G, head = k.kvh * G + r % G;
+                *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + static_cast<size_t>(row) * p.out_stride +
+                                          static_cast<size_t>(head) * DH + cx) =
+                    make_uint4(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv),
+                               pack_bf16(acc[4] * inv, acc[5] * inv), pack_bf16(acc[6] * inv, acc[7] * inv));
+                if (p.lse && cx == 0) p.lse[static_cast<size_t>(row) * p.n_heads + head] = l == 0.f ? -INFINITY : mx * kLn2 + logf(l);
+            } else {
+                if (cx == 0) {
+                    part[r] = mx;
+                    part[RB + r] = l;
+                }
+                float4* dst = reinterpret_cast<float4*>(part + 2 * RB + r * DH + cx);
+                dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+            }
+        }
+    } while (walk_next(p.r, shift, c.n_kv_heads, p.tb_log, share, k));
+    if (tid == 0) p.hdr[blockIdx.x] = header;
+}
+
+// Joins the partial results of blocks that several CTAs worked on.  One CTA per (possible) such block and group of
+// JOIN_ROWS rows; the pieces are added in the order of their tiles.
+constexpr int JOIN_THREADS = 128;
+template <int DH>
+__global__ void __launch_bounds__(JOIN_THREADS)
+paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
+    pdl_wait();
+    const int4 h = p.hdr[blockIdx.x];
+    if (h.x == 0) return;
+    constexpr int LPR = DH / 8;
+    const int r = static_cast<int>(blockIdx.y) * (JOIN_THREADS / LPR) + static_cast<int>(threadIdx.x) / LPR;
+    const SeqView s = load_seq(p.r, p.c.page_shift, h.y, nullptr);
+    const int tok0 = h.w << p.tb_log, rows = min(1 << p.tb_log, s.n - tok0) * p.group;
+    if (r >= rows) return;
+    const int cx = (threadIdx.x % LPR) * 8;
+    // piece 0 is CTA blockIdx.x's tail slot, piece i the head slot of CTA blockIdx.x + i
+    auto slot_of = [&](int i) { return part_slot(p.part, 2 * (static_cast<int>(blockIdx.x) + i) + (i == 0 ? 1 : 0), rows_per_block, DH); };
+    float mx = -INFINITY;
+#pragma unroll 8
+    for (int i = 0; i < h.x; ++i) mx = fmaxf(mx, slot_of(i)[r]);
+    float l = 0.f, acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < h.x; ++i) {
+        const float* part = slot_of(i);
+        const float w = part_weight(part[r], mx);
+        const float4* src = reinterpret_cast<const float4*>(part + 2 * rows_per_block + r * DH + cx);
+        const float4 a = src[0], b = src[1];
+        l += part[rows_per_block + r] * w;
+        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += w == 0.f ? 0.f : x[e] * w;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int row = s.row0 + tok0 + r / p.group, head = h.z * p.group + r % p.group;
+    *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + static_cast<size_t>(row) * p.out_stride + static_cast<size_t>(head) * DH + cx) =
+        make_uint4(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv), pack_bf16(acc[4] * inv, acc[5] * inv),
+                   pack_bf16(acc[6] * inv, acc[7] * inv));
+    if (p.lse && cx == 0) p.lse[static_cast<size_t>(row) * p.n_heads + head] = l == 0.f ? -INFINITY : mx * kLn2 + logf(l);
+}
+
+template <int DH, int NT>
+constexpr size_t rows_smem() {
+    return static_cast<size_t>(PR_WARPS) * 8 * NT * (2 + DH + 4) * 4 + static_cast<size_t>(NT) * (DH / 16) * 32 * 8;
+}
+
+template <int DH, int DTYPE, int NT>
+cudaError_t rows_init() {
+    return cudaFuncSetAttribute(paged_rows_kernel<DH, DTYPE, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                static_cast<int>(rows_smem<DH, NT>()));
+}
+template <int DH, int DTYPE>
+cudaError_t rows_init_all() {
+    cudaError_t e = rows_init<DH, DTYPE, 1>();
+    if (e == cudaSuccess) e = rows_init<DH, DTYPE, 2>();
+    if (e == cudaSuccess) e = rows_init<DH, DTYPE, 4>();
+    return e;
+}
+
+template <int DH, int DTYPE, int NT>
+cudaError_t rows_launch(const PagedAttnParams& p, int grid, cudaStream_t stream) {
+    paged_rows_kernel<DH, DTYPE, NT><<<grid, PR_THREADS, rows_smem<DH, NT>(), stream>>>(p);
+    return cudaGetLastError();
+}
+template <int DH, int DTYPE>
+cudaError_t rows_launch_nt(const PagedAttnParams& p, int nt, int grid, cudaStream_t stream) {
+    if (nt == 1) return rows_launch<DH, DTYPE, 1>(p, grid, stream);
+    if (nt == 2) return rows_launch<DH, DTYPE, 2>(p, grid, stream);
+    return rows_launch<DH, DTYPE, 4>(p, grid, stream);
+}
+template <int DH>
+cudaError_t rows_launch_dtype(const PagedAttnParams& p, int nt, int grid, cudaStream_t stream) {
+    if (p.c.dtype == VERILLM_KV_BF16) return rows_launch_nt<DH, VERILLM_KV_BF16>(p, nt, grid, stream);
+    if (p.c.dtype == VERILLM_KV_E4M3) return rows_launch_nt<DH, VERILLM_KV_E4M3>(p, nt, grid, stream);
+    return rows_launch_nt<DH, VERILLM_KV_INT8>(p, nt, grid, stream);
+}
+
+// Which kernel and block shape serve a call.
+struct Shape {
+    int nt, tb_log, rows_per_block, grid;
+};
+Shape shape_of(int group, int max_rows, int num_sms) {
+    Shape s;
+    const long long r = static_cast<long long>(group) * max_rows;
+    s.nt = r <= 8 ? 1 : r <= 16 ? 2 : 4;
+    s.rows_per_block = 8 * s.nt;
+    s.tb_log = 0;
+    while ((1LL << s.tb_log) < max_rows && (2LL << s.tb_log) * group <= s.rows_per_block) ++s.tb_log;
+    if ((1LL << s.tb_log) < max_rows && r <= s.rows_per_block) ++s.tb_log;  // one block holds them all
+    s.grid = num_sms * (s.nt == 1 ? 4 : s.nt == 2 ? 3 : 2);
+    return s;
+}
+size_t hdr_bytes(int grid) { return (static_cast<size_t>(grid) * sizeof(int4) + 255) & ~static_cast<size_t>(255); }
+
+}  // namespace
+
+size_t paged_attention_workspace(int head_dim, int group, int max_rows, int num_sms) {
+    const Shape s = shape_of(group, max_rows, num_sms);
+    return hdr_bytes(s.grid) + static_cast<size_t>(2) * s.grid * s.rows_per_block * (head_dim + 2) * sizeof(float);
+}
+
+cudaError_t paged_attention_init() {
+    cudaError_t e = rows_init_all<64, VERILLM_KV_BF16>();
+    if (e == cudaSuccess) e = rows_init_all<64, VERILLM_KV_E4M3>();
+    if (e == cudaSuccess) e = rows_init_all<64, VERILLM_KV_INT8>();
+    if (e == cudaSuccess) e = rows_init_all<128, VERILLM_KV_BF16>();
+    if (e == cudaSuccess) e = rows_init_all<128, VERILLM_KV_E4M3>();
+    if (e == cudaSuccess) e = rows_init_all<128, VERILLM_KV_INT8>();
+    return e;
+}
+
+cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_sms, cudaStream_t stream) {
+    const Shape s = shape_of(p.group, p.r.max_rows, num_sms);
+    p.tb_log = s.tb_log;
+    p.hdr = reinterpret_cast<int4*>(workspace);
+    p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + hdr_bytes(s.grid));
+    cudaError_t e = p.c.head_dim == 64 ? rows_launch_dtype<64>(p, s.nt, s.grid, stream) : rows_launch_dtype<128>(p, s.nt, s.grid, stream);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(s.grid, (s.rows_per_block * (p.c.head_dim / 8) + JOIN_THREADS - 1) / JOIN_THREADS);
+    cfg.blockDim = dim3(JOIN_THREADS);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return p.c.head_dim == 64 ? cudaLaunchKernelEx(&cfg, paged_join_kernel<64>, p, s.rows_per_block)
+                              : cudaLaunchKernelEx(&cfg, paged_join_kernel<128>, p, s.rows_per_block);
+}
+
+}  // namespace vl

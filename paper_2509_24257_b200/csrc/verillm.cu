@@ -121,6 +121,7 @@ int ensure_init() {
     CU_TRY(gemm_init());
     CU_TRY(attention_tc_init());
     CU_TRY(merkle_init());
+    CU_TRY(paged_attention_init());
     done[dev] = true;
     return VERILLM_OK;
 }
@@ -319,6 +320,47 @@ int ensure_decode_state(verillm_model* m) {
     if ((rc = dev_alloc(&d.mid, B * c.d_ffn))) return rc;
     if ((rc = dev_alloc(&d.ints, static_cast<size_t>(6) * c.max_tokens + 3 * static_cast<size_t>(std::max(c.max_checks, 1))))) return rc;
     d.ready = true;
+    return VERILLM_OK;
+}
+
+// Checks a paged cache and the rows of a call and converts them to the kernels' views.
+int check_paged(const verillm_kv_cache* c, const verillm_kv_rows* r, PagedCacheDev* cd, PagedRowsDev* rd) {
+    if (!c || !r || !c->k || !c->v || !r->page_table || !r->cu_rows || !r->kv_len) return VERILLM_E_INVAL;
+    if (c->dtype != VERILLM_KV_BF16 && c->dtype != VERILLM_KV_E4M3 && c->dtype != VERILLM_KV_INT8) return VERILLM_E_INVAL;
+    if (c->dtype != VERILLM_KV_BF16 && (!c->k_scale || !c->v_scale)) return VERILLM_E_INVAL;
+    if (c->n_pages < 1 || c->n_kv_heads < 1 || r->batch < 1 || r->table_width < 1 || r->n_rows < 0 || r->max_rows < 1) return VERILLM_E_INVAL;
+    if (c->head_dim != 64 && c->head_dim != 128) return VERILLM_E_SHAPE;
+    int shift = 4;
+    while (shift < 8 && (1 << shift) != c->page_size) ++shift;
+    if ((1 << shift) != c->page_size) return VERILLM_E_SHAPE;
+    // (page, kv head, row in page) is addressed as one 32-bit row number by the tile loads
+    if (static_cast<int64_t>(c->n_pages) * c->n_kv_heads * c->page_size > 0x7FFFFFFFLL) return VERILLM_E_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 15u) return VERILLM_E_SHAPE;
+    cd->k = c->k; cd->v = c->v;
+    cd->k_scale = c->dtype == VERILLM_KV_BF16 ? nullptr : c->k_scale;
+    cd->v_scale = c->dtype == VERILLM_KV_BF16 ? nullptr : c->v_scale;
+    cd->n_pages = c->n_pages; cd->page_shift = shift; cd->n_kv_heads = c->n_kv_heads; cd->head_dim = c->head_dim; cd->dtype = c->dtype;
+    rd->page_table = r->page_table; rd->cu_rows = r->cu_rows; rd->kv_len = r->kv_len;
+    rd->table_width = r->table_width; rd->batch = r->batch; rd->n_rows = r->n_rows;
+    rd->max_rows = std::min(r->max_rows, std::max(r->n_rows, 1));  // no sequence has more rows than the buffers
+    return VERILLM_OK;
+}
+// A matrix of packed rows: 16-byte accesses need its base aligned and its stride a multiple of `align` entries.
+int check_rows(const void* p, int64_t stride, int64_t width, int64_t align) {
+    if (!p) return VERILLM_E_INVAL;
+    return (reinterpret_cast<uintptr_t>(p) & 15u) || stride < width || stride % align ? VERILLM_E_SHAPE : VERILLM_OK;
+}
+int check_group(const verillm_kv_cache* c, int32_t n_heads) {
+    if (n_heads < 1) return VERILLM_E_INVAL;
+    return n_heads % c->n_kv_heads || n_heads / c->n_kv_heads > kPagedMaxGroup ? VERILLM_E_SHAPE : VERILLM_OK;
+}
+int current_sms(int* num_sms) {
+    static int sms[64] = {0};
+    int dev = 0;
+    CU_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return VERILLM_E_INVAL;
+    if (sms[dev] == 0) CU_TRY(cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev));
+    *num_sms = sms[dev];
     return VERILLM_OK;
 }
 
@@ -1031,6 +1073,63 @@ int verillm_op_attention(const void* qkv, const int32_t* cu_seqlens, int32_t bat
     CU_TRY(cudaDeviceGetAttribute(&num_sms, cudaDevAttrMultiProcessorCount, dev));
     CU_TRY(launch_attention_tc(tq, tkv, cu_seqlens, batch, max_seqlen, n_heads, n_kv_heads, head_dim, out, nullptr,
                                num_sms, 0, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int verillm_kv_write(const verillm_kv_cache* cache, const verillm_kv_rows* rows, const void* k, const void* v,
+                     int64_t row_stride, int32_t* status, void* cuda_stream) {
+    PagedCacheDev c;
+    PagedRowsDev r;
+    int rc = check_paged(cache, rows, &c, &r), sms = 0;
+    if (rc || r.n_rows == 0) return rc;
+    const int64_t width = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
+    if ((rc = check_rows(k, row_stride, width, 8)) || (rc = check_rows(v, row_stride, width, 8))) return rc;
+    if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    CU_TRY(launch_kv_write(c, r, k, v, row_stride, status, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int verillm_kv_read(const verillm_kv_cache* cache, const verillm_kv_rows* rows, void* k_out, void* v_out, int64_t row_stride,
+                    int32_t out_dtype, int32_t* status, void* cuda_stream) {
+    PagedCacheDev c;
+    PagedRowsDev r;
+    int rc = check_paged(cache, rows, &c, &r), sms = 0;
+    if (rc) return rc;
+    if (out_dtype != VERILLM_BF16 && out_dtype != VERILLM_F32) return VERILLM_E_INVAL;
+    if (r.n_rows == 0) return VERILLM_OK;
+    const int64_t width = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
+    if ((rc = check_rows(k_out, row_stride, width, 8)) || (rc = check_rows(v_out, row_stride, width, 8))) return rc;
+    if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    CU_TRY(launch_kv_read(c, r, k_out, v_out, row_stride, out_dtype == VERILLM_F32 ? 1 : 0, status, sms,
+                          reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int64_t verillm_op_attention_paged_workspace(const verillm_kv_cache* cache, const verillm_kv_rows* rows, int32_t n_heads) {
+    PagedCacheDev c;
+    PagedRowsDev r;
+    int rc = check_paged(cache, rows, &c, &r), sms = 0;
+    if (rc || (rc = check_group(cache, n_heads)) || (rc = current_sms(&sms))) return rc;
+    return static_cast<int64_t>(paged_attention_workspace(c.head_dim, n_heads / c.n_kv_heads, r.max_rows, sms));
+}
+
+int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_rows* rows, const void* q, int64_t q_stride,
+                               int32_t n_heads, void* out, int64_t out_stride, float* lse, void* workspace,
+                               int64_t workspace_bytes, int32_t* status, void* cuda_stream) {
+    PagedAttnParams p;
+    std::memset(&p, 0, sizeof(p));
+    int rc = check_paged(cache, rows, &p.c, &p.r), sms = 0;
+    if (rc || (rc = check_group(cache, n_heads)) || p.r.n_rows == 0) return rc;
+    const int64_t width = static_cast<int64_t>(n_heads) * p.c.head_dim;
+    if ((rc = check_rows(q, q_stride, width, 8)) || (rc = check_rows(out, out_stride, width, 8))) return rc;
+    if (!workspace) return VERILLM_E_INVAL;
+    if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    p.group = n_heads / p.c.n_kv_heads;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) ||
+        workspace_bytes < static_cast<int64_t>(paged_attention_workspace(p.c.head_dim, p.group, p.r.max_rows, sms)))
+        return VERILLM_E_SHAPE;
+    p.q = q; p.q_stride = q_stride; p.out = out; p.out_stride = out_stride; p.lse = lse; p.n_heads = n_heads; p.status = status;
+    CU_TRY(launch_paged_attention(p, workspace, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
     return VERILLM_OK;
 }
 
