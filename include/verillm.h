@@ -347,7 +347,7 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  *  workspace DEVICE, 16-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code).
  *            It holds nothing between calls, but calls that may overlap (other streams, graphs replayed side by side)
  *            need one each.
- * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 32 per kv head; workspace too
+ * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 128 per kv head; workspace too
  * small), E_ARCH, E_CUDA. */
 int64_t verillm_op_attention_paged_workspace(const verillm_kv_cache *cache, const verillm_kv_rows *rows, int32_t n_heads);
 int verillm_op_attention_paged(const verillm_kv_cache *cache, const verillm_kv_rows *rows, const void *q,

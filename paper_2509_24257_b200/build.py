@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libverillm.so")
-SOURCES = ["gemm_tcgen05.cu", "attention_tcgen05.cu", "elementwise.cu", "merkle.cu", "paged_kv.cu", "paged_attention.cu",
+SOURCES = ["gemm_tcgen05.cu", "attention_tcgen05.cu", "elementwise.cu", "merkle.cu", "paged_kv.cu", "paged_attention.cu", "paged_attention_tcgen05.cu",
            "verillm.cu"]
 HEADERS = ["common.cuh", "compare.cuh", "paged.cuh", "kernels.h", os.path.join("..", "..", "include", "verillm.h")]
 NVCC_FLAGS = [

@@ -116,11 +116,15 @@ struct PagedAttnParams {
     float* part;  // [2 grid][rows][head_dim + 2]
     int* status;
 };
-constexpr int kPagedMaxGroup = 32;  // query heads per kv head
+constexpr int kPagedMaxGroup = 128;  // query heads per kv head
+constexpr int kPagedTcRows = 256;    // packed rows per block of the tcgen05 kernel
 // Bytes of partial results and headers a launch needs; what the rule on sizes picks.
 size_t paged_attention_workspace(int head_dim, int group, int max_rows, int num_sms);
 cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_sms, cudaStream_t stream);
 cudaError_t paged_attention_init();
+// The kernel for many rows per sequence (one CTA per SM: grid <= SMs); called by launch_paged_attention.
+cudaError_t launch_paged_attention_tc(const PagedAttnParams& p, int grid, cudaStream_t stream);
+cudaError_t paged_attention_tc_init();
 
 // ------------------------------------------------------------------ small kernels
 cudaError_t launch_token_maps(const int* cu_seqlens_dev, int batch, int n_tokens, int* pos_of_token,

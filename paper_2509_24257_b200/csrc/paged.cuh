@@ -16,8 +16,6 @@
 
 namespace vl {
 
-constexpr int kTile = 64;  // key positions per tile
-
 // One sequence as the device sees it: its packed rows [row0, row0 + n) and its cached positions.
 struct SeqView {
     int row0, n, len;
@@ -54,22 +52,23 @@ __host__ __device__ __forceinline__ long long sum_ceil(long long z, int s) {
     return ((m * (m + 1)) >> 1) * (1LL << s) + (z - (m << s)) * (m + 1);
 }
 
+// A kernel's tiles hold 2^TL key positions (TL: template argument of what follows).
+//
 // Tiles of the first m blocks of one (sequence, kv head), none of them its last: block i (from 1) ends at position
-// ctx + tb i and takes max(1, ceil((ctx + tb i) / kTile)) tiles.  With tb <= kTile, ceil((ctx + tb i) / kTile) =
-// ceil(z_i / p), p = kTile / tb, z_i = ceil(ctx / tb) + i: a sum over consecutive integers; with tb a multiple of
-// kTile the terms are an arithmetic series.
+// ctx + tb i and takes max(1, ceil((ctx + tb i) / T)) tiles of T = 2^TL.  With tb <= T, ceil((ctx + tb i) / T) =
+// ceil(z_i / p), p = T / tb, z_i = ceil(ctx / tb) + i: a sum over consecutive integers; with tb a multiple of T
+// the terms are an arithmetic series.
+template <int TL>
 __host__ __device__ __forceinline__ long long tiles_before(int ctx, int tb_log, long long m) {
-    constexpr int kTileLog = 6;
-    static_assert(kTile == 1 << kTileLog, "");
     if (m <= 0) return 0;
-    if (tb_log <= kTileLog) {
+    if (tb_log <= TL) {
         const long long z0 = (static_cast<long long>(ctx) + (1 << tb_log) - 1) >> tb_log;  // ceil(ctx / tb)
         if (z0 + m <= 0) return m;
         const long long lo = z0 + 1 > 1 ? z0 + 1 : 1;  // first positive z
-        return (lo - (z0 + 1)) + sum_ceil(z0 + m, kTileLog - tb_log) - sum_ceil(lo - 1, kTileLog - tb_log);
+        return (lo - (z0 + 1)) + sum_ceil(z0 + m, TL - tb_log) - sum_ceil(lo - 1, TL - tb_log);
     }
-    const int q = 1 << (tb_log - kTileLog);
-    const long long c0 = (static_cast<long long>(ctx) + kTile - 1) >> kTileLog;
+    const int q = 1 << (tb_log - TL);
+    const long long c0 = (static_cast<long long>(ctx) + (1 << TL) - 1) >> TL;
     long long ones = c0 >= 1 ? 0 : (-c0) / q;  // i <= ones: c0 + q i <= 0, one tile each
     if (ones > m) ones = m;
     const long long k = m - ones;
@@ -78,16 +77,20 @@ __host__ __device__ __forceinline__ long long tiles_before(int ctx, int tb_log, 
 
 __host__ __device__ __forceinline__ int block_count(int n, int tb_log) { return (n + (1 << tb_log) - 1) >> tb_log; }
 // Tiles of the block that ends before position `end`
-__host__ __device__ __forceinline__ int tiles_of_end(int end) { return end > kTile ? (end + kTile - 1) / kTile : 1; }
+template <int TL>
+__host__ __device__ __forceinline__ int tiles_of_end(int end) {
+    return end > (1 << TL) ? ((end - 1) >> TL) + 1 : 1;
+}
 // End position (exclusive) of block j
 __host__ __device__ __forceinline__ int block_end(const SeqView& s, int tb_log, int j) {
     const int toks = ((j + 1) << tb_log) < s.n ? (j + 1) << tb_log : s.n;
     return s.len - s.n + toks;
 }
 // All tiles of one (sequence, kv head)
+template <int TL>
 __host__ __device__ __forceinline__ long long tiles_of_head(const SeqView& s, int tb_log) {
     if (s.n == 0) return 0;
-    return tiles_before(s.len - s.n, tb_log, block_count(s.n, tb_log) - 1) + tiles_of_end(s.len);
+    return tiles_before<TL>(s.len - s.n, tb_log, block_count(s.n, tb_log) - 1) + tiles_of_end<TL>(s.len);
 }
 
 // The CTA's share of the line of tiles.
@@ -98,18 +101,19 @@ struct WorkShare {
 };
 
 // Finds the CTA's share; to be called by all `nthreads` threads (a multiple of 32, at most 1024) of the block.
-// scratch: 34 long longs + 2 in shared memory.  Ends with a barrier.
-struct ShareScratch {
+// Ends with a barrier.
+struct ShareScratch {  // in shared memory
     long long warp_sum[32];
     long long offset;
     int seq;
 };
+template <int TL>
 __device__ __forceinline__ void find_share(const PagedRowsDev& r, int page_shift, int n_kv_heads, int tb_log, int nthreads,
                                            int min_per, ShareScratch* sc, WorkShare& w, int* status) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps = nthreads >> 5;
     int* st0 = blockIdx.x == 0 ? status : nullptr;  // one CTA reports
     auto tiles = [&](int b) -> long long {
-        return b < r.batch ? tiles_of_head(load_seq(r, page_shift, b, st0), tb_log) * n_kv_heads : 0;
+        return b < r.batch ? tiles_of_head<TL>(load_seq(r, page_shift, b, st0), tb_log) * n_kv_heads : 0;
     };
     // inclusive scan over the block of one value per thread; returns the block's total
     long long mine = 0, incl = 0;
@@ -182,27 +186,29 @@ struct BlockWalk {
 };
 
 // Positions the walk on the first block of a (non-empty) share.
+template <int TL>
 __device__ __forceinline__ void walk_begin(const PagedRowsDev& r, int page_shift, int tb_log, const WorkShare& w, BlockWalk& k) {
     k.seq = w.seq;
     k.s = load_seq(r, page_shift, k.seq, nullptr);
-    const long long per_head = tiles_of_head(k.s, tb_log);
+    const long long per_head = tiles_of_head<TL>(k.s, tb_log);
     k.kvh = static_cast<int>(w.offset / per_head);
     const long long x = w.offset - per_head * k.kvh;
     const int ctx = k.s.len - k.s.n;
     int lo = 0, hi = block_count(k.s.n, tb_log) - 1;  // the last block that begins at or before x
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (tiles_before(ctx, tb_log, mid) <= x) lo = mid;
+        if (tiles_before<TL>(ctx, tb_log, mid) <= x) lo = mid;
         else hi = mid - 1;
     }
     k.j = lo;
-    k.tiles = tiles_of_end(block_end(k.s, tb_log, lo));
-    k.at = w.begin - (x - tiles_before(ctx, tb_log, lo));
+    k.tiles = tiles_of_end<TL>(block_end(k.s, tb_log, lo));
+    k.at = w.begin - (x - tiles_before<TL>(ctx, tb_log, lo));
     k.t0 = static_cast<int>(w.begin - k.at);
     k.t1 = static_cast<int>(min(static_cast<long long>(k.tiles), w.end - k.at));
 }
 
 // Moves to the next block; false at the end of the share.
+template <int TL>
 __device__ __forceinline__ bool walk_next(const PagedRowsDev& r, int page_shift, int n_kv_heads, int tb_log, const WorkShare& w,
                                           BlockWalk& k) {
     k.at += k.tiles;
@@ -216,7 +222,7 @@ __device__ __forceinline__ bool walk_next(const PagedRowsDev& r, int page_shift,
             } while (k.s.n == 0);  // a later sequence has tiles: the share does not end here
         }
     }
-    k.tiles = tiles_of_end(block_end(k.s, tb_log, k.j));
+    k.tiles = tiles_of_end<TL>(block_end(k.s, tb_log, k.j));
     k.t0 = 0;
     k.t1 = static_cast<int>(min(static_cast<long long>(k.tiles), w.end - k.at));
     return true;

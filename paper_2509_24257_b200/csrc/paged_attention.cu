@@ -24,6 +24,7 @@ namespace {
 
 constexpr int PR_THREADS = 128;
 constexpr int PR_WARPS = 4;
+constexpr int PR_TILE_LOG = 6, PR_TILE = 1 << PR_TILE_LOG;  // keys per tile: 16 per warp
 constexpr float PR_RAISE_LOG2 = 8.f;
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -115,14 +116,14 @@ paged_rows_kernel(const PagedAttnParams p) {
     const int G = p.group, shift = c.page_shift, ps_mask = (1 << shift) - 1;
 
     WorkShare share;
-    find_share(p.r, shift, c.n_kv_heads, p.tb_log, PR_THREADS, 1, &sm_share, share, p.status);
+    find_share<PR_TILE_LOG>(p.r, shift, c.n_kv_heads, p.tb_log, PR_THREADS, 1, &sm_share, share, p.status);
     pdl_launch_dependents();
     if (share.begin >= share.end) {
         if (tid == 0) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
     BlockWalk k;
-    walk_begin(p.r, shift, p.tb_log, share, k);
+    walk_begin<PR_TILE_LOG>(p.r, shift, p.tb_log, share, k);
     const float sl2 = rsqrtf(static_cast<float>(DH)) * kLog2e;
     int4 header = make_int4(0, 0, 0, 0);
 
@@ -171,7 +172,7 @@ paged_rows_kernel(const PagedAttnParams p) {
 
         uint4 ka[L::KCHUNKS], kb[L::KCHUNKS], v[L::VPIECES][4];
         float ks0 = 1.f, ks1 = 1.f, vs0 = 1.f, vs1 = 1.f, vs0n = 1.f, vs1n = 1.f;
-        auto token_of = [&](int tile) { return tile * kTile + warp * 16; };
+        auto token_of = [&](int tile) { return tile * PR_TILE + warp * 16; };
         // index of (page, kv head, row in page) in units of vectors
         auto vec_of = [&](int key) -> size_t {
             const int page = load_page(p.r, shift, c.n_pages, k.seq, key, p.status);
@@ -218,9 +219,9 @@ paged_rows_kernel(const PagedAttnParams p) {
         for (; tile < k.t1; ++tile) {
             const int key0 = token_of(tile);
             if (key0 >= end) break;  // the same for every later tile
-            const bool more = tile + 1 < k.t1 && key0 + kTile < end;
+            const bool more = tile + 1 < k.t1 && key0 + PR_TILE < end;
             size_t vec_next = 0;
-            if (more) vec_next = vec_of(key0 + kTile);
+            if (more) vec_next = vec_of(key0 + PR_TILE);
             // ---- S^T = K Q^T: 16 keys x 8 NT rows
             float sc[NT][4];
 #pragma unroll
@@ -473,7 +474,7 @@ paged_rows_kernel(const PagedAttnParams p) {
                 dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
             }
         }
-    } while (walk_next(p.r, shift, c.n_kv_heads, p.tb_log, share, k));
+    } while (walk_next<PR_TILE_LOG>(p.r, shift, c.n_kv_heads, p.tb_log, share, k));
     if (tid == 0) p.hdr[blockIdx.x] = header;
 }
 
@@ -555,19 +556,21 @@ cudaError_t rows_launch_dtype(const PagedAttnParams& p, int nt, int grid, cudaSt
     return rows_launch_nt<DH, VERILLM_KV_INT8>(p, nt, grid, stream);
 }
 
-// Which kernel and block shape serve a call.
+// Which kernel and block shape serve a call.  The few-row kernel takes sequences of up to 32 packed rows, the
+// tcgen05 kernel everything else.
 struct Shape {
-    int nt, tb_log, rows_per_block, grid;
+    int nt;  // 8-row column blocks of the few-row kernel; 0: the tcgen05 kernel
+    int tb_log, rows_per_block, grid;
 };
 Shape shape_of(int group, int max_rows, int num_sms) {
     Shape s;
     const long long r = static_cast<long long>(group) * max_rows;
-    s.nt = r <= 8 ? 1 : r <= 16 ? 2 : 4;
-    s.rows_per_block = 8 * s.nt;
+    s.nt = r <= 8 ? 1 : r <= 16 ? 2 : r <= 32 ? 4 : 0;
+    s.rows_per_block = s.nt ? 8 * s.nt : kPagedTcRows;
+    s.grid = num_sms * (s.nt == 0 ? 1 : s.nt == 1 ? 4 : s.nt == 2 ? 3 : 2);
+    // tokens per block: a power of two; the few-row kernel's single block holds them all
     s.tb_log = 0;
-    while ((1LL << s.tb_log) < max_rows && (2LL << s.tb_log) * group <= s.rows_per_block) ++s.tb_log;
-    if ((1LL << s.tb_log) < max_rows && r <= s.rows_per_block) ++s.tb_log;  // one block holds them all
-    s.grid = num_sms * (s.nt == 1 ? 4 : s.nt == 2 ? 3 : 2);
+    while ((1LL << s.tb_log) < max_rows && (s.nt || (2LL << s.tb_log) * group <= s.rows_per_block)) ++s.tb_log;
     return s;
 }
 size_t hdr_bytes(int grid) { return (static_cast<size_t>(grid) * sizeof(int4) + 255) & ~static_cast<size_t>(255); }
@@ -586,6 +589,7 @@ cudaError_t paged_attention_init() {
     if (e == cudaSuccess) e = rows_init_all<128, VERILLM_KV_BF16>();
     if (e == cudaSuccess) e = rows_init_all<128, VERILLM_KV_E4M3>();
     if (e == cudaSuccess) e = rows_init_all<128, VERILLM_KV_INT8>();
+    if (e == cudaSuccess) e = paged_attention_tc_init();
     return e;
 }
 
@@ -594,7 +598,9 @@ cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_s
     p.tb_log = s.tb_log;
     p.hdr = reinterpret_cast<int4*>(workspace);
     p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + hdr_bytes(s.grid));
-    cudaError_t e = p.c.head_dim == 64 ? rows_launch_dtype<64>(p, s.nt, s.grid, stream) : rows_launch_dtype<128>(p, s.nt, s.grid, stream);
+    cudaError_t e = s.nt == 0              ? launch_paged_attention_tc(p, s.grid, stream)
+                    : p.c.head_dim == 64 ? rows_launch_dtype<64>(p, s.nt, s.grid, stream)
+                                         : rows_launch_dtype<128>(p, s.nt, s.grid, stream);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(s.grid, (s.rows_per_block * (p.c.head_dim / 8) + JOIN_THREADS - 1) / JOIN_THREADS);

@@ -1,0 +1,808 @@
+// Causal grouped-query attention of new tokens over a paged cache, many rows per sequence (chunks of a prompt), on the
+// fifth-generation tensor cores.  The same definition as the few-row kernel; here the products dominate.
+//
+// A block is up to 256 packed rows ((token, query head of the group), so that a kv head's keys and values serve all
+// its query heads) of one (sequence, kv head), against tiles of 128 positions.  One CTA per SM holds the block as two
+// groups of 128 rows; tensor memory is exactly full: per group 128 columns of scores and head_dim of output.
+// While one group's four warps exponentiate a tile, the other group's products run.
+//   warps 0-3, 4-7  softmax of the two groups, one row per thread: scores from tensor memory, running reference maximum
+//                   and sum in registers, probabilities back as 16-bit pairs over the upper half of the score columns
+//                   (each half as soon as it is complete, so that P V starts under the second half's exponentials);
+//                   they also bring the block's queries into shared memory and write the results
+//   warps 8-11      bf16 cache: clean the values of tiles on the diagonal; 8-bit cache: fetch the codes of the next tile
+//                   into registers, widen them and store them as operand tiles
+//   warps 12, 13    one thread each issues the group's S = Q K^T and O += P V (tcgen05.mma)
+//   warp 14         bf16 cache: TMA loads of keys and values, one box per page, a lane per page
+// The 64-column halves of all operand tiles use the 128-byte swizzle; values are consumed as they lie in memory
+// ([key][dh], an MN-major B operand).  The scores are read from tensor memory twice, once for the maximum and
+// once for the exponentials, which keeps a row's 128 scores out of registers.
+//
+// 8-bit caches: both code types are exact in fp16, so keys and values are widened to fp16 and both products
+// are fp16; queries are scaled row by row by a power of two to fit.  Key scales multiply the fp32 scores.  Value scales
+// multiply the probabilities, relative to a power of two that follows the largest scale seen in the block, so that the
+// product fits fp16; its rounding is 2^-11 relative (bf16's probabilities: 2^-8).
+//
+// Masked entries: scores are replaced by -inf.  Values behind the sequence's last position are whatever the page
+// holds and become 0.  An infinite or NaN value (or value scale) in a tile that some rows may not see entirely is
+// taken out of the product and put into the results of the rows that see it at the end ("stray").
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "paged.cuh"
+
+namespace vl {
+
+namespace {
+
+constexpr int PT_TILE_LOG = 7, PT_TILE = 1 << PT_TILE_LOG;
+constexpr int PT_THREADS = 512;
+constexpr int PT_GROUP_ROWS = 128, PT_ROWS = 2 * PT_GROUP_ROWS;
+static_assert(PT_ROWS == kPagedTcRows, "");
+constexpr int PT_KSTAGES = 2, PT_VSTAGES = 2, PT_SCALES = PT_KSTAGES + 1;
+constexpr int PT_TMEM_COLS = 512;  // S of the groups at 0 and 128, O at 256 and 384
+constexpr float PT_RAISE_LOG2 = 8.f;
+// registers per thread of the roles; together what 512 threads are launched with (128 each)
+constexpr int PT_REGS_SOFTMAX = 168, PT_REGS_HELPER = 112, PT_REGS_ISSUE = 64;
+static_assert(2 * PT_REGS_SOFTMAX + PT_REGS_HELPER + PT_REGS_ISSUE <= 4 * 128, "");
+// value scales relative to their reference lie in (.., 2^7]: with probabilities up to 2^8 the product stays below 2^15
+constexpr float PT_VREF_MAX = 128.f;
+
+template <int DH, int DTYPE>
+struct PtSmem {
+    static constexpr bool BF16 = DTYPE == VERILLM_KV_BF16;
+    static constexpr uint32_t Q_HALF = PT_ROWS * 128;  // 64 columns of all rows
+    static constexpr uint32_t KV_HALF = PT_TILE * 128;
+    static constexpr uint32_t KV_BYTES = KV_HALF * (DH / 64);
+    static constexpr uint32_t K_OFF = Q_HALF * (DH / 64);
+    static constexpr uint32_t V_OFF = K_OFF + PT_KSTAGES * KV_BYTES;
+    static constexpr uint32_t SC_OFF = V_OFF + PT_VSTAGES * KV_BYTES;  // per slot: 128 key scales, 128 value scales
+    static constexpr uint32_t SC_BYTES = 2 * PT_TILE * 4;
+    static constexpr uint32_t BAR_OFF = SC_OFF + (BF16 ? 0 : PT_SCALES * SC_BYTES);
+    static constexpr uint32_t TOTAL = BAR_OFF + 512 + sizeof(ShareScratch);
+};
+
+// MN-major operand (V as stored: [key][dh]): 64 columns of a key are a row of 128 bytes, 8 keys per 1024-byte swizzle
+// atom; `lbo_bytes` separates the 64-column halves.
+__device__ __forceinline__ uint64_t pt_desc_mn(uint32_t tile_smem, uint32_t lbo_bytes) {
+    const uint64_t lo = static_cast<uint64_t>((tile_smem & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(lbo_bytes >> 4) << 16);
+    const uint64_t hi = static_cast<uint64_t>(1024u >> 4) | (1ull << 14) | (2ull << 29);
+    return lo | (hi << 32);
+}
+// kind::f16 with fp32 accumulators; operands bf16 or fp16, B K-major or (mn) MN-major
+__host__ __device__ constexpr uint32_t pt_idesc(bool bf16, int n, bool mn) {
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (mn ? 1u << 16 : 0u) | (static_cast<uint32_t>(n >> 3) << 17) |
+           (static_cast<uint32_t>(PT_GROUP_ROWS >> 4) << 24);
+}
+__device__ __forceinline__ float2 pt_fma2(float2 a, float2 b, float2 c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(d)
+        : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+    return reinterpret_cast<float2&>(d);
+}
+__device__ __forceinline__ float2 pt_add2(float2 a, float2 b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+    return reinterpret_cast<float2&>(d);
+}
+__device__ __forceinline__ float2 pt_mul2(float2 a, float2 b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+    return reinterpret_cast<float2&>(d);
+}
+__device__ __forceinline__ float pt_max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void sts16(uint32_t addr, const uint4& x) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t addr) {
+    uint4 x;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(addr) : "memory");
+    return x;
+}
+__device__ __forceinline__ void stg32(void* p, const uint32_t (&r)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+// Bounded wait of a whole warp, with one answer for all its lanes.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, int* status) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, status));
+}
+template <int N>
+__device__ __forceinline__ void set_registers(bool more) {
+    if (more) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// Four codes -> fp16 pairs (0, 1) and (2, 3), exactly.  int8: 0x6400 | (code + 128) is the fp16 number 1152 + code.
+template <int DTYPE>
+__device__ __forceinline__ uint2 widen4_half(uint32_t w) {
+    if (DTYPE == VERILLM_KV_E4M3) {
+        const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w & 0xFFFFu), __NV_E4M3);
+        const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w >> 16), __NV_E4M3);
+        return make_uint2(a.x | (static_cast<uint32_t>(a.y) << 16), b.x | (static_cast<uint32_t>(b.y) << 16));
+    }
+    const uint32_t u = w ^ 0x80808080u;
+    const __half2 off = __half2half2(__ushort_as_half(static_cast<unsigned short>(0x6480)));  // 1152
+    const uint32_t lo = __byte_perm(u, 0x64646464u, 0x4140), hi = __byte_perm(u, 0x64646464u, 0x4342);
+    const __half2 a = __hsub2(*reinterpret_cast<const __half2*>(&lo), off), b = __hsub2(*reinterpret_cast<const __half2*>(&hi), off);
+    return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+__device__ __forceinline__ bool odd_bf16(uint32_t bits16) { return (bits16 & 0x7F80u) == 0x7F80u; }
+
+// The part of a block that a CTA works on, as all its warps see it.
+struct Part {
+    int row0, first_pos, rows, end;  // packed row of the first token, its position, rows, end of the visible keys
+    int mask_tile;                   // first tile that some row may not see entirely
+    __device__ __forceinline__ bool masked(int tile) const { return tile >= mask_tile; }
+};
+__device__ __forceinline__ Part part_of(const BlockWalk& k, int tb_log, int group) {
+    Part u;
+    const int tok0 = k.j << tb_log, toks = min(1 << tb_log, k.s.n - tok0);
+    u.row0 = k.s.row0 + tok0;
+    u.first_pos = k.s.len - k.s.n + tok0;
+    u.rows = toks * group;
+    u.end = u.first_pos + toks;
+    u.mask_tile = u.first_pos < 0 ? 0 : (u.first_pos + 1) >> PT_TILE_LOG;  // tiles before it end at or before first_pos
+    return u;
+}
+
+// Which of the 32 columns from col0 on receive a NaN, +inf or -inf from values of keys [from, to) that are not finite.
+struct Stray {
+    uint32_t nan, pinf, ninf;
+};
+template <int DH, int DTYPE>
+__device__ __noinline__ Stray find_stray(const PagedAttnParams& p, int seq, int kvh, int from, int to, int col0) {
+    Stray x = {0u, 0u, 0u};
+    for (int key = from; key < to; ++key) {
+        const int page = load_page(p.r, p.c.page_shift, p.c.n_pages, seq, key, nullptr);
+        const size_t vec = ((static_cast<size_t>(page) * p.c.n_kv_heads + kvh) << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1));
+        if (DTYPE != VERILLM_KV_BF16) {
+            if (!isfinite(p.c.v_scale[vec])) x.nan = 0xFFFFFFFFu;
+            continue;
+        }
+        const unsigned short* v = reinterpret_cast<const unsigned short*>(p.c.v) + vec * DH + col0;
+        for (int i = 0; i < 32; ++i) {
+            const uint32_t b = v[i];
+            if (!odd_bf16(b)) continue;
+            if (b & 0x7Fu) x.nan |= 1u << i;
+            else if (b & 0x8000u) x.ninf |= 1u << i;
+            else x.pinf |= 1u << i;
+        }
+    }
+    return x;
+}
+
+template <int DH, int DTYPE>
+__global__ void __launch_bounds__(PT_THREADS, 1)
+paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ PagedAttnParams p) {
+    using L = PtSmem<DH, DTYPE>;
+    constexpr bool BF16 = L::BF16;
+    constexpr int HALVES = DH / 64;
+    extern __shared__ __align__(1024) uint8_t pt_smem[];
+    const uint32_t sbase = smem_u32(pt_smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if ((sbase & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
+        if (tid == 0) {
+            raise_status(p.status, VERILLM_DEV_WAIT_TIMEOUT);
+            p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+        }
+        return;
+    }
+    const uint32_t q_s = sbase;
+    auto k_s = [&](int b) { return sbase + L::K_OFF + b * L::KV_BYTES; };
+    auto v_s = [&](int b) { return sbase + L::V_OFF + b * L::KV_BYTES; };
+    float* sc_k = reinterpret_cast<float*>(pt_smem + L::SC_OFF);  // slot s: [s * 256, + 128) keys, then values
+    const uint32_t bar = sbase + L::BAR_OFF;
+    auto q_full = [&](int w) { return bar + 8 * w; };
+    auto s_full = [&](int w) { return bar + 16 + 8 * w; };
+    auto o_done = [&](int w) { return bar + 32 + 8 * w; };
+    auto p_half = [&](int w, int h) { return bar + 48 + 16 * w + 8 * h; };
+    auto k_full = [&](int b) { return bar + 80 + 8 * b; };
+    auto k_empty = [&](int b) { return bar + 112 + 8 * b; };
+    auto v_full = [&](int b) { return bar + 144 + 8 * b; };
+    auto v_empty = [&](int b) { return bar + 176 + 8 * b; };
+    auto sc_full = [&](int s) { return bar + 208 + 8 * s; };
+    auto v_clean = [&](int b) { return bar + 232 + 8 * b; };
+    const uint32_t tmem_slot = bar + 256;
+    volatile uint32_t* tmem_slot_ptr = reinterpret_cast<volatile uint32_t*>(pt_smem + L::BAR_OFF + 256);
+    volatile int* failed = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 260);
+    volatile int* stray = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 264);        // some value was taken out so far
+    volatile float* sc_vref = reinterpret_cast<volatile float*>(pt_smem + L::BAR_OFF + 272);  // [PT_SCALES]
+    ShareScratch* scratch = reinterpret_cast<ShareScratch*>(pt_smem + L::BAR_OFF + 512);
+
+    if (tid == 0) {
+        *failed = 0;
+        *stray = 0;
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(q_full(w), 4);
+            mbar_init(s_full(w), 1);
+            mbar_init(o_done(w), 1);
+            mbar_init(p_half(w, 0), 4);
+            mbar_init(p_half(w, 1), 4);
+        }
+        for (int b = 0; b < PT_KSTAGES; ++b) {
+            mbar_init(k_full(b), BF16 ? 1 : 4);
+            mbar_init(k_empty(b), 2);
+        }
+        for (int b = 0; b < PT_VSTAGES; ++b) {
+            mbar_init(v_full(b), BF16 ? 1 : 4);
+            mbar_init(v_empty(b), 2);
+            mbar_init(v_clean(b), 4);
+        }
+        for (int s = 0; s < PT_SCALES; ++s) mbar_init(sc_full(s), 4);
+        fence_mbar_init();
+    }
+    WorkShare share;
+    find_share<PT_TILE_LOG>(p.r, p.c.page_shift, p.c.n_kv_heads, p.tb_log, PT_THREADS, 1, scratch, share, p.status);
+    pdl_launch_dependents();
+    if (share.begin >= share.end) {
+        if (tid == 0) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+        return;
+    }
+    if (warp == 12) {
+        tmem_alloc(tmem_slot, PT_TMEM_COLS);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot_ptr;
+    int* status = p.status;
+    const int shift = p.c.page_shift, ps_mask = (1 << shift) - 1, n_kv = p.c.n_kv_heads, G = p.group;
+
+    // Every role walks the same blocks; g counts the CTA's tiles (stage g % stages, phase g / stages).
+    BlockWalk k;
+    walk_begin<PT_TILE_LOG>(p.r, shift, p.tb_log, share, k);
+    auto next = [&]() { return walk_next<PT_TILE_LOG>(p.r, shift, n_kv, p.tb_log, share, k); };
+    bool ok = true;
+
+    if (warp < 8) {
+        // ------------------------------------------------------------ softmax, one row per thread
+        set_registers<PT_REGS_SOFTMAX>(true);
+        const int w = warp >> 2;
+        const int r = tid;  // row of the block (the two groups' threads are 0 .. 255)
+        const uint32_t lane_base = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        const uint32_t s_addr = lane_base + w * 128, o_addr = lane_base + 256 + w * 128;
+        const float sl2 = rsqrtf(static_cast<float>(DH)) * kLog2e;
+        int4 header = make_int4(0, 0, 0, 0);
+        int g = 0, sg = 0, au = 0;  // tiles of the CTA, tiles and blocks of this group
+        do {
+            const Part u = part_of(k, p.tb_log, G);
+            if (w * PT_GROUP_ROWS >= u.rows) {  // this group has no rows in the block
+                g += k.t1 - k.t0;
+                continue;
+            }
+            const bool valid = r < u.rows;
+            const int tok = valid ? r / G : 0, hd = k.kvh * G + (valid ? r - tok * G : 0);
+            const int pos = valid ? u.first_pos + tok : -1;  // last visible key
+            float rf = sl2;  // factor of the scores in log2 units
+            {   // ---- the row's queries into the swizzled operand tile.  The group's last Q K^T has completed: its
+                // scores were read above.
+                const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) +
+                                                                  static_cast<size_t>(u.row0 + tok) * p.q_stride + static_cast<size_t>(hd) * DH);
+                const uint32_t dst = q_s + r * 128;
+                if (BF16) {
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) sts16(dst + h * L::Q_HALF + ((c ^ (r & 7)) << 4), __ldg(src + 8 * h + c));
+                } else {
+                    uint4 x[DH / 8];
+                    uint32_t mx = 0;
+#pragma unroll
+                    for (int c = 0; c < DH / 8; ++c) {
+                        x[c] = __ldg(src + c);
+                        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(x[c].x & 0x7FFF7FFFu, x[c].y & 0x7FFF7FFFu), __vmaxu2(x[c].z & 0x7FFF7FFFu, x[c].w & 0x7FFF7FFFu)));
+                    }
+                    // |q| 2^(127 - e) lies in [1, 2), e the exponent field of the row's largest entry
+                    const uint32_t e = min(max(max(mx >> 16, mx & 0xFFFFu) >> 7, 1u), 253u);
+                    const float down = __uint_as_float((254u - e) << 23);
+                    rf = sl2 * __uint_as_float(e << 23);
+#pragma unroll
+                    for (int c = 0; c < DH / 8; ++c) {
+                        const uint4 y = make_uint4(pack_half(bf16_lo(x[c].x) * down, bf16_hi(x[c].x) * down), pack_half(bf16_lo(x[c].y) * down, bf16_hi(x[c].y) * down),
+                                                   pack_half(bf16_lo(x[c].z) * down, bf16_hi(x[c].z) * down), pack_half(bf16_lo(x[c].w) * down, bf16_hi(x[c].w) * down));
+                        sts16(dst + (c >> 3) * L::Q_HALF + (((c & 7) ^ (r & 7)) << 4), y);
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_full(w));
+            }
+            float m_ref = -INFINITY, l_run = 0.f, vref = 0.f;
+            const float2 rf2 = make_float2(rf, rf);
+            for (int t = k.t0; t < k.t1; ++t, ++g, ++sg) {
+                const int key0 = t << PT_TILE_LOG;
+                const bool masked = u.masked(t);
+                const int lim = pos - key0;  // visible: column <= lim
+                const float* ks = sc_k + (g % PT_SCALES) * 256;
+                const float* vs = ks + 128;
+                if (!BF16 && !warp_wait(sc_full(g % PT_SCALES), (g / PT_SCALES) & 1, status)) { ok = false; break; }
+                if (!warp_wait(s_full(w), sg & 1, status)) { ok = false; break; }
+                tc_fence_after();
+                uint32_t v0[32], v1[32];
+                // 32 scores of columns [c, c + 32): key scales, then the mask
+                auto prepare = [&](uint32_t (&v)[32], int c) {
+                    if (!BF16) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 s4 = *reinterpret_cast<const float4*>(ks + c + i);
+                            const float2 a = pt_mul2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(s4.x, s4.y));
+                            const float2 b = pt_mul2(make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), make_float2(s4.z, s4.w));
+                            v[i] = __float_as_uint(a.x);
+                            v[i + 1] = __float_as_uint(a.y);
+                            v[i + 2] = __float_as_uint(b.x);
+                            v[i + 3] = __float_as_uint(b.y);
+                        }
+                    }
+                    if (masked) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (c + i > lim) v[i] = 0xFF800000u;  // -inf
+                    }
+                };
+                float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                tmem_ld32(s_addr, v0);
+                tmem_ld32(s_addr + 32, v1);
+                tmem_ld_wait_regs(v0);
+                tmem_ld_wait_regs(v1);
+                prepare(v0, 0);
+                prepare(v1, 32);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) mx4[i & 3] = pt_max3(mx4[i & 3], __uint_as_float(v0[i]), __uint_as_float(v1[i]));
+                tmem_ld32(s_addr + 64, v0);
+                tmem_ld32(s_addr + 96, v1);
+                tmem_ld_wait_regs(v0);
+                tmem_ld_wait_regs(v1);
+                prepare(v0, 64);
+                prepare(v1, 96);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) mx4[i & 3] = pt_max3(mx4[i & 3], __uint_as_float(v0[i]), __uint_as_float(v1[i]));
+                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * rf;
+                const bool grow = valid && mx > m_ref + PT_RAISE_LOG2;
+                float corr = 1.f;
+                bool fix = grow;
+                if (!BF16) {
+                    const float nv = sc_vref[g % PT_SCALES];
+                    if (nv != vref) {  // the same in all threads
+                        corr = vref / nv;
+                        vref = nv;
+                        fix = true;
+                    }
+                }
+                if (__any_sync(0xFFFFFFFFu, fix)) {
+                    if (grow) {
+                        const float c = exp2_fast(m_ref - mx);
+                        corr *= c;
+                        l_run *= c;
+                        m_ref = mx;
+                    }
+                    if (t != k.t0) {  // O holds the earlier tiles: this tile's scores were issued after their P V
+#pragma unroll 1
+                        for (int c = 0; c < DH / 32; ++c) {
+                            uint32_t o[32];
+                            tmem_ld32(o_addr + c * 32, o);
+                            tmem_ld_wait_regs(o);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+                            tmem_st32(o_addr + c * 32, o);
+                        }
+                        tmem_st_wait();
+                    }
+                }
+                const float nm = m_ref == -INFINITY ? 0.f : -m_ref;
+                const float2 nm2 = make_float2(nm, nm);
+                float2 rs2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                // probabilities of columns [c, c + 32) as 16 packed columns over the upper half of the scores
+                auto probabilities = [&](const uint32_t (&v)[32], int c) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        float2 e[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float2 x = pt_fma2(make_float2(__uint_as_float(v[2 * (i + h)]), __uint_as_float(v[2 * (i + h) + 1])), rf2, nm2);
+                            e[h] = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+                            rs2[h] = pt_add2(rs2[h], e[h]);
+                        }
+                        if (BF16) {
+                            pk[i] = pack_bf16(e[0].x, e[0].y);
+                            pk[i + 1] = pack_bf16(e[1].x, e[1].y);
+                        } else {
+                            const float4 s4 = *reinterpret_cast<const float4*>(vs + c + 2 * i);
+                            const float2 a = pt_mul2(e[0], make_float2(s4.x, s4.y)), b = pt_mul2(e[1], make_float2(s4.z, s4.w));
+                            pk[i] = pack_half(a.x, a.y);
+                            pk[i + 1] = pack_half(b.x, b.y);
+                        }
+                    }
+                    tmem_st16(s_addr + 64 + (c >> 1), pk);
+                };
+                auto deliver = [&](int h) {
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_half(w, h));
+                };
+                probabilities(v0, 64);
+                tmem_ld32(s_addr, v0);
+                probabilities(v1, 96);
+                tmem_ld32(s_addr + 32, v1);
+                deliver(0);
+                tmem_ld_wait_regs(v0);
+                tmem_ld_wait_regs(v1);
+                prepare(v0, 0);
+                probabilities(v0, 0);
+                prepare(v1, 32);
+                probabilities(v1, 32);
+                deliver(1);
+                l_run += (rs2[0].x + rs2[0].y) + (rs2[1].x + rs2[1].y);
+            }
+            if (!ok) break;
+            if (!warp_wait(o_done(w), au & 1, status)) { ok = false; break; }
+            tc_fence_after();
+            // ---- results: the whole block's, or this part's for the join
+            const bool whole = k.t0 == 0 && k.t1 == k.tiles;
+            if (!whole && k.t0 == 0)
+                header = make_int4(static_cast<int>((k.at + k.tiles - 1) / share.per) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
+            float* part = part_slot(p.part, 2 * static_cast<int>(blockIdx.x) + (k.t0 == 0 ? 1 : 0), PT_ROWS, DH);
+            const float inv = (whole ? (l_run == 0.f ? 0.f : 1.f / l_run) : 1.f) * (BF16 ? 1.f : vref);
+            const bool odd = *stray != 0;
+            const size_t row = static_cast<size_t>(u.row0 + tok);
+            if (valid) {
+                if (whole) {
+                    if (p.lse) p.lse[row * p.n_heads + hd] = l_run == 0.f ? -INFINITY : m_ref * kLn2 + logf(l_run);
+                } else {
+                    part[r] = m_ref;
+                    part[PT_ROWS + r] = l_run;
+                }
+            }
+#pragma unroll 1
+            for (int c = 0; c < DH / 32; ++c) {
+                uint32_t o[32];
+                tmem_ld32(o_addr + c * 32, o);
+                tmem_ld_wait_regs(o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = l_run == 0.f ? 0u : __float_as_uint(__uint_as_float(o[i]) * inv);
+                if (odd) {
+                    const Stray x = find_stray<DH, DTYPE>(p, k.seq, k.kvh, max(k.t0, u.mask_tile) << PT_TILE_LOG,
+                                                          min(pos + 1, k.t1 << PT_TILE_LOG), c * 32);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        if ((x.nan >> i) & 1u) o[i] = 0x7FC00000u;
+                        if ((x.pinf >> i) & 1u) o[i] = __float_as_uint(__uint_as_float(o[i]) + INFINITY);
+                        if ((x.ninf >> i) & 1u) o[i] = __float_as_uint(__uint_as_float(o[i]) - INFINITY);
+                    }
+                }
+                if (valid && whole) {
+                    __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + row * p.out_stride + static_cast<size_t>(hd) * DH + c * 32;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        uint4 y;
+                        y.x = pack_bf16(__uint_as_float(o[8 * h]), __uint_as_float(o[8 * h + 1]));
+                        y.y = pack_bf16(__uint_as_float(o[8 * h + 2]), __uint_as_float(o[8 * h + 3]));
+                        y.z = pack_bf16(__uint_as_float(o[8 * h + 4]), __uint_as_float(o[8 * h + 5]));
+                        y.w = pack_bf16(__uint_as_float(o[8 * h + 6]), __uint_as_float(o[8 * h + 7]));
+                        reinterpret_cast<uint4*>(dst)[h] = y;
+                    }
+                } else if (valid) {
+                    float* dst = part + 2 * PT_ROWS + r * DH + c * 32;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        uint32_t y[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] = o[8 * h + i];
+                        stg32(dst + 8 * h, y);
+                    }
+                }
+                __syncwarp();
+            }
+            ++au;
+        } while (next());
+        if (w == 0 && tid == 0) p.hdr[blockIdx.x] = ok ? header : make_int4(0, 0, 0, 0);
+    } else if (warp < 12) {
+        set_registers<PT_REGS_HELPER>(false);
+        const int ht = tid - 256;  // thread of the helper group
+        int g = 0;
+        if (BF16) {
+            // ------------------------------------------------------------ clean the values of masked tiles
+            do {
+                const Part u = part_of(k, p.tb_log, G);
+                for (int t = k.t0; t < k.t1; ++t, ++g) {
+                    if (!u.masked(t)) continue;
+                    if (!warp_wait(v_full(g % PT_VSTAGES), (g / PT_VSTAGES) & 1, status)) { ok = false; break; }
+                    const uint32_t row = v_s(g % PT_VSTAGES) + ht * 128;
+                    const bool gone = (t << PT_TILE_LOG) + ht >= u.end;
+                    bool found = false;
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h)
+#pragma unroll 2
+                        for (int c = 0; c < 8; ++c) {
+                            const uint32_t a = row + h * L::KV_HALF + ((c ^ (ht & 7)) << 4);
+                            if (gone) {
+                                sts16(a, make_uint4(0u, 0u, 0u, 0u));
+                                continue;
+                            }
+                            const uint4 x = lds16(a);
+                            const uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7F807F80u, x.y & 0x7F807F80u), __vmaxu2(x.z & 0x7F807F80u, x.w & 0x7F807F80u));
+                            if (!odd_bf16(m) && !odd_bf16(m >> 16)) continue;
+                            found = true;
+                            uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if (odd_bf16(y[i])) y[i] &= 0xFFFF0000u;
+                                if (odd_bf16(y[i] >> 16)) y[i] &= 0x0000FFFFu;
+                            }
+                            sts16(a, make_uint4(y[0], y[1], y[2], y[3]));
+                        }
+                    if (found) *stray = 1;
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(v_clean(g % PT_VSTAGES));
+                }
+            } while (ok && next());
+        } else {
+            // ------------------------------------------------------------ fetch and widen the codes
+            constexpr int CPR = DH / 16;              // 16-byte pieces of a vector
+            constexpr int RPP = 128 / CPR;            // rows per pass over the 128 threads
+            constexpr int NP = PT_TILE / RPP;         // passes per tile
+            const int c = ht % CPR, r0 = ht / CPR;
+            uint4 rk[NP], rv[NP];
+            float ks = 0.f, vs = 0.f, vq[4] = {0.f, 0.f, 0.f, 0.f};  // scales of this thread's key; value scales of four of the tile's keys
+            // pages of the tile's 16-position groups, one per lane (8 of them), fetched a tile ahead
+            auto pages_of = [&](int tile, int end) {
+                const int key = (tile << PT_TILE_LOG) + (lane & 7) * 16;
+                return key < end ? load_page(p.r, shift, p.c.n_pages, k.seq, key, status) : 0;
+            };
+            auto vec_at = [&](int pages, int key) -> size_t {
+                const int page = __shfl_sync(0xFFFFFFFFu, pages, (key >> 4) & 7);
+                return ((static_cast<size_t>(page) * n_kv + k.kvh) << shift) + (key & ps_mask);
+            };
+            auto fetch = [&](uint4 (&x)[NP], const void* pool, int pages, int tile, int end) {
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    const int key = (tile << PT_TILE_LOG) + i * RPP + r0;
+                    const size_t vec = vec_at(pages, key);
+                    x[i] = key < end ? __ldg(reinterpret_cast<const uint4*>(pool) + vec * CPR + c) : make_uint4(0u, 0u, 0u, 0u);
+                }
+            };
+            auto fetch_scales = [&](int pages, int tile, int end) {
+                const int key = (tile << PT_TILE_LOG) + ht;
+                const size_t vec = vec_at(pages, key);
+                ks = key < end ? __ldg(p.c.k_scale + vec) : 0.f;
+                vs = key < end ? __ldg(p.c.v_scale + vec) : 0.f;
+                // every warp looks at all 128 value scales, so that the warps need not agree on their maximum
+                const int key4 = (tile << PT_TILE_LOG) + 4 * lane;
+                const size_t vec4 = vec_at(pages, key4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) vq[i] = key4 + i < end ? __ldg(p.c.v_scale + vec4 + i) : 0.f;
+            };
+            auto widen = [&](const uint4 (&x)[NP], uint32_t tile_smem) {
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    const int row = i * RPP + r0;
+                    const uint2 a = widen4_half<DTYPE>(x[i].x), b = widen4_half<DTYPE>(x[i].y), d = widen4_half<DTYPE>(x[i].z), e = widen4_half<DTYPE>(x[i].w);
+                    const uint32_t base = tile_smem + (c >> 2) * L::KV_HALF + row * 128;
+                    const int c16 = 2 * (c & 3);
+                    sts16(base + ((c16 ^ (row & 7)) << 4), make_uint4(a.x, a.y, b.x, b.y));
+                    sts16(base + (((c16 + 1) ^ (row & 7)) << 4), make_uint4(d.x, d.y, e.x, e.y));
+                }
+            };
+            Part u = part_of(k, p.tb_log, G);
+            int pages = pages_of(k.t0, u.end);
+            fetch(rk, p.c.k, pages, k.t0, u.end);
+            fetch_scales(pages, k.t0, u.end);
+            fetch(rv, p.c.v, pages, k.t0, u.end);
+            bool more = true;
+            while (more && ok) {
+                float vref = 0.f;
+                for (int t = k.t0; t < k.t1; ++t, ++g) {
+                    const int kb = g % PT_KSTAGES, vb = g % PT_VSTAGES, slot = g % PT_SCALES;
+                    const bool masked = u.masked(t);
+                    if (g >= PT_KSTAGES && !warp_wait(k_empty(kb), ((g / PT_KSTAGES) - 1) & 1, status)) { ok = false; break; }
+                    // the slot's previous scales belong to tile g - KSTAGES - 1, whose probabilities preceded the
+                    // product that freed this key stage
+                    float v = vs;
+                    if (masked && !isfinite(v)) {
+                        v = 0.f;
+                        *stray = 1;
+                    }
+                    float mx = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mx = isfinite(vq[i]) ? fmaxf(mx, vq[i]) : mx;
+                    if (__any_sync(0xFFFFFFFFu, vref == 0.f || mx > vref * PT_VREF_MAX)) {
+                        // 2^-6 of the power of two at or below the largest scale (scales are at least 2^-119)
+                        const uint32_t e = max(__float_as_uint(warp_max(mx)) >> 23, 7u) - 6u;
+                        vref = fmaxf(vref, __uint_as_float(e << 23));
+                    }
+                    sc_k[slot * 256 + ht] = ks;
+                    sc_k[slot * 256 + 128 + ht] = v / vref;
+                    if (ht == 0) sc_vref[slot] = vref;
+                    widen(rk, k_s(kb));
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(sc_full(slot));
+                        mbar_arrive(k_full(kb));
+                    }
+                    // the next tile: of this block, or the first of the next one
+                    const bool last = t + 1 == k.t1;
+                    int nt = t + 1;
+                    if (last) {
+                        more = next();
+                        if (more) {
+                            u = part_of(k, p.tb_log, G);
+                            nt = k.t0;
+                        }
+                    }
+                    const bool fetch_next = !last || more;
+                    if (fetch_next) {
+                        pages = pages_of(nt, u.end);
+                        fetch(rk, p.c.k, pages, nt, u.end);
+                        fetch_scales(pages, nt, u.end);
+                    }
+                    if (g >= PT_VSTAGES && !warp_wait(v_empty(vb), ((g / PT_VSTAGES) - 1) & 1, status)) { ok = false; break; }
+                    widen(rv, v_s(vb));
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(v_full(vb));
+                    if (fetch_next) fetch(rv, p.c.v, pages, nt, u.end);
+                    if (last) {
+                        ++g;
+                        break;
+                    }
+                }
+            }
+        }
+    } else {
+        set_registers<PT_REGS_ISSUE>(false);
+        if (warp < 14) {
+        // ------------------------------------------------------------ product issuer of one group (one thread)
+        if (lane == 0) {
+            const int w = warp - 12;
+            const uint32_t s_tmem = tmem_base + w * 128, o_tmem = tmem_base + 256 + w * 128;
+            const uint64_t q_desc = umma_desc_k_sw128(q_s + w * PT_GROUP_ROWS * 128);
+            constexpr uint32_t idesc_s = pt_idesc(BF16, PT_TILE, false), idesc_o = pt_idesc(BF16, DH, true);
+            int g = 0, sg = 0, au = 0;  // tiles of the CTA, of this group; its blocks
+            uint32_t clean = 0;         // phase of each value stage's cleaning
+            do {
+                const Part u = part_of(k, p.tb_log, G);
+                const bool active = w * PT_GROUP_ROWS < u.rows;
+                if (active && !mbar_wait(q_full(w), au & 1, status)) { ok = false; break; }
+                for (int t = k.t0; t < k.t1; ++t, ++g) {
+                    const int kb = g % PT_KSTAGES, vb = g % PT_VSTAGES;
+                    if (!mbar_wait(k_full(kb), (g / PT_KSTAGES) & 1, status)) { ok = false; break; }
+                    if (!active) {  // the stages count both groups
+                        mbar_arrive(k_empty(kb));
+                        if (!mbar_wait(v_full(vb), (g / PT_VSTAGES) & 1, status)) { ok = false; break; }
+                        mbar_arrive(v_empty(vb));
+                        if (BF16 && u.masked(t)) clean ^= 1u << vb;
+                        continue;
+                    }
+                    tc_fence_after();
+                    const uint64_t kd = umma_desc_k_sw128(k_s(kb));
+#pragma unroll
+                    for (int s = 0; s < DH / 16; ++s)
+                        umma_bf16(s_tmem, q_desc + static_cast<uint64_t>((s / 4) * (L::Q_HALF >> 4) + 2 * (s % 4)),
+                                  kd + static_cast<uint64_t>((s / 4) * (L::KV_HALF >> 4) + 2 * (s % 4)), idesc_s, s != 0 ? 1u : 0u);
+                    umma_commit(s_full(w));
+                    umma_commit(k_empty(kb));
+                    if (!mbar_wait(v_full(vb), (g / PT_VSTAGES) & 1, status)) { ok = false; break; }
+                    if (BF16 && u.masked(t)) {
+                        if (!mbar_wait(v_clean(vb), (clean >> vb) & 1u, status)) { ok = false; break; }
+                        clean ^= 1u << vb;
+                    }
+                    const uint64_t vd = pt_desc_mn(v_s(vb), L::KV_HALF);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {  // keys 64 - 127 first
+                        if (!mbar_wait(p_half(w, h), sg & 1, status)) { ok = false; break; }
+                        tc_fence_after();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int s = (h == 0 ? 4 : 0) + i;
+                            umma_bf16_ts(o_tmem, s_tmem + 64 + s * 8, vd + static_cast<uint64_t>(s * (2048 >> 4)), idesc_o,
+                                         t == k.t0 && h == 0 && i == 0 ? 0u : 1u);
+                        }
+                    }
+                    if (!ok) break;
+                    umma_commit(v_empty(vb));
+                    if (t + 1 == k.t1) umma_commit(o_done(w));
+                    ++sg;
+                }
+                if (active) ++au;
+            } while (ok && next());
+        }
+        } else if (BF16 && warp == 14) {
+        // ------------------------------------------------------------ TMA producer: one box per page, a lane each
+        const int bp = min(1 << shift, PT_TILE);  // positions per box
+        int g = 0;
+        do {
+            const Part u = part_of(k, p.tb_log, G);
+            for (int t = k.t0; t < k.t1; ++t, ++g) {
+                const int kb = g % PT_KSTAGES, vb = g % PT_VSTAGES;
+                const int left = u.end - (t << PT_TILE_LOG);
+                const int boxes = left <= 0 ? 0 : (min(left, PT_TILE) + bp - 1) / bp;
+                int y = 0;
+                if (lane < boxes) {
+                    const int key = (t << PT_TILE_LOG) + lane * bp;
+                    y = ((load_page(p.r, shift, p.c.n_pages, k.seq, key, status) * n_kv + k.kvh) << shift) + (key & ps_mask);
+                }
+                if (g >= PT_KSTAGES && !warp_wait(k_empty(kb), ((g / PT_KSTAGES) - 1) & 1, status)) { ok = false; break; }
+                if (lane == 0) mbar_arrive_expect_tx(k_full(kb), boxes * bp * DH * 2);
+                __syncwarp();
+                if (lane < boxes)
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) tma_load_2d(k_s(kb) + h * L::KV_HALF + lane * bp * 128, &tmap_k, h * 64, y, k_full(kb));
+                if (g >= PT_VSTAGES && !warp_wait(v_empty(vb), ((g / PT_VSTAGES) - 1) & 1, status)) { ok = false; break; }
+                if (lane == 0) mbar_arrive_expect_tx(v_full(vb), boxes * bp * DH * 2);
+                __syncwarp();
+                if (lane < boxes)
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) tma_load_2d(v_s(vb) + h * L::KV_HALF + lane * bp * 128, &tmap_v, h * 64, y, v_full(vb));
+            }
+        } while (ok && next());
+    }
+    }
+    if (!ok) *failed = 1;
+
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (*failed) {
+        if (tid == 0) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+        const long long t0 = clock64();  // let copies and products in flight land
+        while (clock64() - t0 < 2000000LL) {
+        }
+        __syncthreads();
+    }
+    if (warp == 12) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, PT_TMEM_COLS);
+    }
+}
+
+template <int DH, int DTYPE>
+cudaError_t tc_init() {
+    return cudaFuncSetAttribute(paged_tc_kernel<DH, DTYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(PtSmem<DH, DTYPE>::TOTAL));
+}
+template <int DH, int DTYPE>
+cudaError_t tc_launch(const PagedAttnParams& p, int grid, cudaStream_t stream) {
+    CUtensorMap tk = {}, tv = {};
+    if (DTYPE == VERILLM_KV_BF16) {
+        const uint64_t rows = static_cast<uint64_t>(p.c.n_pages) * p.c.n_kv_heads << p.c.page_shift;
+        const uint32_t box = static_cast<uint32_t>(1 << p.c.page_shift) < PT_TILE ? 1u << p.c.page_shift : PT_TILE;
+        if (make_tmap_bf16_2d(&tk, p.c.k, rows, DH, DH, box) != 0 || make_tmap_bf16_2d(&tv, p.c.v, rows, DH, DH, box) != 0) return cudaErrorInvalidValue;
+    }
+    paged_tc_kernel<DH, DTYPE><<<grid, PT_THREADS, PtSmem<DH, DTYPE>::TOTAL, stream>>>(tk, tv, p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t paged_attention_tc_init() {
+    cudaError_t e = tc_init<64, VERILLM_KV_BF16>();
+    if (e == cudaSuccess) e = tc_init<64, VERILLM_KV_E4M3>();
+    if (e == cudaSuccess) e = tc_init<64, VERILLM_KV_INT8>();
+    if (e == cudaSuccess) e = tc_init<128, VERILLM_KV_BF16>();
+    if (e == cudaSuccess) e = tc_init<128, VERILLM_KV_E4M3>();
+    if (e == cudaSuccess) e = tc_init<128, VERILLM_KV_INT8>();
+    return e;
+}
+
+cudaError_t launch_paged_attention_tc(const PagedAttnParams& p, int grid, cudaStream_t stream) {
+    const bool wide = p.c.head_dim == 128;
+    if (p.c.dtype == VERILLM_KV_BF16) return wide ? tc_launch<128, VERILLM_KV_BF16>(p, grid, stream) : tc_launch<64, VERILLM_KV_BF16>(p, grid, stream);
+    if (p.c.dtype == VERILLM_KV_E4M3) return wide ? tc_launch<128, VERILLM_KV_E4M3>(p, grid, stream) : tc_launch<64, VERILLM_KV_E4M3>(p, grid, stream);
+    return wide ? tc_launch<128, VERILLM_KV_INT8>(p, grid, stream) : tc_launch<64, VERILLM_KV_INT8>(p, grid, stream);
+}
+
+}  // namespace vl

@@ -136,6 +136,10 @@ ATTEND = [  # heads, kv heads, head_dim, page, rows, kv
     (2, 1, 128, 16, [1], [5000]),                               # one long sequence over many CTAs
     (8, 1, 128, 64, [200], [1500]),
     (32, 1, 64, 16, [3], [333]),                                # 32 query heads on one kv head
+    (128, 1, 64, 32, [1, 5], [200, 100]),                       # 128: the most
+    (4, 4, 128, 256, [260, 129], [1000, 129]),                  # many tokens per block, a page longer than a tile
+    (14, 2, 64, 16, [300, 31, 2], [300, 2000, 513]),            # blocks that do not fill their rows
+    (32, 8, 128, 64, [64], [8192]),                             # one block whose tiles lie in many CTAs
 ]
 
 
