@@ -236,7 +236,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         }
         for (int b = 0; b < PT_VSTAGES; ++b) {
             mbar_init(v_full(b), BF16 ? 1 : 4);
-            mbar_init(v_empty(b), 2);
+            mbar_init(v_empty(b), BF16 ? 2 + 4 : 2);  // the issuers; the cleaning warps
             mbar_init(v_clean(b), 4);
         }
         for (int s = 0; s < PT_SCALES; ++s) mbar_init(sc_full(s), 4);
@@ -327,8 +327,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                 const int lim = pos - key0;  // visible: column <= lim
                 const float* ks = sc_k + (g % PT_SCALES) * 256;
                 const float* vs = ks + 128;
-                if (!BF16 && !warp_wait(sc_full(g % PT_SCALES), (g / PT_SCALES) & 1, status)) { ok = false; break; }
                 if (!warp_wait(s_full(w), sg & 1, status)) { ok = false; break; }
+                // (after the scores: a group that skipped blocks would misread the phase of a slot it has not reached;
+                // now it has completed, and cannot complete again before this group's probabilities)
+                if (!BF16 && !warp_wait(sc_full(g % PT_SCALES), (g / PT_SCALES) & 1, status)) { ok = false; break; }
                 tc_fence_after();
                 uint32_t v0[32], v1[32];
                 // 32 scores of columns [c, c + 32): key scales, then the mask
@@ -518,8 +520,13 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             do {
                 const Part u = part_of(k, p.tb_log, G);
                 for (int t = k.t0; t < k.t1; ++t, ++g) {
-                    if (!u.masked(t)) continue;
+                    // every tile is awaited and released here too, masked or not: a phase parity says nothing to a
+                    // thread that skipped phases
                     if (!warp_wait(v_full(g % PT_VSTAGES), (g / PT_VSTAGES) & 1, status)) { ok = false; break; }
+                    if (!u.masked(t)) {
+                        if (lane == 0) mbar_arrive(v_empty(g % PT_VSTAGES));
+                        continue;
+                    }
                     const uint32_t row = v_s(g % PT_VSTAGES) + ht * 128;
                     const bool gone = (t << PT_TILE_LOG) + ht >= u.end;
                     bool found = false;
@@ -547,7 +554,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                     if (found) *stray = 1;
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(v_clean(g % PT_VSTAGES));
+                    if (lane == 0) {
+                        mbar_arrive(v_clean(g % PT_VSTAGES));
+                        mbar_arrive(v_empty(g % PT_VSTAGES));
+                    }
                 }
             } while (ok && next());
         } else {

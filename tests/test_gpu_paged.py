@@ -174,6 +174,26 @@ def test_attention_over_many_sequences(dtype):
     assert_within(got[:used].reshape(used, c.H, c.dh), ref[:used], tol[:used])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,kv_heads,dh,page,batch,most_rows,most_kv", [
+    (16, 8, 64, 16, 40, 300, 500),     # several blocks per CTA, many with one group of rows only
+    (16, 4, 128, 32, 24, 70, 1600),    # many tiles per CTA
+    (64, 8, 128, 64, 12, 100, 900),
+])
+def test_chunks_of_a_large_batch(heads, kv_heads, dh, page, batch, most_rows, most_kv, dtype):
+    rng = np.random.default_rng(7)
+    kv = rng.integers(most_kv // 3, most_kv + 1, size=batch)
+    rows = np.minimum(rng.integers(1, most_rows + 1, size=batch), kv)
+    rows[0] = most_rows
+    c = Case(dtype, heads, kv_heads, dh, page, rows.tolist(), kv.tolist(), seed=21)
+    cache, rows_d = c.device()
+    got = vb.op_attention_paged(c.dq, cache, rows_d)
+    rows_d.check()
+    ref, tol, _, _ = c.attention()
+    used = int(c.cu[-1])
+    assert_within(got[:used].reshape(used, c.H, c.dh), ref[:used], tol[:used])
+
+
 @pytest.mark.parametrize("rows,kv", [([1, 2], [100, 40]), ([6, 40], [100, 40])])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_non_finite_entries_reach_exactly_the_rows_that_see_them(dtype, rows, kv):
