@@ -11,7 +11,8 @@
 //                   they also bring the block's queries into shared memory and write the results
 //   warps 8-11      bf16 cache: clean the values of tiles on the diagonal; 8-bit cache: fetch the codes of the next tile
 //                   into registers, widen them and store them as operand tiles
-//   warps 12, 13    one thread each issues the group's S = Q K^T and O += P V (tcgen05.mma)
+//   warp 12         one thread issues S = Q K^T and O += P V of both groups (tcgen05.mma)
+//   warp 13         walks the CTA's share of the work and hands the parts out
 //   warp 14         bf16 cache: TMA loads of keys and values, one box per page, a lane per page
 // The 64-column halves of all operand tiles use the 128-byte swizzle; values are consumed as they lie in memory
 // ([key][dh], an MN-major B operand).  The scores are read from tensor memory twice, once for the maximum and
@@ -116,6 +117,31 @@ __device__ __forceinline__ void stg32(void* p, const uint32_t (&r)[8]) {
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, int* status) {
     return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, status));
 }
+// The issuing warp runs converged, with operands in warp-uniform registers, and one elected lane issues: fewer
+// instructions per product than a lone lane, whose operands have to be moved to uniform registers each time.
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t leader, uint32_t bar) {
+    asm volatile(
+        "{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar), "r"(leader)
+        : "memory");
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
 template <int N>
 __device__ __forceinline__ void set_registers(bool more) {
     if (more) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
@@ -139,22 +165,16 @@ __device__ __forceinline__ uint2 widen4_half(uint32_t w) {
 
 __device__ __forceinline__ bool odd_bf16(uint32_t bits16) { return (bits16 & 0x7F80u) == 0x7F80u; }
 
-// The part of a block that a CTA works on, as all its warps see it.
+// The part of a block that a CTA works on, as the roles see it.  One warp walks the CTA's share and hands the parts
+// out through a small ring in shared memory, which keeps the walk out of everybody else's registers.
 struct Part {
-    int row0, first_pos, rows, end;  // packed row of the first token, its position, rows, end of the visible keys
-    int mask_tile;                   // first tile that some row may not see entirely
-    __device__ __forceinline__ bool masked(int tile) const { return tile >= mask_tile; }
+    int row0, first_pos, rows, seq;  // packed row of the first token, its position, packed rows (0: no more parts), sequence
+    int kvh, t0, t1, whole;          // kv head, tiles, whether these are all of the block's
+    __device__ __forceinline__ int end(int group) const { return first_pos + rows / group; }  // of the visible keys
+    // first tile that some row may not see entirely: the tiles before it end at or before first_pos
+    __device__ __forceinline__ int mask_tile() const { return first_pos < 0 ? 0 : (first_pos + 1) >> PT_TILE_LOG; }
 };
-__device__ __forceinline__ Part part_of(const BlockWalk& k, int tb_log, int group) {
-    Part u;
-    const int tok0 = k.j << tb_log, toks = min(1 << tb_log, k.s.n - tok0);
-    u.row0 = k.s.row0 + tok0;
-    u.first_pos = k.s.len - k.s.n + tok0;
-    u.rows = toks * group;
-    u.end = u.first_pos + toks;
-    u.mask_tile = u.first_pos < 0 ? 0 : (u.first_pos + 1) >> PT_TILE_LOG;  // tiles before it end at or before first_pos
-    return u;
-}
+constexpr int PT_PARTS = 4;  // ring of parts
 
 // Which of the 32 columns from col0 on receive a NaN, +inf or -inf from values of keys [from, to) that are not finite.
 struct Stray {
@@ -190,7 +210,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     constexpr int HALVES = DH / 64;
     extern __shared__ __align__(1024) uint8_t pt_smem[];
     const uint32_t sbase = smem_u32(pt_smem);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     if ((sbase & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
         if (tid == 0) {
             raise_status(p.status, VERILLM_DEV_WAIT_TIMEOUT);
@@ -213,11 +233,14 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     auto v_empty = [&](int b) { return bar + 176 + 8 * b; };
     auto sc_full = [&](int s) { return bar + 208 + 8 * s; };
     auto v_clean = [&](int b) { return bar + 232 + 8 * b; };
-    const uint32_t tmem_slot = bar + 256;
-    volatile uint32_t* tmem_slot_ptr = reinterpret_cast<volatile uint32_t*>(pt_smem + L::BAR_OFF + 256);
-    volatile int* failed = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 260);
-    volatile int* stray = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 264);        // some value was taken out so far
-    volatile float* sc_vref = reinterpret_cast<volatile float*>(pt_smem + L::BAR_OFF + 272);  // [PT_SCALES]
+    auto part_full = [&](int i) { return bar + 248 + 8 * i; };
+    auto part_empty = [&](int i) { return bar + 280 + 8 * i; };
+    const uint32_t tmem_slot = bar + 312;
+    volatile uint32_t* tmem_slot_ptr = reinterpret_cast<volatile uint32_t*>(pt_smem + L::BAR_OFF + 312);
+    volatile int* failed = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 316);
+    volatile int* stray = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 320);        // some value was taken out so far
+    volatile float* sc_vref = reinterpret_cast<volatile float*>(pt_smem + L::BAR_OFF + 328);  // [PT_SCALES]
+    int4* parts = reinterpret_cast<int4*>(pt_smem + L::BAR_OFF + 352);                        // [PT_PARTS][2]
     ShareScratch* scratch = reinterpret_cast<ShareScratch*>(pt_smem + L::BAR_OFF + 512);
 
     if (tid == 0) {
@@ -232,14 +255,18 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         }
         for (int b = 0; b < PT_KSTAGES; ++b) {
             mbar_init(k_full(b), BF16 ? 1 : 4);
-            mbar_init(k_empty(b), 2);
+            mbar_init(k_empty(b), 1);
         }
         for (int b = 0; b < PT_VSTAGES; ++b) {
             mbar_init(v_full(b), BF16 ? 1 : 4);
-            mbar_init(v_empty(b), BF16 ? 2 + 4 : 2);  // the issuers; the cleaning warps
+            mbar_init(v_empty(b), BF16 ? 1 + 4 : 1);  // the issuer; the cleaning warps
             mbar_init(v_clean(b), 4);
         }
         for (int s = 0; s < PT_SCALES; ++s) mbar_init(sc_full(s), 4);
+        for (int i = 0; i < PT_PARTS; ++i) {
+            mbar_init(part_full(i), 1);
+            mbar_init(part_empty(i), BF16 ? 14 : 13);  // one arrival per reading warp
+        }
         fence_mbar_init();
     }
     WorkShare share;
@@ -256,17 +283,38 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem_base = *tmem_slot_ptr;
+    // All 512 columns are this CTA's, so they begin at 0 (known to the compiler); anything else is refused.
+    constexpr uint32_t tmem_base = 0;
+    if (*tmem_slot_ptr != tmem_base) {
+        raise_status(p.status, VERILLM_DEV_WAIT_TIMEOUT);
+        *failed = 1;
+    }
+    __syncthreads();
     int* status = p.status;
     const int shift = p.c.page_shift, ps_mask = (1 << shift) - 1, n_kv = p.c.n_kv_heads, G = p.group;
 
-    // Every role walks the same blocks; g counts the CTA's tiles (stage g % stages, phase g / stages).
-    BlockWalk k;
-    walk_begin<PT_TILE_LOG>(p.r, shift, p.tb_log, share, k);
-    auto next = [&]() { return walk_next<PT_TILE_LOG>(p.r, shift, n_kv, p.tb_log, share, k); };
-    bool ok = true;
+    // Every role goes through the same parts; g counts the CTA's tiles (stage g % stages, phase g / stages).
+    // take_part: the next part, read by whole warps; false at the end or when a wait gave up.
+    auto take_part = [&](int& n, Part& u) -> bool {
+        const int i = n % PT_PARTS;
+        if (!warp_wait(part_full(i), (n / PT_PARTS) & 1, status)) {
+            *failed = 1;
+            return false;
+        }
+        const int4 a = parts[2 * i], b = parts[2 * i + 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(part_empty(i));
+        ++n;
+        u.row0 = a.x; u.first_pos = a.y; u.rows = a.z; u.seq = a.w;
+        u.kvh = b.x; u.t0 = b.y; u.t1 = b.z; u.whole = b.w;
+        return u.rows != 0;
+    };
+    int np = 0;
+    Part u;
+    bool ok = *failed == 0;
 
-    if (warp < 8) {
+    if (!ok) {
+    } else if (warp < 8) {
         // ------------------------------------------------------------ softmax, one row per thread
         set_registers<PT_REGS_SOFTMAX>(true);
         const int w = warp >> 2;
@@ -274,16 +322,15 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         const uint32_t lane_base = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         const uint32_t s_addr = lane_base + w * 128, o_addr = lane_base + 256 + w * 128;
         const float sl2 = rsqrtf(static_cast<float>(DH)) * kLog2e;
-        int4 header = make_int4(0, 0, 0, 0);
-        int g = 0, sg = 0, au = 0;  // tiles of the CTA, tiles and blocks of this group
-        do {
-            const Part u = part_of(k, p.tb_log, G);
+        int g = 0, sg = 0, au = 0;  // tiles of the CTA, tiles and parts of this group
+        while (take_part(np, u)) {
+            const int mask_tile = u.mask_tile();
             if (w * PT_GROUP_ROWS >= u.rows) {  // this group has no rows in the block
-                g += k.t1 - k.t0;
+                g += u.t1 - u.t0;
                 continue;
             }
             const bool valid = r < u.rows;
-            const int tok = valid ? r / G : 0, hd = k.kvh * G + (valid ? r - tok * G : 0);
+            const int tok = valid ? r / G : 0, hd = u.kvh * G + (valid ? r - tok * G : 0);
             const int pos = valid ? u.first_pos + tok : -1;  // last visible key
             float rf = sl2;  // factor of the scores in log2 units
             {   // ---- the row's queries into the swizzled operand tile.  The group's last Q K^T has completed: its
@@ -321,9 +368,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             }
             float m_ref = -INFINITY, l_run = 0.f, vref = 0.f;
             const float2 rf2 = make_float2(rf, rf);
-            for (int t = k.t0; t < k.t1; ++t, ++g, ++sg) {
+            for (int t = u.t0; t < u.t1; ++t, ++g, ++sg) {
                 const int key0 = t << PT_TILE_LOG;
-                const bool masked = u.masked(t);
+                const bool masked = t >= mask_tile;
                 const int lim = pos - key0;  // visible: column <= lim
                 const float* ks = sc_k + (g % PT_SCALES) * 256;
                 const float* vs = ks + 128;
@@ -389,7 +436,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                         l_run *= c;
                         m_ref = mx;
                     }
-                    if (t != k.t0) {  // O holds the earlier tiles: this tile's scores were issued after their P V
+                    if (t != u.t0) {  // O holds the earlier tiles: this tile's scores were issued after their P V
 #pragma unroll 1
                         for (int c = 0; c < DH / 32; ++c) {
                             uint32_t o[32];
@@ -453,10 +500,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             if (!warp_wait(o_done(w), au & 1, status)) { ok = false; break; }
             tc_fence_after();
             // ---- results: the whole block's, or this part's for the join
-            const bool whole = k.t0 == 0 && k.t1 == k.tiles;
-            if (!whole && k.t0 == 0)
-                header = make_int4(static_cast<int>((k.at + k.tiles - 1) / share.per) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
-            float* part = part_slot(p.part, 2 * static_cast<int>(blockIdx.x) + (k.t0 == 0 ? 1 : 0), PT_ROWS, DH);
+            const bool whole = u.whole != 0;
+            float* part = part_slot(p.part, 2 * static_cast<int>(blockIdx.x) + (u.t0 == 0 ? 1 : 0), PT_ROWS, DH);
             const float inv = (whole ? (l_run == 0.f ? 0.f : 1.f / l_run) : 1.f) * (BF16 ? 1.f : vref);
             const bool odd = *stray != 0;
             const size_t row = static_cast<size_t>(u.row0 + tok);
@@ -476,8 +521,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = l_run == 0.f ? 0u : __float_as_uint(__uint_as_float(o[i]) * inv);
                 if (odd) {
-                    const Stray x = find_stray<DH, DTYPE>(p, k.seq, k.kvh, max(k.t0, u.mask_tile) << PT_TILE_LOG,
-                                                          min(pos + 1, k.t1 << PT_TILE_LOG), c * 32);
+                    const Stray x = find_stray<DH, DTYPE>(p, u.seq, u.kvh, max(u.t0, mask_tile) << PT_TILE_LOG,
+                                                          min(pos + 1, u.t1 << PT_TILE_LOG), c * 32);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         if ((x.nan >> i) & 1u) o[i] = 0x7FC00000u;
@@ -509,26 +554,25 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                 __syncwarp();
             }
             ++au;
-        } while (next());
-        if (w == 0 && tid == 0) p.hdr[blockIdx.x] = ok ? header : make_int4(0, 0, 0, 0);
+        }
     } else if (warp < 12) {
         set_registers<PT_REGS_HELPER>(false);
         const int ht = tid - 256;  // thread of the helper group
         int g = 0;
         if (BF16) {
             // ------------------------------------------------------------ clean the values of masked tiles
-            do {
-                const Part u = part_of(k, p.tb_log, G);
-                for (int t = k.t0; t < k.t1; ++t, ++g) {
+            while (ok && take_part(np, u)) {
+                const int mask_tile = u.mask_tile(), end = u.end(G);
+                for (int t = u.t0; t < u.t1; ++t, ++g) {
                     // every tile is awaited and released here too, masked or not: a phase parity says nothing to a
                     // thread that skipped phases
                     if (!warp_wait(v_full(g % PT_VSTAGES), (g / PT_VSTAGES) & 1, status)) { ok = false; break; }
-                    if (!u.masked(t)) {
+                    if (t < mask_tile) {
                         if (lane == 0) mbar_arrive(v_empty(g % PT_VSTAGES));
                         continue;
                     }
                     const uint32_t row = v_s(g % PT_VSTAGES) + ht * 128;
-                    const bool gone = (t << PT_TILE_LOG) + ht >= u.end;
+                    const bool gone = (t << PT_TILE_LOG) + ht >= end;
                     bool found = false;
 #pragma unroll
                     for (int h = 0; h < HALVES; ++h)
@@ -559,7 +603,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                         mbar_arrive(v_empty(g % PT_VSTAGES));
                     }
                 }
-            } while (ok && next());
+            }
         } else {
             // ------------------------------------------------------------ fetch and widen the codes
             constexpr int CPR = DH / 16;              // 16-byte pieces of a vector
@@ -568,14 +612,15 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             const int c = ht % CPR, r0 = ht / CPR;
             uint4 rk[NP], rv[NP];
             float ks = 0.f, vs = 0.f, vq[4] = {0.f, 0.f, 0.f, 0.f};  // scales of this thread's key; value scales of four of the tile's keys
+            int end = 0;
             // pages of the tile's 16-position groups, one per lane (8 of them), fetched a tile ahead
             auto pages_of = [&](int tile, int end) {
                 const int key = (tile << PT_TILE_LOG) + (lane & 7) * 16;
-                return key < end ? load_page(p.r, shift, p.c.n_pages, k.seq, key, status) : 0;
+                return key < end ? load_page(p.r, shift, p.c.n_pages, u.seq, key, status) : 0;
             };
             auto vec_at = [&](int pages, int key) -> size_t {
                 const int page = __shfl_sync(0xFFFFFFFFu, pages, (key >> 4) & 7);
-                return ((static_cast<size_t>(page) * n_kv + k.kvh) << shift) + (key & ps_mask);
+                return ((static_cast<size_t>(page) * n_kv + u.kvh) << shift) + (key & ps_mask);
             };
             auto fetch = [&](uint4 (&x)[NP], const void* pool, int pages, int tile, int end) {
 #pragma unroll
@@ -607,17 +652,21 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                     sts16(base + (((c16 + 1) ^ (row & 7)) << 4), make_uint4(d.x, d.y, e.x, e.y));
                 }
             };
-            Part u = part_of(k, p.tb_log, G);
-            int pages = pages_of(k.t0, u.end);
-            fetch(rk, p.c.k, pages, k.t0, u.end);
-            fetch_scales(pages, k.t0, u.end);
-            fetch(rv, p.c.v, pages, k.t0, u.end);
-            bool more = true;
+            bool more = take_part(np, u);
+            end = u.end(G);
+            int pages = 0;
+            if (more) {
+                pages = pages_of(u.t0, end);
+                fetch(rk, p.c.k, pages, u.t0, end);
+                fetch_scales(pages, u.t0, end);
+                fetch(rv, p.c.v, pages, u.t0, end);
+            }
             while (more && ok) {
                 float vref = 0.f;
-                for (int t = k.t0; t < k.t1; ++t, ++g) {
+                const int t1 = u.t1, mask_tile = u.mask_tile();
+                for (int t = u.t0; t < t1; ++t, ++g) {
                     const int kb = g % PT_KSTAGES, vb = g % PT_VSTAGES, slot = g % PT_SCALES;
-                    const bool masked = u.masked(t);
+                    const bool masked = t >= mask_tile;
                     if (g >= PT_KSTAGES && !warp_wait(k_empty(kb), ((g / PT_KSTAGES) - 1) & 1, status)) { ok = false; break; }
                     // the slot's previous scales belong to tile g - KSTAGES - 1, whose probabilities preceded the
                     // product that freed this key stage
@@ -645,27 +694,27 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                         mbar_arrive(k_full(kb));
                     }
                     // the next tile: of this block, or the first of the next one
-                    const bool last = t + 1 == k.t1;
+                    const bool last = t + 1 == t1;
                     int nt = t + 1;
                     if (last) {
-                        more = next();
+                        more = take_part(np, u);
                         if (more) {
-                            u = part_of(k, p.tb_log, G);
-                            nt = k.t0;
+                            end = u.end(G);
+                            nt = u.t0;
                         }
                     }
                     const bool fetch_next = !last || more;
                     if (fetch_next) {
-                        pages = pages_of(nt, u.end);
-                        fetch(rk, p.c.k, pages, nt, u.end);
-                        fetch_scales(pages, nt, u.end);
+                        pages = pages_of(nt, end);
+                        fetch(rk, p.c.k, pages, nt, end);
+                        fetch_scales(pages, nt, end);
                     }
                     if (g >= PT_VSTAGES && !warp_wait(v_empty(vb), ((g / PT_VSTAGES) - 1) & 1, status)) { ok = false; break; }
                     widen(rv, v_s(vb));
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(v_full(vb));
-                    if (fetch_next) fetch(rv, p.c.v, pages, nt, u.end);
+                    if (fetch_next) fetch(rv, p.c.v, pages, nt, end);
                     if (last) {
                         ++g;
                         break;
@@ -675,76 +724,91 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         }
     } else {
         set_registers<PT_REGS_ISSUE>(false);
-        if (warp < 14) {
-        // ------------------------------------------------------------ product issuer of one group (one thread)
-        if (lane == 0) {
-            const int w = warp - 12;
-            const uint32_t s_tmem = tmem_base + w * 128, o_tmem = tmem_base + 256 + w * 128;
-            const uint64_t q_desc = umma_desc_k_sw128(q_s + w * PT_GROUP_ROWS * 128);
+        if (warp == 12) {
+        // ------------------------------------------------------------ product issuer (one warp)
+        // One warp issues for both groups, P V of a tile and Q K^T of the next back to back, group after group: the
+        // groups then work in opposite phases, one on its exponentials while the other's products run.  (With an issuer
+        // per group the two fell into step: both waited for the products, then both for the exponentials.)
+        {
             constexpr uint32_t idesc_s = pt_idesc(BF16, PT_TILE, false), idesc_o = pt_idesc(BF16, DH, true);
-            int g = 0, sg = 0, au = 0;  // tiles of the CTA, of this group; its blocks
-            uint32_t clean = 0;         // phase of each value stage's cleaning
-            do {
-                const Part u = part_of(k, p.tb_log, G);
-                const bool active = w * PT_GROUP_ROWS < u.rows;
-                if (active && !mbar_wait(q_full(w), au & 1, status)) { ok = false; break; }
-                for (int t = k.t0; t < k.t1; ++t, ++g) {
-                    const int kb = g % PT_KSTAGES, vb = g % PT_VSTAGES;
-                    if (!mbar_wait(k_full(kb), (g / PT_KSTAGES) & 1, status)) { ok = false; break; }
-                    if (!active) {  // the stages count both groups
-                        mbar_arrive(k_empty(kb));
-                        if (!mbar_wait(v_full(vb), (g / PT_VSTAGES) & 1, status)) { ok = false; break; }
-                        mbar_arrive(v_empty(vb));
-                        if (BF16 && u.masked(t)) clean ^= 1u << vb;
-                        continue;
-                    }
-                    tc_fence_after();
-                    const uint64_t kd = umma_desc_k_sw128(k_s(kb));
+            const uint64_t q_desc = umma_desc_k_sw128(q_s);
+            const uint32_t leader = elect_one();
+            int g = 0, sg[2] = {0, 0}, au[2] = {0, 0};  // tiles of the CTA; tiles and blocks of each group
+            uint32_t clean = 0;                         // phase of each value stage's cleaning
+            while (take_part(np, u)) {
+                const int mask_tile = uniform(u.mask_tile()), t0 = uniform(u.t0), t1 = uniform(u.t1);
+                const int groups = uniform(u.rows) > PT_GROUP_ROWS ? 2 : 1;
+                auto scores = [&](int w, int gt) {  // S of group w = Q K^T of the CTA's tile gt
+                    const uint32_t s_tmem = w * 128;
+                    const uint64_t qd = q_desc + static_cast<uint64_t>(w * ((PT_GROUP_ROWS * 128) >> 4));
+                    const uint64_t kd = umma_desc_k_sw128(k_s(gt % PT_KSTAGES));
 #pragma unroll
                     for (int s = 0; s < DH / 16; ++s)
-                        umma_bf16(s_tmem, q_desc + static_cast<uint64_t>((s / 4) * (L::Q_HALF >> 4) + 2 * (s % 4)),
+                        mma_ss(leader, s_tmem, qd + static_cast<uint64_t>((s / 4) * (L::Q_HALF >> 4) + 2 * (s % 4)),
                                   kd + static_cast<uint64_t>((s / 4) * (L::KV_HALF >> 4) + 2 * (s % 4)), idesc_s, s != 0 ? 1u : 0u);
-                    umma_commit(s_full(w));
-                    umma_commit(k_empty(kb));
-                    if (!mbar_wait(v_full(vb), (g / PT_VSTAGES) & 1, status)) { ok = false; break; }
-                    if (BF16 && u.masked(t)) {
-                        if (!mbar_wait(v_clean(vb), (clean >> vb) & 1u, status)) { ok = false; break; }
+                    mma_commit(leader, s_full(w));
+                };
+                if (!warp_wait(k_full(g % PT_KSTAGES), (g / PT_KSTAGES) & 1, status)) { ok = false; break; }
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    if (w >= groups) break;
+                    if (!warp_wait(q_full(w), au[w] & 1, status)) { ok = false; break; }
+                    tc_fence_after();
+                    scores(w, g);
+                    ++au[w];
+                }
+                if (!ok) break;
+                mma_commit(leader, k_empty(g % PT_KSTAGES));
+                for (int t = t0; t < t1; ++t, ++g) {
+                    const int vb = g % PT_VSTAGES;
+                    const bool more = t + 1 < t1;
+                    if (!warp_wait(v_full(vb), (g / PT_VSTAGES) & 1, status)) { ok = false; break; }
+                    if (BF16 && t >= mask_tile) {
+                        if (!warp_wait(v_clean(vb), (clean >> vb) & 1u, status)) { ok = false; break; }
                         clean ^= 1u << vb;
                     }
+                    if (more && !warp_wait(k_full((g + 1) % PT_KSTAGES), ((g + 1) / PT_KSTAGES) & 1, status)) { ok = false; break; }
                     const uint64_t vd = pt_desc_mn(v_s(vb), L::KV_HALF);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {  // keys 64 - 127 first
-                        if (!mbar_wait(p_half(w, h), sg & 1, status)) { ok = false; break; }
-                        tc_fence_after();
+                    for (int w = 0; w < 2; ++w) {
+                        if (w >= groups) break;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int s = (h == 0 ? 4 : 0) + i;
-                            umma_bf16_ts(o_tmem, s_tmem + 64 + s * 8, vd + static_cast<uint64_t>(s * (2048 >> 4)), idesc_o,
-                                         t == k.t0 && h == 0 && i == 0 ? 0u : 1u);
+                        for (int h = 0; h < 2; ++h) {  // keys 64 - 127 first
+                            if (!warp_wait(p_half(w, h), sg[w] & 1, status)) { ok = false; break; }
+                            tc_fence_after();
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int s = (h == 0 ? 4 : 0) + i;
+                                mma_ts(leader, 256 + w * 128, w * 128 + 64 + s * 8, vd + static_cast<uint64_t>(s * (2048 >> 4)), idesc_o,
+                                             t == t0 && h == 0 && i == 0 ? 0u : 1u);
+                            }
                         }
+                        if (!ok) break;
+                        ++sg[w];
+                        if (more) scores(w, g + 1);
+                        else mma_commit(leader, o_done(w));
                     }
                     if (!ok) break;
-                    umma_commit(v_empty(vb));
-                    if (t + 1 == k.t1) umma_commit(o_done(w));
-                    ++sg;
+                    mma_commit(leader, v_empty(vb));
+                    if (more) mma_commit(leader, k_empty((g + 1) % PT_KSTAGES));
                 }
-                if (active) ++au;
-            } while (ok && next());
+                if (!ok) break;
+            }
         }
         } else if (BF16 && warp == 14) {
         // ------------------------------------------------------------ TMA producer: one box per page, a lane each
         const int bp = min(1 << shift, PT_TILE);  // positions per box
         int g = 0;
-        do {
-            const Part u = part_of(k, p.tb_log, G);
-            for (int t = k.t0; t < k.t1; ++t, ++g) {
+        while (ok && take_part(np, u)) {
+            const int end = u.end(G);
+            for (int t = u.t0; t < u.t1; ++t, ++g) {
                 const int kb = g % PT_KSTAGES, vb = g % PT_VSTAGES;
-                const int left = u.end - (t << PT_TILE_LOG);
+                const int left = end - (t << PT_TILE_LOG);
                 const int boxes = left <= 0 ? 0 : (min(left, PT_TILE) + bp - 1) / bp;
                 int y = 0;
                 if (lane < boxes) {
                     const int key = (t << PT_TILE_LOG) + lane * bp;
-                    y = ((load_page(p.r, shift, p.c.n_pages, k.seq, key, status) * n_kv + k.kvh) << shift) + (key & ps_mask);
+                    y = ((load_page(p.r, shift, p.c.n_pages, u.seq, key, status) * n_kv + u.kvh) << shift) + (key & ps_mask);
                 }
                 if (g >= PT_KSTAGES && !warp_wait(k_empty(kb), ((g / PT_KSTAGES) - 1) & 1, status)) { ok = false; break; }
                 if (lane == 0) mbar_arrive_expect_tx(k_full(kb), boxes * bp * DH * 2);
@@ -759,8 +823,36 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
 #pragma unroll
                     for (int h = 0; h < HALVES; ++h) tma_load_2d(v_s(vb) + h * L::KV_HALF + lane * bp * 128, &tmap_v, h * 64, y, v_full(vb));
             }
-        } while (ok && next());
-    }
+        }
+        } else if (warp == 13) {
+        // ------------------------------------------------------------ hands out the parts
+        BlockWalk k;
+        walk_begin<PT_TILE_LOG>(p.r, shift, p.tb_log, share, k);
+        int4 header = make_int4(0, 0, 0, 0);
+        bool more = true;
+        for (int n = 0; ok; ++n) {
+            const int i = n % PT_PARTS;
+            if (n >= PT_PARTS && !warp_wait(part_empty(i), ((n / PT_PARTS) - 1) & 1, status)) { ok = false; break; }
+            if (more) {
+                const int tok0 = k.j << p.tb_log;
+                const bool whole = k.t0 == 0 && k.t1 == k.tiles;
+                if (!whole && k.t0 == 0)
+                    header = make_int4(static_cast<int>((k.at + k.tiles - 1) / share.per) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
+                if (lane == 0) {
+                    parts[2 * i] = make_int4(k.s.row0 + tok0, k.s.len - k.s.n + tok0, min(1 << p.tb_log, k.s.n - tok0) * G, k.seq);
+                    parts[2 * i + 1] = make_int4(k.kvh, k.t0, k.t1, whole ? 1 : 0);
+                }
+            } else if (lane == 0) {
+                parts[2 * i] = make_int4(0, 0, 0, 0);
+                parts[2 * i + 1] = make_int4(0, 0, 0, 0);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(part_full(i));
+            if (!more) break;
+            more = walk_next<PT_TILE_LOG>(p.r, shift, n_kv, p.tb_log, share, k);
+        }
+        if (lane == 0) p.hdr[blockIdx.x] = header;
+        }
     }
     if (!ok) *failed = 1;
 
@@ -776,7 +868,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     }
     if (warp == 12) {
         tc_fence_after();
-        tmem_dealloc(tmem_base, PT_TMEM_COLS);
+        tmem_dealloc(*tmem_slot_ptr, PT_TMEM_COLS);
     }
 }
 
