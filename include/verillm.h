@@ -302,7 +302,7 @@ enum { VERILLM_KV_BF16 = 0, VERILLM_KV_E4M3 = 1, VERILLM_KV_INT8 = 2 };
 
 typedef struct {
     void *k, *v;               /* DEVICE [n_pages][n_kv_heads][page_size][head_dim], bf16 or 8-bit; 16-byte aligned */
-    float *k_scale, *v_scale;  /* DEVICE [n_pages][n_kv_heads][page_size]; 8-bit pools only, else NULL */
+    float *k_scale, *v_scale;  /* DEVICE [n_pages][n_kv_heads][page_size]; 8-bit pools only, else NULL; 16-byte aligned */
     int32_t n_pages;
     int32_t page_size;         /* 16, 32, 64, 128 or 256 */
     int32_t n_kv_heads, head_dim; /* head_dim 64 or 128 */
@@ -344,7 +344,7 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  *  q         DEVICE bf16, n_heads * head_dim entries per row, q_stride entries from row to row, already rotated
  *  out       DEVICE bf16, same form with out_stride; a row that attends to nothing receives zeros
  *  lse       optional DEVICE float32 [n_rows][n_heads]: log of the sum of exp(scores), -inf for such a row
- *  workspace DEVICE, 16-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code).
+ *  workspace DEVICE, 256-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code).
  *            It holds nothing between calls, but calls that may overlap (other streams, graphs replayed side by side)
  *            need one each.
  * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 128 per kv head; workspace too

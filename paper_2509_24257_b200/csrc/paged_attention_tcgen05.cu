@@ -7,7 +7,7 @@
 // While one group's four warps exponentiate a tile, the other group's products run.
 //   warps 0-3, 4-7  softmax of the two groups, one row per thread: scores from tensor memory, running reference maximum
 //                   and sum in registers, probabilities back as 16-bit pairs over the upper half of the score columns
-//                   (each half as soon as it is complete, so that P V starts under the second half's exponentials);
+//                   (three quarters first, so that most of P V runs under the last quarter's exponentials);
 //                   they also bring the block's queries into shared memory and write the results
 //   warps 8-11      bf16 cache: clean the values of tiles on the diagonal; 8-bit cache: fetch the codes of the next tile
 //                   into registers, widen them and store them as operand tiles
@@ -15,8 +15,7 @@
 //   warp 13         walks the CTA's share of the work and hands the parts out
 //   warp 14         bf16 cache: TMA loads of keys and values, one box per page, a lane per page
 // The 64-column halves of all operand tiles use the 128-byte swizzle; values are consumed as they lie in memory
-// ([key][dh], an MN-major B operand).  The scores are read from tensor memory twice, once for the maximum and
-// once for the exponentials, which keeps a row's 128 scores out of registers.
+// ([key][dh], an MN-major B operand).
 //
 // 8-bit caches: both code types are exact in fp16, so keys and values are widened to fp16 and both products
 // are fp16; queries are scaled row by row by a power of two to fit.  Key scales multiply the fp32 scores.  Value scales
@@ -43,8 +42,9 @@ constexpr int PT_KSTAGES = 2, PT_VSTAGES = 2, PT_SCALES = PT_KSTAGES + 1;
 constexpr int PT_TMEM_COLS = 512;  // S of the groups at 0 and 128, O at 256 and 384
 constexpr float PT_RAISE_LOG2 = 8.f;
 // registers per thread of the roles; together what 512 threads are launched with (128 each)
-constexpr int PT_REGS_SOFTMAX = 168, PT_REGS_HELPER = 112, PT_REGS_ISSUE = 64;
-static_assert(2 * PT_REGS_SOFTMAX + PT_REGS_HELPER + PT_REGS_ISSUE <= 4 * 128, "");
+constexpr int PT_REGS_SOFTMAX = 192, PT_REGS_OTHER = 64;
+static_assert(2 * PT_REGS_SOFTMAX + 2 * PT_REGS_OTHER <= 4 * 128, "");
+constexpr int PT_RAW = 3;  // half tiles of codes on their way
 // value scales relative to their reference lie in (.., 2^7]: with probabilities up to 2^8 the product stays below 2^15
 constexpr float PT_VREF_MAX = 128.f;
 
@@ -58,7 +58,9 @@ struct PtSmem {
     static constexpr uint32_t V_OFF = K_OFF + PT_KSTAGES * KV_BYTES;
     static constexpr uint32_t SC_OFF = V_OFF + PT_VSTAGES * KV_BYTES;  // per slot: 128 key scales, 128 value scales
     static constexpr uint32_t SC_BYTES = 2 * PT_TILE * 4;
-    static constexpr uint32_t BAR_OFF = SC_OFF + (BF16 ? 0 : PT_SCALES * SC_BYTES);
+    static constexpr uint32_t RAW_OFF = SC_OFF + (BF16 ? 0 : PT_SCALES * SC_BYTES);
+    static constexpr uint32_t RAW_BYTES = PT_TILE / 2 * DH;  // codes of half a tile
+    static constexpr uint32_t BAR_OFF = RAW_OFF + (BF16 ? 0 : PT_RAW * RAW_BYTES);
     static constexpr uint32_t TOTAL = BAR_OFF + 512 + sizeof(ShareScratch);
 };
 
@@ -152,9 +154,9 @@ __device__ __forceinline__ void set_registers(bool more) {
 template <int DTYPE>
 __device__ __forceinline__ uint2 widen4_half(uint32_t w) {
     if (DTYPE == VERILLM_KV_E4M3) {
-        const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w & 0xFFFFu), __NV_E4M3);
-        const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w >> 16), __NV_E4M3);
-        return make_uint2(a.x | (static_cast<uint32_t>(a.y) << 16), b.x | (static_cast<uint32_t>(b.y) << 16));
+        uint2 h;
+        asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}\n" : "=r"(h.x), "=r"(h.y) : "r"(w));
+        return h;
     }
     const uint32_t u = w ^ 0x80808080u;
     const __half2 off = __half2half2(__ushort_as_half(static_cast<unsigned short>(0x6480)));  // 1152
@@ -323,49 +325,62 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         const uint32_t s_addr = lane_base + w * 128, o_addr = lane_base + 256 + w * 128;
         const float sl2 = rsqrtf(static_cast<float>(DH)) * kLog2e;
         int g = 0, sg = 0, au = 0;  // tiles of the CTA, tiles and parts of this group
-        while (take_part(np, u)) {
-            const int mask_tile = u.mask_tile();
-            if (w * PT_GROUP_ROWS >= u.rows) {  // this group has no rows in the block
+        // the row's place in the current part: packed row, query head, last visible key
+        bool valid = false;
+        size_t row = 0;
+        int hd = 0, pos = -1;
+        float rf = sl2;  // factor of the scores in log2 units
+        auto next_part = [&]() {  // the next part in which this group has rows
+            while (take_part(np, u)) {
+                if (w * PT_GROUP_ROWS < u.rows) return true;
                 g += u.t1 - u.t0;
-                continue;
             }
-            const bool valid = r < u.rows;
-            const int tok = valid ? r / G : 0, hd = u.kvh * G + (valid ? r - tok * G : 0);
-            const int pos = valid ? u.first_pos + tok : -1;  // last visible key
-            float rf = sl2;  // factor of the scores in log2 units
-            {   // ---- the row's queries into the swizzled operand tile.  The group's last Q K^T has completed: its
-                // scores were read above.
-                const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) +
-                                                                  static_cast<size_t>(u.row0 + tok) * p.q_stride + static_cast<size_t>(hd) * DH);
-                const uint32_t dst = q_s + r * 128;
-                if (BF16) {
+            return false;
+        };
+        auto fetch_q = [&](uint4 (&qx)[DH / 8]) {
+            valid = r < u.rows;
+            const int tok = valid ? r / G : 0;
+            hd = u.kvh * G + (valid ? r - tok * G : 0);
+            row = static_cast<size_t>(u.row0 + tok);
+            pos = valid ? u.first_pos + tok : -1;
+            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) + row * p.q_stride + static_cast<size_t>(hd) * DH);
 #pragma unroll
-                    for (int h = 0; h < HALVES; ++h)
+            for (int c = 0; c < DH / 8; ++c) qx[c] = __ldg(src + c);
+        };
+        // into the swizzled operand tile, whose previous contents have been used: the scores of the last tile were read
+        auto store_q = [&](uint4 (&qx)[DH / 8]) {
+            const uint32_t dst = q_s + r * 128;
+            if (!BF16) {
+                uint32_t mx = 0;
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) sts16(dst + h * L::Q_HALF + ((c ^ (r & 7)) << 4), __ldg(src + 8 * h + c));
-                } else {
-                    uint4 x[DH / 8];
-                    uint32_t mx = 0;
+                for (int c = 0; c < DH / 8; ++c)
+                    mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(qx[c].x & 0x7FFF7FFFu, qx[c].y & 0x7FFF7FFFu), __vmaxu2(qx[c].z & 0x7FFF7FFFu, qx[c].w & 0x7FFF7FFFu)));
+                // |q| 2^(127 - e) lies in [1, 2), e the exponent field of the row's largest entry
+                const uint32_t e = min(max(max(mx >> 16, mx & 0xFFFFu) >> 7, 1u), 253u);
+                const float down = __uint_as_float((254u - e) << 23);
+                rf = sl2 * __uint_as_float(e << 23);
 #pragma unroll
-                    for (int c = 0; c < DH / 8; ++c) {
-                        x[c] = __ldg(src + c);
-                        mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(x[c].x & 0x7FFF7FFFu, x[c].y & 0x7FFF7FFFu), __vmaxu2(x[c].z & 0x7FFF7FFFu, x[c].w & 0x7FFF7FFFu)));
-                    }
-                    // |q| 2^(127 - e) lies in [1, 2), e the exponent field of the row's largest entry
-                    const uint32_t e = min(max(max(mx >> 16, mx & 0xFFFFu) >> 7, 1u), 253u);
-                    const float down = __uint_as_float((254u - e) << 23);
-                    rf = sl2 * __uint_as_float(e << 23);
-#pragma unroll
-                    for (int c = 0; c < DH / 8; ++c) {
-                        const uint4 y = make_uint4(pack_half(bf16_lo(x[c].x) * down, bf16_hi(x[c].x) * down), pack_half(bf16_lo(x[c].y) * down, bf16_hi(x[c].y) * down),
-                                                   pack_half(bf16_lo(x[c].z) * down, bf16_hi(x[c].z) * down), pack_half(bf16_lo(x[c].w) * down, bf16_hi(x[c].w) * down));
-                        sts16(dst + (c >> 3) * L::Q_HALF + (((c & 7) ^ (r & 7)) << 4), y);
-                    }
+                for (int c = 0; c < DH / 8; ++c) {
+                    const uint4 x = qx[c];
+                    qx[c] = make_uint4(pack_half(bf16_lo(x.x) * down, bf16_hi(x.x) * down), pack_half(bf16_lo(x.y) * down, bf16_hi(x.y) * down),
+                                       pack_half(bf16_lo(x.z) * down, bf16_hi(x.z) * down), pack_half(bf16_lo(x.w) * down, bf16_hi(x.w) * down));
                 }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(q_full(w));
             }
+#pragma unroll
+            for (int c = 0; c < DH / 8; ++c) sts16(dst + (c >> 3) * L::Q_HALF + (((c & 7) ^ (r & 7)) << 4), qx[c]);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full(w));
+        };
+        const bool wide_out = ((reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(p.out_stride * 2)) & 31u) == 0;
+        bool have = next_part();
+        if (have) {
+            uint4 qx[DH / 8];
+            fetch_q(qx);
+            store_q(qx);
+        }
+        while (have) {
+            const int mask_tile = u.mask_tile();
             float m_ref = -INFINITY, l_run = 0.f, vref = 0.f;
             const float2 rf2 = make_float2(rf, rf);
             for (int t = u.t0; t < u.t1; ++t, ++g, ++sg) {
@@ -379,7 +394,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                 // now it has completed, and cannot complete again before this group's probabilities)
                 if (!BF16 && !warp_wait(sc_full(g % PT_SCALES), (g / PT_SCALES) & 1, status)) { ok = false; break; }
                 tc_fence_after();
-                uint32_t v0[32], v1[32];
+                uint32_t v0[32], v1[32], v2[32], v3[32];
                 // 32 scores of columns [c, c + 32): key scales, then the mask
                 auto prepare = [&](uint32_t (&v)[32], int c) {
                     if (!BF16) {
@@ -403,20 +418,21 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                 float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 tmem_ld32(s_addr, v0);
                 tmem_ld32(s_addr + 32, v1);
+                tmem_ld32(s_addr + 64, v2);
+                tmem_ld32(s_addr + 96, v3);
                 tmem_ld_wait_regs(v0);
                 tmem_ld_wait_regs(v1);
+                tmem_ld_wait_regs(v2);
+                tmem_ld_wait_regs(v3);
                 prepare(v0, 0);
                 prepare(v1, 32);
+                prepare(v2, 64);
+                prepare(v3, 96);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) mx4[i & 3] = pt_max3(mx4[i & 3], __uint_as_float(v0[i]), __uint_as_float(v1[i]));
-                tmem_ld32(s_addr + 64, v0);
-                tmem_ld32(s_addr + 96, v1);
-                tmem_ld_wait_regs(v0);
-                tmem_ld_wait_regs(v1);
-                prepare(v0, 64);
-                prepare(v1, 96);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) mx4[i & 3] = pt_max3(mx4[i & 3], __uint_as_float(v0[i]), __uint_as_float(v1[i]));
+                for (int i = 0; i < 32; ++i) {
+                    mx4[i & 1] = pt_max3(mx4[i & 1], __uint_as_float(v0[i]), __uint_as_float(v1[i]));
+                    mx4[2 + (i & 1)] = pt_max3(mx4[2 + (i & 1)], __uint_as_float(v2[i]), __uint_as_float(v3[i]));
+                }
                 const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * rf;
                 const bool grow = valid && mx > m_ref + PT_RAISE_LOG2;
                 float corr = 1.f;
@@ -482,32 +498,36 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                     __syncwarp();
                     if (lane == 0) mbar_arrive(p_half(w, h));
                 };
-                probabilities(v0, 64);
-                tmem_ld32(s_addr, v0);
-                probabilities(v1, 96);
-                tmem_ld32(s_addr + 32, v1);
-                deliver(0);
-                tmem_ld_wait_regs(v0);
-                tmem_ld_wait_regs(v1);
-                prepare(v0, 0);
-                probabilities(v0, 0);
-                prepare(v1, 32);
+                probabilities(v3, 96);
+                probabilities(v2, 64);
                 probabilities(v1, 32);
+                deliver(0);
+                probabilities(v0, 0);
                 deliver(1);
                 l_run += (rs2[0].x + rs2[0].y) + (rs2[1].x + rs2[1].y);
             }
             if (!ok) break;
-            if (!warp_wait(o_done(w), au & 1, status)) { ok = false; break; }
-            tc_fence_after();
-            // ---- results: the whole block's, or this part's for the join
-            const bool whole = u.whole != 0;
+            // ---- results: the whole block's, or this part's for the join.  The next part's queries go first, so that
+            // its first scores are formed under the output pass.
+            const bool whole = u.whole != 0, row_valid = valid;
+            const size_t out_row = row;
+            const int out_hd = hd, seq = u.seq, kvh = u.kvh;
+            const int odd_from = max(u.t0, mask_tile) << PT_TILE_LOG, odd_to = min(pos + 1, u.t1 << PT_TILE_LOG);
             float* part = part_slot(p.part, 2 * static_cast<int>(blockIdx.x) + (u.t0 == 0 ? 1 : 0), PT_ROWS, DH);
+            have = next_part();
+            uint4 qx[DH / 8];
+#pragma unroll
+            for (int c = 0; c < DH / 8; ++c) qx[c] = make_uint4(0u, 0u, 0u, 0u);
+            if (have) fetch_q(qx);
+            if (!warp_wait(o_done(w), au & 1, status)) { ok = false; break; }
+            ++au;
+            tc_fence_after();
+            if (have) store_q(qx);
             const float inv = (whole ? (l_run == 0.f ? 0.f : 1.f / l_run) : 1.f) * (BF16 ? 1.f : vref);
             const bool odd = *stray != 0;
-            const size_t row = static_cast<size_t>(u.row0 + tok);
-            if (valid) {
+            if (row_valid) {
                 if (whole) {
-                    if (p.lse) p.lse[row * p.n_heads + hd] = l_run == 0.f ? -INFINITY : m_ref * kLn2 + logf(l_run);
+                    if (p.lse) p.lse[out_row * p.n_heads + out_hd] = l_run == 0.f ? -INFINITY : m_ref * kLn2 + logf(l_run);
                 } else {
                     part[r] = m_ref;
                     part[PT_ROWS + r] = l_run;
@@ -521,8 +541,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = l_run == 0.f ? 0u : __float_as_uint(__uint_as_float(o[i]) * inv);
                 if (odd) {
-                    const Stray x = find_stray<DH, DTYPE>(p, u.seq, u.kvh, max(u.t0, mask_tile) << PT_TILE_LOG,
-                                                          min(pos + 1, u.t1 << PT_TILE_LOG), c * 32);
+                    const Stray x = find_stray<DH, DTYPE>(p, seq, kvh, odd_from, odd_to, c * 32);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         if ((x.nan >> i) & 1u) o[i] = 0x7FC00000u;
@@ -530,18 +549,20 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                         if ((x.ninf >> i) & 1u) o[i] = __float_as_uint(__uint_as_float(o[i]) - INFINITY);
                     }
                 }
-                if (valid && whole) {
-                    __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + row * p.out_stride + static_cast<size_t>(hd) * DH + c * 32;
+                if (row_valid && whole) {
+                    __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + out_row * p.out_stride + static_cast<size_t>(out_hd) * DH + c * 32;
+                    uint32_t y[2][8];
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        uint4 y;
-                        y.x = pack_bf16(__uint_as_float(o[8 * h]), __uint_as_float(o[8 * h + 1]));
-                        y.y = pack_bf16(__uint_as_float(o[8 * h + 2]), __uint_as_float(o[8 * h + 3]));
-                        y.z = pack_bf16(__uint_as_float(o[8 * h + 4]), __uint_as_float(o[8 * h + 5]));
-                        y.w = pack_bf16(__uint_as_float(o[8 * h + 6]), __uint_as_float(o[8 * h + 7]));
-                        reinterpret_cast<uint4*>(dst)[h] = y;
+                    for (int i = 0; i < 16; ++i) y[i >> 3][i & 7] = pack_bf16(__uint_as_float(o[2 * i]), __uint_as_float(o[2 * i + 1]));
+                    if (wide_out) {
+                        stg32(dst, y[0]);
+                        stg32(dst + 16, y[1]);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h)
+                            reinterpret_cast<uint4*>(dst)[h] = make_uint4(y[h >> 1][4 * (h & 1)], y[h >> 1][4 * (h & 1) + 1], y[h >> 1][4 * (h & 1) + 2], y[h >> 1][4 * (h & 1) + 3]);
                     }
-                } else if (valid) {
+                } else if (row_valid) {
                     float* dst = part + 2 * PT_ROWS + r * DH + c * 32;
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
@@ -553,10 +574,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                 }
                 __syncwarp();
             }
-            ++au;
         }
     } else if (warp < 12) {
-        set_registers<PT_REGS_HELPER>(false);
+        set_registers<PT_REGS_OTHER>(false);
         const int ht = tid - 256;  // thread of the helper group
         int g = 0;
         if (BF16) {
@@ -606,124 +626,141 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             }
         } else {
             // ------------------------------------------------------------ fetch and widen the codes
-            constexpr int CPR = DH / 16;              // 16-byte pieces of a vector
-            constexpr int RPP = 128 / CPR;            // rows per pass over the 128 threads
-            constexpr int NP = PT_TILE / RPP;         // passes per tile
+            // Half tiles (64 keys' codes, then 64 more, then the values) are copied asynchronously into a ring; a thread
+            // widens the pieces that it copied itself, so the ring needs no barriers.
+            constexpr int CPR = DH / 16;                     // 16-byte pieces of a vector
+            constexpr int RPP = 128 / CPR;                   // rows per pass over the 128 threads
+            constexpr int NP = (PT_TILE / 2) / RPP;          // passes per half tile
             const int c = ht % CPR, r0 = ht / CPR;
-            uint4 rk[NP], rv[NP];
-            float ks = 0.f, vs = 0.f, vq[4] = {0.f, 0.f, 0.f, 0.f};  // scales of this thread's key; value scales of four of the tile's keys
-            int end = 0;
-            // pages of the tile's 16-position groups, one per lane (8 of them), fetched a tile ahead
-            auto pages_of = [&](int tile, int end) {
+            const uint32_t raw = sbase + L::RAW_OFF + ht * 16;
+            // The copy's cursor runs PT_RAW half tiles ahead of the widening.
+            bool more = take_part(np, u);
+            int end = more ? u.end(G) : 0, mask_tile = u.mask_tile(), ft = u.t0, fq = 0, issued = 0;
+            int pages = 0, pages_ahead = 0;  // pages of the tile's 16-position groups, one per lane (8 of them): this tile's and the next one's
+            float4 ks4 = make_float4(0.f, 0.f, 0.f, 0.f), vs4 = ks4;  // scales of keys 4 lane .. 4 lane + 3: every warp looks at all 128 of a tile
+            bool masked = false, first = false;                       // of the tile whose scales these are
+            auto pages_of = [&](int tile) {
                 const int key = (tile << PT_TILE_LOG) + (lane & 7) * 16;
                 return key < end ? load_page(p.r, shift, p.c.n_pages, u.seq, key, status) : 0;
             };
-            auto vec_at = [&](int pages, int key) -> size_t {
+            auto vec_at = [&](int key) -> size_t {
                 const int page = __shfl_sync(0xFFFFFFFFu, pages, (key >> 4) & 7);
                 return ((static_cast<size_t>(page) * n_kv + u.kvh) << shift) + (key & ps_mask);
             };
-            auto fetch = [&](uint4 (&x)[NP], const void* pool, int pages, int tile, int end) {
+            if (more) pages_ahead = pages_of(ft);
+            auto issue = [&]() {
+                if (more) {
+                    const int key0 = ft << PT_TILE_LOG;
+                    if (fq == 0) {
+                        pages = pages_ahead;
+                        first = ft == u.t0;
+                        masked = ft >= mask_tile;
+                        const int key = key0 + 4 * lane;
+                        const size_t vec = vec_at(key);
+                        ks4 = vs4 = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (key < end) {
+                            ks4 = __ldg(reinterpret_cast<const float4*>(p.c.k_scale + vec));
+                            vs4 = __ldg(reinterpret_cast<const float4*>(p.c.v_scale + vec));
+                            if (key + 4 > end) {  // behind the last key: whatever the page holds
+                                if (key + 1 >= end) ks4.y = vs4.y = 0.f;
+                                if (key + 2 >= end) ks4.z = vs4.z = 0.f;
+                                ks4.w = vs4.w = 0.f;
+                            }
+                        }
+                        if (ft + 1 < u.t1) pages_ahead = pages_of(ft + 1);
+                    }
+                    const char* pool = reinterpret_cast<const char*>(fq < 2 ? p.c.k : p.c.v) + c * 16;
+                    const uint32_t dst = raw + (issued % PT_RAW) * L::RAW_BYTES;
 #pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const int key = (tile << PT_TILE_LOG) + i * RPP + r0;
-                    const size_t vec = vec_at(pages, key);
-                    x[i] = key < end ? __ldg(reinterpret_cast<const uint4*>(pool) + vec * CPR + c) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int i = 0; i < NP; ++i) {
+                        const int key = key0 + (fq & 1) * (PT_TILE / 2) + i * RPP + r0;
+                        const size_t vec = vec_at(key);
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + i * 2048), "l"(pool + vec * DH), "r"(key < end ? 16 : 0) : "memory");
+                    }
+                    ++issued;
+                    if (++fq == 4) {
+                        fq = 0;
+                        if (++ft == u.t1) {
+                            more = take_part(np, u);
+                            if (more) {
+                                end = u.end(G);
+                                mask_tile = u.mask_tile();
+                                ft = u.t0;
+                                pages_ahead = pages_of(ft);
+                            }
+                        }
+                    }
                 }
+                asm volatile("cp.async.commit_group;" ::: "memory");  // (empty at the end, so that the waits keep counting)
             };
-            auto fetch_scales = [&](int pages, int tile, int end) {
-                const int key = (tile << PT_TILE_LOG) + ht;
-                const size_t vec = vec_at(pages, key);
-                ks = key < end ? __ldg(p.c.k_scale + vec) : 0.f;
-                vs = key < end ? __ldg(p.c.v_scale + vec) : 0.f;
-                // every warp looks at all 128 value scales, so that the warps need not agree on their maximum
-                const int key4 = (tile << PT_TILE_LOG) + 4 * lane;
-                const size_t vec4 = vec_at(pages, key4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) vq[i] = key4 + i < end ? __ldg(p.c.v_scale + vec4 + i) : 0.f;
-            };
-            auto widen = [&](const uint4 (&x)[NP], uint32_t tile_smem) {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const int row = i * RPP + r0;
-                    const uint2 a = widen4_half<DTYPE>(x[i].x), b = widen4_half<DTYPE>(x[i].y), d = widen4_half<DTYPE>(x[i].z), e = widen4_half<DTYPE>(x[i].w);
-                    const uint32_t base = tile_smem + (c >> 2) * L::KV_HALF + row * 128;
-                    const int c16 = 2 * (c & 3);
-                    sts16(base + ((c16 ^ (row & 7)) << 4), make_uint4(a.x, a.y, b.x, b.y));
-                    sts16(base + (((c16 + 1) ^ (row & 7)) << 4), make_uint4(d.x, d.y, e.x, e.y));
-                }
-            };
-            bool more = take_part(np, u);
-            end = u.end(G);
-            int pages = 0;
-            if (more) {
-                pages = pages_of(u.t0, end);
-                fetch(rk, p.c.k, pages, u.t0, end);
-                fetch_scales(pages, u.t0, end);
-                fetch(rv, p.c.v, pages, u.t0, end);
-            }
-            while (more && ok) {
-                float vref = 0.f;
-                const int t1 = u.t1, mask_tile = u.mask_tile();
-                for (int t = u.t0; t < t1; ++t, ++g) {
-                    const int kb = g % PT_KSTAGES, vb = g % PT_VSTAGES, slot = g % PT_SCALES;
-                    const bool masked = t >= mask_tile;
+            for (int i = 0; i < PT_RAW; ++i) issue();
+            float vref = 0.f;
+            for (int n = 0; n < issued; ++n) {
+                const int q = n & 3, kb = g % PT_KSTAGES, vb = g % PT_VSTAGES, slot = g % PT_SCALES;
+                if (q == 0) {
                     if (g >= PT_KSTAGES && !warp_wait(k_empty(kb), ((g / PT_KSTAGES) - 1) & 1, status)) { ok = false; break; }
                     // the slot's previous scales belong to tile g - KSTAGES - 1, whose probabilities preceded the
                     // product that freed this key stage
-                    float v = vs;
-                    if (masked && !isfinite(v)) {
-                        v = 0.f;
-                        *stray = 1;
-                    }
+                    if (first) vref = 0.f;
                     float mx = 0.f;
+                    const float vq[4] = {vs4.x, vs4.y, vs4.z, vs4.w};
+                    bool bad = false;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mx = isfinite(vq[i]) ? fmaxf(mx, vq[i]) : mx;
+                    for (int i = 0; i < 4; ++i) {
+                        bad |= !isfinite(vq[i]);
+                        mx = isfinite(vq[i]) ? fmaxf(mx, vq[i]) : mx;
+                    }
+                    if (masked && bad) *stray = 1;
                     if (__any_sync(0xFFFFFFFFu, vref == 0.f || mx > vref * PT_VREF_MAX)) {
                         // 2^-6 of the power of two at or below the largest scale (scales are at least 2^-119)
                         const uint32_t e = max(__float_as_uint(warp_max(mx)) >> 23, 7u) - 6u;
                         vref = fmaxf(vref, __uint_as_float(e << 23));
                     }
-                    sc_k[slot * 256 + ht] = ks;
-                    sc_k[slot * 256 + 128 + ht] = v / vref;
-                    if (ht == 0) sc_vref[slot] = vref;
-                    widen(rk, k_s(kb));
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(sc_full(slot));
-                        mbar_arrive(k_full(kb));
-                    }
-                    // the next tile: of this block, or the first of the next one
-                    const bool last = t + 1 == t1;
-                    int nt = t + 1;
-                    if (last) {
-                        more = take_part(np, u);
-                        if (more) {
-                            end = u.end(G);
-                            nt = u.t0;
+                    if ((lane >> 3) == warp - 8) {  // each warp writes a quarter of what all four know
+                        const float up = 1.f / vref;  // a power of two, at most 2^126
+                        float4 v = make_float4(vq[0] * up, vq[1] * up, vq[2] * up, vq[3] * up);
+                        if (masked && bad) {
+                            if (!isfinite(vq[0])) v.x = 0.f;
+                            if (!isfinite(vq[1])) v.y = 0.f;
+                            if (!isfinite(vq[2])) v.z = 0.f;
+                            if (!isfinite(vq[3])) v.w = 0.f;
                         }
+                        *reinterpret_cast<float4*>(sc_k + slot * 256 + 4 * lane) = ks4;
+                        *reinterpret_cast<float4*>(sc_k + slot * 256 + 128 + 4 * lane) = v;
+                        if (lane == 0) sc_vref[slot] = vref;
                     }
-                    const bool fetch_next = !last || more;
-                    if (fetch_next) {
-                        pages = pages_of(nt, end);
-                        fetch(rk, p.c.k, pages, nt, end);
-                        fetch_scales(pages, nt, end);
-                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sc_full(slot));
+                } else if (q == 2) {
                     if (g >= PT_VSTAGES && !warp_wait(v_empty(vb), ((g / PT_VSTAGES) - 1) & 1, status)) { ok = false; break; }
-                    widen(rv, v_s(vb));
+                }
+                asm volatile("cp.async.wait_group %0;" ::"n"(PT_RAW - 1) : "memory");
+                const uint32_t src = raw + (n % PT_RAW) * L::RAW_BYTES;
+                const uint32_t tile_smem = q < 2 ? k_s(kb) : v_s(vb);
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    const uint4 x = lds16(src + i * 2048);
+                    const int row = (q & 1) * (PT_TILE / 2) + i * RPP + r0;
+                    const uint2 a = widen4_half<DTYPE>(x.x), b = widen4_half<DTYPE>(x.y), d = widen4_half<DTYPE>(x.z), e = widen4_half<DTYPE>(x.w);
+                    const uint32_t base = tile_smem + (c >> 2) * L::KV_HALF + row * 128;
+                    // the lanes of the second half store their pieces in the other order: 8 lanes then reach all banks
+                    const int c16 = 2 * (c & 3), sw = c >> 2;
+                    const uint4 lo = make_uint4(a.x, a.y, b.x, b.y), hi = make_uint4(d.x, d.y, e.x, e.y);
+                    sts16(base + (((c16 + sw) ^ (row & 7)) << 4), sw ? hi : lo);
+                    sts16(base + (((c16 + 1 - sw) ^ (row & 7)) << 4), sw ? lo : hi);
+                }
+                if (q & 1) {
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(v_full(vb));
-                    if (fetch_next) fetch(rv, p.c.v, pages, nt, end);
-                    if (last) {
-                        ++g;
-                        break;
-                    }
+                    if (lane == 0) mbar_arrive(q == 1 ? k_full(kb) : v_full(vb));
                 }
+                issue();
+                if (q == 3) ++g;
             }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
     } else {
-        set_registers<PT_REGS_ISSUE>(false);
+        set_registers<PT_REGS_OTHER>(false);
         if (warp == 12) {
         // ------------------------------------------------------------ product issuer (one warp)
         // One warp issues for both groups, P V of a tile and Q K^T of the next back to back, group after group: the
@@ -773,12 +810,12 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                     for (int w = 0; w < 2; ++w) {
                         if (w >= groups) break;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {  // keys 64 - 127 first
+                        for (int h = 0; h < 2; ++h) {  // keys 32 - 127 first
                             if (!warp_wait(p_half(w, h), sg[w] & 1, status)) { ok = false; break; }
                             tc_fence_after();
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int s = (h == 0 ? 4 : 0) + i;
+                            for (int i = 0; i < (h == 0 ? 6 : 2); ++i) {
+                                const int s = (h == 0 ? 2 : 0) + i;
                                 mma_ts(leader, 256 + w * 128, w * 128 + 64 + s * 8, vd + static_cast<uint64_t>(s * (2048 >> 4)), idesc_o,
                                              t == t0 && h == 0 && i == 0 ? 0u : 1u);
                             }

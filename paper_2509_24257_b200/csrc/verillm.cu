@@ -337,6 +337,7 @@ int check_paged(const verillm_kv_cache* c, const verillm_kv_rows* r, PagedCacheD
     if (static_cast<int64_t>(c->n_pages) * c->n_kv_heads * c->page_size > 0x7FFFFFFFLL) return VERILLM_E_SHAPE;
     if (static_cast<int64_t>(r->table_width) * c->page_size > (1LL << 30)) return VERILLM_E_SHAPE;  // positions in 32 bits
     if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 15u) return VERILLM_E_SHAPE;
+    if (c->dtype != VERILLM_KV_BF16 && ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 15u)) return VERILLM_E_SHAPE;
     cd->k = c->k; cd->v = c->v;
     cd->k_scale = c->dtype == VERILLM_KV_BF16 ? nullptr : c->k_scale;
     cd->v_scale = c->dtype == VERILLM_KV_BF16 ? nullptr : c->v_scale;
@@ -1126,7 +1127,7 @@ int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_r
     if (!workspace) return VERILLM_E_INVAL;
     if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
     p.group = n_heads / p.c.n_kv_heads;
-    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) ||
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) ||
         workspace_bytes < static_cast<int64_t>(paged_attention_workspace(p.c.head_dim, p.group, p.r.max_rows, sms)))
         return VERILLM_E_SHAPE;
     p.q = q; p.q_stride = q_stride; p.out = out; p.out_stride = out_stride; p.lse = lse; p.n_heads = n_heads; p.status = status;
