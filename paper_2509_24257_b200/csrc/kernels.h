@@ -72,6 +72,8 @@ struct GemmParams {
 // Maps are encoded for a box of 64 (K) x 128 rows (A) and 64 x 256 rows (B), 128-byte swizzle.
 int make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld_elems,
                       uint32_t box_rows);
+// A packed matrix of bytes, boxes of whole rows (cols <= 256, a multiple of 16), no swizzle.
+int make_tmap_bytes_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
 cudaError_t launch_gemm(int epilogue, const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const GemmParams& p,
                         int num_sms, cudaStream_t stream);
 cudaError_t gemm_init();  // raises the dynamic shared memory limit of every instantiation

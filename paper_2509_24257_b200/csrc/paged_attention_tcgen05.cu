@@ -9,18 +9,23 @@
 //                   and sum in registers, probabilities back as 16-bit pairs over the upper half of the score columns
 //                   (three quarters first, so that most of P V runs under the last quarter's exponentials);
 //                   they also bring the block's queries into shared memory and write the results
-//   warps 8-11      bf16 cache: clean the values of tiles on the diagonal; 8-bit cache: fetch the codes of the next tile
-//                   into registers, widen them and store them as operand tiles
+//   warps 8-11      bf16 cache: clean the values of tiles on the diagonal; 8-bit cache: widen the codes, half a tile at a
+//                   time, and store them as operand tiles
 //   warp 12         one thread issues S = Q K^T and O += P V of both groups (tcgen05.mma)
 //   warp 13         walks the CTA's share of the work and hands the parts out
-//   warp 14         bf16 cache: TMA loads of keys and values, one box per page, a lane per page
+//   warp 14         TMA loads of keys and values (8-bit cache: of codes into a ring of half tiles), a box and a lane per page
+//   warp 15         8-bit cache: the scales of the next tiles
 // The 64-column halves of all operand tiles use the 128-byte swizzle; values are consumed as they lie in memory
 // ([key][dh], an MN-major B operand).
 //
-// 8-bit caches: both code types are exact in fp16, so keys and values are widened to fp16 and both products
-// are fp16; queries are scaled row by row by a power of two to fit.  Key scales multiply the fp32 scores.  Value scales
-// multiply the probabilities, relative to a power of two that follows the largest scale seen in the block, so that the
-// product fits fp16; its rounding is 2^-11 relative (bf16's probabilities: 2^-8).
+// 8-bit caches: codes are widened to fp16 operands with their scales in them, so that the softmax is the same as for
+// bf16: an operand is code * scale / ref rounded once to fp16's 11 bits (bf16 keys and values have 8), with ref a
+// power of two that brings the tile's largest scale into [2^6, 2^7): at most 448 * 2^7 fits.  The keys' ref multiplies the
+// tile's scores; the values' ref is kept over the tiles of a block while it fits, and a larger one rescales the output.
+// Queries are scaled row by row by a power of two into [1, 2), probabilities are taken 2^6 above the reference (up to
+// 2^14), so that what fp16 cannot hold is below 2^-30 of the largest.  (Scales applied to the fp32 scores and
+// probabilities instead cost the softmax two shared-memory reads and two products per four entries, which it had to wait
+// for: 744 - 840 us for 1024 rows over 32768 positions.)
 //
 // Masked entries: scores are replaced by -inf.  Values behind the sequence's last position are whatever the page
 // holds and become 0.  An infinite or NaN value (or value scale) in a tile that some rows may not see entirely is
@@ -40,13 +45,14 @@ constexpr int PT_GROUP_ROWS = 128, PT_ROWS = 2 * PT_GROUP_ROWS;
 static_assert(PT_ROWS == kPagedTcRows, "");
 constexpr int PT_KSTAGES = 2, PT_VSTAGES = 2, PT_SCALES = PT_KSTAGES + 1;
 constexpr int PT_TMEM_COLS = 512;  // S of the groups at 0 and 128, O at 256 and 384
-constexpr float PT_RAISE_LOG2 = 8.f;
+// The reference maximum is raised when a score exceeds it by pt_raise (log2), to the score less pt_lift.
+constexpr float pt_raise(bool bf16) { return bf16 ? 8.f : 14.f; }
+constexpr float pt_lift(bool bf16) { return bf16 ? 0.f : 6.f; }
+constexpr float PT_REF_MAX = 128.f;  // largest scale in units of its reference
 // registers per thread of the roles; together what 512 threads are launched with (128 each)
 constexpr int PT_REGS_SOFTMAX = 192, PT_REGS_OTHER = 64;
 static_assert(2 * PT_REGS_SOFTMAX + 2 * PT_REGS_OTHER <= 4 * 128, "");
 constexpr int PT_RAW = 3;  // half tiles of codes on their way
-// value scales relative to their reference lie in (.., 2^7]: with probabilities up to 2^8 the product stays below 2^15
-constexpr float PT_VREF_MAX = 128.f;
 
 template <int DH, int DTYPE>
 struct PtSmem {
@@ -56,12 +62,12 @@ struct PtSmem {
     static constexpr uint32_t KV_BYTES = KV_HALF * (DH / 64);
     static constexpr uint32_t K_OFF = Q_HALF * (DH / 64);
     static constexpr uint32_t V_OFF = K_OFF + PT_KSTAGES * KV_BYTES;
-    static constexpr uint32_t SC_OFF = V_OFF + PT_VSTAGES * KV_BYTES;  // per slot: 128 key scales, 128 value scales
+    static constexpr uint32_t SC_OFF = V_OFF + PT_VSTAGES * KV_BYTES;  // per slot: 128 key and 128 value scales, a word each
     static constexpr uint32_t SC_BYTES = 2 * PT_TILE * 4;
     static constexpr uint32_t RAW_OFF = SC_OFF + (BF16 ? 0 : PT_SCALES * SC_BYTES);
     static constexpr uint32_t RAW_BYTES = PT_TILE / 2 * DH;  // codes of half a tile
     static constexpr uint32_t BAR_OFF = RAW_OFF + (BF16 ? 0 : PT_RAW * RAW_BYTES);
-    static constexpr uint32_t TOTAL = BAR_OFF + 512 + sizeof(ShareScratch);
+    static constexpr uint32_t TOTAL = BAR_OFF + 640 + sizeof(ShareScratch);
 };
 
 // MN-major operand (V as stored: [key][dh]): 64 columns of a key are a row of 128 bytes, 8 keys per 1024-byte swizzle
@@ -86,11 +92,6 @@ __device__ __forceinline__ float2 pt_fma2(float2 a, float2 b, float2 c) {
 __device__ __forceinline__ float2 pt_add2(float2 a, float2 b) {
     uint64_t d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
-    return reinterpret_cast<float2&>(d);
-}
-__device__ __forceinline__ float2 pt_mul2(float2 a, float2 b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
     return reinterpret_cast<float2&>(d);
 }
 __device__ __forceinline__ float pt_max3(float a, float b, float c) {
@@ -165,6 +166,17 @@ __device__ __forceinline__ uint2 widen4_half(uint32_t w) {
     return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
+// The same times a scale given as the sum of two fp16 numbers (both halves of sh, sl): code * sh + code * sl, rounded
+// once to fp16 but for the rounding of the small second product.
+template <int DTYPE>
+__device__ __forceinline__ uint2 scaled4(uint32_t w, uint32_t sh, uint32_t sl) {
+    const uint2 x = widen4_half<DTYPE>(w);
+    uint2 y;
+    asm("{\n.reg .b32 t;\nmul.rn.f16x2 t, %1, %3;\nfma.rn.f16x2 %0, %1, %2, t;\n}\n" : "=r"(y.x) : "r"(x.x), "r"(sh), "r"(sl));
+    asm("{\n.reg .b32 t;\nmul.rn.f16x2 t, %1, %3;\nfma.rn.f16x2 %0, %1, %2, t;\n}\n" : "=r"(y.y) : "r"(x.y), "r"(sh), "r"(sl));
+    return y;
+}
+
 __device__ __forceinline__ bool odd_bf16(uint32_t bits16) { return (bits16 & 0x7F80u) == 0x7F80u; }
 
 // The part of a block that a CTA works on, as the roles see it.  One warp walks the CTA's share and hands the parts
@@ -223,7 +235,6 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     const uint32_t q_s = sbase;
     auto k_s = [&](int b) { return sbase + L::K_OFF + b * L::KV_BYTES; };
     auto v_s = [&](int b) { return sbase + L::V_OFF + b * L::KV_BYTES; };
-    float* sc_k = reinterpret_cast<float*>(pt_smem + L::SC_OFF);  // slot s: [s * 256, + 128) keys, then values
     const uint32_t bar = sbase + L::BAR_OFF;
     auto q_full = [&](int w) { return bar + 8 * w; };
     auto s_full = [&](int w) { return bar + 16 + 8 * w; };
@@ -237,13 +248,18 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     auto v_clean = [&](int b) { return bar + 232 + 8 * b; };
     auto part_full = [&](int i) { return bar + 248 + 8 * i; };
     auto part_empty = [&](int i) { return bar + 280 + 8 * i; };
-    const uint32_t tmem_slot = bar + 312;
-    volatile uint32_t* tmem_slot_ptr = reinterpret_cast<volatile uint32_t*>(pt_smem + L::BAR_OFF + 312);
-    volatile int* failed = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 316);
-    volatile int* stray = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 320);        // some value was taken out so far
-    volatile float* sc_vref = reinterpret_cast<volatile float*>(pt_smem + L::BAR_OFF + 328);  // [PT_SCALES]
-    int4* parts = reinterpret_cast<int4*>(pt_smem + L::BAR_OFF + 352);                        // [PT_PARTS][2]
-    ShareScratch* scratch = reinterpret_cast<ShareScratch*>(pt_smem + L::BAR_OFF + 512);
+    auto raw_full = [&](int i) { return bar + 312 + 8 * i; };
+    auto raw_empty = [&](int i) { return bar + 336 + 8 * i; };
+    auto word_full = [&](int i) { return bar + 360 + 8 * i; };
+    auto word_empty = [&](int i) { return bar + 384 + 8 * i; };
+    const uint32_t tmem_slot = bar + 408;
+    volatile uint32_t* tmem_slot_ptr = reinterpret_cast<volatile uint32_t*>(pt_smem + L::BAR_OFF + 408);
+    volatile int* failed = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 412);
+    volatile int* stray = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 416);        // some value was taken out so far
+    volatile float* sc_ref = reinterpret_cast<volatile float*>(pt_smem + L::BAR_OFF + 424);   // [PT_SCALES][2]: refs of a tile's keys and values
+    volatile float* new_ref = reinterpret_cast<volatile float*>(pt_smem + L::BAR_OFF + 448);  // [PT_SCALES][2]: the same, beside the scale words
+    int4* parts = reinterpret_cast<int4*>(pt_smem + L::BAR_OFF + 480);                        // [PT_PARTS][2]
+    ShareScratch* scratch = reinterpret_cast<ShareScratch*>(pt_smem + L::BAR_OFF + 640);
 
     if (tid == 0) {
         *failed = 0;
@@ -264,10 +280,18 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             mbar_init(v_empty(b), BF16 ? 1 + 4 : 1);  // the issuer; the cleaning warps
             mbar_init(v_clean(b), 4);
         }
-        for (int s = 0; s < PT_SCALES; ++s) mbar_init(sc_full(s), 4);
+        for (int s = 0; s < PT_SCALES; ++s) {
+            mbar_init(sc_full(s), 1);
+            mbar_init(word_full(s), 1);
+            mbar_init(word_empty(s), 4);
+        }
+        for (int i = 0; i < PT_RAW; ++i) {
+            mbar_init(raw_full(i), 1);
+            mbar_init(raw_empty(i), 4);
+        }
         for (int i = 0; i < PT_PARTS; ++i) {
             mbar_init(part_full(i), 1);
-            mbar_init(part_empty(i), BF16 ? 14 : 13);  // one arrival per reading warp
+            mbar_init(part_empty(i), BF16 ? 14 : 15);  // one arrival per reading warp
         }
         fence_mbar_init();
     }
@@ -382,33 +406,22 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
         while (have) {
             const int mask_tile = u.mask_tile();
             float m_ref = -INFINITY, l_run = 0.f, vref = 0.f;
-            const float2 rf2 = make_float2(rf, rf);
             for (int t = u.t0; t < u.t1; ++t, ++g, ++sg) {
                 const int key0 = t << PT_TILE_LOG;
                 const bool masked = t >= mask_tile;
                 const int lim = pos - key0;  // visible: column <= lim
-                const float* ks = sc_k + (g % PT_SCALES) * 256;
-                const float* vs = ks + 128;
                 if (!warp_wait(s_full(w), sg & 1, status)) { ok = false; break; }
                 // (after the scores: a group that skipped blocks would misread the phase of a slot it has not reached;
                 // now it has completed, and cannot complete again before this group's probabilities)
                 if (!BF16 && !warp_wait(sc_full(g % PT_SCALES), (g / PT_SCALES) & 1, status)) { ok = false; break; }
                 tc_fence_after();
                 uint32_t v0[32], v1[32], v2[32], v3[32];
-                // 32 scores of columns [c, c + 32): key scales, then the mask
-                auto prepare = [&](uint32_t (&v)[32], int c) {
-                    if (!BF16) {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            const float4 s4 = *reinterpret_cast<const float4*>(ks + c + i);
-                            const float2 a = pt_mul2(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), make_float2(s4.x, s4.y));
-                            const float2 b = pt_mul2(make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])), make_float2(s4.z, s4.w));
-                            v[i] = __float_as_uint(a.x);
-                            v[i + 1] = __float_as_uint(a.y);
-                            v[i + 2] = __float_as_uint(b.x);
-                            v[i + 3] = __float_as_uint(b.y);
-                        }
-                    }
+                float rt = rf, vnew = 0.f;
+                if (!BF16) {
+                    rt = rf * sc_ref[2 * (g % PT_SCALES)];
+                    vnew = sc_ref[2 * (g % PT_SCALES) + 1];
+                }
+                auto prepare = [&](uint32_t (&v)[32], int c) {  // masks the scores of columns [c, c + 32)
                     if (masked) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
@@ -433,24 +446,21 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                     mx4[i & 1] = pt_max3(mx4[i & 1], __uint_as_float(v0[i]), __uint_as_float(v1[i]));
                     mx4[2 + (i & 1)] = pt_max3(mx4[2 + (i & 1)], __uint_as_float(v2[i]), __uint_as_float(v3[i]));
                 }
-                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * rf;
-                const bool grow = valid && mx > m_ref + PT_RAISE_LOG2;
+                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * rt;
+                const bool grow = valid && mx > m_ref + pt_raise(BF16);
                 float corr = 1.f;
                 bool fix = grow;
-                if (!BF16) {
-                    const float nv = sc_vref[g % PT_SCALES];
-                    if (nv != vref) {  // the same in all threads
-                        corr = vref / nv;
-                        vref = nv;
-                        fix = true;
-                    }
+                if (!BF16 && vnew != vref) {  // the same in all threads
+                    corr = vref / vnew;
+                    vref = vnew;
+                    fix = true;
                 }
                 if (__any_sync(0xFFFFFFFFu, fix)) {
                     if (grow) {
-                        const float c = exp2_fast(m_ref - mx);
+                        const float c = exp2_fast(m_ref - (mx - pt_lift(BF16)));
                         corr *= c;
                         l_run *= c;
-                        m_ref = mx;
+                        m_ref = mx - pt_lift(BF16);
                     }
                     if (t != u.t0) {  // O holds the earlier tiles: this tile's scores were issued after their P V
 #pragma unroll 1
@@ -466,29 +476,17 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                     }
                 }
                 const float nm = m_ref == -INFINITY ? 0.f : -m_ref;
-                const float2 nm2 = make_float2(nm, nm);
+                const float2 nm2 = make_float2(nm, nm), rt2 = make_float2(rt, rt);
                 float2 rs2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 // probabilities of columns [c, c + 32) as 16 packed columns over the upper half of the scores
                 auto probabilities = [&](const uint32_t (&v)[32], int c) {
                     uint32_t pk[16];
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        float2 e[2];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float2 x = pt_fma2(make_float2(__uint_as_float(v[2 * (i + h)]), __uint_as_float(v[2 * (i + h) + 1])), rf2, nm2);
-                            e[h] = make_float2(exp2_fast(x.x), exp2_fast(x.y));
-                            rs2[h] = pt_add2(rs2[h], e[h]);
-                        }
-                        if (BF16) {
-                            pk[i] = pack_bf16(e[0].x, e[0].y);
-                            pk[i + 1] = pack_bf16(e[1].x, e[1].y);
-                        } else {
-                            const float4 s4 = *reinterpret_cast<const float4*>(vs + c + 2 * i);
-                            const float2 a = pt_mul2(e[0], make_float2(s4.x, s4.y)), b = pt_mul2(e[1], make_float2(s4.z, s4.w));
-                            pk[i] = pack_half(a.x, a.y);
-                            pk[i + 1] = pack_half(b.x, b.y);
-                        }
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 x = pt_fma2(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), rt2, nm2);
+                        const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+                        rs2[i & 1] = pt_add2(rs2[i & 1], e);
+                        pk[i] = BF16 ? pack_bf16(e.x, e.y) : pack_half(e.x, e.y);
                     }
                     tmem_st16(s_addr + 64 + (c >> 1), pk);
                 };
@@ -625,139 +623,73 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                 }
             }
         } else {
-            // ------------------------------------------------------------ fetch and widen the codes
-            // Half tiles (64 keys' codes, then 64 more, then the values) are copied asynchronously into a ring; a thread
-            // widens the pieces that it copied itself, so the ring needs no barriers.
-            constexpr int CPR = DH / 16;                     // 16-byte pieces of a vector
-            constexpr int RPP = 128 / CPR;                   // rows per pass over the 128 threads
-            constexpr int NP = (PT_TILE / 2) / RPP;          // passes per half tile
+            // ------------------------------------------------------------ widen the codes, half a tile at a time
+            constexpr int CPR = DH / 16;             // 16-byte pieces of a vector
+            constexpr int RPP = 128 / CPR;           // rows per pass over the 128 threads
+            constexpr int NP = (PT_TILE / 2) / RPP;  // passes per half tile
             const int c = ht % CPR, r0 = ht / CPR;
-            const uint32_t raw = sbase + L::RAW_OFF + ht * 16;
-            // The copy's cursor runs PT_RAW half tiles ahead of the widening.
-            bool more = take_part(np, u);
-            int end = more ? u.end(G) : 0, mask_tile = u.mask_tile(), ft = u.t0, fq = 0, issued = 0;
-            int pages = 0, pages_ahead = 0;  // pages of the tile's 16-position groups, one per lane (8 of them): this tile's and the next one's
-            float4 ks4 = make_float4(0.f, 0.f, 0.f, 0.f), vs4 = ks4;  // scales of keys 4 lane .. 4 lane + 3: every warp looks at all 128 of a tile
-            bool masked = false, first = false;                       // of the tile whose scales these are
-            auto pages_of = [&](int tile) {
-                const int key = (tile << PT_TILE_LOG) + (lane & 7) * 16;
-                return key < end ? load_page(p.r, shift, p.c.n_pages, u.seq, key, status) : 0;
-            };
-            auto vec_at = [&](int key) -> size_t {
-                const int page = __shfl_sync(0xFFFFFFFFu, pages, (key >> 4) & 7);
-                return ((static_cast<size_t>(page) * n_kv + u.kvh) << shift) + (key & ps_mask);
-            };
-            if (more) pages_ahead = pages_of(ft);
-            auto issue = [&]() {
-                if (more) {
-                    const int key0 = ft << PT_TILE_LOG;
-                    if (fq == 0) {
-                        pages = pages_ahead;
-                        first = ft == u.t0;
-                        masked = ft >= mask_tile;
-                        const int key = key0 + 4 * lane;
-                        const size_t vec = vec_at(key);
-                        ks4 = vs4 = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (key < end) {
-                            ks4 = __ldg(reinterpret_cast<const float4*>(p.c.k_scale + vec));
-                            vs4 = __ldg(reinterpret_cast<const float4*>(p.c.v_scale + vec));
-                            if (key + 4 > end) {  // behind the last key: whatever the page holds
-                                if (key + 1 >= end) ks4.y = vs4.y = 0.f;
-                                if (key + 2 >= end) ks4.z = vs4.z = 0.f;
-                                ks4.w = vs4.w = 0.f;
+            int n = 0;  // half tiles so far
+            while (ok && take_part(np, u)) {
+                const int end = u.end(G);
+                for (int t = u.t0; t < u.t1 && ok; ++t, ++g) {
+                    const int kb = g % PT_KSTAGES, vb = g % PT_VSTAGES, slot = g % PT_SCALES;
+                    const int left = end - (t << PT_TILE_LOG);  // visible keys from the tile's first on
+                    const uint32_t words = sbase + L::SC_OFF + slot * L::SC_BYTES;
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q, ++n) {  // keys 0 - 63, 64 - 127, values 0 - 63, 64 - 127
+                        if (q == 0) {
+                            if (g >= PT_KSTAGES && !warp_wait(k_empty(kb), ((g / PT_KSTAGES) - 1) & 1, status)) { ok = false; break; }
+                            if (!warp_wait(word_full(slot), (g / PT_SCALES) & 1, status)) { ok = false; break; }
+                            // The refs go on to the softmax in a ring of their own: its slot's previous ones belong to tile
+                            // g - KSTAGES - 1, whose probabilities preceded the product that freed this key stage.
+                            if (warp == 8 && lane == 0) {
+                                sc_ref[2 * slot] = new_ref[2 * slot];
+                                sc_ref[2 * slot + 1] = new_ref[2 * slot + 1];
+                                mbar_arrive(sc_full(slot));
+                            }
+                        } else if (q == 2) {
+                            if (g >= PT_VSTAGES && !warp_wait(v_empty(vb), ((g / PT_VSTAGES) - 1) & 1, status)) { ok = false; break; }
+                        }
+                        if (!warp_wait(raw_full(n % PT_RAW), (n / PT_RAW) & 1, status)) { ok = false; break; }
+                        const uint32_t src = sbase + L::RAW_OFF + (n % PT_RAW) * L::RAW_BYTES + ht * 16;
+                        const uint32_t dst = (q < 2 ? k_s(kb) : v_s(vb)) + (c >> 2) * L::KV_HALF;
+                        const uint32_t ws = words + (q < 2 ? 0 : PT_TILE * 4);
+                        uint4 x[NP];
+                        uint32_t sw[NP];
+#pragma unroll
+                        for (int i = 0; i < NP; ++i) {
+                            x[i] = lds16(src + i * 2048);
+                            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sw[i]) : "r"(ws + ((q & 1) * (PT_TILE / 2) + i * RPP + r0) * 4) : "memory");
+                        }
+                        if (left < PT_TILE) {  // codes behind the last key are whatever the page holds, NaN codes too
+#pragma unroll
+                            for (int i = 0; i < NP; ++i)
+                                if ((q & 1) * (PT_TILE / 2) + i * RPP + r0 >= left) x[i] = make_uint4(0u, 0u, 0u, 0u);
+                        }
+#pragma unroll
+                        for (int i = 0; i < NP; ++i) {
+                            const int row = (q & 1) * (PT_TILE / 2) + i * RPP + r0;
+                            const uint32_t sh = __byte_perm(sw[i], 0u, 0x1010), sl = __byte_perm(sw[i], 0u, 0x3232);
+                            const uint2 a = scaled4<DTYPE>(x[i].x, sh, sl), b = scaled4<DTYPE>(x[i].y, sh, sl), d = scaled4<DTYPE>(x[i].z, sh, sl), e = scaled4<DTYPE>(x[i].w, sh, sl);
+                            // the lanes of the second half store their pieces in the other order: 8 lanes then reach all banks
+                            const int c16 = 2 * (c & 3), odd = c >> 2;
+                            const uint4 lo = make_uint4(a.x, a.y, b.x, b.y), hi = make_uint4(d.x, d.y, e.x, e.y);
+                            sts16(dst + row * 128 + (((c16 + odd) ^ (row & 7)) << 4), odd ? hi : lo);
+                            sts16(dst + row * 128 + (((c16 + 1 - odd) ^ (row & 7)) << 4), odd ? lo : hi);
+                        }
+                        if (q & 1) fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive(raw_empty(n % PT_RAW));
+                            if (q == 1) mbar_arrive(k_full(kb));
+                            if (q == 3) {
+                                mbar_arrive(v_full(vb));
+                                mbar_arrive(word_empty(slot));
                             }
                         }
-                        if (ft + 1 < u.t1) pages_ahead = pages_of(ft + 1);
-                    }
-                    const char* pool = reinterpret_cast<const char*>(fq < 2 ? p.c.k : p.c.v) + c * 16;
-                    const uint32_t dst = raw + (issued % PT_RAW) * L::RAW_BYTES;
-#pragma unroll
-                    for (int i = 0; i < NP; ++i) {
-                        const int key = key0 + (fq & 1) * (PT_TILE / 2) + i * RPP + r0;
-                        const size_t vec = vec_at(key);
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + i * 2048), "l"(pool + vec * DH), "r"(key < end ? 16 : 0) : "memory");
-                    }
-                    ++issued;
-                    if (++fq == 4) {
-                        fq = 0;
-                        if (++ft == u.t1) {
-                            more = take_part(np, u);
-                            if (more) {
-                                end = u.end(G);
-                                mask_tile = u.mask_tile();
-                                ft = u.t0;
-                                pages_ahead = pages_of(ft);
-                            }
-                        }
                     }
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");  // (empty at the end, so that the waits keep counting)
-            };
-            for (int i = 0; i < PT_RAW; ++i) issue();
-            float vref = 0.f;
-            for (int n = 0; n < issued; ++n) {
-                const int q = n & 3, kb = g % PT_KSTAGES, vb = g % PT_VSTAGES, slot = g % PT_SCALES;
-                if (q == 0) {
-                    if (g >= PT_KSTAGES && !warp_wait(k_empty(kb), ((g / PT_KSTAGES) - 1) & 1, status)) { ok = false; break; }
-                    // the slot's previous scales belong to tile g - KSTAGES - 1, whose probabilities preceded the
-                    // product that freed this key stage
-                    if (first) vref = 0.f;
-                    float mx = 0.f;
-                    const float vq[4] = {vs4.x, vs4.y, vs4.z, vs4.w};
-                    bool bad = false;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        bad |= !isfinite(vq[i]);
-                        mx = isfinite(vq[i]) ? fmaxf(mx, vq[i]) : mx;
-                    }
-                    if (masked && bad) *stray = 1;
-                    if (__any_sync(0xFFFFFFFFu, vref == 0.f || mx > vref * PT_VREF_MAX)) {
-                        // 2^-6 of the power of two at or below the largest scale (scales are at least 2^-119)
-                        const uint32_t e = max(__float_as_uint(warp_max(mx)) >> 23, 7u) - 6u;
-                        vref = fmaxf(vref, __uint_as_float(e << 23));
-                    }
-                    if ((lane >> 3) == warp - 8) {  // each warp writes a quarter of what all four know
-                        const float up = 1.f / vref;  // a power of two, at most 2^126
-                        float4 v = make_float4(vq[0] * up, vq[1] * up, vq[2] * up, vq[3] * up);
-                        if (masked && bad) {
-                            if (!isfinite(vq[0])) v.x = 0.f;
-                            if (!isfinite(vq[1])) v.y = 0.f;
-                            if (!isfinite(vq[2])) v.z = 0.f;
-                            if (!isfinite(vq[3])) v.w = 0.f;
-                        }
-                        *reinterpret_cast<float4*>(sc_k + slot * 256 + 4 * lane) = ks4;
-                        *reinterpret_cast<float4*>(sc_k + slot * 256 + 128 + 4 * lane) = v;
-                        if (lane == 0) sc_vref[slot] = vref;
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(sc_full(slot));
-                } else if (q == 2) {
-                    if (g >= PT_VSTAGES && !warp_wait(v_empty(vb), ((g / PT_VSTAGES) - 1) & 1, status)) { ok = false; break; }
-                }
-                asm volatile("cp.async.wait_group %0;" ::"n"(PT_RAW - 1) : "memory");
-                const uint32_t src = raw + (n % PT_RAW) * L::RAW_BYTES;
-                const uint32_t tile_smem = q < 2 ? k_s(kb) : v_s(vb);
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const uint4 x = lds16(src + i * 2048);
-                    const int row = (q & 1) * (PT_TILE / 2) + i * RPP + r0;
-                    const uint2 a = widen4_half<DTYPE>(x.x), b = widen4_half<DTYPE>(x.y), d = widen4_half<DTYPE>(x.z), e = widen4_half<DTYPE>(x.w);
-                    const uint32_t base = tile_smem + (c >> 2) * L::KV_HALF + row * 128;
-                    // the lanes of the second half store their pieces in the other order: 8 lanes then reach all banks
-                    const int c16 = 2 * (c & 3), sw = c >> 2;
-                    const uint4 lo = make_uint4(a.x, a.y, b.x, b.y), hi = make_uint4(d.x, d.y, e.x, e.y);
-                    sts16(base + (((c16 + sw) ^ (row & 7)) << 4), sw ? hi : lo);
-                    sts16(base + (((c16 + 1 - sw) ^ (row & 7)) << 4), sw ? lo : hi);
-                }
-                if (q & 1) {
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(q == 1 ? k_full(kb) : v_full(vb));
-                }
-                issue();
-                if (q == 3) ++g;
             }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
     } else {
         set_registers<PT_REGS_OTHER>(false);
@@ -861,6 +793,83 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                     for (int h = 0; h < HALVES; ++h) tma_load_2d(v_s(vb) + h * L::KV_HALF + lane * bp * 128, &tmap_v, h * 64, y, v_full(vb));
             }
         }
+        } else if (!BF16 && warp == 14) {
+        // ------------------------------------------------------------ TMA producer of codes: half tiles, a box per page
+        const int bp = min(1 << shift, PT_TILE / 2), per_half = (PT_TILE / 2) / bp;
+        int n = 0;
+        while (ok && take_part(np, u)) {
+            const int end = u.end(G);
+            for (int t = u.t0; t < u.t1 && ok; ++t) {
+                const int key = (t << PT_TILE_LOG) + lane * bp;  // lanes 0 .. 2 per_half - 1
+                const bool live = lane < 2 * per_half && key < end;
+                const int y = live ? ((load_page(p.r, shift, p.c.n_pages, u.seq, key, status) * n_kv + u.kvh) << shift) + (key & ps_mask) : 0;
+                const int boxes = __popc(__ballot_sync(0xFFFFFFFFu, live));
+#pragma unroll 1
+                for (int q = 0; q < 4; ++q, ++n) {
+                    const int slot = n % PT_RAW, h = q & 1;
+                    if (n >= PT_RAW && !warp_wait(raw_empty(slot), ((n / PT_RAW) - 1) & 1, status)) { ok = false; break; }
+                    if (lane == 0) mbar_arrive_expect_tx(raw_full(slot), min(max(boxes - h * per_half, 0), per_half) * bp * DH);
+                    __syncwarp();
+                    if (live && lane / per_half == h)
+                        tma_load_2d(sbase + L::RAW_OFF + slot * L::RAW_BYTES + (lane - h * per_half) * bp * DH, q < 2 ? &tmap_k : &tmap_v, 0, y, raw_full(slot));
+                }
+            }
+        }
+        } else if (!BF16 && warp == 15) {
+        // ------------------------------------------------------------ scales of a tile: refs, and a word per key and value
+        int g = 0;
+        while (ok && take_part(np, u)) {
+            const int end = u.end(G), mask_tile = u.mask_tile();
+            float vref = 0.f;
+            for (int t = u.t0; t < u.t1; ++t, ++g) {
+                const int slot = g % PT_SCALES;
+                const int key = (t << PT_TILE_LOG) + 4 * lane;
+                float kq[4] = {0.f, 0.f, 0.f, 0.f}, vq[4] = {0.f, 0.f, 0.f, 0.f}, km = 0.f, vm = 0.f;
+                if (key < end) {
+                    const int page = load_page(p.r, shift, p.c.n_pages, u.seq, key, status);
+                    const size_t vec = ((static_cast<size_t>(page) * n_kv + u.kvh) << shift) + (key & ps_mask);
+                    const float4 a = __ldg(reinterpret_cast<const float4*>(p.c.k_scale + vec)), b = __ldg(reinterpret_cast<const float4*>(p.c.v_scale + vec));
+                    kq[0] = a.x; kq[1] = a.y; kq[2] = a.z; kq[3] = a.w;
+                    vq[0] = b.x; vq[1] = b.y; vq[2] = b.z; vq[3] = b.w;
+#pragma unroll
+                    for (int i = 1; i < 4; ++i)
+                        if (key + i >= end) kq[i] = vq[i] = 0.f;  // behind the last key: whatever the page holds
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (t >= mask_tile && !isfinite(vq[i])) {
+                        *stray = 1;
+                        vq[i] = 0.f;
+                    }
+                    km = isfinite(kq[i]) ? fmaxf(km, kq[i]) : km;
+                    vm = isfinite(vq[i]) ? fmaxf(vm, vq[i]) : vm;
+                }
+                // 2^-6 of the power of two at or below the largest scale (scales are at least 2^-119)
+                auto ref_of = [](float m) { return __uint_as_float((max(__float_as_uint(m) >> 23, 7u) - 6u) << 23); };
+                const float kref = ref_of(warp_max(km));
+                if (__any_sync(0xFFFFFFFFu, vref == 0.f || vm > vref * PT_REF_MAX)) vref = fmaxf(vref, ref_of(warp_max(vm)));
+                // scale / ref as the sum of two fp16 numbers
+                const float kup = 1.f / kref, vup = 1.f / vref;  // powers of two, at most 2^126
+                uint32_t kw[4], vw[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float kx = kq[i] * kup, vx = vq[i] * vup;
+                    const float kh = __half2float(__float2half_rn(kx)), vh = __half2float(__float2half_rn(vx));
+                    kw[i] = pack_half(kh, kx - kh);
+                    vw[i] = pack_half(vh, vx - vh);
+                }
+                if (g >= PT_SCALES && !warp_wait(word_empty(slot), ((g / PT_SCALES) - 1) & 1, status)) { ok = false; break; }
+                const uint32_t words = sbase + L::SC_OFF + slot * L::SC_BYTES + lane * 16;
+                sts16(words, make_uint4(kw[0], kw[1], kw[2], kw[3]));
+                sts16(words + PT_TILE * 4, make_uint4(vw[0], vw[1], vw[2], vw[3]));
+                if (lane == 0) {
+                    new_ref[2 * slot] = kref;
+                    new_ref[2 * slot + 1] = vref;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(word_full(slot));
+            }
+        }
         } else if (warp == 13) {
         // ------------------------------------------------------------ hands out the parts
         BlockWalk k;
@@ -915,11 +924,15 @@ cudaError_t tc_init() {
 }
 template <int DH, int DTYPE>
 cudaError_t tc_launch(const PagedAttnParams& p, int grid, cudaStream_t stream) {
-    CUtensorMap tk = {}, tv = {};
+    CUtensorMap tk, tv;
+    const uint64_t rows = static_cast<uint64_t>(p.c.n_pages) * p.c.n_kv_heads << p.c.page_shift;
+    const uint32_t page = 1u << p.c.page_shift;
     if (DTYPE == VERILLM_KV_BF16) {
-        const uint64_t rows = static_cast<uint64_t>(p.c.n_pages) * p.c.n_kv_heads << p.c.page_shift;
-        const uint32_t box = static_cast<uint32_t>(1 << p.c.page_shift) < PT_TILE ? 1u << p.c.page_shift : PT_TILE;
+        const uint32_t box = page < PT_TILE ? page : PT_TILE;
         if (make_tmap_bf16_2d(&tk, p.c.k, rows, DH, DH, box) != 0 || make_tmap_bf16_2d(&tv, p.c.v, rows, DH, DH, box) != 0) return cudaErrorInvalidValue;
+    } else {
+        const uint32_t box = page < PT_TILE / 2 ? page : PT_TILE / 2;
+        if (make_tmap_bytes_2d(&tk, p.c.k, rows, DH, box) != 0 || make_tmap_bytes_2d(&tv, p.c.v, rows, DH, box) != 0) return cudaErrorInvalidValue;
     }
     paged_tc_kernel<DH, DTYPE><<<grid, PT_THREADS, PtSmem<DH, DTYPE>::TOTAL, stream>>>(tk, tv, p);
     return cudaGetLastError();

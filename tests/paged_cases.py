@@ -93,14 +93,15 @@ class Case:
         three factors: off by at most d = (dh + 4) e sum |q_d k_d| / sqrt(dh), which changes a probability by a
         factor within 1 +- 2 d and its exponential by 2^-21 more (exp2 in float32 of an argument below 64 in size);
         the products and sums over L keys in float32 add at most (L + 64) e of sum p |v|.
-        With 8-bit pools the products may run in float16: a query row is scaled so that its largest entry lies in
-        [1, 2), so an entry is off by at most 2^-25 of the largest, max |q| 2^-25 sum |k_d| / sqrt(dh) in the score;
-        a probability times its value scale, kept below 2^7 2^8 for the largest scale, is off by 2^-12 of itself
-        (within u) or by 2^-25, i.e. 2^-25 2^-5 max(scale) per code in units where the probabilities sum to 1 or more."""
+        With 8-bit pools the products may run in float16, operands and probabilities scaled so that the largest lies near
+        its top: a key or value entry is rounded to 11 bits (half = 2^-11), which adds half sum |q_d k_d| / sqrt(dh) to
+        a score and half to the factor of sum p |v|, or is off by at most 2^-30 of the largest; a query row is scaled
+        so that its largest entry lies in [1, 2), so an entry is off by at most 2^-25 of the largest; a probability is
+        rounded to 11 bits (within u) or, for each key, off by 2^-31 where they sum to 1 or more."""
         n, H, dh = self.n, self.H, self.dh
         out, tol = torch.zeros(n, H, dh, dtype=torch.float64), torch.zeros(n, H, dh, dtype=torch.float64)
         lse, ltol = torch.full((n, H), -float("inf"), dtype=torch.float64), torch.zeros(n, H, dtype=torch.float64)
-        u, e = 2.0 ** -8, 2.0 ** -24
+        u, e, half = 2.0 ** -8, 2.0 ** -24, 0.0 if self.dtype == torch.bfloat16 else 2.0 ** -11
         for b, nb in enumerate(self.rows):
             if nb == 0 or self.kv[b] == 0:
                 continue
@@ -117,7 +118,8 @@ class Case:
                 tiny = 0.0
                 if self.dtype != torch.bfloat16:
                     row = torch.where(keep, k[:, kh].abs().sum(-1)[None].expand(nb, L), torch.zeros(()).double()).nan_to_num(0, 0, 0)
-                    d = d + 2.0 ** -25 * q[:, h].abs().amax(-1) * row.amax(-1) / dh ** 0.5
+                    d = d + 2.0 ** -24 * q[:, h].abs().amax(-1) * row.amax(-1) / dh ** 0.5
+                    d = d + half * size.nan_to_num(0, 0, 0).amax(-1)
                     vmax = v[:, kh].abs().nan_to_num(0, 0, 0).amax()
                     tiny = L * 2.0 ** -30 * float(vmax)
                 s = torch.where(keep, s, torch.full((), -float("inf")).double())
@@ -130,7 +132,7 @@ class Case:
                     clean = torch.isfinite(x).all()
                     y = p @ x if clean else torch.where(keep[:, :, None], p[:, :, None] * x[None], torch.zeros(()).double()).sum(1)
                     dst[r0:r0 + nb, h, cols] = torch.where(some[:, None], y, torch.zeros(()).double())
-                tol[r0:r0 + nb, h] = tol[r0:r0 + nb, h] * (u + 2 * d[:, None] + 2.0 ** -21 + (L + 64) * e) * (1 + u) + u * out[r0:r0 + nb, h].abs() + tiny
+                tol[r0:r0 + nb, h] = tol[r0:r0 + nb, h] * (u + half + 2 * d[:, None] + 2.0 ** -21 + (L + 64) * e) * (1 + u) + u * out[r0:r0 + nb, h].abs() + tiny
         return out, tol, lse, ltol
 
 
