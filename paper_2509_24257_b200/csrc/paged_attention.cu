@@ -98,8 +98,14 @@ struct Layout {
     }
 };
 
+// CTAs per SM, all resident at once: what the registers allow (65536 / 128 threads / CTAs).
+__host__ __device__ constexpr int rows_ctas(int dh, int dtype, int nt) {
+    if (dh == 64) return nt <= 2 ? 4 : 2;
+    return dtype == VERILLM_KV_BF16 ? (nt == 1 ? 3 : 2) : (nt == 1 ? 4 : nt == 2 ? 3 : 2);
+}
+
 template <int DH, int DTYPE, int NT>
-__global__ void __launch_bounds__(PR_THREADS)
+__global__ void __launch_bounds__(PR_THREADS, rows_ctas(DH, DTYPE, NT))
 paged_rows_kernel(const PagedAttnParams p) {
     using L = Layout<DH, DTYPE>;
     constexpr int RB = 8 * NT;
@@ -479,45 +485,64 @@ paged_rows_kernel(const PagedAttnParams p) {
 }
 
 // Joins the partial results of blocks that several CTAs worked on.  One CTA per (possible) such block and group of
-// JOIN_ROWS rows; the pieces are added in the order of their tiles.
-constexpr int JOIN_THREADS = 128;
+// JOIN_ROWS rows, a warp per row: the lanes first look at all pieces' maxima and sums, then each adds its columns of the
+// pieces in the order of their tiles, eight loads in flight.
+constexpr int JOIN_THREADS = 256, JOIN_ROWS = 32;
 template <int DH>
 __global__ void __launch_bounds__(JOIN_THREADS)
 paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
+    constexpr int W = DH / 32;  // columns per lane
     pdl_wait();
     const int4 h = p.hdr[blockIdx.x];
     if (h.x == 0) return;
-    constexpr int LPR = DH / 8;
-    const int r = static_cast<int>(blockIdx.y) * (JOIN_THREADS / LPR) + static_cast<int>(threadIdx.x) / LPR;
     const SeqView s = load_seq(p.r, p.c.page_shift, h.y, nullptr);
     const int tok0 = h.w << p.tb_log, rows = min(1 << p.tb_log, s.n - tok0) * p.group;
-    if (r >= rows) return;
-    const int cx = (threadIdx.x % LPR) * 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // piece 0 is CTA blockIdx.x's tail slot, piece i the head slot of CTA blockIdx.x + i
-    auto slot_of = [&](int i) { return part_slot(p.part, 2 * (static_cast<int>(blockIdx.x) + i) + (i == 0 ? 1 : 0), rows_per_block, DH); };
-    float mx = -INFINITY;
+    const float* slot0 = part_slot(p.part, 2 * static_cast<int>(blockIdx.x), rows_per_block, DH);
+    const size_t slot = static_cast<size_t>(rows_per_block) * (DH + 2);
+    auto part_of = [&](int i) { return slot0 + slot * (i == 0 ? 1 : 2 * i); };
+    const int r_end = min(rows, (static_cast<int>(blockIdx.y) + 1) * JOIN_ROWS);
+    for (int r = static_cast<int>(blockIdx.y) * JOIN_ROWS + warp; r < r_end; r += JOIN_THREADS / 32) {
+        float mx = -INFINITY;
+        for (int i = lane; i < h.x; i += 32) mx = fmaxf(mx, part_of(i)[r]);
+        mx = warp_max(mx);
+        float l = 0.f, acc[W];
+#pragma unroll
+        for (int c = 0; c < W; ++c) acc[c] = 0.f;
+        for (int i0 = 0; i0 < h.x; i0 += 32) {
+            const int i = i0 + lane;
+            float w = 0.f, li = 0.f;
+            if (i < h.x) {
+                w = part_weight(part_of(i)[r], mx);
+                li = part_of(i)[rows_per_block + r] * w;
+            }
+            l += warp_sum(li);
+            const int n = min(32, h.x - i0);
 #pragma unroll 8
-    for (int i = 0; i < h.x; ++i) mx = fmaxf(mx, slot_of(i)[r]);
-    float l = 0.f, acc[8];
+            for (int j = 0; j < n; ++j) {
+                const float wj = __shfl_sync(0xFFFFFFFFu, w, j);
+                const float* src = part_of(i0 + j) + 2 * rows_per_block + r * DH + lane * W;
+                float x[W];
+                if (W == 4) {
+                    const float4 v = *reinterpret_cast<const float4*>(src);
+                    x[0] = v.x; x[1] = v.y; x[W - 2] = v.z; x[W - 1] = v.w;
+                } else {
+                    const float2 v = *reinterpret_cast<const float2*>(src);
+                    x[0] = v.x; x[1] = v.y;
+                }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < h.x; ++i) {
-        const float* part = slot_of(i);
-        const float w = part_weight(part[r], mx);
-        const float4* src = reinterpret_cast<const float4*>(part + 2 * rows_per_block + r * DH + cx);
-        const float4 a = src[0], b = src[1];
-        l += part[rows_per_block + r] * w;
-        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += w == 0.f ? 0.f : x[e] * w;
+                for (int c = 0; c < W; ++c) acc[c] += wj == 0.f ? 0.f : x[c] * wj;
+            }
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int row = s.row0 + tok0 + r / p.group, head = h.z * p.group + r % p.group;
+        uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + static_cast<size_t>(row) * p.out_stride +
+                                                    static_cast<size_t>(head) * DH + lane * W);
+        if (W == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[W - 2] * inv, acc[W - 1] * inv));
+        else dst[0] = pack_bf16(acc[0] * inv, acc[1] * inv);
+        if (p.lse && lane == 0) p.lse[static_cast<size_t>(row) * p.n_heads + head] = l == 0.f ? -INFINITY : mx * kLn2 + logf(l);
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int row = s.row0 + tok0 + r / p.group, head = h.z * p.group + r % p.group;
-    *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + static_cast<size_t>(row) * p.out_stride + static_cast<size_t>(head) * DH + cx) =
-        make_uint4(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv), pack_bf16(acc[4] * inv, acc[5] * inv),
-                   pack_bf16(acc[6] * inv, acc[7] * inv));
-    if (p.lse && cx == 0) p.lse[static_cast<size_t>(row) * p.n_heads + head] = l == 0.f ? -INFINITY : mx * kLn2 + logf(l);
 }
 
 template <int DH, int NT>
@@ -534,6 +559,7 @@ template <int DH, int DTYPE>
 cudaError_t rows_init_all() {
     cudaError_t e = rows_init<DH, DTYPE, 1>();
     if (e == cudaSuccess) e = rows_init<DH, DTYPE, 2>();
+    if (e == cudaSuccess) e = rows_init<DH, DTYPE, 3>();
     if (e == cudaSuccess) e = rows_init<DH, DTYPE, 4>();
     return e;
 }
@@ -547,6 +573,7 @@ template <int DH, int DTYPE>
 cudaError_t rows_launch_nt(const PagedAttnParams& p, int nt, int grid, cudaStream_t stream) {
     if (nt == 1) return rows_launch<DH, DTYPE, 1>(p, grid, stream);
     if (nt == 2) return rows_launch<DH, DTYPE, 2>(p, grid, stream);
+    if (nt == 3) return rows_launch<DH, DTYPE, 3>(p, grid, stream);
     return rows_launch<DH, DTYPE, 4>(p, grid, stream);
 }
 template <int DH>
@@ -562,12 +589,12 @@ struct Shape {
     int nt;  // 8-row column blocks of the few-row kernel; 0: the tcgen05 kernel
     int tb_log, rows_per_block, grid;
 };
-Shape shape_of(int group, int max_rows, int num_sms) {
+Shape shape_of(int head_dim, int dtype, int group, int max_rows, int num_sms) {
     Shape s;
     const long long r = static_cast<long long>(group) * max_rows;
-    s.nt = r <= 8 ? 1 : r <= 16 ? 2 : r <= 32 ? 4 : 0;
+    s.nt = r <= 32 ? static_cast<int>((r + 7) / 8) : 0;
     s.rows_per_block = s.nt ? 8 * s.nt : kPagedTcRows;
-    s.grid = num_sms * (s.nt == 0 ? 1 : s.nt == 1 ? 4 : s.nt == 2 ? 3 : 2);
+    s.grid = num_sms * (s.nt == 0 ? 1 : rows_ctas(head_dim, dtype, s.nt));
     // tokens per block: a power of two; the few-row kernel's single block holds them all
     s.tb_log = 0;
     while ((1LL << s.tb_log) < max_rows && (s.nt || (2LL << s.tb_log) * group <= s.rows_per_block)) ++s.tb_log;
@@ -577,8 +604,8 @@ size_t hdr_bytes(int grid) { return (static_cast<size_t>(grid) * sizeof(int4) + 
 
 }  // namespace
 
-size_t paged_attention_workspace(int head_dim, int group, int max_rows, int num_sms) {
-    const Shape s = shape_of(group, max_rows, num_sms);
+size_t paged_attention_workspace(int head_dim, int dtype, int group, int max_rows, int num_sms) {
+    const Shape s = shape_of(head_dim, dtype, group, max_rows, num_sms);
     return hdr_bytes(s.grid) + static_cast<size_t>(2) * s.grid * s.rows_per_block * (head_dim + 2) * sizeof(float);
 }
 
@@ -594,7 +621,7 @@ cudaError_t paged_attention_init() {
 }
 
 cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_sms, cudaStream_t stream) {
-    const Shape s = shape_of(p.group, p.r.max_rows, num_sms);
+    const Shape s = shape_of(p.c.head_dim, p.c.dtype, p.group, p.r.max_rows, num_sms);
     p.tb_log = s.tb_log;
     p.hdr = reinterpret_cast<int4*>(workspace);
     p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + hdr_bytes(s.grid));
@@ -603,7 +630,7 @@ cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_s
                                          : rows_launch_dtype<128>(p, s.nt, s.grid, stream);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(s.grid, (s.rows_per_block * (p.c.head_dim / 8) + JOIN_THREADS - 1) / JOIN_THREADS);
+    cfg.gridDim = dim3(s.grid, (s.rows_per_block + JOIN_ROWS - 1) / JOIN_ROWS);
     cfg.blockDim = dim3(JOIN_THREADS);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];

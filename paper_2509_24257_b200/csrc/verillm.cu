@@ -1112,7 +1112,7 @@ int64_t verillm_op_attention_paged_workspace(const verillm_kv_cache* cache, cons
     PagedRowsDev r;
     int rc = check_paged(cache, rows, &c, &r), sms = 0;
     if (rc || (rc = check_group(cache, n_heads)) || (rc = current_sms(&sms))) return rc;
-    return static_cast<int64_t>(paged_attention_workspace(c.head_dim, n_heads / c.n_kv_heads, r.max_rows, sms));
+    return static_cast<int64_t>(paged_attention_workspace(c.head_dim, c.dtype, n_heads / c.n_kv_heads, r.max_rows, sms));
 }
 
 int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_rows* rows, const void* q, int64_t q_stride,
@@ -1128,7 +1128,7 @@ int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_r
     if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
     p.group = n_heads / p.c.n_kv_heads;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) ||
-        workspace_bytes < static_cast<int64_t>(paged_attention_workspace(p.c.head_dim, p.group, p.r.max_rows, sms)))
+        workspace_bytes < static_cast<int64_t>(paged_attention_workspace(p.c.head_dim, p.c.dtype, p.group, p.r.max_rows, sms)))
         return VERILLM_E_SHAPE;
     p.q = q; p.q_stride = q_stride; p.out = out; p.out_stride = out_stride; p.lse = lse; p.n_heads = n_heads; p.status = status;
     CU_TRY(launch_paged_attention(p, workspace, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
