@@ -11,6 +11,8 @@
 // them in the order of the tiles, so that results do not depend on timing.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "common.cuh"
 #include "kernels.h"
 
@@ -242,6 +244,40 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 // weight of a partial result with maximum m in one with maximum mx >= m (both may be -inf: nothing to weigh)
 __device__ __forceinline__ float part_weight(float m, float mx) { return m == -INFINITY ? 0.f : exp2_fast(m - mx); }
+
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Four codes -> fp16 pairs (0, 1) and (2, 3), exactly.  int8: 0x6400 | (code + 128) is the fp16 number 1152 + code.
+template <int DTYPE>
+__device__ __forceinline__ uint2 widen4_half(uint32_t w) {
+    if (DTYPE == VERILLM_KV_E4M3) {
+        uint2 h;
+        asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}\n" : "=r"(h.x), "=r"(h.y) : "r"(w));
+        return h;
+    }
+    const uint32_t u = w ^ 0x80808080u;
+    const __half2 off = __half2half2(__ushort_as_half(static_cast<unsigned short>(0x6480)));  // 1152
+    const uint32_t lo = __byte_perm(u, 0x64646464u, 0x4140), hi = __byte_perm(u, 0x64646464u, 0x4342);
+    const __half2 a = __hsub2(*reinterpret_cast<const __half2*>(&lo), off), b = __hsub2(*reinterpret_cast<const __half2*>(&hi), off);
+    return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+// Scales of 8-bit pools enter fp16 operands relative to a power of two: 2^-6 of the one at or below the largest scale m of
+// a tile, so that the largest lies in [2^6, 2^7) (scales are at least 2^-119).  A reference is kept while scales
+// stay at or below kScaleRefMax of it.
+constexpr float kScaleRefMax = 128.f;
+__device__ __forceinline__ float scale_ref(float m) { return __uint_as_float((max(__float_as_uint(m) >> 23, 7u) - 6u) << 23); }
+// Exponent field e such that |q| 2^(127 - e) lies in [1, 2) for the largest entry, whose 15-bit pattern is given.
+__device__ __forceinline__ uint32_t row_exponent(uint32_t abs_bits) { return min(max(abs_bits >> 7, 1u), 253u); }
+// largest |x| of 8 packed bf16 values as a 15-bit pattern (ordered like the values; >= 0x7F80: not finite)
+__device__ __forceinline__ uint32_t abs_max8(const uint4& x) {
+    const uint32_t a = __vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), b = __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu);
+    const uint32_t m = __vmaxu2(a, b);
+    return max(m & 0xFFFFu, m >> 16);
+}
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;

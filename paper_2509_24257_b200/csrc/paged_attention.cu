@@ -10,12 +10,14 @@
 // 16 bytes are consecutive head_dim entries, and because both products sum over (or tile) head_dim in any order,
 // the order in which the fragments name them is chosen to fit the loads (Q is laid out once to match).  Each of the
 // CTA's four warps takes 16 of a tile's 64 keys and keeps its own running maximum, sum and output; they are joined
-// once per block.  8-bit codes are widened exactly to bf16 in registers (both code types fit bf16's 8 significant
-// bits); key scales multiply the scores and value scales the probabilities, both in fp32.
+// once per block.  8-bit codes are widened to fp16 in registers (both code types are exact there) and the products are
+// fp16; key scales multiply the scores and value scales the probabilities, both in fp32.  To fit fp16, a query row is
+// scaled by a power of two into [1, 2), and value scales are taken relative to a power of two that follows the largest
+// seen: a probability times its scale is below 2^15 and loses at most 2^-25, 2^-31 of the largest.
 //
 // The running maximum is a reference that is only raised when a score exceeds it by 2^8, as in the packed
-// attention kernel: probabilities stay below 256 and the sum divides the stale reference out.  Probabilities are
-// rounded to bf16 for the second product, everything else is fp32.
+// attention kernel: probabilities stay below 256 and the sum divides the stale reference out.  Probabilities (times
+// scales) are rounded to bf16 or fp16 for the second product, everything else is fp32.
 #include "paged.cuh"
 
 namespace vl {
@@ -27,10 +29,17 @@ constexpr int PR_WARPS = 4;
 constexpr int PR_TILE_LOG = 6, PR_TILE = 1 << PR_TILE_LOG;  // keys per tile: 16 per warp
 constexpr float PR_RAISE_LOG2 = 8.f;
 
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+// d += a b, 16 x 8 x 16, operands bf16 or fp16
+template <bool BF16>
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // 8 x 8 transpose of 16-bit values over the warp
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
@@ -38,35 +47,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-
-// Four codes in a word -> bf16 pairs of bytes (0, 2) and (1, 3), exactly.
-// e4m3 s eeee mmm: the 7 low bits moved to the bottom of a bf16's exponent and the top of its mantissa are the value
-// times 2^-120 (subnormal codes included), and a product with 2^120 is exact.
-// int8: 0x4300 | low 7 bits = 128 + (x & 127), and 0x4300 | sign bit = 128 or 256: their difference is x.
-template <int DTYPE>
-__device__ __forceinline__ void widen4(uint32_t w, uint32_t& even, uint32_t& odd) {
-    if (DTYPE == VERILLM_KV_E4M3) {
-        const uint32_t e = ((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u);
-        const uint32_t o = ((w >> 4) & 0x07F007F0u) | (w & 0x80008000u);
-        even = mul_bf16x2(e, 0x7B807B80u);  // 2^120
-        odd = mul_bf16x2(o, 0x7B807B80u);
-    } else {
-        const uint32_t h = w >> 8;
-        even = sub_bf16x2((w & 0x007F007Fu) | 0x43004300u, (w & 0x00800080u) | 0x43004300u);
-        odd = sub_bf16x2((h & 0x007F007Fu) | 0x43004300u, (h & 0x00800080u) | 0x43004300u);
-    }
-}
-
 // Whether one of 8 packed bf16 values is infinite or NaN, and the 8 values with those replaced by 0.
 __device__ __forceinline__ bool not_finite8(const uint4& x) {
     const uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7F807F80u, x.y & 0x7F807F80u), __vmaxu2(x.z & 0x7F807F80u, x.w & 0x7F807F80u));
@@ -116,6 +96,7 @@ paged_rows_kernel(const PagedAttnParams p) {
     float* sm_o = sm_l + PR_WARPS * RB;                 // [PR_WARPS][RB][OLD]
     uint2* sm_q = reinterpret_cast<uint2*>(sm_o + PR_WARPS * RB * OLD);  // [NT][KSTEPS][32]
     __shared__ ShareScratch sm_share;
+    __shared__ uint32_t sm_exp[RB];  // 8-bit pools: the query rows' exponents
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const PagedCacheDev& c = p.c;
@@ -142,26 +123,39 @@ paged_rows_kernel(const PagedAttnParams p) {
         const int end = ctx + tok0 + toks;        // keys [0, end) are visible to some row
         // ---- Q into fragment order: b registers of k step ks, rows 8 nt + g
         __syncthreads();  // the previous block's rows have been read
+        const __nv_bfloat16* q0 = reinterpret_cast<const __nv_bfloat16*>(p.q) + static_cast<size_t>(s.row0 + tok0) * p.q_stride + static_cast<size_t>(k.kvh * G) * DH;
+        if (!L::BF16) {
+            constexpr int LPQ = NT == 1 ? 16 : NT == 2 ? 8 : 4;  // lanes per row
+            const int r = tid / LPQ;
+            uint32_t mx = 0;
+            if (r < rows) {
+                const uint4* src = reinterpret_cast<const uint4*>(q0 + static_cast<size_t>(r / G) * p.q_stride + static_cast<size_t>(r % G) * DH);
+                for (int i = tid % LPQ; i < DH / 8; i += LPQ) mx = max(mx, abs_max8(__ldg(src + i)));
+            }
+#pragma unroll
+            for (int x = 1; x < LPQ; x <<= 1) mx = max(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
+            if (r < RB && tid % LPQ == 0) sm_exp[r] = row_exponent(mx);
+            __syncthreads();
+        }
         for (int i = tid; i < NT * L::KSTEPS * 32; i += PR_THREADS) {
             const int ln = i & 31, ks = (i >> 5) % L::KSTEPS, nt = i / (32 * L::KSTEPS);
             const int r = 8 * nt + (ln >> 2), lt = ln & 3;
             uint2 b = make_uint2(0u, 0u);
             if (r < rows) {
-                const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.q) +
-                                           static_cast<size_t>(s.row0 + tok0 + r / G) * p.q_stride +
-                                           static_cast<size_t>(k.kvh * G + r % G) * DH;
+                const __nv_bfloat16* src = q0 + static_cast<size_t>(r / G) * p.q_stride + static_cast<size_t>(r % G) * DH;
                 if (L::BF16) {  // chunk of 32 entries = 2 steps; lane's entries 8 lt .. 8 lt + 7
                     b = __ldg(reinterpret_cast<const uint2*>(src + (ks >> 1) * 32 + 8 * lt + 4 * (ks & 1)));
-                } else {  // chunk of 64 entries = 4 steps; lane's entries 16 lt + 4 step .. + 3, even ones first
+                } else {  // chunk of 64 entries = 4 steps; lane's entries 16 lt + 4 step .. + 3
                     const uint2 x = __ldg(reinterpret_cast<const uint2*>(src + (ks >> 2) * 64 + 16 * lt + 4 * (ks & 3)));
-                    b = make_uint2(__byte_perm(x.x, x.y, 0x5410), __byte_perm(x.x, x.y, 0x7632));
+                    const float down = __uint_as_float((254u - sm_exp[r]) << 23);
+                    b = make_uint2(pack_half(bf16_lo(x.x) * down, bf16_hi(x.x) * down), pack_half(bf16_lo(x.y) * down, bf16_hi(x.y) * down));
                 }
             }
             sm_q[i] = b;
         }
         __syncthreads();
 
-        float o[NT][L::MT][4], m_ref[NT][2], l_run[NT][2];
+        float o[NT][L::MT][4], m_ref[NT][2], l_run[NT][2], rf[NT][2], vref = 0.f, vup = 0.f;
         int pos[NT][2];  // last visible key of this lane's rows, -1: none
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -171,6 +165,7 @@ paged_rows_kernel(const PagedAttnParams p) {
             for (int h = 0; h < 2; ++h) {
                 const int r = 8 * nt + 2 * t + h;
                 pos[nt][h] = r < rows ? first_pos + r / G : -1;
+                rf[nt][h] = L::BF16 ? sl2 : sl2 * __uint_as_float(r < rows ? sm_exp[r] << 23 : 0u);
                 m_ref[nt][h] = -INFINITY;
                 l_run[nt][h] = 0.f;
             }
@@ -241,23 +236,21 @@ paged_rows_kernel(const PagedAttnParams p) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             const uint2 b = sm_q[(nt * L::KSTEPS + 2 * i + h) * 32 + lane];
-                            mma_bf16(sc[nt], wa[2 * h], wb[2 * h], wa[2 * h + 1], wb[2 * h + 1], b.x, b.y);
+                            mma16<L::BF16>(sc[nt], wa[2 * h], wb[2 * h], wa[2 * h + 1], wb[2 * h + 1], b.x, b.y);
                         }
                 } else {
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        uint32_t a0, a1, a2, a3;
-                        widen4<DTYPE>(wa[w], a0, a2);
-                        widen4<DTYPE>(wb[w], a1, a3);
+                        const uint2 a = widen4_half<DTYPE>(wa[w]), e = widen4_half<DTYPE>(wb[w]);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             const uint2 b = sm_q[(nt * L::KSTEPS + 4 * i + w) * 32 + lane];
-                            mma_bf16(sc[nt], a0, a1, a2, a3, b.x, b.y);
+                            mma16<L::BF16>(sc[nt], a.x, e.x, a.y, e.y, b.x, b.y);
                         }
                     }
                 }
             }
-            const float f0 = L::BF16 ? sl2 : sl2 * ks0, f1 = L::BF16 ? sl2 : sl2 * ks1;
+            const float f0 = ks0, f1 = ks1;
             vs0 = vs0n;
             vs1 = vs1n;
             if (more) load_keys(vec_next);
@@ -266,10 +259,11 @@ paged_rows_kernel(const PagedAttnParams p) {
             bool raise = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                sc[nt][0] *= f0;
-                sc[nt][1] *= f0;
-                sc[nt][2] *= f1;
-                sc[nt][3] *= f1;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    sc[nt][h] *= L::BF16 ? sl2 : f0 * rf[nt][h];
+                    sc[nt][2 + h] *= L::BF16 ? sl2 : f1 * rf[nt][h];
+                }
                 if (masked) {  // (rows past the block's last hold zeros and are not written)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -280,7 +274,21 @@ paged_rows_kernel(const PagedAttnParams p) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) raise |= fmaxf(sc[nt][h], sc[nt][2 + h]) > m_ref[nt][h] + PR_RAISE_LOG2;
             }
+            if (!L::BF16) {
+                if (key0 + 16 > end) {  // scales behind the last key are whatever the page holds
+                    if (key0 + g >= end) vs0 = 0.f;
+                    if (key0 + 8 + g >= end) vs1 = 0.f;
+                }
+                raise |= vref == 0.f || fmaxf(vs0, vs1) > vref * kScaleRefMax;
+            }
             if (__any_sync(0xFFFFFFFFu, raise)) {
+                float ratio = 1.f;
+                if (!L::BF16) {
+                    const float ref = fmaxf(vref, scale_ref(warp_max(fmaxf(isfinite(vs0) ? vs0 : 0.f, isfinite(vs1) ? vs1 : 0.f))));
+                    ratio = vref / ref;  // at most 1: the reference falls below the largest scale only by its power of two
+                    vref = ref;
+                    vup = 1.f / ref;  // a power of two, at most 2^126
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float f[2];
@@ -295,6 +303,7 @@ paged_rows_kernel(const PagedAttnParams p) {
                             m_ref[nt][h] = mx;
                         }
                         l_run[nt][h] *= f[h];
+                        f[h] *= ratio;
                     }
 #pragma unroll
                     for (int i = 0; i < L::MT; ++i) {
@@ -360,16 +369,17 @@ paged_rows_kernel(const PagedAttnParams p) {
                     l_run[nt][h] += e[h] + e[2 + h];
                 }
                 if (!L::BF16) {
+                    const float w0 = vs0 * vup, w1 = vs1 * vup;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {  // a masked key's scale may be anything: 0 stays 0
-                        e[h] = masked && key0 + g > pos[nt][h] ? 0.f : e[h] * vs0;
-                        e[2 + h] = masked && key0 + 8 + g > pos[nt][h] ? 0.f : e[2 + h] * vs1;
+                    for (int h = 0; h < 2; ++h) {  // a masked key's scale may be NaN: 0 stays 0
+                        e[h] = masked && key0 + g > pos[nt][h] ? 0.f : e[h] * w0;
+                        e[2 + h] = masked && key0 + 8 + g > pos[nt][h] ? 0.f : e[2 + h] * w1;
                     }
                 } else if (stray) {
                     add_stray(nt, e);
                 }
-                pb[nt][0] = transpose8(pack_bf16(e[0], e[1]));
-                pb[nt][1] = transpose8(pack_bf16(e[2], e[3]));
+                pb[nt][0] = transpose8(L::BF16 ? pack_bf16(e[0], e[1]) : pack_half(e[0], e[1]));
+                pb[nt][1] = transpose8(L::BF16 ? pack_bf16(e[2], e[3]) : pack_half(e[2], e[3]));
             }
             if (L::BF16 && stray) {
 #pragma unroll
@@ -388,15 +398,15 @@ paged_rows_kernel(const PagedAttnParams p) {
                         const uint32_t a0 = __byte_perm(w0[w], w1[w], 0x5410), a1 = __byte_perm(w0[w], w1[w], 0x7632);
                         const uint32_t a2 = __byte_perm(w2[w], w3[w], 0x5410), a3 = __byte_perm(w2[w], w3[w], 0x7632);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][4 * i + w], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                        for (int nt = 0; nt < NT; ++nt) mma16<L::BF16>(o[nt][4 * i + w], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
                     } else {  // four columns: two m tiles
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            uint32_t a0, a1, a2, a3;
-                            widen4<DTYPE>(__byte_perm(w0[w], w1[w], h ? 0x7632 : 0x5410), a0, a1);
-                            widen4<DTYPE>(__byte_perm(w2[w], w3[w], h ? 0x7632 : 0x5410), a2, a3);
+                            // the two keys of a pair side by side, column by column
+                            const uint2 a = widen4_half<DTYPE>(__byte_perm(w0[w], w1[w], h ? 0x7362 : 0x5140));
+                            const uint2 e = widen4_half<DTYPE>(__byte_perm(w2[w], w3[w], h ? 0x7362 : 0x5140));
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][2 * w + h], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                            for (int nt = 0; nt < NT; ++nt) mma16<L::BF16>(o[nt][2 * w + h], a.x, a.y, e.x, e.y, pb[nt][0], pb[nt][1]);
                         }
                     }
                 }
@@ -425,7 +435,7 @@ paged_rows_kernel(const PagedAttnParams p) {
             for (int h = 0; h < 2; ++h) {
                 const int r = 8 * nt + 2 * t + h;
                 const float mx = fmaxf(fmaxf(sm_m[r], sm_m[RB + r]), fmaxf(sm_m[2 * RB + r], sm_m[3 * RB + r]));
-                f[h] = part_weight(m_ref[nt][h], mx);
+                f[h] = part_weight(m_ref[nt][h], mx) * (L::BF16 ? 1.f : vref);
             }
 #pragma unroll
             for (int i = 0; i < L::MT; ++i)

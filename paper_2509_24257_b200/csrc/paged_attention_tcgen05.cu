@@ -30,9 +30,6 @@
 // Masked entries: scores are replaced by -inf.  Values behind the sequence's last position are whatever the page
 // holds and become 0.  An infinite or NaN value (or value scale) in a tile that some rows may not see entirely is
 // taken out of the product and put into the results of the rows that see it at the end ("stray").
-#include <cuda_fp16.h>
-#include <cuda_fp8.h>
-
 #include "paged.cuh"
 
 namespace vl {
@@ -48,7 +45,6 @@ constexpr int PT_TMEM_COLS = 512;  // S of the groups at 0 and 128, O at 256 and
 // The reference maximum is raised when a score exceeds it by pt_raise (log2), to the score less pt_lift.
 constexpr float pt_raise(bool bf16) { return bf16 ? 8.f : 14.f; }
 constexpr float pt_lift(bool bf16) { return bf16 ? 0.f : 6.f; }
-constexpr float PT_REF_MAX = 128.f;  // largest scale in units of its reference
 // registers per thread of the roles; together what 512 threads are launched with (128 each)
 constexpr int PT_REGS_SOFTMAX = 192, PT_REGS_OTHER = 64;
 static_assert(2 * PT_REGS_SOFTMAX + 2 * PT_REGS_OTHER <= 4 * 128, "");
@@ -99,10 +95,6 @@ __device__ __forceinline__ float pt_max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
 __device__ __forceinline__ void sts16(uint32_t addr, const uint4& x) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
 }
@@ -149,21 +141,6 @@ template <int N>
 __device__ __forceinline__ void set_registers(bool more) {
     if (more) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
-
-// Four codes -> fp16 pairs (0, 1) and (2, 3), exactly.  int8: 0x6400 | (code + 128) is the fp16 number 1152 + code.
-template <int DTYPE>
-__device__ __forceinline__ uint2 widen4_half(uint32_t w) {
-    if (DTYPE == VERILLM_KV_E4M3) {
-        uint2 h;
-        asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}\n" : "=r"(h.x), "=r"(h.y) : "r"(w));
-        return h;
-    }
-    const uint32_t u = w ^ 0x80808080u;
-    const __half2 off = __half2half2(__ushort_as_half(static_cast<unsigned short>(0x6480)));  // 1152
-    const uint32_t lo = __byte_perm(u, 0x64646464u, 0x4140), hi = __byte_perm(u, 0x64646464u, 0x4342);
-    const __half2 a = __hsub2(*reinterpret_cast<const __half2*>(&lo), off), b = __hsub2(*reinterpret_cast<const __half2*>(&hi), off);
-    return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
 // The same times a scale given as the sum of two fp16 numbers (both halves of sh, sl): code * sh + code * sl, rounded
@@ -377,10 +354,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             if (!BF16) {
                 uint32_t mx = 0;
 #pragma unroll
-                for (int c = 0; c < DH / 8; ++c)
-                    mx = __vmaxu2(mx, __vmaxu2(__vmaxu2(qx[c].x & 0x7FFF7FFFu, qx[c].y & 0x7FFF7FFFu), __vmaxu2(qx[c].z & 0x7FFF7FFFu, qx[c].w & 0x7FFF7FFFu)));
-                // |q| 2^(127 - e) lies in [1, 2), e the exponent field of the row's largest entry
-                const uint32_t e = min(max(max(mx >> 16, mx & 0xFFFFu) >> 7, 1u), 253u);
+                for (int c = 0; c < DH / 8; ++c) mx = max(mx, abs_max8(qx[c]));
+                const uint32_t e = row_exponent(mx);
                 const float down = __uint_as_float((254u - e) << 23);
                 rf = sl2 * __uint_as_float(e << 23);
 #pragma unroll
@@ -844,10 +819,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                     km = isfinite(kq[i]) ? fmaxf(km, kq[i]) : km;
                     vm = isfinite(vq[i]) ? fmaxf(vm, vq[i]) : vm;
                 }
-                // 2^-6 of the power of two at or below the largest scale (scales are at least 2^-119)
-                auto ref_of = [](float m) { return __uint_as_float((max(__float_as_uint(m) >> 23, 7u) - 6u) << 23); };
-                const float kref = ref_of(warp_max(km));
-                if (__any_sync(0xFFFFFFFFu, vref == 0.f || vm > vref * PT_REF_MAX)) vref = fmaxf(vref, ref_of(warp_max(vm)));
+                const float kref = scale_ref(warp_max(km));
+                if (__any_sync(0xFFFFFFFFu, vref == 0.f || vm > vref * kScaleRefMax)) vref = fmaxf(vref, scale_ref(warp_max(vm)));
                 // scale / ref as the sum of two fp16 numbers
                 const float kup = 1.f / kref, vup = 1.f / vref;  // powers of two, at most 2^126
                 uint32_t kw[4], vw[4];

@@ -59,13 +59,6 @@ __device__ __forceinline__ const int* cached_cu(const PagedRowsDev& r, int* sm) 
     return sm;
 }
 
-// largest |x| of 8 packed bf16 values as a 15-bit pattern (ordered like the values; >= 0x7F80: not finite)
-__device__ __forceinline__ uint32_t abs_max8(const uint4& x) {
-    const uint32_t a = __vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), b = __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu);
-    const uint32_t m = __vmaxu2(a, b);
-    return max(m & 0xFFFFu, m >> 16);
-}
-
 template <int DTYPE>
 __device__ __forceinline__ uint2 quantise8(const uint4& x, float inv) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
