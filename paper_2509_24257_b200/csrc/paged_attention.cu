@@ -174,11 +174,6 @@ paged_rows_kernel(const PagedAttnParams p) {
         uint4 ka[L::KCHUNKS], kb[L::KCHUNKS], v[L::VPIECES][4];
         float ks0 = 1.f, ks1 = 1.f, vs0 = 1.f, vs1 = 1.f, vs0n = 1.f, vs1n = 1.f;
         auto token_of = [&](int tile) { return tile * PR_TILE + warp * 16; };
-        // index of (page, kv head, row in page) in units of vectors
-        auto vec_of = [&](int key) -> size_t {
-            const int page = load_page(p.r, shift, c.n_pages, k.seq, key, p.status);
-            return ((static_cast<size_t>(page) * c.n_kv_heads + k.kvh) << shift) + (key & ps_mask);
-        };
         auto load_keys = [&](size_t vec) {
             const char* base = reinterpret_cast<const char*>(c.k) + (vec + g) * L::ROW_BYTES + t * 16;
 #pragma unroll
@@ -210,19 +205,44 @@ paged_rows_kernel(const PagedAttnParams p) {
             }
         };
 
+        // Page numbers are read ahead.  With 8-bit pools, whose tiles bring half the bytes, they are read three tiles ahead
+        // and the tile two ahead is asked into L2 (a line per lane), so that the register loads, one tile ahead, find a
+        // short way: 112 -> 100 us for two contexts of 131072.  bf16 has enough in flight without, and reads them one tile
+        // ahead (64 contexts of 2600 on average: 114 us, 119 with the longer chain).
+        auto page_at = [&](int key) { return key < min(end, k.t1 << PR_TILE_LOG) ? load_page(p.r, shift, c.n_pages, k.seq, key, p.status) : 0; };
+        auto vec_in = [&](int page, int key) -> size_t { return ((static_cast<size_t>(page) * c.n_kv_heads + k.kvh) << shift) + (key & ps_mask); };
+        auto prefetch = [&](size_t vec) {
+            const char* row = reinterpret_cast<const char*>(lane < 16 ? c.k : c.v) + (vec + (lane & 15)) * L::ROW_BYTES;
+#pragma unroll
+            for (int i = 0; i < L::ROW_BYTES; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + i));
+        };
         int tile = k.t0;
-        size_t vec = 0;
-        if (token_of(tile) < end) {
-            vec = vec_of(token_of(tile));
-            load_keys(vec);
-            load_values(vec);
+        size_t vec = 0, vec_next = 0;
+        int page2 = 0;
+        {
+            const int key = token_of(tile);
+            const int page0 = page_at(key), page1 = L::BF16 ? 0 : page_at(key + PR_TILE);
+            if (!L::BF16) page2 = page_at(key + 2 * PR_TILE);
+            vec = vec_in(page0, key);
+            vec_next = vec_in(page1, key + PR_TILE);
+            if (key < end) {
+                load_keys(vec);
+                load_values(vec);
+            }
+            if (!L::BF16 && tile + 1 < k.t1 && key + PR_TILE < end) prefetch(vec_next);
         }
         for (; tile < k.t1; ++tile) {
             const int key0 = token_of(tile);
             if (key0 >= end) break;  // the same for every later tile
             const bool more = tile + 1 < k.t1 && key0 + PR_TILE < end;
-            size_t vec_next = 0;
-            if (more) vec_next = vec_of(key0 + PR_TILE);
+            size_t vec2 = 0;
+            if (L::BF16) {
+                vec_next = vec_in(page_at(key0 + PR_TILE), key0 + PR_TILE);
+            } else {
+                vec2 = vec_in(page2, key0 + 2 * PR_TILE);
+                if (tile + 2 < k.t1 && key0 + 2 * PR_TILE < end) prefetch(vec2);
+                page2 = page_at(key0 + 3 * PR_TILE);
+            }
             // ---- S^T = K Q^T: 16 keys x 8 NT rows
             float sc[NT][4];
 #pragma unroll
@@ -413,6 +433,7 @@ paged_rows_kernel(const PagedAttnParams p) {
             }
             if (more) load_values(vec_next);
             vec = vec_next;
+            if (!L::BF16) vec_next = vec2;
         }
 
         // ---- join the four warps: maxima and sums first, then outputs on the common reference
@@ -495,63 +516,84 @@ paged_rows_kernel(const PagedAttnParams p) {
 }
 
 // Joins the partial results of blocks that several CTAs worked on.  One CTA per (possible) such block and group of
-// JOIN_ROWS rows, a warp per row: the lanes first look at all pieces' maxima and sums, then each adds its columns of the
-// pieces in the order of their tiles, eight loads in flight.
-constexpr int JOIN_THREADS = 256, JOIN_ROWS = 32;
-template <int DH>
+// 8 RPW rows, RPW rows per warp: the lanes first look at all pieces' maxima and sums, then each adds its columns of
+// the pieces in the order of their tiles.  The time is that of a few dependent reads of L2, so the reads of one
+// step are all in flight together, and nothing waits for the sequence's description before the results are stored.
+constexpr int JOIN_THREADS = 256;
+template <int DH, int RPW>
 __global__ void __launch_bounds__(JOIN_THREADS)
 paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
-    constexpr int W = DH / 32;  // columns per lane
+    constexpr int W = DH / 32;           // columns per lane
+    constexpr int AHEAD = 8 / RPW;       // pieces in flight
     pdl_wait();
     const int4 h = p.hdr[blockIdx.x];
     if (h.x == 0) return;
-    const SeqView s = load_seq(p.r, p.c.page_shift, h.y, nullptr);
-    const int tok0 = h.w << p.tb_log, rows = min(1 << p.tb_log, s.n - tok0) * p.group;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int r0 = (static_cast<int>(blockIdx.y) * (JOIN_THREADS / 32) + warp) * RPW;  // rows_per_block is a multiple of 8 RPW
+    const SeqView s = load_seq(p.r, p.c.page_shift, h.y, nullptr);
     // piece 0 is CTA blockIdx.x's tail slot, piece i the head slot of CTA blockIdx.x + i
     const float* slot0 = part_slot(p.part, 2 * static_cast<int>(blockIdx.x), rows_per_block, DH);
     const size_t slot = static_cast<size_t>(rows_per_block) * (DH + 2);
     auto part_of = [&](int i) { return slot0 + slot * (i == 0 ? 1 : 2 * i); };
-    const int r_end = min(rows, (static_cast<int>(blockIdx.y) + 1) * JOIN_ROWS);
-    for (int r = static_cast<int>(blockIdx.y) * JOIN_ROWS + warp; r < r_end; r += JOIN_THREADS / 32) {
-        float mx = -INFINITY;
-        for (int i = lane; i < h.x; i += 32) mx = fmaxf(mx, part_of(i)[r]);
-        mx = warp_max(mx);
-        float l = 0.f, acc[W];
-#pragma unroll
-        for (int c = 0; c < W; ++c) acc[c] = 0.f;
-        for (int i0 = 0; i0 < h.x; i0 += 32) {
-            const int i = i0 + lane;
-            float w = 0.f, li = 0.f;
-            if (i < h.x) {
-                w = part_weight(part_of(i)[r], mx);
-                li = part_of(i)[rows_per_block + r] * w;
-            }
-            l += warp_sum(li);
-            const int n = min(32, h.x - i0);
-#pragma unroll 8
-            for (int j = 0; j < n; ++j) {
-                const float wj = __shfl_sync(0xFFFFFFFFu, w, j);
-                const float* src = part_of(i0 + j) + 2 * rows_per_block + r * DH + lane * W;
-                float x[W];
-                if (W == 4) {
-                    const float4 v = *reinterpret_cast<const float4*>(src);
-                    x[0] = v.x; x[1] = v.y; x[W - 2] = v.z; x[W - 1] = v.w;
-                } else {
-                    const float2 v = *reinterpret_cast<const float2*>(src);
-                    x[0] = v.x; x[1] = v.y;
-                }
-#pragma unroll
-                for (int c = 0; c < W; ++c) acc[c] += wj == 0.f ? 0.f : x[c] * wj;
-            }
+    auto columns = [&](int i, int r, float (&x)[W]) {
+        const float* src = part_of(i) + 2 * rows_per_block + r * DH + lane * W;
+        if (W == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(src);
+            x[0] = v.x; x[1] = v.y; x[W - 2] = v.z; x[W - 1] = v.w;
+        } else {
+            const float2 v = *reinterpret_cast<const float2*>(src);
+            x[0] = v.x; x[1] = v.y;
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+    };
+    float mx[RPW], l[RPW], acc[RPW][W];
+#pragma unroll
+    for (int j = 0; j < RPW; ++j) {
+        mx[j] = -INFINITY;
+        l[j] = 0.f;
+#pragma unroll
+        for (int c = 0; c < W; ++c) acc[j][c] = 0.f;
+    }
+    for (int i = lane; i < h.x; i += 32)
+#pragma unroll
+        for (int j = 0; j < RPW; ++j) mx[j] = fmaxf(mx[j], part_of(i)[r0 + j]);
+#pragma unroll
+    for (int j = 0; j < RPW; ++j) mx[j] = warp_max(mx[j]);
+    for (int i0 = 0; i0 < h.x; i0 += 32) {
+        const int i = i0 + lane, n = min(32, h.x - i0);
+        float w[RPW];
+#pragma unroll
+        for (int j = 0; j < RPW; ++j) {
+            w[j] = i < h.x ? part_weight(part_of(i)[r0 + j], mx[j]) : 0.f;
+            l[j] += warp_sum(i < h.x ? part_of(i)[rows_per_block + r0 + j] * w[j] : 0.f);
+        }
+        for (int q0 = 0; q0 < n; q0 += AHEAD) {
+            float x[AHEAD][RPW][W];
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+                for (int j = 0; j < RPW; ++j) columns(i0 + min(q0 + q, n - 1), r0 + j, x[q][j]);
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+                for (int j = 0; j < RPW; ++j) {
+                    const float wq = q0 + q < n ? __shfl_sync(0xFFFFFFFFu, w[j], q0 + q) : 0.f;  // (q0 + q is uniform)
+#pragma unroll
+                    for (int c = 0; c < W; ++c) acc[j][c] += wq == 0.f ? 0.f : x[q][j][c] * wq;
+                }
+        }
+    }
+    const int tok0 = h.w << p.tb_log, rows = min(1 << p.tb_log, s.n - tok0) * p.group;
+#pragma unroll
+    for (int j = 0; j < RPW; ++j) {
+        const int r = r0 + j;
+        if (r >= rows) return;  // (what lies behind the block's rows was never written)
+        const float inv = l[j] == 0.f ? 0.f : 1.f / l[j];
         const int row = s.row0 + tok0 + r / p.group, head = h.z * p.group + r % p.group;
         uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + static_cast<size_t>(row) * p.out_stride +
                                                     static_cast<size_t>(head) * DH + lane * W);
-        if (W == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[W - 2] * inv, acc[W - 1] * inv));
-        else dst[0] = pack_bf16(acc[0] * inv, acc[1] * inv);
-        if (p.lse && lane == 0) p.lse[static_cast<size_t>(row) * p.n_heads + head] = l == 0.f ? -INFINITY : mx * kLn2 + logf(l);
+        if (W == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc[j][0] * inv, acc[j][1] * inv), pack_bf16(acc[j][W - 2] * inv, acc[j][W - 1] * inv));
+        else dst[0] = pack_bf16(acc[j][0] * inv, acc[j][1] * inv);
+        if (p.lse && lane == 0) p.lse[static_cast<size_t>(row) * p.n_heads + head] = l[j] == 0.f ? -INFINITY : mx[j] * kLn2 + logf(l[j]);
     }
 }
 
@@ -640,7 +682,8 @@ cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_s
                                          : rows_launch_dtype<128>(p, s.nt, s.grid, stream);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(s.grid, (s.rows_per_block + JOIN_ROWS - 1) / JOIN_ROWS);
+    const int rpw = s.nt ? 1 : 4;  // rows per warp of the join
+    cfg.gridDim = dim3(s.grid, s.rows_per_block / (JOIN_THREADS / 32 * rpw));
     cfg.blockDim = dim3(JOIN_THREADS);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -648,8 +691,11 @@ cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_s
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return p.c.head_dim == 64 ? cudaLaunchKernelEx(&cfg, paged_join_kernel<64>, p, s.rows_per_block)
-                              : cudaLaunchKernelEx(&cfg, paged_join_kernel<128>, p, s.rows_per_block);
+    if (rpw == 1)
+        return p.c.head_dim == 64 ? cudaLaunchKernelEx(&cfg, paged_join_kernel<64, 1>, p, s.rows_per_block)
+                                  : cudaLaunchKernelEx(&cfg, paged_join_kernel<128, 1>, p, s.rows_per_block);
+    return p.c.head_dim == 64 ? cudaLaunchKernelEx(&cfg, paged_join_kernel<64, 4>, p, s.rows_per_block)
+                              : cudaLaunchKernelEx(&cfg, paged_join_kernel<128, 4>, p, s.rows_per_block);
 }
 
 }  // namespace vl
