@@ -571,10 +571,14 @@ class PagedRows:
             raise ValueError("page_table is [batch][width], cu_rows [batch + 1], kv_len [batch]")
         self.page_table, self.cu_rows, self.kv_len, self.max_rows, self.status = page_table, cu_rows, kv_len, int(max_rows), status
         self.device = page_table.device
+        self._last: Optional[KVRowsC] = None
 
     def c_struct(self, n_rows: int) -> KVRowsC:
-        return KVRowsC(self.page_table.data_ptr(), self.cu_rows.data_ptr(), self.kv_len.data_ptr(), self.page_table.shape[1],
-                       self.kv_len.shape[0], n_rows, self.max_rows)
+        last = self._last  # the struct of the last call, if it had as many rows; never changed once made
+        if last is None or last.n_rows != n_rows:
+            last = self._last = KVRowsC(self.page_table.data_ptr(), self.cu_rows.data_ptr(), self.kv_len.data_ptr(),
+                                        self.page_table.shape[1], self.kv_len.shape[0], n_rows, self.max_rows)
+        return last
 
     def check(self) -> None:
         """Waits for the device and raises if a call reported a problem."""
@@ -593,13 +597,21 @@ def _packed_rows(t: torch.Tensor, what: str, width: int, device: torch.device, d
     return t.stride(0) if t.shape[0] > 1 else width
 
 
-def _on_stream(stream: Optional[torch.cuda.Stream], device: torch.device):
-    """Makes `device`, and `stream` if one is given, current: what a call allocates then belongs to the stream it runs on."""
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # as current_stream().cuda_stream, without the object
+
+
+def _launch(device: torch.device, stream: Optional[torch.cuda.Stream], call):
+    """call(stream pointer) with `device`, and `stream` if one is given, current: what the call allocates then belongs to
+    the stream it runs on.  The common case, current device and stream, takes a short way: a decode step makes many calls."""
     if stream is None:
-        return torch.cuda.device(device)
+        if _raw_stream is not None and torch.cuda.current_device() == device.index:
+            return call(_raw_stream(device.index))
+        with torch.cuda.device(device):
+            return call(_stream_ptr(None))
     if stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the cache on {device}")
-    return torch.cuda.stream(stream)
+    with torch.cuda.stream(stream):
+        return call(stream.cuda_stream)
 
 
 def kv_write(cache: KVCache, rows: PagedRows, k: torch.Tensor, v: torch.Tensor,
@@ -613,9 +625,9 @@ def kv_write(cache: KVCache, rows: PagedRows, k: torch.Tensor, v: torch.Tensor,
     if rows.device != cache.device:
         raise ValueError("rows and cache must be on one device")
     rc = rows.c_struct(k.shape[0])
-    with _on_stream(stream, cache.device):
-        _check(lib().verillm_kv_write(C.byref(cache.c_struct), C.byref(rc), k.data_ptr(), v.data_ptr(), stride, _ptr(rows.status),
-                                      _stream_ptr(stream)), "verillm_kv_write")
+    code = _launch(cache.device, stream, lambda st: lib().verillm_kv_write(
+        C.byref(cache.c_struct), C.byref(rc), k.data_ptr(), v.data_ptr(), stride, _ptr(rows.status), st))
+    _check(code, "verillm_kv_write")
 
 
 def kv_read(cache: KVCache, rows: PagedRows, n_rows: int, dtype: torch.dtype = torch.bfloat16, out=None,
@@ -627,17 +639,20 @@ def kv_read(cache: KVCache, rows: PagedRows, n_rows: int, dtype: torch.dtype = t
     if rows.device != cache.device:
         raise ValueError("rows and cache must be on one device")
     width = cache.n_kv_heads * cache.head_dim
-    with _on_stream(stream, cache.device):
-        if out is None:
-            out = tuple(torch.empty(n_rows, cache.n_kv_heads, cache.head_dim, dtype=dtype, device=cache.device) for _ in range(2))
-        k, v = out
-        stride = _packed_rows(k, "k", width, cache.device, (dtype,))
-        if _packed_rows(v, "v", width, cache.device, (dtype,)) != stride or k.shape[0] != n_rows or v.shape[0] != n_rows:
-            raise ValueError("out must be two tensors of n_rows rows with the same row stride")
+
+    def call(st):
+        k, v = out or [torch.empty(n_rows, cache.n_kv_heads, cache.head_dim, dtype=dtype, device=cache.device) for _ in range(2)]
+        stride = width
+        if out is not None:
+            stride = _packed_rows(k, "k", width, cache.device, (dtype,))
+            if _packed_rows(v, "v", width, cache.device, (dtype,)) != stride or k.shape[0] != n_rows or v.shape[0] != n_rows:
+                raise ValueError("out must be two tensors of n_rows rows with the same row stride")
         rc = rows.c_struct(n_rows)
         _check(lib().verillm_kv_read(C.byref(cache.c_struct), C.byref(rc), k.data_ptr(), v.data_ptr(), stride,
-                                     F32 if dtype == torch.float32 else BF16, _ptr(rows.status), _stream_ptr(stream)), "verillm_kv_read")
-    return k, v
+                                     F32 if dtype == torch.float32 else BF16, _ptr(rows.status), st), "verillm_kv_read")
+        return k, v
+
+    return _launch(cache.device, stream, call)
 
 
 def op_attention_paged(q: torch.Tensor, cache: KVCache, rows: PagedRows, out: Optional[torch.Tensor] = None,
@@ -659,23 +674,28 @@ def op_attention_paged(q: torch.Tensor, cache: KVCache, rows: PagedRows, out: Op
         raise ValueError("lse must be a contiguous float32 [n_rows][n_heads] tensor on the cache's device")
     rc = rows.c_struct(n_rows)
     L = lib()
-    with _on_stream(stream, cache.device):
-        if out is None:
-            out = torch.empty(n_rows, width, dtype=torch.bfloat16, device=cache.device)
-        out_stride = _packed_rows(out, "out", width, cache.device)
-        if out.shape[0] != n_rows:
-            raise ValueError("out must have as many rows as q")
-        if workspace is None:
+
+    def call(st):
+        o, stride, ws = out, width, workspace
+        if o is None:
+            o = torch.empty(n_rows, width, dtype=torch.bfloat16, device=cache.device)
+        else:
+            stride = _packed_rows(o, "out", width, cache.device)
+            if o.shape[0] != n_rows:
+                raise ValueError("out must have as many rows as q")
+        if ws is None:
             need = L.verillm_op_attention_paged_workspace(C.byref(cache.c_struct), C.byref(rc), n_heads)
             if need < 0:
                 raise VerillmError(int(need), "verillm_op_attention_paged_workspace")
-            workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
-        elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != cache.device:
+            ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
+        elif ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != cache.device:
             raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
-        _check(L.verillm_op_attention_paged(C.byref(cache.c_struct), C.byref(rc), q.data_ptr(), q_stride, n_heads, out.data_ptr(),
-                                            out_stride, _ptr(lse), workspace.data_ptr(), workspace.numel(), _ptr(rows.status),
-                                            _stream_ptr(stream)), "verillm_op_attention_paged")
-    return out
+        _check(L.verillm_op_attention_paged(C.byref(cache.c_struct), C.byref(rc), q.data_ptr(), q_stride, n_heads, o.data_ptr(),
+                                            stride, _ptr(lse), ws.data_ptr(), ws.numel(), _ptr(rows.status), st),
+               "verillm_op_attention_paged")
+        return o
+
+    return _launch(cache.device, stream, call)
 
 
 def attention_paged_workspace(cache: KVCache, rows: PagedRows, n_rows: int, n_heads: int) -> int:
