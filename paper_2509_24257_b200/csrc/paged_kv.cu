@@ -7,9 +7,9 @@
 // NaN throughout, and attention sees NaN exactly in the rows that may see the token.  Reading is code * scale, rounded
 // once to the output type.
 //
-// Both kernels move every byte once and are bound by HBM (by latency for a decode step's few rows).  head_dim / 8
-// lanes share a vector, 16-byte loads and stores, the maximum by shuffles; many independent vectors per SM keep
-// the loads in flight.
+// Both kernels move every byte once and are bound by HBM (by latency for a decode step's few rows).  head_dim / 16 lanes
+// share a vector of keys and one of values, 16-byte loads and stores, the maximum by shuffles: a lane then finds the row's
+// place once for 64 bytes.  (8 entries per lane spent the time on finding places: 55 us for 8 x 4096 rows.)
 #include <cuda_fp8.h>
 
 #include "paged.cuh"
@@ -70,34 +70,36 @@ __device__ __forceinline__ uint2 quantise8(const uint4& x, float inv) {
             const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
             const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
             r[h] = lo | (hi << 16);
-        } else {
-            r[h] = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[h] |= (static_cast<uint32_t>(max(-127, min(127, __float2int_rn(f[i])))) & 0xFFu) << (8 * i);
+        } else {  // |f| is at most 127 and a rounding, which rounds to 127
+            const int i0 = __float2int_rn(f[0]), i1 = __float2int_rn(f[1]), i2 = __float2int_rn(f[2]), i3 = __float2int_rn(f[3]);
+            r[h] = __byte_perm(__byte_perm(i0, i1, 0x0040), __byte_perm(i2, i3, 0x0040), 0x5410);
         }
     }
     return make_uint2(r[0], r[1]);
 }
 
-// The vector's codes (this lane's 8) and its scale; called by whole warps.
+// The vector's codes (this lane's 16) and its scale; called by whole warps.
 template <int DH, int DTYPE>
-__device__ __forceinline__ uint2 quantise_vector(const uint4& x, float* scale) {
-    constexpr int LANES = DH / 8;
+__device__ __forceinline__ uint4 quantise_vector(const uint4 (&x)[2], float* scale) {
+    constexpr int LANES = DH / 16;
     constexpr float Q = DTYPE == VERILLM_KV_E4M3 ? 448.f : 127.f;
-    uint32_t bits = abs_max8(x);
+    uint32_t bits = max(abs_max8(x[0]), abs_max8(x[1]));
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) bits = max(bits, __shfl_xor_sync(0xFFFFFFFFu, bits, o));
     const bool finite = bits < 0x7F80u;
     const float amax = fmaxf(bf16_bits_to_float(bits), kMinAmax);
     *scale = finite ? __fdiv_rn(amax, Q) : __int_as_float(0x7FC00000);
-    return finite ? quantise8<DTYPE>(x, __fdiv_rn(Q, amax)) : make_uint2(0u, 0u);
+    if (!finite) return make_uint4(0u, 0u, 0u, 0u);
+    const float inv = __fdiv_rn(Q, amax);
+    const uint2 a = quantise8<DTYPE>(x[0], inv), b = quantise8<DTYPE>(x[1], inv);
+    return make_uint4(a.x, a.y, b.x, b.y);
 }
 
 template <int DH, int DTYPE>
 __global__ void __launch_bounds__(KV_THREADS)
 kv_write_kernel(const PagedCacheDev c, const PagedRowsDev r, const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __restrict__ v,
                 long long row_stride, int* status) {
-    constexpr int LANES = DH / 8, VECS = KV_THREADS / LANES;
+    constexpr int LANES = DH / 16, VECS = KV_THREADS / LANES;
     __shared__ int sm_cu[KV_CACHED_CU];
     const int* cu = cached_cu(r, sm_cu);
     const int lane = threadIdx.x % LANES;
@@ -108,22 +110,26 @@ kv_write_kernel(const PagedCacheDev c, const PagedRowsDev r, const __nv_bfloat16
         const bool in = i < n_vec;
         const int row = in ? static_cast<int>(i / c.n_kv_heads) : 0;
         const int head = in ? static_cast<int>(i - static_cast<long long>(row) * c.n_kv_heads) : 0;
-        const long long src = row * row_stride + head * DH + lane * 8;
-        const uint4 xk = __ldg(reinterpret_cast<const uint4*>(k + src)), xv = __ldg(reinterpret_cast<const uint4*>(v + src));
+        const long long src = row * row_stride + head * DH + lane * 16;
+        const uint4 *pk = reinterpret_cast<const uint4*>(k + src), *pv = reinterpret_cast<const uint4*>(v + src);
+        const uint4 xk[2] = {__ldg(pk), __ldg(pk + 1)}, xv[2] = {__ldg(pv), __ldg(pv + 1)};
         const RowPlace p = place_of_row(r, c, cu, row, status);
         const bool store = in && p.kind == 2;
         const size_t vec = ((static_cast<size_t>(p.page) * c.n_kv_heads + head) << c.page_shift) + p.off;
         if (DTYPE == VERILLM_KV_BF16) {
             if (store) {
-                reinterpret_cast<uint4*>(c.k)[vec * LANES + lane] = xk;
-                reinterpret_cast<uint4*>(c.v)[vec * LANES + lane] = xv;
+                uint4 *dk = reinterpret_cast<uint4*>(c.k) + (vec * LANES + lane) * 2, *dv = reinterpret_cast<uint4*>(c.v) + (vec * LANES + lane) * 2;
+                dk[0] = xk[0];
+                dk[1] = xk[1];
+                dv[0] = xv[0];
+                dv[1] = xv[1];
             }
         } else {
             float ks, vs;
-            const uint2 kc = quantise_vector<DH, DTYPE>(xk, &ks), vc = quantise_vector<DH, DTYPE>(xv, &vs);
+            const uint4 kc = quantise_vector<DH, DTYPE>(xk, &ks), vc = quantise_vector<DH, DTYPE>(xv, &vs);
             if (store) {
-                reinterpret_cast<uint2*>(c.k)[vec * LANES + lane] = kc;
-                reinterpret_cast<uint2*>(c.v)[vec * LANES + lane] = vc;
+                reinterpret_cast<uint4*>(c.k)[vec * LANES + lane] = kc;
+                reinterpret_cast<uint4*>(c.v)[vec * LANES + lane] = vc;
                 if (lane == 0) {
                     c.k_scale[vec] = ks;
                     c.v_scale[vec] = vs;
@@ -152,7 +158,7 @@ __device__ __forceinline__ void decode4(uint32_t w, float* f) {
 
 // One lane's 16 bytes of a stored vector (8 bf16 or 16 codes), times the scale, into the output.
 template <int DTYPE, bool F32>
-__device__ __forceinline__ void read_piece(const uint4& x, float scale, void* out) {
+__device__ __forceinline__ void read_piece(const uint4& x, float scale, void* out, bool wide) {
     constexpr int E = DTYPE == VERILLM_KV_BF16 ? 8 : 16;
     if (DTYPE == VERILLM_KV_BF16 && !F32) {
         *reinterpret_cast<uint4*>(out) = x;
@@ -173,27 +179,37 @@ __device__ __forceinline__ void read_piece(const uint4& x, float scale, void* ou
 #pragma unroll
         for (int i = 0; i < E; ++i) f[i] *= scale;
     }
-    if (F32) {
+    constexpr int WORDS = F32 ? E : E / 2;
+    uint32_t y[WORDS];
 #pragma unroll
-        for (int i = 0; i < E / 4; ++i) reinterpret_cast<float4*>(out)[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+    for (int i = 0; i < WORDS; ++i) y[i] = F32 ? __float_as_uint(f[i]) : pack_bf16(f[2 * i], f[(2 * i + 1) % E]);
+    if (WORDS >= 8 && wide) {  // whole sectors
+#pragma unroll
+        for (int i = 0; i < WORDS / 8; ++i)
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(static_cast<char*>(out) + 32 * i), "r"(y[(8 * i) % WORDS]),
+                         "r"(y[(8 * i + 1) % WORDS]), "r"(y[(8 * i + 2) % WORDS]), "r"(y[(8 * i + 3) % WORDS]), "r"(y[(8 * i + 4) % WORDS]),
+                         "r"(y[(8 * i + 5) % WORDS]), "r"(y[(8 * i + 6) % WORDS]), "r"(y[(8 * i + 7) % WORDS])
+                         : "memory");
     } else {
 #pragma unroll
-        for (int i = 0; i < E / 8; ++i)
-            reinterpret_cast<uint4*>(out)[i] = make_uint4(pack_bf16(f[8 * i], f[8 * i + 1]), pack_bf16(f[8 * i + 2], f[8 * i + 3]),
-                                                          pack_bf16(f[8 * i + 4], f[8 * i + 5]), pack_bf16(f[8 * i + 6], f[8 * i + 7]));
+        for (int i = 0; i < WORDS / 4; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
     }
 }
 
 template <int DH, int DTYPE, bool F32>
 __global__ void __launch_bounds__(KV_THREADS)
-kv_read_kernel(const PagedCacheDev c, const PagedRowsDev r, void* __restrict__ k, void* __restrict__ v, long long row_stride, int* status) {
+kv_read_kernel(const PagedCacheDev c, const PagedRowsDev r, void* __restrict__ k, void* __restrict__ v, long long row_stride, bool wide, int* status) {
     constexpr int E = DTYPE == VERILLM_KV_BF16 ? 8 : 16, LANES = DH / E, VECS = KV_THREADS / LANES;
     __shared__ int sm_cu[KV_CACHED_CU];
     const int* cu = cached_cu(r, sm_cu);
     const int lane = threadIdx.x % LANES;
-    const long long n_vec = static_cast<long long>(r.n_rows) * c.n_kv_heads;
+    // 16 rows of one head, then the next head: the rows of a page lie together in the pool
+    const long long n_vec = static_cast<long long>((r.n_rows + 15) / 16) * 16 * c.n_kv_heads;
     for (long long i = static_cast<long long>(blockIdx.x) * VECS + threadIdx.x / LANES; i < n_vec; i += static_cast<long long>(gridDim.x) * VECS) {
-        const int row = static_cast<int>(i / c.n_kv_heads), head = static_cast<int>(i - static_cast<long long>(row) * c.n_kv_heads);
+        const long long q = i >> 4;
+        const int block = static_cast<int>(q / c.n_kv_heads), head = static_cast<int>(q - static_cast<long long>(block) * c.n_kv_heads);
+        const int row = block * 16 + static_cast<int>(i & 15);
+        if (row >= r.n_rows) continue;
         const RowPlace p = place_of_row(r, c, cu, row, status);
         if (p.kind == 0) continue;  // behind the last sequence: left as it is
         const long long dst = (row * row_stride + head * DH + lane * E) * (F32 ? 4 : 2);
@@ -208,15 +224,15 @@ kv_read_kernel(const PagedCacheDev c, const PagedRowsDev r, void* __restrict__ k
                 vs = __ldg(c.v_scale + vec);
             }
         }
-        read_piece<DTYPE, F32>(xk, ks, static_cast<char*>(k) + dst);
-        read_piece<DTYPE, F32>(xv, vs, static_cast<char*>(v) + dst);
+        read_piece<DTYPE, F32>(xk, ks, static_cast<char*>(k) + dst, wide);
+        read_piece<DTYPE, F32>(xv, vs, static_cast<char*>(v) + dst, wide);
     }
 }
 
 template <int DH, int DTYPE>
 cudaError_t write_one(const PagedCacheDev& c, const PagedRowsDev& r, const void* k, const void* v, long long row_stride, int* status,
                       int num_sms, cudaStream_t stream) {
-    constexpr int VECS = KV_THREADS / (DH / 8);
+    constexpr int VECS = KV_THREADS / (DH / 16);
     const long long blocks = (static_cast<long long>(r.n_rows) * c.n_kv_heads + VECS - 1) / VECS;
     kv_write_kernel<DH, DTYPE><<<static_cast<unsigned>(blocks < 8LL * num_sms ? blocks : 8LL * num_sms), KV_THREADS, 0, stream>>>(
         c, r, reinterpret_cast<const __nv_bfloat16*>(k), reinterpret_cast<const __nv_bfloat16*>(v), row_stride, status);
@@ -227,9 +243,11 @@ template <int DH, int DTYPE, bool F32>
 cudaError_t read_one(const PagedCacheDev& c, const PagedRowsDev& r, void* k, void* v, long long row_stride, int* status, int num_sms,
                      cudaStream_t stream) {
     constexpr int VECS = KV_THREADS / (DH / (DTYPE == VERILLM_KV_BF16 ? 8 : 16));
-    const long long blocks = (static_cast<long long>(r.n_rows) * c.n_kv_heads + VECS - 1) / VECS;
+    const long long blocks = (static_cast<long long>((r.n_rows + 15) / 16) * 16 * c.n_kv_heads + VECS - 1) / VECS;
+    // 32-byte stores where the rows allow them
+    const bool wide = ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | static_cast<uintptr_t>(row_stride * (F32 ? 4 : 2))) & 31u) == 0;
     kv_read_kernel<DH, DTYPE, F32><<<static_cast<unsigned>(blocks < 8LL * num_sms ? blocks : 8LL * num_sms), KV_THREADS, 0, stream>>>(
-        c, r, k, v, row_stride, status);
+        c, r, k, v, row_stride, wide, status);
     return cudaGetLastError();
 }
 
