@@ -898,6 +898,20 @@ int make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_
     return r == CUDA_SUCCESS ? 0 : -3;
 }
 
+int make_tmap_bf16_heads(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint64_t head_dim, uint64_t ld_elems,
+                         uint32_t box_heads, uint32_t box_rows) {
+    if (!g_encode) return -1;
+    if ((reinterpret_cast<uintptr_t>(base) & 15u) != 0 || (ld_elems * 2) % 16 != 0 || head_dim % 64 != 0) return -2;
+    const cuuint64_t dims[3] = {head_dim, heads, rows};
+    const cuuint64_t strides[2] = {head_dim * 2, ld_elems * 2};
+    const cuuint32_t box[3] = {64, box_heads, box_rows};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? 0 : -3;
+}
+
 int make_tmap_bytes_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
     if (!g_encode) return -1;
     if ((reinterpret_cast<uintptr_t>(base) & 15u) != 0 || cols % 16 != 0 || cols > 256) return -2;

@@ -72,6 +72,9 @@ struct GemmParams {
 // Maps are encoded for a box of 64 (K) x 128 rows (A) and 64 x 256 rows (B), 128-byte swizzle.
 int make_tmap_bf16_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld_elems,
                       uint32_t box_rows);
+// Rows of `heads` vectors of head_dim bf16 (head_dim a multiple of 64): boxes of 64 columns x box_heads x box_rows, 128-byte swizzle.
+int make_tmap_bf16_heads(CUtensorMap* map, const void* base, uint64_t rows, uint64_t heads, uint64_t head_dim, uint64_t ld_elems,
+                         uint32_t box_heads, uint32_t box_rows);
 // A packed matrix of bytes, boxes of whole rows (cols <= 256, a multiple of 16), no swizzle.
 int make_tmap_bytes_2d(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
 cudaError_t launch_gemm(int epilogue, const CUtensorMap& tmap_a, const CUtensorMap& tmap_b, const GemmParams& p,

@@ -8,11 +8,11 @@
 //   warps 0-3, 4-7  softmax of the two groups, one row per thread: scores from tensor memory, running reference maximum
 //                   and sum in registers, probabilities back as 16-bit pairs over the upper half of the score columns
 //                   (three quarters first, so that most of P V runs under the last quarter's exponentials);
-//                   they also bring the block's queries into shared memory and write the results
+//                   they also write the results (and, 8-bit cache, scale the queries)
 //   warps 8-11      bf16 cache: clean the values of tiles on the diagonal; 8-bit cache: widen the codes, half a tile at a
 //                   time, and store them as operand tiles
 //   warp 12         one thread issues S = Q K^T and O += P V of both groups (tcgen05.mma)
-//   warp 13         walks the CTA's share of the work and hands the parts out
+//   warp 13         walks the CTA's share of the work, hands the parts out and loads their queries (TMA)
 //   warp 14         TMA loads of keys and values (8-bit cache: of codes into a ring of half tiles), a box and a lane per page
 //   warp 15         8-bit cache: the scales of the next tiles
 // The 64-column halves of all operand tiles use the 128-byte swizzle; values are consumed as they lie in memory
@@ -195,7 +195,8 @@ __device__ __noinline__ Stray find_stray(const PagedAttnParams& p, int seq, int 
 
 template <int DH, int DTYPE>
 __global__ void __launch_bounds__(PT_THREADS, 1)
-paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ PagedAttnParams p) {
+paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                const __grid_constant__ PagedAttnParams p) {
     using L = PtSmem<DH, DTYPE>;
     constexpr bool BF16 = L::BF16;
     constexpr int HALVES = DH / 64;
@@ -229,6 +230,8 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     auto raw_empty = [&](int i) { return bar + 336 + 8 * i; };
     auto word_full = [&](int i) { return bar + 360 + 8 * i; };
     auto word_empty = [&](int i) { return bar + 384 + 8 * i; };
+    const uint32_t q_loaded = bar + 608, q_empty = bar + 616;
+    auto q_ready = [&](int w) { return bar + 624 + 8 * w; };
     const uint32_t tmem_slot = bar + 408;
     volatile uint32_t* tmem_slot_ptr = reinterpret_cast<volatile uint32_t*>(pt_smem + L::BAR_OFF + 408);
     volatile int* failed = reinterpret_cast<volatile int*>(pt_smem + L::BAR_OFF + 412);
@@ -241,6 +244,10 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
     if (tid == 0) {
         *failed = 0;
         *stray = 0;
+        mbar_init(q_loaded, 1);
+        mbar_init(q_empty, 1);
+        mbar_init(q_ready(0), 1);
+        mbar_init(q_ready(1), 1);
         for (int w = 0; w < 2; ++w) {
             mbar_init(q_full(w), 4);
             mbar_init(s_full(w), 1);
@@ -338,47 +345,48 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             }
             return false;
         };
-        auto fetch_q = [&](uint4 (&qx)[DH / 8]) {
+        int nq = 0;  // parts of this group whose queries were awaited
+        auto place = [&]() {
             valid = r < u.rows;
             const int tok = valid ? r / G : 0;
             hd = u.kvh * G + (valid ? r - tok * G : 0);
             row = static_cast<size_t>(u.row0 + tok);
             pos = valid ? u.first_pos + tok : -1;
-            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.q) + row * p.q_stride + static_cast<size_t>(hd) * DH);
-#pragma unroll
-            for (int c = 0; c < DH / 8; ++c) qx[c] = __ldg(src + c);
         };
-        // into the swizzled operand tile, whose previous contents have been used: the scores of the last tile were read
-        auto store_q = [&](uint4 (&qx)[DH / 8]) {
-            const uint32_t dst = q_s + r * 128;
-            if (!BF16) {
-                uint32_t mx = 0;
+        // 8-bit pools: the row's queries to fp16, in place
+        auto convert_q = [&]() -> bool {
+            if (BF16) return true;
+            if (!warp_wait(q_ready(w), nq++ & 1, status)) return false;
+            uint4 qx[DH / 8];
+            const uint32_t at = q_s + r * 128;
+            uint32_t mx = 0;
 #pragma unroll
-                for (int c = 0; c < DH / 8; ++c) mx = max(mx, abs_max8(qx[c]));
-                const uint32_t e = row_exponent(mx);
-                const float down = __uint_as_float((254u - e) << 23);
-                rf = sl2 * __uint_as_float(e << 23);
-#pragma unroll
-                for (int c = 0; c < DH / 8; ++c) {
-                    const uint4 x = qx[c];
-                    qx[c] = make_uint4(pack_half(bf16_lo(x.x) * down, bf16_hi(x.x) * down), pack_half(bf16_lo(x.y) * down, bf16_hi(x.y) * down),
-                                       pack_half(bf16_lo(x.z) * down, bf16_hi(x.z) * down), pack_half(bf16_lo(x.w) * down, bf16_hi(x.w) * down));
-                }
+            for (int c = 0; c < DH / 8; ++c) {
+                qx[c] = lds16(at + (c >> 3) * L::Q_HALF + (((c & 7) ^ (r & 7)) << 4));
+                mx = max(mx, abs_max8(qx[c]));
             }
+            const uint32_t e = row_exponent(mx);
+            const float down = __uint_as_float((254u - e) << 23);
+            rf = sl2 * __uint_as_float(e << 23);
 #pragma unroll
-            for (int c = 0; c < DH / 8; ++c) sts16(dst + (c >> 3) * L::Q_HALF + (((c & 7) ^ (r & 7)) << 4), qx[c]);
+            for (int c = 0; c < DH / 8; ++c) {
+                const uint4 x = qx[c];
+                sts16(at + (c >> 3) * L::Q_HALF + (((c & 7) ^ (r & 7)) << 4),
+                      make_uint4(pack_half(bf16_lo(x.x) * down, bf16_hi(x.x) * down), pack_half(bf16_lo(x.y) * down, bf16_hi(x.y) * down),
+                                 pack_half(bf16_lo(x.z) * down, bf16_hi(x.z) * down), pack_half(bf16_lo(x.w) * down, bf16_hi(x.w) * down)));
+            }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full(w));
+            return true;
         };
         const bool wide_out = ((reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(p.out_stride * 2)) & 31u) == 0;
         bool have = next_part();
         if (have) {
-            uint4 qx[DH / 8];
-            fetch_q(qx);
-            store_q(qx);
+            place();
+            ok = convert_q();
         }
-        while (have) {
+        while (have && ok) {
             const int mask_tile = u.mask_tile();
             float m_ref = -INFINITY, l_run = 0.f, vref = 0.f;
             for (int t = u.t0; t < u.t1; ++t, ++g, ++sg) {
@@ -480,22 +488,19 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                 l_run += (rs2[0].x + rs2[0].y) + (rs2[1].x + rs2[1].y);
             }
             if (!ok) break;
-            // ---- results: the whole block's, or this part's for the join.  The next part's queries go first, so that
-            // its first scores are formed under the output pass.
+            // ---- results: the whole block's, or this part's for the join.  The next part's queries are prepared first, so
+            // that its first scores are formed under the output pass.
             const bool whole = u.whole != 0, row_valid = valid;
             const size_t out_row = row;
             const int out_hd = hd, seq = u.seq, kvh = u.kvh;
             const int odd_from = max(u.t0, mask_tile) << PT_TILE_LOG, odd_to = min(pos + 1, u.t1 << PT_TILE_LOG);
             float* part = part_slot(p.part, 2 * static_cast<int>(blockIdx.x) + (u.t0 == 0 ? 1 : 0), PT_ROWS, DH);
             have = next_part();
-            uint4 qx[DH / 8];
-#pragma unroll
-            for (int c = 0; c < DH / 8; ++c) qx[c] = make_uint4(0u, 0u, 0u, 0u);
-            if (have) fetch_q(qx);
+            if (have) place();
+            if (have && !convert_q()) { ok = false; break; }
             if (!warp_wait(o_done(w), au & 1, status)) { ok = false; break; }
             ++au;
             tc_fence_after();
-            if (have) store_q(qx);
             const float inv = (whole ? (l_run == 0.f ? 0.f : 1.f / l_run) : 1.f) * (BF16 ? 1.f : vref);
             const bool odd = *stray != 0;
             if (row_valid) {
@@ -696,13 +701,14 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
                     if (w >= groups) break;
-                    if (!warp_wait(q_full(w), au[w] & 1, status)) { ok = false; break; }
+                    if (!warp_wait(BF16 ? q_loaded : q_full(w), (BF16 ? np - 1 : au[w]) & 1, status)) { ok = false; break; }
                     tc_fence_after();
                     scores(w, g);
                     ++au[w];
                 }
                 if (!ok) break;
                 mma_commit(leader, k_empty(g % PT_KSTAGES));
+                if (t0 + 1 == t1) mma_commit(leader, q_empty);
                 for (int t = t0; t < t1; ++t, ++g) {
                     const int vb = g % PT_VSTAGES;
                     const bool more = t + 1 < t1;
@@ -735,6 +741,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
                     if (!ok) break;
                     mma_commit(leader, v_empty(vb));
                     if (more) mma_commit(leader, k_empty((g + 1) % PT_KSTAGES));
+                    if (t + 2 == t1) mma_commit(leader, q_empty);  // the part's last scores are under way
                 }
                 if (!ok) break;
             }
@@ -868,6 +875,23 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constan
             __syncwarp();
             if (lane == 0) mbar_arrive(part_full(i));
             if (!more) break;
+            // the part's queries, one box of (64 columns, heads of the group, tokens of a block) per half, once the
+            // previous part's last scores are formed; rows behind the part's are other rows of q or zeros
+            if (n > 0 && !warp_wait(q_empty, (n - 1) & 1, status)) { ok = false; break; }
+            if (lane == 0) {
+                mbar_arrive_expect_tx(q_loaded, static_cast<uint32_t>(G << p.tb_log) * DH * 2);
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) tma_load_3d(q_s + h * L::Q_HALF, &tmap_q, h * 64, k.kvh * G, k.s.row0 + (k.j << p.tb_log), q_loaded);
+            }
+            __syncwarp();
+            if (!BF16) {  // passed on to the groups that have rows: a group that skips parts would misread q_loaded's phase
+                if (!warp_wait(q_loaded, n & 1, status)) { ok = false; break; }
+                if (lane == 0) {
+                    mbar_arrive(q_ready(0));
+                    if (min(1 << p.tb_log, k.s.n - (k.j << p.tb_log)) * G > PT_GROUP_ROWS) mbar_arrive(q_ready(1));
+                }
+                __syncwarp();
+            }
             more = walk_next<PT_TILE_LOG>(p.r, shift, n_kv, p.tb_log, share, k);
         }
         if (lane == 0) p.hdr[blockIdx.x] = header;
@@ -897,7 +921,10 @@ cudaError_t tc_init() {
 }
 template <int DH, int DTYPE>
 cudaError_t tc_launch(const PagedAttnParams& p, int grid, cudaStream_t stream) {
-    CUtensorMap tk, tv;
+    CUtensorMap tq, tk, tv;
+    if (make_tmap_bf16_heads(&tq, p.q, static_cast<uint64_t>(p.r.n_rows), static_cast<uint64_t>(p.n_heads), DH, static_cast<uint64_t>(p.q_stride),
+                             static_cast<uint32_t>(p.group), 1u << p.tb_log) != 0)
+        return cudaErrorInvalidValue;
     const uint64_t rows = static_cast<uint64_t>(p.c.n_pages) * p.c.n_kv_heads << p.c.page_shift;
     const uint32_t page = 1u << p.c.page_shift;
     if (DTYPE == VERILLM_KV_BF16) {
@@ -907,7 +934,7 @@ cudaError_t tc_launch(const PagedAttnParams& p, int grid, cudaStream_t stream) {
         const uint32_t box = page < PT_TILE / 2 ? page : PT_TILE / 2;
         if (make_tmap_bytes_2d(&tk, p.c.k, rows, DH, box) != 0 || make_tmap_bytes_2d(&tv, p.c.v, rows, DH, box) != 0) return cudaErrorInvalidValue;
     }
-    paged_tc_kernel<DH, DTYPE><<<grid, PT_THREADS, PtSmem<DH, DTYPE>::TOTAL, stream>>>(tk, tv, p);
+    paged_tc_kernel<DH, DTYPE><<<grid, PT_THREADS, PtSmem<DH, DTYPE>::TOTAL, stream>>>(tq, tk, tv, p);
     return cudaGetLastError();
 }
 

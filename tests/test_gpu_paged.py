@@ -179,6 +179,8 @@ def test_attention_over_many_sequences(dtype):
     (16, 8, 64, 16, 40, 300, 500),     # several blocks per CTA, many with one group of rows only
     (16, 4, 128, 32, 24, 70, 1600),    # many tiles per CTA
     (64, 8, 128, 64, 12, 100, 900),
+    (28, 4, 64, 32, 30, 90, 300),      # 7 query heads per kv head: blocks of 224 rows
+    (4, 4, 128, 16, 60, 400, 450),     # blocks of one and of two groups in turn
 ])
 def test_chunks_of_a_large_batch(heads, kv_heads, dh, page, batch, most_rows, most_kv, dtype):
     rng = np.random.default_rng(7)
