@@ -95,6 +95,11 @@ __host__ __device__ __forceinline__ long long tiles_of_head(const SeqView& s, in
     return tiles_before<TL>(s.len - s.n, tb_log, block_count(s.n, tb_log) - 1) + tiles_of_end<TL>(s.len);
 }
 
+// a / b of numbers that are not negative and mostly fit 32 bits, where the division is much shorter
+__device__ __forceinline__ long long short_div(long long a, long long b) {
+    return ((a | b) >> 31) == 0 ? static_cast<long long>(static_cast<unsigned>(a) / static_cast<unsigned>(b)) : a / b;
+}
+
 // The CTA's share of the line of tiles.
 struct WorkShare {
     long long begin, end, total, per;
@@ -117,6 +122,7 @@ __device__ __forceinline__ void find_share(const PagedRowsDev& r, int page_shift
     auto tiles = [&](int b) -> long long {
         return b < r.batch ? tiles_of_head<TL>(load_seq(r, page_shift, b, st0), tb_log) * n_kv_heads : 0;
     };
+    const int live = min(nwarps, (r.batch + 31) >> 5);  // the other warps have nothing to add
     // inclusive scan over the block of one value per thread; returns the block's total
     long long mine = 0, incl = 0;
     auto scan = [&](long long v) -> long long {
@@ -130,7 +136,7 @@ __device__ __forceinline__ void find_share(const PagedRowsDev& r, int page_shift
         if (lane == 31) sc->warp_sum[warp] = incl;
         __syncthreads();
         long long before = 0, total = 0;
-        for (int i = 0; i < nwarps; ++i) {
+        for (int i = 0; i < live; ++i) {
             const long long s = sc->warp_sum[i];
             before += i < warp ? s : 0;
             total += s;
@@ -149,7 +155,7 @@ __device__ __forceinline__ void find_share(const PagedRowsDev& r, int page_shift
         total = scan(v);
     }
     w.total = total;
-    long long per = (total + gridDim.x - 1) / gridDim.x;
+    long long per = short_div(total + gridDim.x - 1, gridDim.x);
     if (per < min_per) per = min_per;
     w.per = per;
     w.begin = min(per * blockIdx.x, total);
@@ -193,7 +199,7 @@ __device__ __forceinline__ void walk_begin(const PagedRowsDev& r, int page_shift
     k.seq = w.seq;
     k.s = load_seq(r, page_shift, k.seq, nullptr);
     const long long per_head = tiles_of_head<TL>(k.s, tb_log);
-    k.kvh = static_cast<int>(w.offset / per_head);
+    k.kvh = static_cast<int>(short_div(w.offset, per_head));
     const long long x = w.offset - per_head * k.kvh;
     const int ctx = k.s.len - k.s.n;
     int lo = 0, hi = block_count(k.s.n, tb_log) - 1;  // the last block that begins at or before x

@@ -471,7 +471,7 @@ paged_rows_kernel(const PagedAttnParams p) {
         const int slot = 2 * blockIdx.x + (k.t0 == 0 ? 1 : 0);
         float* part = part_slot(p.part, slot, RB, DH);
         if (!whole && k.t0 == 0)
-            header = make_int4(static_cast<int>((k.at + k.tiles - 1) / share.per) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
+            header = make_int4(static_cast<int>(short_div(k.at + k.tiles - 1, share.per)) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
         constexpr int LPR = DH / 8;  // lanes per row, 8 columns each
         for (int r = tid / LPR; r < rows; r += PR_THREADS / LPR) {
             const int cx = (tid % LPR) * 8;

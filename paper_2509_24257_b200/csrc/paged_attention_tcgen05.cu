@@ -279,27 +279,27 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
         }
         fence_mbar_init();
     }
-    WorkShare share;
-    find_share<PT_TILE_LOG>(p.r, p.c.page_shift, p.c.n_kv_heads, p.tb_log, PT_THREADS, 1, scratch, share, p.status);
-    pdl_launch_dependents();
-    if (share.begin >= share.end) {
-        if (tid == 0) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
-        return;
-    }
-    if (warp == 12) {
+    if (warp == 12) {  // (under the reads below)
         tmem_alloc(tmem_slot, PT_TMEM_COLS);
         tmem_relinquish();
     }
     tc_fence_before();
-    __syncthreads();
+    WorkShare share;
+    find_share<PT_TILE_LOG>(p.r, p.c.page_shift, p.c.n_kv_heads, p.tb_log, PT_THREADS, 1, scratch, share, p.status);
+    pdl_launch_dependents();
     tc_fence_after();
+    if (share.begin >= share.end) {
+        if (tid == 0) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (warp == 12) tmem_dealloc(*tmem_slot_ptr, PT_TMEM_COLS);
+        return;
+    }
     // All 512 columns are this CTA's, so they begin at 0 (known to the compiler); anything else is refused.
     constexpr uint32_t tmem_base = 0;
-    if (*tmem_slot_ptr != tmem_base) {
+    const bool based = *tmem_slot_ptr == tmem_base;  // the same in all threads
+    if (!based && tid == 0) {
         raise_status(p.status, VERILLM_DEV_WAIT_TIMEOUT);
         *failed = 1;
     }
-    __syncthreads();
     int* status = p.status;
     const int shift = p.c.page_shift, ps_mask = (1 << shift) - 1, n_kv = p.c.n_kv_heads, G = p.group;
 
@@ -321,7 +321,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     };
     int np = 0;
     Part u;
-    bool ok = *failed == 0;
+    bool ok = based;
 
     if (!ok) {
     } else if (warp < 8) {
@@ -511,11 +511,14 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
                     part[PT_ROWS + r] = l_run;
                 }
             }
-#pragma unroll 1
+            uint32_t oo[DH / 32][32];  // all at once: one latency
+#pragma unroll
+            for (int c = 0; c < DH / 32; ++c) tmem_ld32(o_addr + c * 32, oo[c]);
+#pragma unroll
+            for (int c = 0; c < DH / 32; ++c) tmem_ld_wait_regs(oo[c]);
+#pragma unroll
             for (int c = 0; c < DH / 32; ++c) {
-                uint32_t o[32];
-                tmem_ld32(o_addr + c * 32, o);
-                tmem_ld_wait_regs(o);
+                uint32_t(&o)[32] = oo[c];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = l_run == 0.f ? 0u : __float_as_uint(__uint_as_float(o[i]) * inv);
                 if (odd) {
@@ -863,7 +866,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
                 const int tok0 = k.j << p.tb_log;
                 const bool whole = k.t0 == 0 && k.t1 == k.tiles;
                 if (!whole && k.t0 == 0)
-                    header = make_int4(static_cast<int>((k.at + k.tiles - 1) / share.per) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
+                    header = make_int4(static_cast<int>(short_div(k.at + k.tiles - 1, share.per)) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
                 if (lane == 0) {
                     parts[2 * i] = make_int4(k.s.row0 + tok0, k.s.len - k.s.n + tok0, min(1 << p.tb_log, k.s.n - tok0) * G, k.seq);
                     parts[2 * i + 1] = make_int4(k.kvh, k.t0, k.t1, whole ? 1 : 0);
