@@ -345,7 +345,7 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  *  out       DEVICE bf16, same form with out_stride; a row that attends to nothing receives zeros
  *  lse       optional DEVICE float32 [n_rows][n_heads]: log of the sum of exp(scores), -inf for such a row
  *  workspace DEVICE, 256-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code).
- *            It holds nothing between calls, but calls that may overlap (other streams, graphs replayed side by side)
+ *            May be NULL where that is 0.  It holds nothing between calls, but calls that may overlap (other streams, graphs replayed side by side)
  *            need one each.
  * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 128 per kv head; workspace too
  * small), E_ARCH, E_CUDA. */

@@ -526,23 +526,24 @@ class KVCache:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
-        dtype = _KV_DTYPES.get(k.dtype)
-        if dtype is None or k.dim() != 4 or v.dtype != k.dtype or v.shape != k.shape:
+        dtype, shape, dev = _KV_DTYPES.get(k.dtype), k.shape, k.get_device()
+        if dtype is None or len(shape) != 4 or v.dtype != k.dtype or v.shape != shape:
             raise ValueError("k and v pools must be [n_pages][n_kv_heads][page_size][head_dim] of one type: bf16, float8_e4m3fn or int8")
-        tensors = [k, v]
         if dtype != KV_BF16:
             if k_scale is None or v_scale is None:
                 raise ValueError("8-bit pools need k_scale and v_scale")
-            if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
-                raise ValueError("scales must be float32 [n_pages][n_kv_heads][page_size]")
-            tensors += [k_scale, v_scale]
+            for t in (k_scale, v_scale):
+                if t.dtype != torch.float32 or t.shape != shape[:3]:
+                    raise ValueError("scales must be float32 [n_pages][n_kv_heads][page_size]")
+                if t.get_device() != dev or not t.is_contiguous():
+                    raise ValueError("pools and scales must be contiguous and on one CUDA device")
         elif k_scale is not None or v_scale is not None:
             raise ValueError("bf16 pools have no scales")
-        if not k.is_cuda or any(t.device != k.device or not t.is_contiguous() for t in tensors):
+        if dev < 0 or v.get_device() != dev or not k.is_contiguous() or not v.is_contiguous():
             raise ValueError("pools and scales must be contiguous and on one CUDA device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.device = k.device
-        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
         self.c_struct = KVCacheC(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), self.n_pages, self.page_size,
                                  self.n_kv_heads, self.head_dim, dtype)
 
@@ -563,11 +564,12 @@ class PagedRows:
 
     def __init__(self, page_table: torch.Tensor, cu_rows: torch.Tensor, kv_len: torch.Tensor, max_rows: int,
                  status: Optional[torch.Tensor] = None):
+        dev = page_table.get_device()
         for t in (page_table, cu_rows, kv_len) if status is None else (page_table, cu_rows, kv_len, status):
-            if t.dtype != torch.int32 or not t.is_cuda or t.device != page_table.device or not t.is_contiguous():
+            if t.dtype != torch.int32 or t.get_device() != dev or dev < 0 or not t.is_contiguous():
                 raise ValueError("page_table, cu_rows, kv_len and status must be contiguous int32 tensors on one CUDA device")
-        batch = kv_len.shape[0]
-        if page_table.dim() != 2 or page_table.shape[0] != batch or tuple(cu_rows.shape) != (batch + 1,) or kv_len.dim() != 1:
+        table = page_table.shape
+        if len(table) != 2 or kv_len.shape != table[:1] or cu_rows.shape != (table[0] + 1,):
             raise ValueError("page_table is [batch][width], cu_rows [batch + 1], kv_len [batch]")
         self.page_table, self.cu_rows, self.kv_len, self.max_rows, self.status = page_table, cu_rows, kv_len, int(max_rows), status
         self.device = page_table.device
@@ -588,13 +590,14 @@ class PagedRows:
 
 def _packed_rows(t: torch.Tensor, what: str, width: int, device: torch.device, dtypes=(torch.bfloat16,)) -> int:
     """Row stride of a [rows][width] or [rows][heads][head_dim] tensor whose rows are contiguous."""
-    if t.dtype not in dtypes or t.device != device or t.dim() not in (2, 3):
+    shape, strides = t.shape, t.stride()
+    if t.dtype not in dtypes or t.device != device or len(shape) not in (2, 3):
         raise ValueError(f"{what} must be a 2- or 3-dimensional {' / '.join(str(d) for d in dtypes)} tensor on {device}")
-    inner = t.shape[1] if t.dim() == 2 else t.shape[1] * t.shape[2]
-    packed = t.stride(-1) == 1 and (t.dim() == 2 or t.shape[1] == 1 or t.stride(1) == t.shape[2])
+    inner = shape[1] if len(shape) == 2 else shape[1] * shape[2]
+    packed = strides[-1] == 1 and (len(shape) == 2 or shape[1] == 1 or strides[1] == shape[2])
     if inner != width or not packed:
         raise ValueError(f"{what} must have {width} consecutive entries per row")
-    return t.stride(0) if t.shape[0] > 1 else width
+    return strides[0] if shape[0] > 1 else width
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # as current_stream().cuda_stream, without the object
@@ -687,11 +690,11 @@ def op_attention_paged(q: torch.Tensor, cache: KVCache, rows: PagedRows, out: Op
             need = L.verillm_op_attention_paged_workspace(C.byref(cache.c_struct), C.byref(rc), n_heads)
             if need < 0:
                 raise VerillmError(int(need), "verillm_op_attention_paged_workspace")
-            ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
+            ws = torch.empty(need, dtype=torch.uint8, device=cache.device) if need else None
         elif ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != cache.device:
             raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
         _check(L.verillm_op_attention_paged(C.byref(cache.c_struct), C.byref(rc), q.data_ptr(), q_stride, n_heads, o.data_ptr(),
-                                            stride, _ptr(lse), ws.data_ptr(), ws.numel(), _ptr(rows.status), st),
+                                            stride, _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _ptr(rows.status), st),
                "verillm_op_attention_paged")
         return o
 

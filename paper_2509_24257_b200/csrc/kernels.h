@@ -117,6 +117,7 @@ struct PagedAttnParams {
     float* lse;  // optional [n_rows][n_heads]
     int n_heads, group;
     int tb_log;   // tokens per block, log2
+    int share_log;  // few-row kernel: positions per unit of a CTA's share, log2 (30: whole blocks)
     int4* hdr;    // [grid]
     float* part;  // [2 grid][rows][head_dim + 2]
     int* status;
@@ -124,7 +125,7 @@ struct PagedAttnParams {
 constexpr int kPagedMaxGroup = 128;  // query heads per kv head
 constexpr int kPagedTcRows = 256;    // packed rows per block of the tcgen05 kernel
 // Bytes of partial results and headers a launch needs; what the rule on sizes picks.
-size_t paged_attention_workspace(int head_dim, int dtype, int group, int max_rows, int num_sms);
+size_t paged_attention_workspace(int head_dim, int dtype, int group, int max_rows, long long max_positions, int num_sms);
 cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_sms, cudaStream_t stream);
 cudaError_t paged_attention_init();
 // The kernel for many rows per sequence (one CTA per SM: grid <= SMs); called by launch_paged_attention.

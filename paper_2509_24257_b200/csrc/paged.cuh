@@ -54,23 +54,22 @@ __host__ __device__ __forceinline__ long long sum_ceil(long long z, int s) {
     return ((m * (m + 1)) >> 1) * (1LL << s) + (z - (m << s)) * (m + 1);
 }
 
-// A kernel's tiles hold 2^TL key positions (TL: template argument of what follows).
+// A kernel's tiles hold T = 2^tl key positions.  (With tl = 30 every block is one tile: shares of whole blocks.)
 //
 // Tiles of the first m blocks of one (sequence, kv head), none of them its last: block i (from 1) ends at position
-// ctx + tb i and takes max(1, ceil((ctx + tb i) / T)) tiles of T = 2^TL.  With tb <= T, ceil((ctx + tb i) / T) =
+// ctx + tb i and takes max(1, ceil((ctx + tb i) / T)) tiles.  With tb <= T, ceil((ctx + tb i) / T) =
 // ceil(z_i / p), p = T / tb, z_i = ceil(ctx / tb) + i: a sum over consecutive integers; with tb a multiple of T
 // the terms are an arithmetic series.
-template <int TL>
-__host__ __device__ __forceinline__ long long tiles_before(int ctx, int tb_log, long long m) {
+__host__ __device__ __forceinline__ long long tiles_before(int tl, int ctx, int tb_log, long long m) {
     if (m <= 0) return 0;
-    if (tb_log <= TL) {
+    if (tb_log <= tl) {
         const long long z0 = (static_cast<long long>(ctx) + (1 << tb_log) - 1) >> tb_log;  // ceil(ctx / tb)
         if (z0 + m <= 0) return m;
         const long long lo = z0 + 1 > 1 ? z0 + 1 : 1;  // first positive z
-        return (lo - (z0 + 1)) + sum_ceil(z0 + m, TL - tb_log) - sum_ceil(lo - 1, TL - tb_log);
+        return (lo - (z0 + 1)) + sum_ceil(z0 + m, tl - tb_log) - sum_ceil(lo - 1, tl - tb_log);
     }
-    const int q = 1 << (tb_log - TL);
-    const long long c0 = (static_cast<long long>(ctx) + (1 << TL) - 1) >> TL;
+    const int q = 1 << (tb_log - tl);
+    const long long c0 = (static_cast<long long>(ctx) + (1 << tl) - 1) >> tl;
     long long ones = c0 >= 1 ? 0 : (-c0) / q;  // i <= ones: c0 + q i <= 0, one tile each
     if (ones > m) ones = m;
     const long long k = m - ones;
@@ -79,9 +78,8 @@ __host__ __device__ __forceinline__ long long tiles_before(int ctx, int tb_log, 
 
 __host__ __device__ __forceinline__ int block_count(int n, int tb_log) { return (n + (1 << tb_log) - 1) >> tb_log; }
 // Tiles of the block that ends before position `end`
-template <int TL>
-__host__ __device__ __forceinline__ int tiles_of_end(int end) {
-    return end > (1 << TL) ? ((end - 1) >> TL) + 1 : 1;
+__host__ __device__ __forceinline__ int tiles_of_end(int tl, int end) {
+    return end > (1 << tl) ? ((end - 1) >> tl) + 1 : 1;
 }
 // End position (exclusive) of block j
 __host__ __device__ __forceinline__ int block_end(const SeqView& s, int tb_log, int j) {
@@ -89,10 +87,9 @@ __host__ __device__ __forceinline__ int block_end(const SeqView& s, int tb_log, 
     return s.len - s.n + toks;
 }
 // All tiles of one (sequence, kv head)
-template <int TL>
-__host__ __device__ __forceinline__ long long tiles_of_head(const SeqView& s, int tb_log) {
+__host__ __device__ __forceinline__ long long tiles_of_head(int tl, const SeqView& s, int tb_log) {
     if (s.n == 0) return 0;
-    return tiles_before<TL>(s.len - s.n, tb_log, block_count(s.n, tb_log) - 1) + tiles_of_end<TL>(s.len);
+    return tiles_before(tl, s.len - s.n, tb_log, block_count(s.n, tb_log) - 1) + tiles_of_end(tl, s.len);
 }
 
 // a / b of numbers that are not negative and mostly fit 32 bits, where the division is much shorter
@@ -114,13 +111,12 @@ struct ShareScratch {  // in shared memory
     long long offset;
     int seq;
 };
-template <int TL>
-__device__ __forceinline__ void find_share(const PagedRowsDev& r, int page_shift, int n_kv_heads, int tb_log, int nthreads,
+__device__ __forceinline__ void find_share(int tl, const PagedRowsDev& r, int page_shift, int n_kv_heads, int tb_log, int nthreads,
                                            int min_per, ShareScratch* sc, WorkShare& w, int* status) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps = nthreads >> 5;
     int* st0 = blockIdx.x == 0 ? status : nullptr;  // one CTA reports
     auto tiles = [&](int b) -> long long {
-        return b < r.batch ? tiles_of_head<TL>(load_seq(r, page_shift, b, st0), tb_log) * n_kv_heads : 0;
+        return b < r.batch ? tiles_of_head(tl, load_seq(r, page_shift, b, st0), tb_log) * n_kv_heads : 0;
     };
     const int live = min(nwarps, (r.batch + 31) >> 5);  // the other warps have nothing to add
     // inclusive scan over the block of one value per thread; returns the block's total
@@ -194,30 +190,28 @@ struct BlockWalk {
 };
 
 // Positions the walk on the first block of a (non-empty) share.
-template <int TL>
-__device__ __forceinline__ void walk_begin(const PagedRowsDev& r, int page_shift, int tb_log, const WorkShare& w, BlockWalk& k) {
+__device__ __forceinline__ void walk_begin(int tl, const PagedRowsDev& r, int page_shift, int tb_log, const WorkShare& w, BlockWalk& k) {
     k.seq = w.seq;
     k.s = load_seq(r, page_shift, k.seq, nullptr);
-    const long long per_head = tiles_of_head<TL>(k.s, tb_log);
+    const long long per_head = tiles_of_head(tl, k.s, tb_log);
     k.kvh = static_cast<int>(short_div(w.offset, per_head));
     const long long x = w.offset - per_head * k.kvh;
     const int ctx = k.s.len - k.s.n;
     int lo = 0, hi = block_count(k.s.n, tb_log) - 1;  // the last block that begins at or before x
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (tiles_before<TL>(ctx, tb_log, mid) <= x) lo = mid;
+        if (tiles_before(tl, ctx, tb_log, mid) <= x) lo = mid;
         else hi = mid - 1;
     }
     k.j = lo;
-    k.tiles = tiles_of_end<TL>(block_end(k.s, tb_log, lo));
-    k.at = w.begin - (x - tiles_before<TL>(ctx, tb_log, lo));
+    k.tiles = tiles_of_end(tl, block_end(k.s, tb_log, lo));
+    k.at = w.begin - (x - tiles_before(tl, ctx, tb_log, lo));
     k.t0 = static_cast<int>(w.begin - k.at);
     k.t1 = static_cast<int>(min(static_cast<long long>(k.tiles), w.end - k.at));
 }
 
 // Moves to the next block; false at the end of the share.
-template <int TL>
-__device__ __forceinline__ bool walk_next(const PagedRowsDev& r, int page_shift, int n_kv_heads, int tb_log, const WorkShare& w,
+__device__ __forceinline__ bool walk_next(int tl, const PagedRowsDev& r, int page_shift, int n_kv_heads, int tb_log, const WorkShare& w,
                                           BlockWalk& k) {
     k.at += k.tiles;
     if (k.at >= w.end) return false;
@@ -230,7 +224,7 @@ __device__ __forceinline__ bool walk_next(const PagedRowsDev& r, int page_shift,
             } while (k.s.n == 0);  // a later sequence has tiles: the share does not end here
         }
     }
-    k.tiles = tiles_of_end<TL>(block_end(k.s, tb_log, k.j));
+    k.tiles = tiles_of_end(tl, block_end(k.s, tb_log, k.j));
     k.t0 = 0;
     k.t1 = static_cast<int>(min(static_cast<long long>(k.tiles), w.end - k.at));
     return true;

@@ -103,14 +103,14 @@ paged_rows_kernel(const PagedAttnParams p) {
     const int G = p.group, shift = c.page_shift, ps_mask = (1 << shift) - 1;
 
     WorkShare share;
-    find_share<PR_TILE_LOG>(p.r, shift, c.n_kv_heads, p.tb_log, PR_THREADS, 1, &sm_share, share, p.status);
+    find_share(p.share_log, p.r, shift, c.n_kv_heads, p.tb_log, PR_THREADS, 1, &sm_share, share, p.status);
     pdl_launch_dependents();
     if (share.begin >= share.end) {
-        if (tid == 0) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (tid == 0 && p.hdr) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
     BlockWalk k;
-    walk_begin<PR_TILE_LOG>(p.r, shift, p.tb_log, share, k);
+    walk_begin(p.share_log, p.r, shift, p.tb_log, share, k);
     const float sl2 = rsqrtf(static_cast<float>(DH)) * kLog2e;
     int4 header = make_int4(0, 0, 0, 0);
 
@@ -121,6 +121,7 @@ paged_rows_kernel(const PagedAttnParams p) {
         const int ctx = s.len - s.n;
         const int first_pos = ctx + tok0;         // position of the block's first token
         const int end = ctx + tok0 + toks;        // keys [0, end) are visible to some row
+        if (!p.hdr) k.t1 = tiles_of_end(PR_TILE_LOG, end);  // a share of whole blocks: in tiles of this kernel's size
         // ---- Q into fragment order: b registers of k step ks, rows 8 nt + g
         __syncthreads();  // the previous block's rows have been read
         const __nv_bfloat16* q0 = reinterpret_cast<const __nv_bfloat16*>(p.q) + static_cast<size_t>(s.row0 + tok0) * p.q_stride + static_cast<size_t>(k.kvh * G) * DH;
@@ -467,9 +468,9 @@ paged_rows_kernel(const PagedAttnParams p) {
         }
         __syncthreads();
 
-        const bool whole = k.t0 == 0 && k.t1 == k.tiles;
+        const bool whole = !p.hdr || (k.t0 == 0 && k.t1 == k.tiles);
         const int slot = 2 * blockIdx.x + (k.t0 == 0 ? 1 : 0);
-        float* part = part_slot(p.part, slot, RB, DH);
+        float* part = whole ? nullptr : part_slot(p.part, slot, RB, DH);
         if (!whole && k.t0 == 0)
             header = make_int4(static_cast<int>(short_div(k.at + k.tiles - 1, share.per)) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
         constexpr int LPR = DH / 8;  // lanes per row, 8 columns each
@@ -511,8 +512,8 @@ paged_rows_kernel(const PagedAttnParams p) {
                 dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
             }
         }
-    } while (walk_next<PR_TILE_LOG>(p.r, shift, c.n_kv_heads, p.tb_log, share, k));
-    if (tid == 0) p.hdr[blockIdx.x] = header;
+    } while (walk_next(p.share_log, p.r, shift, c.n_kv_heads, p.tb_log, share, k));
+    if (tid == 0 && p.hdr) p.hdr[blockIdx.x] = header;
 }
 
 // Joins the partial results of blocks that several CTAs worked on.  One CTA per (possible) such block and group of
@@ -640,12 +641,18 @@ cudaError_t rows_launch_dtype(const PagedAttnParams& p, int nt, int grid, cudaSt
 struct Shape {
     int nt;  // 8-row column blocks of the few-row kernel; 0: the tcgen05 kernel
     int tb_log, rows_per_block, grid;
+    bool split;  // blocks may be split over CTAs and joined
 };
-Shape shape_of(int head_dim, int dtype, int group, int max_rows, int num_sms) {
+// Sequences that cannot be longer than this are not split by the few-row kernel: a CTA's walk over so few tiles takes
+// no longer than the second launch and its reads (16 sequences of 500 positions: 10.2 us whole, 10.0
+// split and joined; of 250: 6.9 and 9.0).
+constexpr long long kWholePositions = 256;
+Shape shape_of(int head_dim, int dtype, int group, int max_rows, long long max_positions, int num_sms) {
     Shape s;
     const long long r = static_cast<long long>(group) * max_rows;
     s.nt = r <= 32 ? static_cast<int>((r + 7) / 8) : 0;
     s.rows_per_block = s.nt ? 8 * s.nt : kPagedTcRows;
+    s.split = s.nt == 0 || max_positions > kWholePositions;
     s.grid = num_sms * (s.nt == 0 ? 1 : rows_ctas(head_dim, dtype, s.nt));
     // tokens per block: a power of two; the few-row kernel's single block holds them all
     s.tb_log = 0;
@@ -656,8 +663,9 @@ size_t hdr_bytes(int grid) { return (static_cast<size_t>(grid) * sizeof(int4) + 
 
 }  // namespace
 
-size_t paged_attention_workspace(int head_dim, int dtype, int group, int max_rows, int num_sms) {
-    const Shape s = shape_of(head_dim, dtype, group, max_rows, num_sms);
+size_t paged_attention_workspace(int head_dim, int dtype, int group, int max_rows, long long max_positions, int num_sms) {
+    const Shape s = shape_of(head_dim, dtype, group, max_rows, max_positions, num_sms);
+    if (!s.split) return 0;
     return hdr_bytes(s.grid) + static_cast<size_t>(2) * s.grid * s.rows_per_block * (head_dim + 2) * sizeof(float);
 }
 
@@ -673,14 +681,15 @@ cudaError_t paged_attention_init() {
 }
 
 cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_sms, cudaStream_t stream) {
-    const Shape s = shape_of(p.c.head_dim, p.c.dtype, p.group, p.r.max_rows, num_sms);
+    const Shape s = shape_of(p.c.head_dim, p.c.dtype, p.group, p.r.max_rows, static_cast<long long>(p.r.table_width) << p.c.page_shift, num_sms);
     p.tb_log = s.tb_log;
-    p.hdr = reinterpret_cast<int4*>(workspace);
-    p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + hdr_bytes(s.grid));
+    p.share_log = s.split ? PR_TILE_LOG : 30;
+    p.hdr = s.split ? reinterpret_cast<int4*>(workspace) : nullptr;
+    p.part = s.split ? reinterpret_cast<float*>(static_cast<char*>(workspace) + hdr_bytes(s.grid)) : nullptr;
     cudaError_t e = s.nt == 0              ? launch_paged_attention_tc(p, s.grid, stream)
                     : p.c.head_dim == 64 ? rows_launch_dtype<64>(p, s.nt, s.grid, stream)
                                          : rows_launch_dtype<128>(p, s.nt, s.grid, stream);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || !s.split) return e;
     cudaLaunchConfig_t cfg = {};
     const int rpw = s.nt ? 1 : 4;  // rows per warp of the join
     cfg.gridDim = dim3(s.grid, s.rows_per_block / (JOIN_THREADS / 32 * rpw));

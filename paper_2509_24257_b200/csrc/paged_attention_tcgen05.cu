@@ -285,7 +285,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     }
     tc_fence_before();
     WorkShare share;
-    find_share<PT_TILE_LOG>(p.r, p.c.page_shift, p.c.n_kv_heads, p.tb_log, PT_THREADS, 1, scratch, share, p.status);
+    find_share(PT_TILE_LOG, p.r, p.c.page_shift, p.c.n_kv_heads, p.tb_log, PT_THREADS, 1, scratch, share, p.status);
     pdl_launch_dependents();
     tc_fence_after();
     if (share.begin >= share.end) {
@@ -856,7 +856,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
         } else if (warp == 13) {
         // ------------------------------------------------------------ hands out the parts
         BlockWalk k;
-        walk_begin<PT_TILE_LOG>(p.r, shift, p.tb_log, share, k);
+        walk_begin(PT_TILE_LOG, p.r, shift, p.tb_log, share, k);
         int4 header = make_int4(0, 0, 0, 0);
         bool more = true;
         for (int n = 0; ok; ++n) {
@@ -895,7 +895,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
                 }
                 __syncwarp();
             }
-            more = walk_next<PT_TILE_LOG>(p.r, shift, n_kv, p.tb_log, share, k);
+            more = walk_next(PT_TILE_LOG, p.r, shift, n_kv, p.tb_log, share, k);
         }
         if (lane == 0) p.hdr[blockIdx.x] = header;
         }

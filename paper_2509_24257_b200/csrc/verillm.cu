@@ -1112,7 +1112,7 @@ int64_t verillm_op_attention_paged_workspace(const verillm_kv_cache* cache, cons
     PagedRowsDev r;
     int rc = check_paged(cache, rows, &c, &r), sms = 0;
     if (rc || (rc = check_group(cache, n_heads)) || (rc = current_sms(&sms))) return rc;
-    return static_cast<int64_t>(paged_attention_workspace(c.head_dim, c.dtype, n_heads / c.n_kv_heads, r.max_rows, sms));
+    return static_cast<int64_t>(paged_attention_workspace(c.head_dim, c.dtype, n_heads / c.n_kv_heads, r.max_rows, static_cast<long long>(r.table_width) << c.page_shift, sms));
 }
 
 int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_rows* rows, const void* q, int64_t q_stride,
@@ -1124,12 +1124,13 @@ int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_r
     if (rc || (rc = check_group(cache, n_heads)) || p.r.n_rows == 0) return rc;
     const int64_t width = static_cast<int64_t>(n_heads) * p.c.head_dim;
     if ((rc = check_rows(q, q_stride, width, 8)) || (rc = check_rows(out, out_stride, width, 8))) return rc;
-    if (!workspace) return VERILLM_E_INVAL;
-    if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    if ((rc = current_sms(&sms))) return rc;
     p.group = n_heads / p.c.n_kv_heads;
-    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) ||
-        workspace_bytes < static_cast<int64_t>(paged_attention_workspace(p.c.head_dim, p.c.dtype, p.group, p.r.max_rows, sms)))
-        return VERILLM_E_SHAPE;
+    const int64_t need = static_cast<int64_t>(paged_attention_workspace(p.c.head_dim, p.c.dtype, p.group, p.r.max_rows,
+                                                                        static_cast<long long>(p.r.table_width) << p.c.page_shift, sms));
+    if (need > 0 && !workspace) return VERILLM_E_INVAL;
+    if (need > 0 && ((reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < need)) return VERILLM_E_SHAPE;
+    if ((rc = ensure_init())) return rc;
     p.q = q; p.q_stride = q_stride; p.out = out; p.out_stride = out_stride; p.lse = lse; p.n_heads = n_heads; p.status = status;
     CU_TRY(launch_paged_attention(p, workspace, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
     return VERILLM_OK;

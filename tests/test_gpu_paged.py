@@ -402,9 +402,11 @@ def test_wrapper_refuses_what_the_kernels_cannot_take():
     with pytest.raises(vb.VerillmError) as e:
         vb.op_attention_paged(odd, cache, rows)
     assert e.value.code == vb.E_SHAPE
-    with pytest.raises(vb.VerillmError) as e:
-        vb.op_attention_paged(c.dq, cache, rows, workspace=torch.empty(64, dtype=torch.uint8, device=DEV))
-    assert e.value.code == vb.E_SHAPE
+    long = vb.PagedRows(rows.page_table[:, :1].repeat(1, 60), rows.cu_rows, rows.kv_len, 2)  # 960 positions may be split
+    for ws in (torch.empty(64, dtype=torch.uint8, device=DEV), torch.empty(1 << 28, dtype=torch.uint8, device=DEV)[16:]):
+        with pytest.raises(vb.VerillmError) as e:
+            vb.op_attention_paged(c.dq, cache, long, workspace=ws)
+        assert e.value.code == vb.E_SHAPE
     with pytest.raises(vb.VerillmError) as e:
         vb.op_attention_paged(c.dq[:, :192], cache, rows)  # 3 query heads over 2 kv heads
     assert e.value.code == vb.E_SHAPE
