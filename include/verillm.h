@@ -199,6 +199,15 @@ int verillm_decode_commit(verillm_model *model, const int32_t *tokens, const int
                           int32_t n_prefill, const int32_t *check_seq, const int32_t *check_pos, int32_t n_check,
                           void *committed_out, int32_t commit_dtype, int32_t *status, void *cuda_stream);
 
+/* The same loop over a paged key/value cache of type cache_dtype (VERILLM_KV_*, see the paged cache below): the trace of
+ * a prover that serves with such a cache, e.g. an 8-bit one.  The parallel pass over the prompts attends to its own
+ * unquantised keys and values, as serving stacks do; decoded tokens attend to what the cache holds, their own token
+ * included.  The first call allocates the pools (as large as the bf16 cache, plus the scales) inside the handle. */
+int verillm_decode_commit_paged(verillm_model *model, const int32_t *tokens, const int32_t *cu_seqlens, int32_t batch,
+                                int32_t n_prefill, const int32_t *check_seq, const int32_t *check_pos, int32_t n_check,
+                                void *committed_out, int32_t commit_dtype, int32_t cache_dtype, int32_t *status,
+                                void *cuda_stream);
+
 /* Tail token check (the TokenMatch equation; token-state cross-check of the forged-output analysis): the
  * last-layer states at the checked positions go through the final RMSNorm and the output
  * head, and the arg-max token of each row is compared with the token the prover claims to have emitted there.

@@ -230,14 +230,29 @@ def forward_prefill(m: Model, tokens: np.ndarray) -> np.ndarray:
     return forward_prefill_batch(m, [tokens])[0]
 
 
-def forward_decode_kvcache(m: Model, tokens: np.ndarray, precision: str = "f64") -> np.ndarray:
+def quantised_vectors(x: np.ndarray, kind: str) -> np.ndarray:
+    """What an 8-bit cache keeps of vectors x [..., d]: code * scale with one scale per vector, scale = max|x| / Q, code =
+    x / scale to the nearest code, ties to even; Q = 448 (e4m3: 4 significant bits, steps of 2^-9 below 2^-6) or 127."""
+    q = {"e4m3": 448.0, "int8": 127.0}[kind]
+    scale = np.maximum(np.max(np.abs(x), axis=-1, keepdims=True), 2.0 ** -110) / q
+    y = x / scale
+    if kind == "int8":
+        return np.rint(y) * scale
+    _, e = np.frexp(y)  # |y| in [2^(e-1), 2^e)
+    step = np.exp2(np.maximum(e - 1, -6) - 3.0)
+    return np.clip(np.rint(y / step) * step, -q, q) * scale
+
+
+def forward_decode_kvcache(m: Model, tokens: np.ndarray, precision: str = "f64", cache: Optional[str] = None) -> np.ndarray:
     """The prover's loop: one position at a time, keys/values of earlier positions taken from a cache.
 
     precision "f64": exact twin of forward_prefill (brute-force check of the paper's equivalence claim).
     precision "bf16": emulates a bf16 serving stack: the normed activations, rotated q/k, v, the
     attention output and the FFN product are rounded to bf16 where such a stack stores them
     (so the cache holds bf16 keys/values); accumulation and the residual stream stay wide.
+    cache "e4m3" / "int8": every key and value vector is stored quantised and attended to as stored.
     Returns [n_layers, T, d_model] (not rounded; the caller serialises)."""
+    keep = (lambda x: x) if cache is None else (lambda x: quantised_vectors(x, cache))
     rnd = (lambda x: x) if precision == "f64" else round_to_bf16
     T = len(tokens)
     H, KV, dh = m.n_heads, m.n_kv_heads, m.head_dim
@@ -251,8 +266,8 @@ def forward_decode_kvcache(m: Model, tokens: np.ndarray, precision: str = "f64")
             w = m.layers[l]
             a = rnd(rmsnorm(h, w["attn_norm"], m.rms_eps))
             q = rnd(rope((w["wq"] @ a).reshape(1, H, dh), p, m.rope_base))[0]
-            kc[l, t] = rnd(rope((w["wk"] @ a).reshape(1, KV, dh), p, m.rope_base))[0]
-            vc[l, t] = rnd((w["wv"] @ a).reshape(KV, dh))
+            kc[l, t] = keep(rnd(rope((w["wk"] @ a).reshape(1, KV, dh), p, m.rope_base))[0])
+            vc[l, t] = keep(rnd((w["wv"] @ a).reshape(KV, dh)))
             o = np.empty((H, dh))
             for g in range(H):
                 kv = g * KV // H

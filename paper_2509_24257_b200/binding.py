@@ -33,7 +33,7 @@ EXPORTS = (
     "verillm_last_launch_count", "verillm_profile_enable", "verillm_profile_read",
     "verillm_load_lm_head", "verillm_token_match", "verillm_verify_segment", "verillm_spot_check", "verillm_merkle_roots",
     "verillm_threshold_sweep", "verillm_selftest_wait_timeout", "verillm_kv_write", "verillm_kv_read",
-    "verillm_op_attention_paged", "verillm_op_attention_paged_workspace",
+    "verillm_op_attention_paged", "verillm_op_attention_paged_workspace", "verillm_decode_commit_paged",
 )
 PROF_CLASSES = ("setup", "rmsnorm", "gemm_qkv_rope", "attention", "gemm_o_resid", "gemm_gate_up_swiglu",
                 "gemm_down_resid_compare", "verdict")
@@ -143,6 +143,8 @@ def lib() -> C.CDLL:
         L.verillm_op_gemm.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
         L.verillm_op_rmsnorm.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_void_p]
         L.verillm_op_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
+        L.verillm_decode_commit_paged.argtypes = L.verillm_decode_commit.argtypes[:10] + [C.c_int32, C.c_void_p, C.c_void_p]
+        L.verillm_decode_commit_paged.restype = C.c_int
         cache_p, rows_p = C.POINTER(KVCacheC), C.POINTER(KVRowsC)
         L.verillm_kv_write.argtypes = [cache_p, rows_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
         L.verillm_kv_write.restype = C.c_int
@@ -323,17 +325,23 @@ class Model:
 
     def decode_commit(self, tokens: torch.Tensor, cu_seqlens: Sequence[int], n_prefill: int, check_seq: Sequence[int],
                       check_pos: Sequence[int], commit_dtype: torch.dtype = torch.bfloat16,
-                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+                      stream: Optional[torch.cuda.Stream] = None, cache_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+        """cache_dtype: bf16, float8_e4m3fn or int8 decodes over a paged cache of that type; None over the contiguous bf16 one."""
         cu = _i32(cu_seqlens)
         cs, cp = _i32(check_seq), _i32(check_pos)
         n_check, batch = int(cs.shape[0]), int(cu.shape[0]) - 1
+        if cache_dtype is not None and cache_dtype not in _KV_DTYPES:
+            raise ValueError("cache_dtype must be bf16, float8_e4m3fn or int8")
         out = torch.zeros(self.shape.n_layers, max(n_check, 1), self.shape.d_model, dtype=commit_dtype, device=self.device)
         status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        args = [self._h, tokens.data_ptr(), cu.ctypes.data, batch, int(n_prefill), cs.ctypes.data, cp.ctypes.data, n_check,
+                out.data_ptr(), BF16 if commit_dtype == torch.bfloat16 else F32]
         with torch.cuda.device(self.device):
-            code = lib().verillm_decode_commit(
-                self._h, tokens.data_ptr(), cu.ctypes.data, batch, int(n_prefill), cs.ctypes.data, cp.ctypes.data, n_check,
-                out.data_ptr(), BF16 if commit_dtype == torch.bfloat16 else F32, status.data_ptr(), _stream_ptr(stream))
-        _check(code, "verillm_decode_commit")
+            if cache_dtype is None:
+                code = lib().verillm_decode_commit(*args, status.data_ptr(), _stream_ptr(stream))
+            else:
+                code = lib().verillm_decode_commit_paged(*args, _KV_DTYPES[cache_dtype], status.data_ptr(), _stream_ptr(stream))
+        _check(code, "verillm_decode_commit" if cache_dtype is None else "verillm_decode_commit_paged")
         if int(status.item()) != 0:
             raise RuntimeError(f"verillm_decode_commit: device status {int(status.item())}")
         return out[:, :n_check]

@@ -1,19 +1,20 @@
 """Threshold sensitivity of the bit-aware tests on honest and quantised-prover traces.
 
-    python -m paper_2509_24257_b200.calibrate [--workload small] [--bits 8] [--check-frac 0.25]
+    python -m paper_2509_24257_b200.calibrate [--workload small] [--bits 8 | --cache e4m3] [--check-frac 0.25]
 
 Follows the paper's "Threshold Sensitivity Analysis": each of the four thresholds (P_e, |e|, P_m, P_w) is
 varied while the others stay at their selected values, and FPR / FNR / TPR / TNR are read off cells of
 honest traces and of attack traces.  Here the honest prover is the library's bf16 KV-cache decode, the
 attacker is the same decode on fake-quantised weights (synth.fake_quantise), the verifier recomputes with
-the true weights; every step runs in the library's kernels (decode_commit, verify_prefill,
+the true weights.  With --cache the attacker keeps the true weights and serves with a quantised key/value cache instead
+(the paged cache of decode_commit).  Every step runs in the library's kernels (decode_commit, verify_prefill,
 threshold_sweep), this module only arranges the calls and prints the table.
 """
 from __future__ import annotations
 
 import argparse
 import dataclasses
-from typing import Dict, List, Sequence, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -44,21 +45,28 @@ def variants(selected: Dict[str, float] = SELECTED, grid: Dict[str, Sequence[flo
     return tols, labels
 
 
-def trace_stats(wl: synth.Workload, bits: int, device: torch.device):
-    """Statistics [n_cells][NSTAT] (device) of honest cells followed by attack cells, and the class flags."""
+CACHES = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+def trace_stats(wl: synth.Workload, bits: int, device: torch.device, cache: Optional[str] = None):
+    """Statistics [n_cells][NSTAT] (device) of honest cells followed by attack cells, and the class flags.  cache: the
+    attacker's key/value cache type; None: the attacker quantises its weights to `bits` instead."""
     w = synth.model_weights(wl, device)
     cs, cp = synth.check_positions(wl)
     cu = synth.cu_seqlens(wl)
     flat = torch.from_numpy(synth.token_streams(wl).reshape(-1)).to(device)
     verifier = vb.Model.from_weights(wl.shape, w, wl.n_tokens, len(cs), wl.batch, device)
-    attacker = vb.Model.from_weights(wl.shape, synth.quantised_model_weights(w, bits), wl.n_tokens, len(cs), wl.batch, device)
+    attacker = verifier
+    if cache is None:
+        attacker = vb.Model.from_weights(wl.shape, synth.quantised_model_weights(w, bits), wl.n_tokens, len(cs), wl.batch, device)
     tol = vb.default_tol()
     parts = []
-    for prover in (verifier, attacker):
-        committed = prover.decode_commit(flat, cu, wl.prompt_len, cs, cp, torch.bfloat16).contiguous()
+    for prover, cache_dtype in ((verifier, None), (attacker, CACHES[cache] if cache else None)):
+        committed = prover.decode_commit(flat, cu, wl.prompt_len, cs, cp, torch.bfloat16, cache_dtype=cache_dtype).contiguous()
         rep = verifier.verify_prefill(flat, cu, committed, cs, cp, tol)
         parts.append(rep.stats.reshape(-1, vb.NSTAT).clone())
-    attacker.close()
+    if attacker is not verifier:
+        attacker.close()
     verifier.close()
     stats = torch.cat(parts).contiguous()
     is_attack = torch.zeros(stats.shape[0], dtype=torch.uint8, device=device)
@@ -81,11 +89,13 @@ def main() -> None:
     ap = argparse.ArgumentParser()
     ap.add_argument("--workload", default="small")
     ap.add_argument("--bits", type=int, default=8)
+    ap.add_argument("--cache", choices=sorted(CACHES), help="the attacker quantises its key/value cache, not its weights")
     ap.add_argument("--check-frac", type=float, default=0.25)
     args = ap.parse_args()
     wl = dataclasses.replace(synth.WORKLOADS[args.workload], check_frac=args.check_frac)
-    stats, is_attack = trace_stats(wl, args.bits, torch.device("cuda", 0))
-    print(f"{wl.name}: {int((is_attack == 0).sum())} honest and {int(is_attack.sum())} int{args.bits} attack cells")
+    stats, is_attack = trace_stats(wl, args.bits, torch.device("cuda", 0), args.cache)
+    print(f"{wl.name}: {int((is_attack == 0).sum())} honest and {int(is_attack.sum())} "
+          f"{args.cache + ' cache' if args.cache else 'int' + str(args.bits)} attack cells")
     print(f"{'threshold':>22} {'FPR':>8} {'FNR':>8} {'TPR':>8} {'TNR':>8}")
     for name, val, fpr, fnr, tpr, tnr in sensitivity_rows(stats, is_attack):
         mark = " (selected)" if SELECTED[name] == val else ""

@@ -51,6 +51,32 @@ struct DecodeState {
     float *resid = nullptr, *qkv = nullptr, *gu = nullptr;  // [max_batch][...]
     bf16 *xn = nullptr, *q = nullptr, *attn = nullptr, *mid = nullptr;
     int* ints = nullptr;  // index scratch: 6 * max_tokens + 3 * max_checks
+    // paged cache (allocated by the first call that uses it): pools of all layers, sized for bf16 and used by all types
+    int n_pages = 0;
+    unsigned char* pool = nullptr;   // [n_layers][2][n_pages][KV][kDecodePage][dh]
+    float* pool_scale = nullptr;     // [n_layers][2][n_pages][KV][kDecodePage]
+    bf16* kv_row = nullptr;          // [max_batch][2 * KV * dh]: keys and values of a step's rows
+    int* iota = nullptr;             // [max_batch]: 0, 1, ..
+    void* attn_ws = nullptr;
+};
+constexpr int kDecodePage = 16;  // positions per page of the decode path's cache
+
+// Memory from the stream-ordered allocator, returned to it on every way out.
+struct StreamBuffer {
+    void* p = nullptr;
+    cudaStream_t stream;
+    explicit StreamBuffer(cudaStream_t s) : stream(s) {}
+    ~StreamBuffer() {
+        if (p) cudaFreeAsync(p, stream);
+    }
+    StreamBuffer(const StreamBuffer&) = delete;
+    StreamBuffer& operator=(const StreamBuffer&) = delete;
+};
+
+// Contents of a paged decode: which pools, and where the sequences' pages and a step's rows are described.
+struct PagedDecode {
+    int width = 0;
+    int *table = nullptr, *cu = nullptr, *len = nullptr;  // [batch][width]; steps: [batch + 1] and [batch] each; prompts: [batch]
 };
 
 // Optional per-kernel timing: one event after every launch of a verify_prefill call.
@@ -303,13 +329,13 @@ int run_layer(verillm_model* m, int l, LayerRun& r, int* status, cudaStream_t st
     return VERILLM_OK;
 }
 
-int ensure_decode_state(verillm_model* m) {
-    if (m->dec.ready) return VERILLM_OK;
+int ensure_decode_state(verillm_model* m, bool paged) {
     const verillm_config& c = m->cfg;
     DecodeState& d = m->dec;
     int rc;
+    if (!paged && !d.kv_cache && (rc = dev_alloc(&d.kv_cache, static_cast<size_t>(c.n_layers) * c.max_tokens * 2 * m->d_kv))) return rc;
+    if (d.ready) return VERILLM_OK;
     const size_t B = c.max_batch;
-    if ((rc = dev_alloc(&d.kv_cache, static_cast<size_t>(c.n_layers) * c.max_tokens * 2 * m->d_kv))) return rc;
     if ((rc = dev_alloc(&d.hidden_tmp, static_cast<size_t>(c.n_layers) * std::max(c.max_checks, 1) * c.d_model))) return rc;
     if ((rc = dev_alloc(&d.resid, B * c.d_model))) return rc;
     if ((rc = dev_alloc(&d.qkv, B * m->n_qkv))) return rc;
@@ -366,6 +392,61 @@ int current_sms(int* num_sms) {
     return VERILLM_OK;
 }
 
+// The paged cache of one layer of the decode path.
+verillm_kv_cache decode_cache(const verillm_model* m, int layer, int dtype) {
+    const verillm_config& c = m->cfg;
+    const DecodeState& d = m->dec;
+    const size_t vecs = static_cast<size_t>(d.n_pages) * c.n_kv_heads * kDecodePage;  // of one pool
+    const size_t bytes = vecs * c.head_dim * 2;
+    verillm_kv_cache k;
+    k.k = d.pool + (2 * static_cast<size_t>(layer)) * bytes;
+    k.v = d.pool + (2 * static_cast<size_t>(layer) + 1) * bytes;
+    k.k_scale = dtype == VERILLM_KV_BF16 ? nullptr : d.pool_scale + (2 * static_cast<size_t>(layer)) * vecs;
+    k.v_scale = dtype == VERILLM_KV_BF16 ? nullptr : d.pool_scale + (2 * static_cast<size_t>(layer) + 1) * vecs;
+    k.n_pages = d.n_pages;
+    k.page_size = kDecodePage;
+    k.n_kv_heads = c.n_kv_heads;
+    k.head_dim = c.head_dim;
+    k.dtype = dtype;
+    return k;
+}
+verillm_kv_rows decode_rows(const PagedDecode& g, const int* cu, const int* len, int batch, int n_rows, int max_rows) {
+    verillm_kv_rows r;
+    r.page_table = g.table;
+    r.cu_rows = cu;
+    r.kv_len = len;
+    r.table_width = g.width;
+    r.batch = batch;
+    r.n_rows = n_rows;
+    r.max_rows = max_rows;
+    return r;
+}
+int ensure_paged_decode(verillm_model* m) {
+    DecodeState& d = m->dec;
+    const verillm_config& c = m->cfg;
+    if (!d.attn_ws) {
+        // sequences take whole pages: at most one partly filled page each
+        d.n_pages = c.max_tokens / kDecodePage + c.max_batch;
+        const size_t vecs = static_cast<size_t>(c.n_layers) * 2 * d.n_pages * c.n_kv_heads * kDecodePage;
+        int rc;
+        if (!d.pool && (rc = dev_alloc(&d.pool, vecs * c.head_dim * 2))) return rc;
+        if (!d.pool_scale && (rc = dev_alloc(&d.pool_scale, vecs))) return rc;
+        if (!d.kv_row && (rc = dev_alloc(&d.kv_row, static_cast<size_t>(c.max_batch) * 2 * m->d_kv))) return rc;
+        if (!d.iota && (rc = dev_alloc(&d.iota, c.max_batch))) return rc;
+        std::vector<int> iota(c.max_batch);
+        for (int i = 0; i < c.max_batch; ++i) iota[i] = i;
+        CU_TRY(cudaMemcpy(d.iota, iota.data(), sizeof(int) * c.max_batch, cudaMemcpyHostToDevice));
+        // a decode step has one row per sequence; the largest need over the pool types and lengths
+        size_t need = 256;
+        for (int t = 0; t < 3; ++t)
+            need = std::max(need, paged_attention_workspace(c.head_dim, t, c.n_heads / c.n_kv_heads, 1, 1LL << 30, m->num_sms));
+        unsigned char* ws = nullptr;
+        if ((rc = dev_alloc(&ws, need))) return rc;
+        d.attn_ws = ws;
+    }
+    return VERILLM_OK;
+}
+
 }  // namespace
 
 // =============================================================================== C ABI
@@ -409,6 +490,7 @@ void verillm_free(verillm_model* m) {
     DecodeState& d = m->dec;
     cudaFree(d.kv_cache); cudaFree(d.hidden_tmp); cudaFree(d.resid); cudaFree(d.qkv); cudaFree(d.gu);
     cudaFree(d.xn); cudaFree(d.q); cudaFree(d.attn); cudaFree(d.mid); cudaFree(d.ints);
+    cudaFree(d.pool); cudaFree(d.pool_scale); cudaFree(d.kv_row); cudaFree(d.iota); cudaFree(d.attn_ws);
     for (cudaEvent_t e : m->prof.ev) cudaEventDestroy(e);
     delete m;
 }
@@ -868,9 +950,10 @@ int verillm_merkle_roots(const float* states, int32_t n_vec, int32_t d_model, ui
     return VERILLM_OK;
 }
 
-int verillm_decode_commit(verillm_model* m, const int32_t* tokens, const int32_t* cu_seqlens, int32_t batch,
-                          int32_t n_prefill, const int32_t* check_seq, const int32_t* check_pos, int32_t n_check,
-                          void* committed_out, int32_t commit_dtype, int32_t* status, void* cuda_stream) {
+// cache_dtype: -1 for the contiguous bf16 cache, else VERILLM_KV_* for the paged one.
+static int decode_impl(verillm_model* m, const int32_t* tokens, const int32_t* cu_seqlens, int32_t batch, int32_t n_prefill,
+                       const int32_t* check_seq, const int32_t* check_pos, int32_t n_check, void* committed_out, int32_t commit_dtype,
+                       int32_t cache_dtype, int32_t* status, void* cuda_stream) {
     if (!m || !tokens || n_prefill < 0) return VERILLM_E_INVAL;
     if (commit_dtype != VERILLM_BF16 && commit_dtype != VERILLM_F32) return VERILLM_E_INVAL;
     if (n_check > 0 && !committed_out) return VERILLM_E_INVAL;
@@ -878,7 +961,10 @@ int verillm_decode_commit(verillm_model* m, const int32_t* tokens, const int32_t
     if ((rc = check_batch(m, cu_seqlens, batch, &M, &max_len))) return rc;
     std::vector<int> tok_of_slot;
     if ((rc = check_slots(m, cu_seqlens, batch, check_seq, check_pos, n_check, &tok_of_slot))) return rc;
-    if ((rc = ensure_decode_state(m))) return rc;
+    const bool paged = cache_dtype >= 0;
+    if ((rc = ensure_decode_state(m, paged))) return rc;
+    if (paged && m->cfg.n_heads / m->cfg.n_kv_heads > kPagedMaxGroup) return VERILLM_E_SHAPE;
+    if (paged && (rc = ensure_paged_decode(m))) return rc;
 
     const verillm_config& c = m->cfg;
     DecodeState& d = m->dec;
@@ -904,6 +990,34 @@ int verillm_decode_commit(verillm_model* m, const int32_t* tokens, const int32_t
         cu_p[b + 1] = cu_p[b] + np[b];
     }
     const int Mp = cu_p[batch];
+    PagedDecode pg;
+    const int t_first = *std::min_element(np.begin(), np.end());
+    StreamBuffer paged_ints(st);  // page table, prompt lengths, then cu_rows and kv_len of every step
+    if (paged) {
+        pg.width = (max_len + kDecodePage - 1) / kDecodePage;
+        std::vector<int> h(static_cast<size_t>(batch) * pg.width, 0);
+        int page = 0;
+        for (int b = 0; b < batch; ++b)
+            for (int i = 0; i * kDecodePage < cu_seqlens[b + 1] - cu_seqlens[b]; ++i) h[static_cast<size_t>(b) * pg.width + i] = page++;
+        const size_t at_len = h.size();
+        h.insert(h.end(), np.begin(), np.end());
+        const size_t at_steps = h.size();
+        for (int t = t_first; t < max_len; ++t) {  // in step t the sequences with n_prefill <= t < len have one row, the others none
+            int rows = 0;
+            h.push_back(0);
+            for (int b = 0; b < batch; ++b) {
+                if (t >= np[b] && t < cu_seqlens[b + 1] - cu_seqlens[b]) ++rows;
+                h.push_back(rows);
+            }
+            for (int b = 0; b < batch; ++b) h.push_back(std::min(t + 1, cu_seqlens[b + 1] - cu_seqlens[b]));
+        }
+        CU_TRY(cudaMallocAsync(&paged_ints.p, h.size() * sizeof(int), st));
+        pg.table = static_cast<int*>(paged_ints.p);
+        pg.len = pg.table + at_len;
+        pg.cu = pg.table + at_steps;
+        CU_TRY(cudaMemcpyAsync(pg.table, h.data(), h.size() * sizeof(int), cudaMemcpyHostToDevice, st));
+        CU_TRY(cudaStreamSynchronize(st));  // (h is pageable and goes out of scope)
+    }
     if (Mp > 0) {
         std::vector<int> src(Mp), slot_row(n_check);
         int max_np = 0;
@@ -933,6 +1047,12 @@ int verillm_decode_commit(verillm_model* m, const int32_t* tokens, const int32_t
             cl.hidden_out = d.hidden_tmp + static_cast<size_t>(l) * n_check * c.d_model;
             if ((rc = run_layer(m, l, run, dev_status, st, &launches))) return rc;
             // run_layer leaves this layer's rotated keys and values in qkv: append them to the cache
+            if (paged) {
+                const verillm_kv_cache kc = decode_cache(m, l, cache_dtype);
+                const verillm_kv_rows kr = decode_rows(pg, m->cu_dev, pg.len, batch, Mp, max_np);
+                if ((rc = verillm_kv_write(&kc, &kr, m->qkv + m->d_q, m->qkv + m->d_q + m->d_kv, m->n_qkv, dev_status, cuda_stream))) return rc;
+                continue;
+            }
             CU_TRY(launch_scatter_kv(m->qkv, i_src, Mp, c.n_heads, c.n_kv_heads, c.head_dim,
                                      d.kv_cache + static_cast<size_t>(l) * T * 2 * m->d_kv, st));
         }
@@ -996,11 +1116,20 @@ int verillm_decode_commit(verillm_model* m, const int32_t* tokens, const int32_t
             CU_TRY(launch_embed(i_tok, m->embed, rows, c.d_model, c.vocab, d.resid, dev_status, st));
             for (int l = 0; l < c.n_layers; ++l) {
                 const LayerDev& w = m->layers[l];
-                bf16* cache_l = d.kv_cache + static_cast<size_t>(l) * T * 2 * m->d_kv;
+                bf16* cache_l = paged ? d.kv_row : d.kv_cache + static_cast<size_t>(l) * T * 2 * m->d_kv;
                 CU_TRY(launch_rmsnorm(d.resid, w.attn_norm, d.xn, rows, c.d_model, c.rms_eps, st));
                 CU_TRY(launch_skinny_gemm(d.xn, w.wqkv, d.qkv, rows, m->n_qkv, c.d_model, 0, st));
-                CU_TRY(launch_decode_rope_append(d.qkv, i_row_tok + r0, i_row_pos + r0, rows, c.n_heads, c.n_kv_heads,
+                CU_TRY(launch_decode_rope_append(d.qkv, paged ? d.iota : i_row_tok + r0, i_row_pos + r0, rows, c.n_heads, c.n_kv_heads,
                                                  c.head_dim, m->rope_cs, d.q, cache_l, st));
+                if (paged) {
+                    const int* step = pg.cu + static_cast<size_t>(t - t_first) * (2 * batch + 1);
+                    const verillm_kv_cache kc = decode_cache(m, l, cache_dtype);
+                    const verillm_kv_rows kr = decode_rows(pg, step, step + batch + 1, batch, rows, 1);
+                    if ((rc = verillm_kv_write(&kc, &kr, d.kv_row, d.kv_row + m->d_kv, 2 * m->d_kv, dev_status, cuda_stream))) return rc;
+                    if ((rc = verillm_op_attention_paged(&kc, &kr, d.q, m->d_q, c.n_heads, d.attn, m->d_q, nullptr, d.attn_ws,
+                                                         INT64_MAX, dev_status, cuda_stream)))
+                        return rc;
+                } else
                 CU_TRY(launch_decode_attention(d.q, cache_l, i_row_start + r0, i_row_pos + r0, rows, c.n_heads,
                                                c.n_kv_heads, c.head_dim, t + 1, d.attn, st));
                 CU_TRY(launch_skinny_gemm(d.attn, w.wo, d.resid, rows, c.d_model, m->d_q, 1, st));
@@ -1019,6 +1148,21 @@ int verillm_decode_commit(verillm_model* m, const int32_t* tokens, const int32_t
                                      commit_dtype, st));
     CU_TRY(cudaStreamSynchronize(st));
     return VERILLM_OK;
+}
+
+int verillm_decode_commit(verillm_model* m, const int32_t* tokens, const int32_t* cu_seqlens, int32_t batch,
+                          int32_t n_prefill, const int32_t* check_seq, const int32_t* check_pos, int32_t n_check,
+                          void* committed_out, int32_t commit_dtype, int32_t* status, void* cuda_stream) {
+    return decode_impl(m, tokens, cu_seqlens, batch, n_prefill, check_seq, check_pos, n_check, committed_out, commit_dtype, -1, status,
+                       cuda_stream);
+}
+
+int verillm_decode_commit_paged(verillm_model* m, const int32_t* tokens, const int32_t* cu_seqlens, int32_t batch, int32_t n_prefill,
+                                const int32_t* check_seq, const int32_t* check_pos, int32_t n_check, void* committed_out,
+                                int32_t commit_dtype, int32_t cache_dtype, int32_t* status, void* cuda_stream) {
+    if (cache_dtype != VERILLM_KV_BF16 && cache_dtype != VERILLM_KV_E4M3 && cache_dtype != VERILLM_KV_INT8) return VERILLM_E_INVAL;
+    return decode_impl(m, tokens, cu_seqlens, batch, n_prefill, check_seq, check_pos, n_check, committed_out, commit_dtype, cache_dtype,
+                       status, cuda_stream);
 }
 
 int verillm_selftest_wait_timeout(int64_t limit_cycles, int32_t* status, int32_t* gave_up, void* cuda_stream) {
