@@ -306,7 +306,8 @@ int verillm_op_attention(const void *qkv, const int32_t *cu_seqlens, int32_t bat
  * 8-bit pools hold, per (position, kv head) and separately for keys and values, the codes round(x_d * (Q / a)) (to
  * nearest, ties to even) and the float32 scale a / Q, a = max(max_d |x_d|, 2^-110), Q = 448 (e4m3, finite codes
  * only) or 127 (int8): they stand for code * scale.  A vector with an infinite or NaN entry gets the scale NaN and
- * codes 0 and so stands for NaN.  Pools filled by other means hold no e4m3 NaN codes (0x7F, 0xFF) and no int8 -128. */
+ * codes 0 and so stands for NaN.  Pools filled by other means hold no e4m3 NaN codes (0x7F, 0xFF), no int8 -128, and
+ * scales that are positive or NaN (in positions that are attended to or read; the others may hold anything). */
 enum { VERILLM_KV_BF16 = 0, VERILLM_KV_E4M3 = 1, VERILLM_KV_INT8 = 2 };
 
 typedef struct {
@@ -339,7 +340,8 @@ typedef struct {
  * next (e.g. the k and v columns of a fused projection); keys already rotated.  Pointers 16-byte aligned, strides
  * multiples of 8 entries (E_SHAPE).
  * status (all three calls): optional DEVICE word; raised from 0 to the first VERILLM_DEV_* problem met, never
- * cleared by the call.  All three allocate nothing and are safe under stream capture. */
+ * cleared by the call.  All three allocate nothing and may be captured into graphs; make the first call on a device
+ * outside a capture (it sets the kernels up). */
 int verillm_kv_write(const verillm_kv_cache *cache, const verillm_kv_rows *rows, const void *k, const void *v,
                      int64_t row_stride, int32_t *status, void *cuda_stream);
 
@@ -356,8 +358,11 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  *  workspace DEVICE, 256-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code).
  *            May be NULL where that is 0.  It holds nothing between calls, but calls that may overlap (other streams, graphs replayed side by side)
  *            need one each.
+ * Keys and values of 8-bit pools enter products in fp16, scaled to its range: rounded to 11 bits where the call has many
+ * rows per sequence, exact where it has few.  Probabilities are rounded to bf16 (bf16 pools) or fp16; sums are fp32.
+ * status also receives VERILLM_DEV_WAIT_TIMEOUT when a wait inside the kernel gave up; the results are then invalid.
  * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 128 per kv head; workspace too
- * small), E_ARCH, E_CUDA. */
+ * small or not aligned), E_ARCH, E_CUDA. */
 int64_t verillm_op_attention_paged_workspace(const verillm_kv_cache *cache, const verillm_kv_rows *rows, int32_t n_heads);
 int verillm_op_attention_paged(const verillm_kv_cache *cache, const verillm_kv_rows *rows, const void *q,
                                int64_t q_stride, int32_t n_heads, void *out, int64_t out_stride, float *lse,

@@ -613,7 +613,7 @@ cudaError_t rows_init_all() {
     cudaError_t e = rows_init<DH, DTYPE, 1>();
     if (e == cudaSuccess) e = rows_init<DH, DTYPE, 2>();
     if (e == cudaSuccess) e = rows_init<DH, DTYPE, 3>();
-    if (e == cudaSuccess) e = rows_init<DH, DTYPE, 4>();
+    if (e == cudaSuccess && DTYPE != VERILLM_KV_BF16) e = rows_init<DH, DTYPE, (DTYPE != VERILLM_KV_BF16 ? 4 : 3)>();
     return e;
 }
 
@@ -627,7 +627,7 @@ cudaError_t rows_launch_nt(const PagedAttnParams& p, int nt, int grid, cudaStrea
     if (nt == 1) return rows_launch<DH, DTYPE, 1>(p, grid, stream);
     if (nt == 2) return rows_launch<DH, DTYPE, 2>(p, grid, stream);
     if (nt == 3) return rows_launch<DH, DTYPE, 3>(p, grid, stream);
-    return rows_launch<DH, DTYPE, 4>(p, grid, stream);
+    return rows_launch<DH, DTYPE, (DTYPE != VERILLM_KV_BF16 ? 4 : 3)>(p, grid, stream);  // (bf16 takes up to three blocks)
 }
 template <int DH>
 cudaError_t rows_launch_dtype(const PagedAttnParams& p, int nt, int grid, cudaStream_t stream) {
@@ -636,8 +636,9 @@ cudaError_t rows_launch_dtype(const PagedAttnParams& p, int nt, int grid, cudaSt
     return rows_launch_nt<DH, VERILLM_KV_INT8>(p, nt, grid, stream);
 }
 
-// Which kernel and block shape serve a call.  The few-row kernel takes sequences of up to 32 packed rows, the
-// tcgen05 kernel everything else.
+// Which kernel and block shape serve a call.  The few-row kernel takes sequences of up to 24 (bf16) or 32 (8-bit) packed
+// rows, the tcgen05 kernel everything else.  Measured for 16 contexts of 4096, 8 kv heads of 128, few-row against
+// tcgen05: bf16 16 rows 61 / 69 us, 24 rows 69 / 70, 32 rows 118 / 70; int8 16 rows 57 / 91, 24 rows 61 / 91, 32 rows 80 / 91.
 struct Shape {
     int nt;  // 8-row column blocks of the few-row kernel; 0: the tcgen05 kernel
     int tb_log, rows_per_block, grid;
@@ -650,7 +651,7 @@ constexpr long long kWholePositions = 256;
 Shape shape_of(int head_dim, int dtype, int group, int max_rows, long long max_positions, int num_sms) {
     Shape s;
     const long long r = static_cast<long long>(group) * max_rows;
-    s.nt = r <= 32 ? static_cast<int>((r + 7) / 8) : 0;
+    s.nt = r <= (dtype == VERILLM_KV_BF16 ? 24 : 32) ? static_cast<int>((r + 7) / 8) : 0;
     s.rows_per_block = s.nt ? 8 * s.nt : kPagedTcRows;
     s.split = s.nt == 0 || max_positions > kWholePositions;
     s.grid = num_sms * (s.nt == 0 ? 1 : rows_ctas(head_dim, dtype, s.nt));
@@ -664,9 +665,13 @@ size_t hdr_bytes(int grid) { return (static_cast<size_t>(grid) * sizeof(int4) + 
 }  // namespace
 
 size_t paged_attention_workspace(int head_dim, int dtype, int group, int max_rows, long long max_positions, int num_sms) {
-    const Shape s = shape_of(head_dim, dtype, group, max_rows, max_positions, num_sms);
-    if (!s.split) return 0;
-    return hdr_bytes(s.grid) + static_cast<size_t>(2) * s.grid * s.rows_per_block * (head_dim + 2) * sizeof(float);
+    size_t need = 0;  // that of calls with fewer rows too: the shapes' needs are not quite in their order
+    for (int r = 1;; r = r < 32 && r + 1 < max_rows ? r + 1 : max_rows) {
+        const Shape s = shape_of(head_dim, dtype, group, r < max_rows ? r : max_rows, max_positions, num_sms);
+        const size_t bytes = hdr_bytes(s.grid) + static_cast<size_t>(2) * s.grid * s.rows_per_block * (head_dim + 2) * sizeof(float);
+        if (s.split && bytes > need) need = bytes;
+        if (r >= max_rows || s.nt == 0) return need;  // (the tcgen05 kernel needs the most)
+    }
 }
 
 cudaError_t paged_attention_init() {

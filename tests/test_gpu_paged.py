@@ -175,12 +175,49 @@ def test_attention_over_many_sequences(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_more_sequences_than_the_kernels_keep_at_hand(dtype):
+    """1100 sequences: beyond the boundaries that write and read keep in shared memory, and beyond the threads of both
+    attention kernels.  Written, read back and attended to, with and without a long chunk among the rows."""
+    rng = np.random.default_rng(9)
+    kv = rng.integers(1, 60, size=1100)
+    for most in (2, 40):
+        rows = np.minimum(rng.integers(0, 3, size=1100), kv)
+        kv[700], rows[700] = 59, min(most, 59)
+        c = Case(dtype, 4, 2, 64, 16, rows.tolist(), kv.tolist(), seed=22)
+        cache, rows_d = c.device()
+        vb.kv_write(cache, rows_d, c.dk_new, c.dv_new)
+        k, v = vb.kv_read(cache, rows_d, c.n, torch.float32)
+        used = int(c.cu[-1])
+        for got, src in ((k, c.k_new), (v, c.v_new)):
+            x = src[:used].float().reshape(used, 2, 64)
+            if dtype != BF16:
+                codes, scale = quantise(x, dtype)
+                x = codes.float() * scale[..., None]
+            assert torch.equal(got[:used].cpu(), x)
+        c.k, c.v = cache.k.cpu(), cache.v.cpu()
+        c.k_scale, c.v_scale = (None, None) if dtype == BF16 else (cache.k_scale.cpu(), cache.v_scale.cpu())
+        got = vb.op_attention_paged(c.dq, cache, rows_d)
+        rows_d.check()
+        ref, tol, _, _ = c.attention()
+        assert_within(got[:used].reshape(used, c.H, c.dh), ref[:used], tol[:used])
+
+
+def test_workspace_of_a_larger_call_serves_smaller_ones():
+    c = Case(INT8, 8, 2, 128, 16, [40], [600], seed=23)
+    cache, r = c.device()
+    needs = [vb.attention_paged_workspace(cache, r, n, 8) for n in range(1, 41)]
+    assert all(a <= b for a, b in zip(needs, needs[1:]))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("heads,kv_heads,dh,page,batch,most_rows,most_kv", [
     (16, 8, 64, 16, 40, 300, 500),     # several blocks per CTA, many with one group of rows only
     (16, 4, 128, 32, 24, 70, 1600),    # many tiles per CTA
     (64, 8, 128, 64, 12, 100, 900),
     (28, 4, 64, 32, 30, 90, 300),      # 7 query heads per kv head: blocks of 224 rows
     (4, 4, 128, 16, 60, 400, 450),     # blocks of one and of two groups in turn
+    (32, 8, 128, 16, 20, 24, 2500),    # up to 96 rows per block: both groups on the same rows
+    (16, 2, 64, 64, 50, 16, 400),      # the same with few tiles, one in many cases
 ])
 def test_chunks_of_a_large_batch(heads, kv_heads, dh, page, batch, most_rows, most_kv, dtype):
     rng = np.random.default_rng(7)
