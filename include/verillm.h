@@ -359,7 +359,8 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  *            May be NULL where that is 0.  It holds nothing between calls, but calls that may overlap (other streams, graphs replayed side by side)
  *            need one each.
  * Keys and values of 8-bit pools enter products in fp16, scaled to its range: rounded to 11 bits where the call has many
- * rows per sequence, exact where it has few.  Probabilities are rounded to bf16 (bf16 pools) or fp16; sums are fp32.
+ * rows per sequence, exact where it has few.  Probabilities are rounded to bf16 (bf16 pools; 16 bits where the call has
+ * few rows per sequence) or fp16; sums are fp32.
  * status also receives VERILLM_DEV_WAIT_TIMEOUT when a wait inside the kernel gave up; the results are then invalid.
  * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 128 per kv head; workspace too
  * small or not aligned), E_ARCH, E_CUDA. */
