@@ -311,7 +311,7 @@ int verillm_op_attention(const void *qkv, const int32_t *cu_seqlens, int32_t bat
 enum { VERILLM_KV_BF16 = 0, VERILLM_KV_E4M3 = 1, VERILLM_KV_INT8 = 2 };
 
 typedef struct {
-    void *k, *v;               /* DEVICE [n_pages][n_kv_heads][page_size][head_dim], bf16 or 8-bit; 16-byte aligned */
+    void *k, *v;               /* DEVICE [n_pages][n_kv_heads][page_size][head_dim], bf16 or 8-bit; 32-byte aligned */
     float *k_scale, *v_scale;  /* DEVICE [n_pages][n_kv_heads][page_size]; 8-bit pools only, else NULL; 16-byte aligned */
     int32_t n_pages;
     int32_t page_size;         /* 16, 32, 64, 128 or 256 */

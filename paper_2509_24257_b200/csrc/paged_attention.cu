@@ -62,14 +62,23 @@ __device__ __forceinline__ uint32_t finite2(uint32_t w) {
 __device__ __forceinline__ uint4 finite8(const uint4& x) { return make_uint4(finite2(x.x), finite2(x.y), finite2(x.z), finite2(x.w)); }
 
 // How a warp holds 16 keys and 16 values (lane = 4 g + t).
-// Keys: lane loads 16 bytes of rows g and g + 8 per chunk; a chunk is 4 lanes x 16 bytes = 32 (bf16) or 64 (8-bit) entries.
+// Keys: lane loads KBYTES of rows g and g + 8 per chunk of 4 KBYTES; 32 bytes where the row has them, so that the four
+// lanes of a row take a whole line at a time (8 rows x 64 bytes per load kept the L1 busy twice as long).
 // Values: lane loads VB bytes of rows 2t, 2t + 1, 2t + 8, 2t + 9; the 8 lanes g cover VB * 8 bytes of a row.
 template <int DH, int DTYPE>
 struct Layout {
     static constexpr bool BF16 = DTYPE == VERILLM_KV_BF16;
     static constexpr int ROW_BYTES = DH * (BF16 ? 2 : 1);
-    static constexpr int KCHUNKS = ROW_BYTES / 64;
+    static constexpr int KBYTES = ROW_BYTES >= 128 ? 32 : 16;
+    static constexpr int KWORDS = KBYTES / 4;
+    static constexpr int KCHUNKS = ROW_BYTES / (4 * KBYTES);
     static constexpr int KSTEPS = DH / 16;
+    static constexpr int KSTEP_WORDS = BF16 ? 2 : 1;  // words of a lane and row per step of 16 entries
+    // the 4 entries of a row that lane t names in step ks
+    static __device__ __forceinline__ int entry(int ks, int t) {
+        constexpr int per_chunk = KWORDS / KSTEP_WORDS, lane_entries = KBYTES / (BF16 ? 2 : 1);
+        return (ks / per_chunk) * 4 * lane_entries + t * lane_entries + 4 * (ks % per_chunk);
+    }
     static constexpr int VPIECES = ROW_BYTES >= 128 ? ROW_BYTES / 128 : 1;  // 16-byte pieces per lane and row
     static constexpr int VWORDS = ROW_BYTES >= 128 ? 4 : 2;                 // words per piece (8-byte pieces: 64 8-bit entries)
     static constexpr int MT = DH / 16;                                      // m tiles of O^T
@@ -79,6 +88,20 @@ struct Layout {
         return (i >> 2) * 64 + 8 * g + 2 * (i & 3);
     }
 };
+
+// a lane's words of a row: 16 or (aligned) 32 bytes
+__device__ __forceinline__ void load_words(uint32_t (&w)[4], const char* p) {
+    const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
+    w[0] = x.x;
+    w[1] = x.y;
+    w[2] = x.z;
+    w[3] = x.w;
+}
+__device__ __forceinline__ void load_words(uint32_t (&w)[8], const char* p) {
+    asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p));
+}
 
 // CTAs per SM, all resident at once: what the registers allow (65536 / 128 threads / CTAs).
 __host__ __device__ constexpr int rows_ctas(int dh, int dtype, int nt) {
@@ -146,10 +169,10 @@ paged_rows_kernel(const PagedAttnParams p) {
             uint2 b = make_uint2(0u, 0u);
             if (r < rows) {
                 const __nv_bfloat16* src = q0 + static_cast<size_t>(r / G) * p.q_stride + static_cast<size_t>(r % G) * DH;
-                if (L::BF16) {  // chunk of 32 entries = 2 steps; lane's entries 8 lt .. 8 lt + 7
-                    b = __ldg(reinterpret_cast<const uint2*>(src + (ks >> 1) * 32 + 8 * lt + 4 * (ks & 1)));
-                } else {  // chunk of 64 entries = 4 steps; lane's entries 16 lt + 4 step .. + 3
-                    const uint2 x = __ldg(reinterpret_cast<const uint2*>(src + (ks >> 2) * 64 + 16 * lt + 4 * (ks & 3)));
+                const uint2 x = __ldg(reinterpret_cast<const uint2*>(src + L::entry(ks, lt)));
+                if (L::BF16) {
+                    b = x;
+                } else {
                     const float down = __uint_as_float((254u - sm_exp[r]) << 23);
                     b = make_uint2(pack_half(bf16_lo(x.x) * down, bf16_hi(x.x) * down), pack_half(bf16_lo(x.y) * down, bf16_hi(x.y) * down));
                 }
@@ -174,15 +197,16 @@ paged_rows_kernel(const PagedAttnParams p) {
             }
         }
 
-        uint4 ka[L::KCHUNKS], kb[L::KCHUNKS], v[L::VPIECES][4];
+        uint32_t ka[L::KCHUNKS][L::KWORDS], kb[L::KCHUNKS][L::KWORDS];
+        uint4 v[L::VPIECES][4];
         float ks0 = 1.f, ks1 = 1.f, vs0 = 1.f, vs1 = 1.f, vs0n = 1.f, vs1n = 1.f;
         auto token_of = [&](int tile) { return tile * PR_TILE + warp * 16; };
         auto load_keys = [&](size_t vec) {
-            const char* base = reinterpret_cast<const char*>(c.k) + (vec + g) * L::ROW_BYTES + t * 16;
+            const char* base = reinterpret_cast<const char*>(c.k) + (vec + g) * L::ROW_BYTES + t * L::KBYTES;
 #pragma unroll
             for (int i = 0; i < L::KCHUNKS; ++i) {
-                ka[i] = __ldg(reinterpret_cast<const uint4*>(base + i * 64));
-                kb[i] = __ldg(reinterpret_cast<const uint4*>(base + 8 * L::ROW_BYTES + i * 64));
+                load_words(ka[i], base + i * 4 * L::KBYTES);
+                load_words(kb[i], base + 8 * L::ROW_BYTES + i * 4 * L::KBYTES);
             }
             if (!L::BF16) {
                 ks0 = __ldg(c.k_scale + vec + g);
@@ -251,26 +275,21 @@ paged_rows_kernel(const PagedAttnParams p) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
 #pragma unroll
-            for (int i = 0; i < L::KCHUNKS; ++i) {
-                const uint32_t wa[4] = {ka[i].x, ka[i].y, ka[i].z, ka[i].w}, wb[4] = {kb[i].x, kb[i].y, kb[i].z, kb[i].w};
+            for (int ks = 0; ks < L::KSTEPS; ++ks) {
+                constexpr int per_chunk = L::KWORDS / L::KSTEP_WORDS;
+                const int i = ks / per_chunk, w = (ks % per_chunk) * L::KSTEP_WORDS;
+                uint2 a, e;  // rows g and g + 8
                 if (L::BF16) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            const uint2 b = sm_q[(nt * L::KSTEPS + 2 * i + h) * 32 + lane];
-                            mma16<L::BF16>(sc[nt], wa[2 * h], wb[2 * h], wa[2 * h + 1], wb[2 * h + 1], b.x, b.y);
-                        }
+                    a = make_uint2(ka[i][w], ka[i][(w + 1) % L::KWORDS]);
+                    e = make_uint2(kb[i][w], kb[i][(w + 1) % L::KWORDS]);
                 } else {
+                    a = widen4_half<DTYPE>(ka[i][w]);
+                    e = widen4_half<DTYPE>(kb[i][w]);
+                }
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const uint2 a = widen4_half<DTYPE>(wa[w]), e = widen4_half<DTYPE>(wb[w]);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            const uint2 b = sm_q[(nt * L::KSTEPS + 4 * i + w) * 32 + lane];
-                            mma16<L::BF16>(sc[nt], a.x, e.x, a.y, e.y, b.x, b.y);
-                        }
-                    }
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint2 b = sm_q[(nt * L::KSTEPS + ks) * 32 + lane];
+                    mma16<L::BF16>(sc[nt], a.x, e.x, a.y, e.y, b.x, b.y);
                 }
             }
             const float f0 = ks0, f1 = ks1;

@@ -362,7 +362,7 @@ int check_paged(const verillm_kv_cache* c, const verillm_kv_rows* r, PagedCacheD
     // (page, kv head, row in page) is addressed as one 32-bit row number by the tile loads
     if (static_cast<int64_t>(c->n_pages) * c->n_kv_heads * c->page_size > 0x7FFFFFFFLL) return VERILLM_E_SHAPE;
     if (static_cast<int64_t>(r->table_width) * c->page_size > (1LL << 30)) return VERILLM_E_SHAPE;  // positions in 32 bits
-    if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 15u) return VERILLM_E_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 31u) return VERILLM_E_SHAPE;  // 32-byte loads
     if (c->dtype != VERILLM_KV_BF16 && ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 15u)) return VERILLM_E_SHAPE;
     cd->k = c->k; cd->v = c->v;
     cd->k_scale = c->dtype == VERILLM_KV_BF16 ? nullptr : c->k_scale;

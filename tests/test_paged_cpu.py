@@ -42,7 +42,7 @@ def _codes(library, cache, rows):
     (dict(k=None), vb.E_INVAL), (dict(v=None), vb.E_INVAL), (dict(k_scale=None), vb.E_INVAL), (dict(v_scale=None), vb.E_INVAL),
     (dict(dtype=3), vb.E_INVAL), (dict(dtype=-1), vb.E_INVAL), (dict(n_pages=0), vb.E_INVAL), (dict(n_kv_heads=0), vb.E_INVAL),
     (dict(page_size=8), vb.E_SHAPE), (dict(page_size=48), vb.E_SHAPE), (dict(page_size=512), vb.E_SHAPE), (dict(page_size=0), vb.E_SHAPE),
-    (dict(head_dim=96), vb.E_SHAPE), (dict(head_dim=256), vb.E_SHAPE), (dict(k=PTR + 8), vb.E_SHAPE), (dict(v=PTR + 1), vb.E_SHAPE), (dict(k_scale=PTR + 4), vb.E_SHAPE), (dict(v_scale=PTR + 8), vb.E_SHAPE),
+    (dict(head_dim=96), vb.E_SHAPE), (dict(head_dim=256), vb.E_SHAPE), (dict(k=PTR + 8), vb.E_SHAPE), (dict(v=PTR + 1), vb.E_SHAPE), (dict(k=PTR + 16), vb.E_SHAPE), (dict(v=PTR + 16), vb.E_SHAPE), (dict(k_scale=PTR + 4), vb.E_SHAPE), (dict(v_scale=PTR + 8), vb.E_SHAPE),
     (dict(n_pages=1 << 27, page_size=16, n_kv_heads=2), vb.E_SHAPE),  # rows beyond 32 bits
 ])
 def test_bad_caches_are_refused(library, kw, code):
