@@ -401,7 +401,9 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
                 uint32_t v0[32], v1[32], v2[32], v3[32];
                 float rt = rf, vnew = 0.f;
                 if (!BF16) {
-                    rt = rf * sc_ref[2 * (g % PT_SCALES)];
+                    // not below the smallest normal number: 0 times a masked entry's -inf would be NaN (a score is
+                    // below 2^24 before this factor, so none of those it concerns reaches 2^-100)
+                    rt = fmaxf(rf * sc_ref[2 * (g % PT_SCALES)], 1.17549435e-38f);
                     vnew = sc_ref[2 * (g % PT_SCALES) + 1];
                 }
                 auto prepare = [&](uint32_t (&v)[32], int c) {  // masks the scores of columns [c, c + 32)

@@ -277,6 +277,28 @@ def test_large_scores_and_a_late_maximum(dtype):
     assert_within(got[:used].reshape(used, c.H, c.dh), ref[:used], tol[:used])
 
 
+@pytest.mark.parametrize("rows,kv", [([1, 2], [100, 40]), ([6, 40], [300, 140])])
+@pytest.mark.parametrize("q_size,k_size", [(0.0, 1e-6), (0.0, 0.0), (1e-30, 1e-3), (1e25, 1e-25), (1e-25, 1e25)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_very_small_and_large_queries_and_keys(dtype, q_size, k_size, rows, kv):
+    """Queries of zero over small keys (every visible key weighs the same), and sizes that only their product makes moderate."""
+    c = Case(dtype, 8, 2, 128, 16, rows, kv, seed=24)
+    k, v = (torch.zeros_like(t, dtype=torch.float32) for t in (c.k, c.v))
+    g = torch.Generator().manual_seed(2)
+    k.copy_(torch.randn(k.shape, generator=g) * k_size)
+    v.copy_(torch.randn(v.shape, generator=g))
+    c.set_pools(k.to(BF16), v.to(BF16))
+    c.q.copy_(c.q.float() * q_size)
+    cache, rows_d = c.device()
+    lse = torch.zeros(c.n, c.H, device=DEV)
+    got = vb.op_attention_paged(c.dq, cache, rows_d, lse=lse)
+    rows_d.check()
+    ref, tol, lref, ltol = c.attention()
+    used = int(c.cu[-1])
+    assert_within(got[:used].reshape(used, c.H, c.dh), ref[:used], tol[:used])
+    assert_within(lse[:used], lref[:used], ltol[:used], "lse")
+
+
 def test_attention_agrees_with_the_packed_operator():
     """Whole sequences written into a bf16 cache and attended to from all their rows are op_attention."""
     lens, H, KV, dh = [130, 1, 257, 64], 32, 8, 128
