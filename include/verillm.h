@@ -325,13 +325,14 @@ typedef struct {
  * page_table[b * table_width + p / page_size].  A row whose position is negative does not exist: it is not
  * written, reads as zeros, and attends to nothing.  Rows behind the last sequence (padding of a captured batch)
  * are left as they are.  The arrays are DEVICE memory and are read when the kernels run, so a captured graph sees
- * their current contents; entries of the table behind a sequence's last page are never used.
+ * their current contents; they must not change while a call that reads them runs.  Entries of the table behind a
+ * sequence's last page are never used.
  * Pages may be shared between sequences; a position that one call writes must belong to one row only. */
 typedef struct {
     const int32_t *page_table; /* [batch][table_width] */
     const int32_t *cu_rows;    /* [batch + 1] */
     const int32_t *kv_len;     /* [batch] */
-    int32_t table_width, batch;
+    int32_t table_width, batch; /* table_width * page_size at most 2^26 */
     int32_t n_rows;            /* rows that the packed buffers of the call hold; 0: the call does nothing */
     int32_t max_rows;          /* at least every n_b; a sequence with more is skipped (VERILLM_DEV_ROWS_RANGE) */
 } verillm_kv_rows;
@@ -353,7 +354,7 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  * sequence; conventions as verillm_op_attention (scale 1/sqrt(head_dim), query head g reads kv head
  * g * n_kv_heads / n_heads).
  *  q         DEVICE bf16, n_heads * head_dim entries per row, q_stride entries from row to row, already rotated
- *  out       DEVICE bf16, same form with out_stride; a row that attends to nothing receives zeros
+ *  out       DEVICE bf16, same form with out_stride, not overlapping q; a row that attends to nothing receives zeros
  *  lse       optional DEVICE float32 [n_rows][n_heads]: log of the sum of exp(scores), -inf for such a row
  *  workspace DEVICE, 256-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code).
  *            May be NULL where that is 0.  It holds nothing between calls, but calls that may overlap (other streams, graphs replayed side by side)

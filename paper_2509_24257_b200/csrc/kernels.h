@@ -123,6 +123,7 @@ struct PagedAttnParams {
     int* status;
 };
 constexpr int kPagedMaxGroup = 128;  // query heads per kv head
+constexpr long long kPagedMaxPositions = 1LL << 26;  // table_width * page_size
 constexpr int kPagedTcRows = 256;    // packed rows per block of the tcgen05 kernel
 // Bytes of partial results and headers a launch needs; what the rule on sizes picks.
 size_t paged_attention_workspace(int head_dim, int dtype, int group, int max_rows, long long max_positions, int num_sms);

@@ -219,9 +219,10 @@ __device__ __forceinline__ bool walk_next(int tl, const PagedRowsDev& r, int pag
         k.j = 0;
         if (++k.kvh == n_kv_heads) {
             k.kvh = 0;
-            do {
-                k.s = load_seq(r, page_shift, ++k.seq, nullptr);
-            } while (k.s.n == 0);  // a later sequence has tiles: the share does not end here
+            do {  // (a later sequence has tiles, as the share does not end here; the bound is for arrays that change meanwhile)
+                if (++k.seq >= r.batch) return false;
+                k.s = load_seq(r, page_shift, k.seq, nullptr);
+            } while (k.s.n == 0);
         }
     }
     k.tiles = tiles_of_end(tl, block_end(k.s, tb_log, k.j));

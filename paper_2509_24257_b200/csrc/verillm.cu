@@ -361,7 +361,8 @@ int check_paged(const verillm_kv_cache* c, const verillm_kv_rows* r, PagedCacheD
     if ((1 << shift) != c->page_size) return VERILLM_E_SHAPE;
     // (page, kv head, row in page) is addressed as one 32-bit row number by the tile loads
     if (static_cast<int64_t>(c->n_pages) * c->n_kv_heads * c->page_size > 0x7FFFFFFFLL) return VERILLM_E_SHAPE;
-    if (static_cast<int64_t>(r->table_width) * c->page_size > (1LL << 30)) return VERILLM_E_SHAPE;  // positions in 32 bits
+    // a block's walk over this many positions stays well inside the limit of the kernels' bounded waits
+    if (static_cast<int64_t>(r->table_width) * c->page_size > kPagedMaxPositions) return VERILLM_E_SHAPE;
     if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 31u) return VERILLM_E_SHAPE;  // 32-byte loads
     if (c->dtype != VERILLM_KV_BF16 && ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 15u)) return VERILLM_E_SHAPE;
     cd->k = c->k; cd->v = c->v;
@@ -439,7 +440,7 @@ int ensure_paged_decode(verillm_model* m) {
         // a decode step has one row per sequence; the largest need over the pool types and lengths
         size_t need = 256;
         for (int t = 0; t < 3; ++t)
-            need = std::max(need, paged_attention_workspace(c.head_dim, t, c.n_heads / c.n_kv_heads, 1, 1LL << 30, m->num_sms));
+            need = std::max(need, paged_attention_workspace(c.head_dim, t, c.n_heads / c.n_kv_heads, 1, kPagedMaxPositions, m->num_sms));
         unsigned char* ws = nullptr;
         if ((rc = dev_alloc(&ws, need))) return rc;
         d.attn_ws = ws;
@@ -1129,9 +1130,10 @@ static int decode_impl(verillm_model* m, const int32_t* tokens, const int32_t* c
                     if ((rc = verillm_op_attention_paged(&kc, &kr, d.q, m->d_q, c.n_heads, d.attn, m->d_q, nullptr, d.attn_ws,
                                                          INT64_MAX, dev_status, cuda_stream)))
                         return rc;
-                } else
-                CU_TRY(launch_decode_attention(d.q, cache_l, i_row_start + r0, i_row_pos + r0, rows, c.n_heads,
-                                               c.n_kv_heads, c.head_dim, t + 1, d.attn, st));
+                } else {
+                    CU_TRY(launch_decode_attention(d.q, cache_l, i_row_start + r0, i_row_pos + r0, rows, c.n_heads,
+                                                   c.n_kv_heads, c.head_dim, t + 1, d.attn, st));
+                }
                 CU_TRY(launch_skinny_gemm(d.attn, w.wo, d.resid, rows, c.d_model, m->d_q, 1, st));
                 CU_TRY(launch_rmsnorm(d.resid, w.ffn_norm, d.xn, rows, c.d_model, c.rms_eps, st));
                 CU_TRY(launch_skinny_gemm(d.xn, w.wgu, d.gu, rows, 2 * c.d_ffn, c.d_model, 0, st));
@@ -1152,17 +1154,21 @@ static int decode_impl(verillm_model* m, const int32_t* tokens, const int32_t* c
 
 int verillm_decode_commit(verillm_model* m, const int32_t* tokens, const int32_t* cu_seqlens, int32_t batch,
                           int32_t n_prefill, const int32_t* check_seq, const int32_t* check_pos, int32_t n_check,
-                          void* committed_out, int32_t commit_dtype, int32_t* status, void* cuda_stream) {
+                          void* committed_out, int32_t commit_dtype, int32_t* status, void* cuda_stream) try {
     return decode_impl(m, tokens, cu_seqlens, batch, n_prefill, check_seq, check_pos, n_check, committed_out, commit_dtype, -1, status,
                        cuda_stream);
+} catch (const std::bad_alloc&) {  // host index tables
+    return VERILLM_E_NOMEM;
 }
 
 int verillm_decode_commit_paged(verillm_model* m, const int32_t* tokens, const int32_t* cu_seqlens, int32_t batch, int32_t n_prefill,
                                 const int32_t* check_seq, const int32_t* check_pos, int32_t n_check, void* committed_out,
-                                int32_t commit_dtype, int32_t cache_dtype, int32_t* status, void* cuda_stream) {
+                                int32_t commit_dtype, int32_t cache_dtype, int32_t* status, void* cuda_stream) try {
     if (cache_dtype != VERILLM_KV_BF16 && cache_dtype != VERILLM_KV_E4M3 && cache_dtype != VERILLM_KV_INT8) return VERILLM_E_INVAL;
     return decode_impl(m, tokens, cu_seqlens, batch, n_prefill, check_seq, check_pos, n_check, committed_out, commit_dtype, cache_dtype,
                        status, cuda_stream);
+} catch (const std::bad_alloc&) {
+    return VERILLM_E_NOMEM;
 }
 
 int verillm_selftest_wait_timeout(int64_t limit_cycles, int32_t* status, int32_t* gave_up, void* cuda_stream) {
@@ -1268,6 +1274,7 @@ int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_r
     if (rc || (rc = check_group(cache, n_heads)) || p.r.n_rows == 0) return rc;
     const int64_t width = static_cast<int64_t>(n_heads) * p.c.head_dim;
     if ((rc = check_rows(q, q_stride, width, 8)) || (rc = check_rows(out, out_stride, width, 8))) return rc;
+    if (q == out) return VERILLM_E_INVAL;
     if ((rc = current_sms(&sms))) return rc;
     p.group = n_heads / p.c.n_kv_heads;
     const int64_t need = static_cast<int64_t>(paged_attention_workspace(p.c.head_dim, p.c.dtype, p.group, p.r.max_rows,

@@ -82,3 +82,10 @@ def test_null_descriptions_are_refused(library):
     assert library.verillm_kv_read(None, None, PTR, PTR, 128, 0, None, None) == vb.E_INVAL
     assert library.verillm_op_attention_paged(None, None, PTR, 256, 4, PTR, 256, None, PTR, 0, None, None) == vb.E_INVAL
     assert library.verillm_op_attention_paged_workspace(None, None, 4) == vb.E_INVAL
+
+
+def test_contexts_beyond_the_bound_and_output_over_the_queries_are_refused(library):
+    cache = _cache(page_size=256, n_pages=1 << 18)
+    assert _codes(library, cache, _rows(table_width=(1 << 18) + 1)) == [vb.E_SHAPE] * 4
+    c, r = C.byref(cache), C.byref(_rows())
+    assert library.verillm_op_attention_paged(c, r, PTR, 256, 4, PTR, 256, None, PTR, 1 << 40, None, None) == vb.E_INVAL
