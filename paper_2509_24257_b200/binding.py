@@ -527,7 +527,16 @@ def op_attention(qkv: torch.Tensor, cu_seqlens: Sequence[int], n_heads: int, n_k
 _KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_E4M3, torch.int8: KV_INT8}
 
 
-class KVCache:
+class _Fixed:
+    """Attributes are set once: what the C side is told about them was taken when they were set."""
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__ and not name.startswith("_"):
+            raise AttributeError(f"{type(self).__name__}.{name} cannot be replaced; make a new {type(self).__name__}")
+        object.__setattr__(self, name, value)
+
+
+class KVCache(_Fixed):
     """The paged cache of one layer: pools k, v [n_pages][n_kv_heads][page_size][head_dim] (bf16, float8_e4m3fn or int8)
     and, for 8-bit pools, float32 scales [n_pages][n_kv_heads][page_size].  Wraps the caller's tensors; `alloc` makes
     zeroed ones."""
@@ -565,7 +574,7 @@ class KVCache:
         return cls(*pools, *scales)
 
 
-class PagedRows:
+class PagedRows(_Fixed):
     """The rows of a paged call: int32 device tensors page_table [batch][width], cu_rows [batch+1], kv_len [batch] and
     max_rows, at least every sequence's number of rows.  Row i of sequence b is position kv_len[b] - n_b + i of it.
     Pass `status` (int32 [1], zeroed) to have problems that only the device can see reported there; `check` reads it."""
@@ -596,15 +605,17 @@ class PagedRows:
             raise RuntimeError(f"paged cache: device status {int(self.status.item())}")
 
 
-def _packed_rows(t: torch.Tensor, what: str, width: int, device: torch.device, dtypes=(torch.bfloat16,)) -> int:
+def _packed_rows(t: torch.Tensor, what: str, width: int, head_dim: int, device: torch.device, dtype=torch.bfloat16) -> int:
     """Row stride of a [rows][width] or [rows][heads][head_dim] tensor whose rows are contiguous."""
     shape, strides = t.shape, t.stride()
-    if t.dtype not in dtypes or t.device != device or len(shape) not in (2, 3):
-        raise ValueError(f"{what} must be a 2- or 3-dimensional {' / '.join(str(d) for d in dtypes)} tensor on {device}")
-    inner = shape[1] if len(shape) == 2 else shape[1] * shape[2]
-    packed = strides[-1] == 1 and (len(shape) == 2 or shape[1] == 1 or strides[1] == shape[2])
-    if inner != width or not packed:
-        raise ValueError(f"{what} must have {width} consecutive entries per row")
+    if t.dtype != dtype or t.device != device or len(shape) not in (2, 3):
+        raise ValueError(f"{what} must be a 2- or 3-dimensional {dtype} tensor on {device}")
+    if len(shape) == 2:
+        packed = shape[1] == width
+    else:
+        packed = shape[2] == head_dim and shape[1] * head_dim == width and (shape[1] == 1 or strides[1] == head_dim)
+    if not packed or strides[-1] != 1:
+        raise ValueError(f"{what} must have {width} consecutive entries per row, in heads of {head_dim}")
     return strides[0] if shape[0] > 1 else width
 
 
@@ -630,8 +641,8 @@ def kv_write(cache: KVCache, rows: PagedRows, k: torch.Tensor, v: torch.Tensor,
     """Stores the rows' keys and values (bf16 [n_rows][n_kv_heads * head_dim], e.g. column slices of a fused
     projection; keys already rotated) at their positions, quantised to the cache's type."""
     width = cache.n_kv_heads * cache.head_dim
-    stride = _packed_rows(k, "k", width, cache.device)
-    if _packed_rows(v, "v", width, cache.device) != stride or v.shape[0] != k.shape[0]:
+    stride = _packed_rows(k, "k", width, cache.head_dim, cache.device)
+    if _packed_rows(v, "v", width, cache.head_dim, cache.device) != stride or v.shape[0] != k.shape[0]:
         raise ValueError("k and v must have the same rows and row stride")
     if rows.device != cache.device:
         raise ValueError("rows and cache must be on one device")
@@ -655,8 +666,8 @@ def kv_read(cache: KVCache, rows: PagedRows, n_rows: int, dtype: torch.dtype = t
         k, v = out or [torch.empty(n_rows, cache.n_kv_heads, cache.head_dim, dtype=dtype, device=cache.device) for _ in range(2)]
         stride = width
         if out is not None:
-            stride = _packed_rows(k, "k", width, cache.device, (dtype,))
-            if _packed_rows(v, "v", width, cache.device, (dtype,)) != stride or k.shape[0] != n_rows or v.shape[0] != n_rows:
+            stride = _packed_rows(k, "k", width, cache.head_dim, cache.device, dtype)
+            if _packed_rows(v, "v", width, cache.head_dim, cache.device, dtype) != stride or k.shape[0] != n_rows or v.shape[0] != n_rows:
                 raise ValueError("out must be two tensors of n_rows rows with the same row stride")
         rc = rows.c_struct(n_rows)
         _check(lib().verillm_kv_read(C.byref(cache.c_struct), C.byref(rc), k.data_ptr(), v.data_ptr(), stride,
@@ -673,12 +684,12 @@ def op_attention_paged(q: torch.Tensor, cache: KVCache, rows: PagedRows, out: Op
     the cache -> bf16 [n_rows][n_heads * head_dim].  lse: optional float32 [n_rows][n_heads] that receives the log of
     the sum of exp(scores).  workspace: optional uint8 tensor of `attention_paged_workspace` bytes to use instead of
     allocating one for the call."""
-    n_rows = q.shape[0]
-    width = q.shape[1] if q.dim() == 2 else q.shape[1] * q.shape[-1]
-    if width == 0 or width % cache.head_dim:
-        raise ValueError("q must have n_heads * head_dim entries per row")
-    n_heads = width // cache.head_dim
-    q_stride = _packed_rows(q, "q", width, cache.device)
+    shape = q.shape
+    if len(shape) not in (2, 3):
+        raise ValueError("q must be [n_rows][n_heads * head_dim] or [n_rows][n_heads][head_dim]")
+    n_rows, n_heads = shape[0], shape[1] if len(shape) == 3 else shape[1] // cache.head_dim
+    width = n_heads * cache.head_dim
+    q_stride = _packed_rows(q, "q", width, cache.head_dim, cache.device)
     if rows.device != cache.device:
         raise ValueError("rows and cache must be on one device")
     if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (n_rows, n_heads) or not lse.is_contiguous() or lse.device != cache.device):
@@ -691,7 +702,7 @@ def op_attention_paged(q: torch.Tensor, cache: KVCache, rows: PagedRows, out: Op
         if o is None:
             o = torch.empty(n_rows, width, dtype=torch.bfloat16, device=cache.device)
         else:
-            stride = _packed_rows(o, "out", width, cache.device)
+            stride = _packed_rows(o, "out", width, cache.head_dim, cache.device)
             if o.shape[0] != n_rows:
                 raise ValueError("out must have as many rows as q")
         if ws is None:

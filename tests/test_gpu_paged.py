@@ -470,3 +470,95 @@ def test_wrapper_refuses_what_the_kernels_cannot_take():
         vb.op_attention_paged(c.dq[:, :192], cache, rows)  # 3 query heads over 2 kv heads
     assert e.value.code == vb.E_SHAPE
     rows.check()
+
+
+def test_descriptions_are_fixed_and_head_shapes_checked():
+    c = Case(E4M3, 4, 2, 64, 16, [2], [20], seed=25, strided=False)
+    cache, rows = c.device()
+    for obj, name in ((rows, "kv_len"), (rows, "max_rows"), (rows, "page_table"), (cache, "k"), (cache, "v_scale")):
+        with pytest.raises(AttributeError):
+            setattr(obj, name, getattr(obj, name))
+    q3 = c.dq.reshape(c.n, 4, 64)
+    assert torch.equal(vb.op_attention_paged(q3, cache, rows)[:2], vb.op_attention_paged(c.dq, cache, rows)[:2])
+    for bad in (c.dq.reshape(c.n, 2, 128), c.dq.reshape(c.n, 4, 2, 32), c.dq.flatten(), c.dq[:, :200], c.dq[:, :0]):
+        with pytest.raises((ValueError, vb.VerillmError)):
+            vb.op_attention_paged(bad, cache, rows)
+    with pytest.raises(ValueError):
+        vb.kv_write(cache, rows, c.dk_new.reshape(c.n, 1, 128), c.dv_new.reshape(c.n, 1, 128))
+    q = c.dq.contiguous()
+    with pytest.raises(vb.VerillmError) as e:
+        vb.op_attention_paged(q, cache, rows, out=q)
+    assert e.value.code == vb.E_INVAL
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_pools_of_more_than_four_gigabytes(dtype):
+    """Pages at the far end of pools whose byte offsets pass 32 bits: writing, reading, and both attention kernels."""
+    for rows, kv in (([1, 3], [200, 90]), ([40, 70], [200, 90])):
+        c = Case(dtype, 8, 8, 128, 256, rows, kv, seed=26)
+        n = c.k.shape[0]
+        small, r = c.device()
+        pages = (5 << 30) // (8 * 256 * 128 * small.k.element_size())
+        big = [torch.empty((pages,) + tuple(t.shape[1:]), dtype=t.dtype, device=DEV) for t in (small.k, small.v)]
+        scales = [None if t is None else torch.empty((pages,) + tuple(t.shape[1:]), device=DEV) for t in (small.k_scale, small.v_scale)]
+        for dst, src in zip(big + scales, (small.k, small.v, small.k_scale, small.v_scale)):
+            if dst is not None:
+                dst[pages - n:] = src
+        cache = vb.KVCache(*big, *scales)
+        far = vb.PagedRows(torch.where(r.page_table < n, r.page_table + (pages - n), r.page_table), r.cu_rows, r.kv_len, r.max_rows, r.status)
+        used = int(c.cu[-1])
+        assert torch.equal(vb.op_attention_paged(c.dq, cache, far)[:used], vb.op_attention_paged(c.dq, small, r)[:used])
+        vb.kv_write(cache, far, c.dk_new, c.dv_new)
+        vb.kv_write(small, r, c.dk_new, c.dv_new)
+        for got, want in zip(vb.kv_read(cache, far, used), vb.kv_read(small, r, used)):
+            assert torch.equal(got, want)
+        far.check()
+        del cache, big, scales
+
+
+def test_two_calls_at_once_and_replayed_chunks():
+    """A chunk and a decode step side by side on two streams, each with its own workspace, eagerly and as captured graphs
+    replayed after the cache, the lengths and the queries changed: the bits of the calls made one after the other."""
+    for dtype in DTYPES:
+        a = Case(dtype, 32, 8, 128, 16, [200, 60], [900, 700], seed=27, pad=0)
+        b = Case(dtype, 32, 8, 128, 16, [1] * 20, [1000 + 50 * i for i in range(20)], seed=28, pad=0)
+        calls = []
+        for c in (a, b):
+            cache, rows = c.device()
+            ws = torch.empty(vb.attention_paged_workspace(cache, rows, c.n, 32), dtype=torch.uint8, device=DEV)
+            q, out = c.dq.clone(), torch.zeros(c.n, 32 * 128, dtype=BF16, device=DEV)
+            calls.append((cache, rows, ws, q, out, c))
+        alone = [vb.op_attention_paged(q, cache, rows) for cache, rows, ws, q, out, c in calls]
+        streams = [torch.cuda.Stream() for _ in calls]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for st, (cache, rows, ws, q, out, c) in zip(streams, calls):
+                vb.op_attention_paged(q, cache, rows, out=out, workspace=ws, stream=st)
+        torch.cuda.synchronize()
+        for want, call in zip(alone, calls):
+            assert torch.equal(call[4], want)
+        graphs = []
+        for cache, rows, ws, q, out, c in calls:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                vb.kv_write(cache, rows, c.dk_new, c.dv_new)
+                vb.op_attention_paged(q, cache, rows, out=out, workspace=ws)
+            graphs.append(graph)
+        for step in range(3):
+            want = []
+            for cache, rows, ws, q, out, c in calls:
+                q.mul_(-1.0 if step else 0.5)
+                rows.kv_len.sub_(7)
+                c.dk_new.mul_(0.5)
+                out.zero_()
+                vb.kv_write(cache, rows, c.dk_new, c.dv_new)
+                want.append(vb.op_attention_paged(q, cache, rows))
+            torch.cuda.synchronize()
+            for st, graph in zip(streams, graphs):
+                with torch.cuda.stream(st):
+                    graph.replay()
+                    graph.replay()
+            torch.cuda.synchronize()
+            for call, w in zip(calls, want):
+                call[1].check()
+                assert torch.equal(call[4], w)
