@@ -531,7 +531,7 @@ class _Fixed:
     """Attributes are set once: what the C side is told about them was taken when they were set."""
 
     def __setattr__(self, name, value):
-        if name in self.__dict__ and not name.startswith("_"):
+        if name in self.__dict__:
             raise AttributeError(f"{type(self).__name__}.{name} cannot be replaced; make a new {type(self).__name__}")
         object.__setattr__(self, name, value)
 
@@ -558,11 +558,10 @@ class KVCache(_Fixed):
             raise ValueError("bf16 pools have no scales")
         if dev < 0 or v.get_device() != dev or not k.is_contiguous() or not v.is_contiguous():
             raise ValueError("pools and scales must be contiguous and on one CUDA device")
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device = k.device
-        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
-        self.c_struct = KVCacheC(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), self.n_pages, self.page_size,
-                                 self.n_kv_heads, self.head_dim, dtype)
+        n_pages, n_kv_heads, page_size, head_dim = shape
+        self.__dict__.update(  # (at once: a program may wrap its tensors for every call)
+            k=k, v=v, k_scale=k_scale, v_scale=v_scale, device=k.device, n_pages=n_pages, n_kv_heads=n_kv_heads, page_size=page_size, head_dim=head_dim,
+            c_struct=KVCacheC(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), n_pages, page_size, n_kv_heads, head_dim, dtype))
 
     @classmethod
     def alloc(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16,
@@ -588,15 +587,15 @@ class PagedRows(_Fixed):
         table = page_table.shape
         if len(table) != 2 or kv_len.shape != table[:1] or cu_rows.shape != (table[0] + 1,):
             raise ValueError("page_table is [batch][width], cu_rows [batch + 1], kv_len [batch]")
-        self.page_table, self.cu_rows, self.kv_len, self.max_rows, self.status = page_table, cu_rows, kv_len, int(max_rows), status
-        self.device = page_table.device
-        self._last: Optional[KVRowsC] = None
+        self.__dict__.update(page_table=page_table, cu_rows=cu_rows, kv_len=kv_len, max_rows=int(max_rows), status=status,
+                             device=page_table.device, _last=None)
 
     def c_struct(self, n_rows: int) -> KVRowsC:
         last = self._last  # the struct of the last call, if it had as many rows; never changed once made
         if last is None or last.n_rows != n_rows:
-            last = self._last = KVRowsC(self.page_table.data_ptr(), self.cu_rows.data_ptr(), self.kv_len.data_ptr(),
-                                        self.page_table.shape[1], self.kv_len.shape[0], n_rows, self.max_rows)
+            batch, width = self.page_table.shape
+            last = self.__dict__["_last"] = KVRowsC(self.page_table.data_ptr(), self.cu_rows.data_ptr(), self.kv_len.data_ptr(),
+                                                    width, batch, n_rows, self.max_rows)
         return last
 
     def check(self) -> None:
