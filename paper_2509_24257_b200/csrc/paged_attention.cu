@@ -583,7 +583,14 @@ paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
 #pragma unroll
         for (int c = 0; c < W; ++c) acc[j][c] = 0.f;
     }
-    for (int i = lane; i < h.x; i += 32)
+    float m_part[RPW], l_part[RPW];  // of the piece that this lane looks at; read once where there are up to 32
+#pragma unroll
+    for (int j = 0; j < RPW; ++j) {
+        m_part[j] = lane < h.x ? part_of(lane)[r0 + j] : -INFINITY;
+        l_part[j] = lane < h.x ? part_of(lane)[rows_per_block + r0 + j] : 0.f;
+        mx[j] = fmaxf(mx[j], m_part[j]);
+    }
+    for (int i = lane + 32; i < h.x; i += 32)
 #pragma unroll
         for (int j = 0; j < RPW; ++j) mx[j] = fmaxf(mx[j], part_of(i)[r0 + j]);
 #pragma unroll
@@ -593,8 +600,12 @@ paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
         float w[RPW];
 #pragma unroll
         for (int j = 0; j < RPW; ++j) {
-            w[j] = i < h.x ? part_weight(part_of(i)[r0 + j], mx[j]) : 0.f;
-            l[j] += warp_sum(i < h.x ? part_of(i)[rows_per_block + r0 + j] * w[j] : 0.f);
+            if (i0 != 0) {
+                m_part[j] = i < h.x ? part_of(i)[r0 + j] : -INFINITY;
+                l_part[j] = i < h.x ? part_of(i)[rows_per_block + r0 + j] : 0.f;
+            }
+            w[j] = part_weight(m_part[j], mx[j]);
+            l[j] += warp_sum(l_part[j] * w[j]);
         }
         for (int q0 = 0; q0 < n; q0 += AHEAD) {
             float x[AHEAD][RPW][W];
