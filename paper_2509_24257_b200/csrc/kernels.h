@@ -118,7 +118,7 @@ struct PagedAttnParams {
     int n_heads, group;
     int tb_log;   // tokens per block, log2
     int share_log;  // few-row kernel: positions per unit of a CTA's share, log2 (30: whole blocks)
-    int4* hdr;    // [grid]
+    int4* hdr;    // [grid][2]
     float* part;  // [2 grid][rows][head_dim + 2]
     int* status;
 };

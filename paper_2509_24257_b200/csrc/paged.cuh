@@ -231,9 +231,21 @@ __device__ __forceinline__ bool walk_next(int tl, const PagedRowsDev& r, int pag
     return true;
 }
 
-// Partial results.  hdr[c]: {pieces, sequence, kv head, block} of the block whose first tiles CTA c holds and whose
-// last it does not (pieces 0: none).  Slot 2 c: the block that began before CTA c; slot 2 c + 1: hdr[c]'s block.
+// Partial results.  hdr[2 c]: {pieces, sequence, kv head, block} of the block whose first tiles CTA c holds and whose
+// last it does not (pieces 0: none).  Slot 2 c: the block that began before CTA c; slot 2 c + 1: hdr[2 c]'s block.
+// hdr[2 c + 1].x (few-row kernel): the CTA in which slot 2 c's block began, if it has more than kJoinAlone pieces and is joined
+// by the CTAs of all of them, else -1.
 // A slot holds `rows` maxima (log2 units, -inf: no key yet), `rows` sums, and `rows` x head_dim outputs.
+constexpr int kJoinAlone = 16;
+__device__ __forceinline__ int last_cta(const WorkShare& w, const BlockWalk& k) { return static_cast<int>(short_div(k.at + k.tiles - 1, w.per)); }
+__device__ __forceinline__ void no_headers(int4* hdr) {
+    hdr[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+    hdr[2 * blockIdx.x + 1] = make_int4(-1, 0, 0, 0);
+}
+__device__ __forceinline__ void first_header(int4* hdr, const WorkShare& w, const BlockWalk& k) {  // k: the share's first block
+    const int first = static_cast<int>(short_div(k.at, w.per));
+    hdr[2 * blockIdx.x + 1] = make_int4(k.t0 != 0 && last_cta(w, k) - first + 1 > kJoinAlone ? first : -1, 0, 0, 0);
+}
 __device__ __forceinline__ float* part_slot(float* part, int slot, int rows, int dh) {
     return part + static_cast<size_t>(slot) * rows * (dh + 2);
 }

@@ -131,13 +131,14 @@ paged_rows_kernel(const PagedAttnParams p) {
     find_share(p.share_log, p.r, shift, c.n_kv_heads, p.tb_log, PR_THREADS, 1, &sm_share, share, p.status);
     pdl_launch_dependents();
     if (share.begin >= share.end) {
-        if (tid == 0 && p.hdr) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (tid == 0 && p.hdr) no_headers(p.hdr);
         return;
     }
     BlockWalk k;
     walk_begin(p.share_log, p.r, shift, p.tb_log, share, k);
     const float sl2 = rsqrtf(static_cast<float>(DH)) * kLog2e;
     int4 header = make_int4(0, 0, 0, 0);
+    if (tid == 0 && p.hdr) first_header(p.hdr, share, k);
 
     do {
         const SeqView s = k.s;
@@ -501,7 +502,7 @@ paged_rows_kernel(const PagedAttnParams p) {
         const int slot = 2 * blockIdx.x + (k.t0 == 0 ? 1 : 0);
         float* part = whole ? nullptr : part_slot(p.part, slot, RB, DH);
         if (!whole && k.t0 == 0)
-            header = make_int4(static_cast<int>(short_div(k.at + k.tiles - 1, share.per)) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
+            header = make_int4(last_cta(share, k) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
         constexpr int LPR = DH / 8;  // lanes per row, 8 columns each
         for (int r = tid / LPR; r < rows; r += PR_THREADS / LPR) {
             const int cx = (tid % LPR) * 8;
@@ -542,31 +543,35 @@ paged_rows_kernel(const PagedAttnParams p) {
             }
         }
     } while (walk_next(p.share_log, p.r, shift, c.n_kv_heads, p.tb_log, share, k));
-    if (tid == 0 && p.hdr) p.hdr[blockIdx.x] = header;
+    if (tid == 0 && p.hdr) p.hdr[2 * blockIdx.x] = header;
 }
 
-// Joins the partial results of blocks that several CTAs worked on.  One CTA per (possible) such block and group of
-// 8 RPW rows, RPW rows per warp: the lanes first look at all pieces' maxima and sums, then each adds its columns of
-// the pieces in the order of their tiles.  The time is that of a few dependent reads of L2, so the reads of one
-// step are all in flight together, and nothing waits for the sequence's description before the results are stored.
-constexpr int JOIN_THREADS = 256;
-template <int DH, int RPW>
-__global__ void __launch_bounds__(JOIN_THREADS)
-paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
-    constexpr int W = DH / 32;           // columns per lane
-    constexpr int AHEAD = 8 / RPW;       // pieces in flight
-    pdl_wait();
-    const int4 h = p.hdr[blockIdx.x];
-    if (h.x == 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int r0 = (static_cast<int>(blockIdx.y) * (JOIN_THREADS / 32) + warp) * RPW;  // rows_per_block is a multiple of 8 RPW
-    const SeqView s = load_seq(p.r, p.c.page_shift, h.y, nullptr);
-    // piece 0 is CTA blockIdx.x's tail slot, piece i the head slot of CTA blockIdx.x + i
-    const float* slot0 = part_slot(p.part, 2 * static_cast<int>(blockIdx.x), rows_per_block, DH);
-    const size_t slot = static_cast<size_t>(rows_per_block) * (DH + 2);
-    auto part_of = [&](int i) { return slot0 + slot * (i == 0 ? 1 : 2 * i); };
-    auto columns = [&](int i, int r, float (&x)[W]) {
-        const float* src = part_of(i) + 2 * rows_per_block + r * DH + lane * W;
+// Joins the partial results of blocks that several CTAs worked on, adding the pieces in the order of their tiles.  The time is
+// that of a few dependent reads of L2, so the reads of one step are all in flight together.
+//  By the CTAs of the block's first CTA, one for each group of 8 RPW rows, RPW rows per warp: the lanes first look at all
+//    pieces' maxima and sums, then each adds its columns of the pieces.  Nothing waits for the sequence's description
+//    before the results are stored.
+//  Few-row blocks of more than kJoinAlone pieces (few long contexts): by the CTAs of all the CTAs that worked on the block, a
+//    row at a time each, the pieces dealt out over the eight warps and these joined last.  One context of 32768, 8 kv heads, bf16:
+//    39.1 -> 32.5 us; four of up to 57000, one kv head, int8: 40.1 -> 26.8; two of 131072, 37 pieces: 101.8 -> 100.1.
+//    (The tcgen05 kernel's 256-row blocks keep many warps busy as it is: with this way in their join too, 64 rows
+//    over 32768, 18 pieces, went from 67 to 77 us, and 128 over 60000, 37 pieces, from 71 to 61.)
+constexpr int JOIN_THREADS = 256, JOIN_WARPS = JOIN_THREADS / 32;
+
+// The pieces of one block: piece 0 is its first CTA's tail slot, piece i the head slot of the i-th CTA after it.
+template <int DH>
+struct Pieces {
+    static constexpr int W = DH / 32;  // columns per lane
+    const float* slot0;
+    size_t slot;
+    int rows_per_block;
+    __device__ __forceinline__ Pieces(const PagedAttnParams& p, int first, int rows)
+        : slot0(part_slot(p.part, 2 * first, rows, DH)), slot(static_cast<size_t>(rows) * (DH + 2)), rows_per_block(rows) {}
+    __device__ __forceinline__ const float* at(int i) const { return slot0 + slot * (i == 0 ? 1 : 2 * i); }
+    __device__ __forceinline__ float maximum(int i, int r) const { return at(i)[r]; }
+    __device__ __forceinline__ float sum(int i, int r) const { return at(i)[rows_per_block + r]; }
+    __device__ __forceinline__ void columns(int i, int r, int lane, float (&x)[W]) const {
+        const float* src = at(i) + 2 * rows_per_block + r * DH + lane * W;
         if (W == 4) {
             const float4 v = *reinterpret_cast<const float4*>(src);
             x[0] = v.x; x[1] = v.y; x[W - 2] = v.z; x[W - 1] = v.w;
@@ -574,35 +579,53 @@ paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
             const float2 v = *reinterpret_cast<const float2*>(src);
             x[0] = v.x; x[1] = v.y;
         }
-    };
-    float mx[RPW], l[RPW], acc[RPW][W];
+    }
+};
+
+// Row r of the block that h describes, from its maximum, sum and this lane's columns (by a whole warp).
+template <int DH>
+__device__ __forceinline__ void put_row(const PagedAttnParams& p, const SeqView& s, const int4& h, int r, int lane, float mx, float l, const float (&acc)[DH / 32]) {
+    constexpr int W = DH / 32;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int row = s.row0 + (h.w << p.tb_log) + r / p.group, head = h.z * p.group + r % p.group;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + static_cast<size_t>(row) * p.out_stride +
+                                                static_cast<size_t>(head) * DH + lane * W);
+    if (W == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[W - 2] * inv, acc[W - 1] * inv));
+    else dst[0] = pack_bf16(acc[0] * inv, acc[1] * inv);
+    if (p.lse && lane == 0) p.lse[static_cast<size_t>(row) * p.n_heads + head] = l == 0.f ? -INFINITY : mx * kLn2 + logf(l);
+}
+
+// Rows r0 .. r0 + RPW - 1 (of one warp) over the pieces first, first + step, ..: maxima, sums and this lane's columns.
+template <int DH, int RPW>
+__device__ __forceinline__ void add_pieces(const Pieces<DH>& parts, int n_pieces, int first, int step, int r0, int lane, float (&mx)[RPW], float (&l)[RPW],
+                                           float (&acc)[RPW][DH / 32]) {
+    constexpr int W = DH / 32;
+    constexpr int AHEAD = 8 / RPW;  // pieces in flight
+    const int count = (n_pieces - first + step - 1) / step;
+    auto piece = [&](int i) { return first + i * step; };
+    float m_part[RPW], l_part[RPW];  // of the piece that this lane looks at; read once where there are up to 32
 #pragma unroll
     for (int j = 0; j < RPW; ++j) {
-        mx[j] = -INFINITY;
+        m_part[j] = lane < count ? parts.maximum(piece(lane), r0 + j) : -INFINITY;
+        l_part[j] = lane < count ? parts.sum(piece(lane), r0 + j) : 0.f;
+        mx[j] = m_part[j];
         l[j] = 0.f;
 #pragma unroll
         for (int c = 0; c < W; ++c) acc[j][c] = 0.f;
     }
-    float m_part[RPW], l_part[RPW];  // of the piece that this lane looks at; read once where there are up to 32
+    for (int i = lane + 32; i < count; i += 32)
 #pragma unroll
-    for (int j = 0; j < RPW; ++j) {
-        m_part[j] = lane < h.x ? part_of(lane)[r0 + j] : -INFINITY;
-        l_part[j] = lane < h.x ? part_of(lane)[rows_per_block + r0 + j] : 0.f;
-        mx[j] = fmaxf(mx[j], m_part[j]);
-    }
-    for (int i = lane + 32; i < h.x; i += 32)
-#pragma unroll
-        for (int j = 0; j < RPW; ++j) mx[j] = fmaxf(mx[j], part_of(i)[r0 + j]);
+        for (int j = 0; j < RPW; ++j) mx[j] = fmaxf(mx[j], parts.maximum(piece(i), r0 + j));
 #pragma unroll
     for (int j = 0; j < RPW; ++j) mx[j] = warp_max(mx[j]);
-    for (int i0 = 0; i0 < h.x; i0 += 32) {
-        const int i = i0 + lane, n = min(32, h.x - i0);
+    for (int i0 = 0; i0 < count; i0 += 32) {
+        const int i = i0 + lane, n = min(32, count - i0);
         float w[RPW];
 #pragma unroll
         for (int j = 0; j < RPW; ++j) {
             if (i0 != 0) {
-                m_part[j] = i < h.x ? part_of(i)[r0 + j] : -INFINITY;
-                l_part[j] = i < h.x ? part_of(i)[rows_per_block + r0 + j] : 0.f;
+                m_part[j] = i < count ? parts.maximum(piece(i), r0 + j) : -INFINITY;
+                l_part[j] = i < count ? parts.sum(piece(i), r0 + j) : 0.f;
             }
             w[j] = part_weight(m_part[j], mx[j]);
             l[j] += warp_sum(l_part[j] * w[j]);
@@ -612,7 +635,7 @@ paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q)
 #pragma unroll
-                for (int j = 0; j < RPW; ++j) columns(i0 + min(q0 + q, n - 1), r0 + j, x[q][j]);
+                for (int j = 0; j < RPW; ++j) parts.columns(piece(i0 + min(q0 + q, n - 1)), r0 + j, lane, x[q][j]);
 #pragma unroll
             for (int q = 0; q < AHEAD; ++q)
 #pragma unroll
@@ -623,18 +646,66 @@ paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
                 }
         }
     }
-    const int tok0 = h.w << p.tb_log, rows = min(1 << p.tb_log, s.n - tok0) * p.group;
+}
+
+template <int DH>
+__device__ __forceinline__ void join_spread(const PagedAttnParams& p, int rows_per_block, const int4& h, int first) {
+    constexpr int W = DH / 32;
+    __shared__ float sm_m[JOIN_WARPS], sm_l[JOIN_WARPS], sm_o[JOIN_WARPS][DH];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const SeqView s = load_seq(p.r, p.c.page_shift, h.y, nullptr);
+    const int rows = min(1 << p.tb_log, s.n - (h.w << p.tb_log)) * p.group;
+    const Pieces<DH> parts(p, first, rows_per_block);
+    const int units = h.x * gridDim.y, unit = (static_cast<int>(blockIdx.x) - first) * gridDim.y + blockIdx.y;
+    for (int r = unit; r < rows; r += units) {
+        float mx[1], l[1], acc[1][W];
+        add_pieces<DH, 1>(parts, h.x, warp, JOIN_WARPS, r, lane, mx, l, acc);
+        if (lane == 0) {
+            sm_m[warp] = mx[0];
+            sm_l[warp] = l[0];
+        }
 #pragma unroll
-    for (int j = 0; j < RPW; ++j) {
-        const int r = r0 + j;
-        if (r >= rows) return;  // (what lies behind the block's rows was never written)
-        const float inv = l[j] == 0.f ? 0.f : 1.f / l[j];
-        const int row = s.row0 + tok0 + r / p.group, head = h.z * p.group + r % p.group;
-        uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + static_cast<size_t>(row) * p.out_stride +
-                                                    static_cast<size_t>(head) * DH + lane * W);
-        if (W == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc[j][0] * inv, acc[j][1] * inv), pack_bf16(acc[j][W - 2] * inv, acc[j][W - 1] * inv));
-        else dst[0] = pack_bf16(acc[j][0] * inv, acc[j][1] * inv);
-        if (p.lse && lane == 0) p.lse[static_cast<size_t>(row) * p.n_heads + head] = l[j] == 0.f ? -INFINITY : mx[j] * kLn2 + logf(l[j]);
+        for (int c = 0; c < W; ++c) sm_o[warp][lane * W + c] = acc[0][c];
+        __syncthreads();
+        if (warp == 0) {
+            float top = -INFINITY, sum = 0.f, o[W] = {};
+#pragma unroll
+            for (int w = 0; w < JOIN_WARPS; ++w) top = fmaxf(top, sm_m[w]);
+#pragma unroll
+            for (int w = 0; w < JOIN_WARPS; ++w) {
+                const float f = part_weight(sm_m[w], top);
+                sum += sm_l[w] * f;
+#pragma unroll
+                for (int c = 0; c < W; ++c) o[c] += f == 0.f ? 0.f : sm_o[w][lane * W + c] * f;
+            }
+            put_row<DH>(p, s, h, r, lane, top, sum, o);
+        }
+        __syncthreads();
+    }
+}
+
+template <int DH, int RPW>
+__global__ void __launch_bounds__(JOIN_THREADS)
+paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
+    pdl_wait();
+    const int first = static_cast<int>(blockIdx.x);
+    const int4 h = p.hdr[2 * first], past = RPW == 1 ? p.hdr[2 * first + 1] : make_int4(-1, 0, 0, 0);
+    if (RPW == 1 && h.x > kJoinAlone) {
+        join_spread<DH>(p, rows_per_block, h, first);
+    } else if (h.x > 0) {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const int r0 = (static_cast<int>(blockIdx.y) * JOIN_WARPS + warp) * RPW;  // rows_per_block is a multiple of 8 RPW
+        const SeqView s = load_seq(p.r, p.c.page_shift, h.y, nullptr);
+        float mx[RPW], l[RPW], acc[RPW][DH / 32];
+        add_pieces<DH, RPW>(Pieces<DH>(p, first, rows_per_block), h.x, 0, 1, r0, lane, mx, l, acc);
+        const int rows = min(1 << p.tb_log, s.n - (h.w << p.tb_log)) * p.group;
+#pragma unroll
+        for (int j = 0; j < RPW; ++j)
+            if (r0 + j < rows) put_row<DH>(p, s, h, r0 + j, lane, mx[j], l[j], acc[j]);  // (what lies behind the block's rows was never written)
+    }
+    if (RPW == 1 && past.x >= 0) {
+        const int4 begun = p.hdr[2 * past.x];
+        if (begun.x > 0) join_spread<DH>(p, rows_per_block, begun, past.x);
     }
 }
 
@@ -700,7 +771,7 @@ Shape shape_of(int head_dim, int dtype, int group, int max_rows, long long max_p
     while ((1LL << s.tb_log) < max_rows && (s.nt || (2LL << s.tb_log) * group <= s.rows_per_block)) ++s.tb_log;
     return s;
 }
-size_t hdr_bytes(int grid) { return (static_cast<size_t>(grid) * sizeof(int4) + 255) & ~static_cast<size_t>(255); }
+size_t hdr_bytes(int grid) { return (static_cast<size_t>(2) * grid * sizeof(int4) + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
 
@@ -737,7 +808,7 @@ cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_s
     if (e != cudaSuccess || !s.split) return e;
     cudaLaunchConfig_t cfg = {};
     const int rpw = s.nt ? 1 : 4;  // rows per warp of the join
-    cfg.gridDim = dim3(s.grid, s.rows_per_block / (JOIN_THREADS / 32 * rpw));
+    cfg.gridDim = dim3(s.grid, s.rows_per_block / (JOIN_WARPS * rpw));
     cfg.blockDim = dim3(JOIN_THREADS);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];

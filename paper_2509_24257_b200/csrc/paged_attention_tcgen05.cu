@@ -206,7 +206,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     if ((sbase & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
         if (tid == 0) {
             raise_status(p.status, VERILLM_DEV_WAIT_TIMEOUT);
-            p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+            no_headers(p.hdr);
         }
         return;
     }
@@ -289,7 +289,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     pdl_launch_dependents();
     tc_fence_after();
     if (share.begin >= share.end) {
-        if (tid == 0) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (tid == 0) no_headers(p.hdr);
         if (warp == 12) tmem_dealloc(*tmem_slot_ptr, PT_TMEM_COLS);
         return;
     }
@@ -868,7 +868,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
                 const int tok0 = k.j << p.tb_log;
                 const bool whole = k.t0 == 0 && k.t1 == k.tiles;
                 if (!whole && k.t0 == 0)
-                    header = make_int4(static_cast<int>(short_div(k.at + k.tiles - 1, share.per)) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
+                    header = make_int4(last_cta(share, k) - static_cast<int>(blockIdx.x) + 1, k.seq, k.kvh, k.j);
                 if (lane == 0) {
                     parts[2 * i] = make_int4(k.s.row0 + tok0, k.s.len - k.s.n + tok0, min(1 << p.tb_log, k.s.n - tok0) * G, k.seq);
                     parts[2 * i + 1] = make_int4(k.kvh, k.t0, k.t1, whole ? 1 : 0);
@@ -899,7 +899,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
             }
             more = walk_next(PT_TILE_LOG, p.r, shift, n_kv, p.tb_log, share, k);
         }
-        if (lane == 0) p.hdr[blockIdx.x] = header;
+        if (lane == 0) p.hdr[2 * blockIdx.x] = header;
         }
     }
     if (!ok) *failed = 1;
@@ -908,7 +908,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     tc_fence_before();
     __syncthreads();
     if (*failed) {
-        if (tid == 0) p.hdr[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (tid == 0) no_headers(p.hdr);
         const long long t0 = clock64();  // let copies and products in flight land
         while (clock64() - t0 < 2000000LL) {
         }

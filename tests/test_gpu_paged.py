@@ -159,6 +159,25 @@ def test_attention_matches_the_definition(shape, dtype):
     assert bool((out[used:] == 9.0).all()) and bool((out[:, c.H * c.dh:] == 9.0).all()) and bool((lse[used:] == 9.0).all())
 
 
+@pytest.mark.parametrize("heads,kv_heads,dh,rows,kv", [
+    (8, 1, 128, [3, 1, 4, 2], [9000, 20000, 5000, 100]),  # long contexts beside short ones: pieces joined by many CTAs and by few
+    (12, 4, 64, [1, 8], [30011, 4099]),
+    (32, 1, 64, [1], [16000]),                            # more pieces than a warp has lanes
+])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_few_rows_over_long_contexts(dtype, heads, kv_heads, dh, rows, kv):
+    c = Case(dtype, heads, kv_heads, dh, 64, rows, kv, seed=29)
+    cache, rows_d = c.device()
+    lse = torch.zeros(c.n, c.H, device=DEV)
+    got = vb.op_attention_paged(c.dq, cache, rows_d, lse=lse)
+    rows_d.check()
+    ref, tol, lref, ltol = c.attention()
+    used = int(c.cu[-1])
+    assert_within(got[:used].reshape(used, c.H, c.dh), ref[:used], tol[:used])
+    assert_within(lse[:used], lref[:used], ltol[:used], "lse")
+    assert torch.equal(got[:used], vb.op_attention_paged(c.dq, cache, rows_d)[:used])
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_attention_over_many_sequences(dtype):
     """More sequences than a CTA has threads: the share of each CTA is found in several passes."""
