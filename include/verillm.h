@@ -356,12 +356,12 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  *  q         DEVICE bf16, n_heads * head_dim entries per row, q_stride entries from row to row, already rotated
  *  out       DEVICE bf16, same form with out_stride, not overlapping q; a row that attends to nothing receives zeros
  *  lse       optional DEVICE float32 [n_rows][n_heads]: log of the sum of exp(scores), -inf for such a row
- *  workspace DEVICE, 256-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code).
- *            May be NULL where that is 0.  It holds nothing between calls, but calls that may overlap (other streams, graphs replayed side by side)
- *            need one each.
- * Keys and values of 8-bit pools enter products in fp16, scaled to its range: rounded to 11 bits where the call has many
- * rows per sequence, exact where it has few.  Probabilities are rounded to bf16 (bf16 pools; 16 bits where the call has
- * few rows per sequence) or fp16; sums are fp32.
+ *  workspace DEVICE, 256-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code),
+ *            which suffice for smaller calls too.  May be NULL where that is 0.  It holds nothing between calls, but calls
+ *            that may overlap (other streams, graphs replayed side by side) need one each.
+ * Keys and values of 8-bit pools enter products in fp16, scaled to its range: rounded to 11 bits in large calls of many
+ * rows per sequence, exact in others.  Probabilities are rounded to bf16 (bf16 pools; 16 bits outside such calls) or fp16;
+ * sums are fp32.  The rounding and the order of the sums follow from the sizes of the call alone.
  * status also receives VERILLM_DEV_WAIT_TIMEOUT when a wait inside the kernel gave up; the results are then invalid.
  * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 128 per kv head; workspace too
  * small or not aligned), E_ARCH, E_CUDA. */

@@ -118,6 +118,7 @@ struct PagedAttnParams {
     int n_heads, group;
     int tb_log;   // tokens per block, log2
     int share_log;  // few-row kernel: positions per unit of a CTA's share, log2 (30: whole blocks)
+    int spread;     // tcgen05 kernel: blocks of many pieces are joined by all their CTAs
     int4* hdr;    // [grid][2]
     float* part;  // [2 grid][rows][head_dim + 2]
     int* status;
@@ -126,7 +127,7 @@ constexpr int kPagedMaxGroup = 128;  // query heads per kv head
 constexpr long long kPagedMaxPositions = 1LL << 26;  // table_width * page_size
 constexpr int kPagedTcRows = 256;    // packed rows per block of the tcgen05 kernel
 // Bytes of partial results and headers a launch needs; what the rule on sizes picks.
-size_t paged_attention_workspace(int head_dim, int dtype, int group, int max_rows, long long max_positions, int num_sms);
+size_t paged_attention_workspace(const PagedCacheDev& c, const PagedRowsDev& rows, int group, int num_sms);
 cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_sms, cudaStream_t stream);
 cudaError_t paged_attention_init();
 // The kernel for many rows per sequence (one CTA per SM: grid <= SMs); called by launch_paged_attention.

@@ -233,8 +233,8 @@ __device__ __forceinline__ bool walk_next(int tl, const PagedRowsDev& r, int pag
 
 // Partial results.  hdr[2 c]: {pieces, sequence, kv head, block} of the block whose first tiles CTA c holds and whose
 // last it does not (pieces 0: none).  Slot 2 c: the block that began before CTA c; slot 2 c + 1: hdr[2 c]'s block.
-// hdr[2 c + 1].x (few-row kernel): the CTA in which slot 2 c's block began, if it has more than kJoinAlone pieces and is joined
-// by the CTAs of all of them, else -1.
+// hdr[2 c + 1].x (where the join is spread): the CTA in which slot 2 c's block began, if it has more than kJoinAlone pieces and
+// is joined by the CTAs of all of them, else -1.
 // A slot holds `rows` maxima (log2 units, -inf: no key yet), `rows` sums, and `rows` x head_dim outputs.
 constexpr int kJoinAlone = 16;
 __device__ __forceinline__ int last_cta(const WorkShare& w, const BlockWalk& k) { return static_cast<int>(short_div(k.at + k.tiles - 1, w.per)); }

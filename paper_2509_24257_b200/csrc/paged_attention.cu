@@ -20,6 +20,8 @@
 // scales) are rounded to fp16 for the second product with 8-bit pools; with bf16 pools they enter it as the sum of two
 // bf16 numbers (16 significant bits), whose second product hides under the loads (114.4 -> 114.8 us for 64 contexts of
 // 2600 on average, and the error of the result falls from 2.3e-3 to the 1.7e-3 of its own rounding).  All else is fp32.
+#include <algorithm>
+
 #include "paged.cuh"
 
 namespace vl {
@@ -551,11 +553,12 @@ paged_rows_kernel(const PagedAttnParams p) {
 //  By the CTAs of the block's first CTA, one for each group of 8 RPW rows, RPW rows per warp: the lanes first look at all
 //    pieces' maxima and sums, then each adds its columns of the pieces.  Nothing waits for the sequence's description
 //    before the results are stored.
-//  Few-row blocks of more than kJoinAlone pieces (few long contexts): by the CTAs of all the CTAs that worked on the block, a
+//  Blocks of more than kJoinAlone pieces (few long contexts; SPREAD): by the CTAs of all the CTAs that worked on the block, a
 //    row at a time each, the pieces dealt out over the eight warps and these joined last.  One context of 32768, 8 kv heads, bf16:
 //    39.1 -> 32.5 us; four of up to 57000, one kv head, int8: 40.1 -> 26.8; two of 131072, 37 pieces: 101.8 -> 100.1.
-//    (The tcgen05 kernel's 256-row blocks keep many warps busy as it is: with this way in their join too, 64 rows
-//    over 32768, 18 pieces, went from 67 to 77 us, and 128 over 60000, 37 pieces, from 71 to 61.)
+//    The tcgen05 kernel's 256-row blocks keep many warps busy as it is; their join is spread where there are fewer than
+//    grid / kSpreadPieces of them (one block of 128 rows over 16000, 125 pieces: 58 -> 20 us; four over 60000, 37 pieces: 77 -> 67;
+//    but with 18 pieces, 64 rows over 32768, 67 would become 77).
 constexpr int JOIN_THREADS = 256, JOIN_WARPS = JOIN_THREADS / 32;
 
 // The pieces of one block: piece 0 is its first CTA's tail slot, piece i the head slot of the i-th CTA after it.
@@ -684,13 +687,13 @@ __device__ __forceinline__ void join_spread(const PagedAttnParams& p, int rows_p
     }
 }
 
-template <int DH, int RPW>
+template <int DH, int RPW, bool SPREAD>
 __global__ void __launch_bounds__(JOIN_THREADS)
 paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
     pdl_wait();
     const int first = static_cast<int>(blockIdx.x);
-    const int4 h = p.hdr[2 * first], past = RPW == 1 ? p.hdr[2 * first + 1] : make_int4(-1, 0, 0, 0);
-    if (RPW == 1 && h.x > kJoinAlone) {
+    const int4 h = p.hdr[2 * first], past = SPREAD ? p.hdr[2 * first + 1] : make_int4(-1, 0, 0, 0);
+    if (SPREAD && h.x > kJoinAlone) {
         join_spread<DH>(p, rows_per_block, h, first);
     } else if (h.x > 0) {
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -703,7 +706,7 @@ paged_join_kernel(const PagedAttnParams p, int rows_per_block) {
         for (int j = 0; j < RPW; ++j)
             if (r0 + j < rows) put_row<DH>(p, s, h, r0 + j, lane, mx[j], l[j], acc[j]);  // (what lies behind the block's rows was never written)
     }
-    if (RPW == 1 && past.x >= 0) {
+    if (SPREAD && past.x >= 0) {
         const int4 begun = p.hdr[2 * past.x];
         if (begun.x > 0) join_spread<DH>(p, rows_per_block, begun, past.x);
     }
@@ -747,41 +750,70 @@ cudaError_t rows_launch_dtype(const PagedAttnParams& p, int nt, int grid, cudaSt
     return rows_launch_nt<DH, VERILLM_KV_INT8>(p, nt, grid, stream);
 }
 
-// Which kernel and block shape serve a call.  The few-row kernel takes sequences of up to 24 (bf16) or 32 (8-bit) packed
-// rows, the tcgen05 kernel everything else.  Measured for 16 contexts of 4096, 8 kv heads of 128, few-row against
-// tcgen05: bf16 16 rows 61 / 69 us, 24 rows 69 / 70, 32 rows 118 / 70; int8 16 rows 57 / 91, 24 rows 61 / 91, 32 rows 80 / 91.
+// Which kernel and block shape serve a call.  The few-row kernel takes
+//  - sequences of up to 24 (bf16) or 32 (8-bit) packed rows, a block each.  Measured for 16 contexts of 4096, 8 kv heads of 128,
+//    few-row against tcgen05: bf16 16 rows 61 / 69 us, 24 rows 69 / 70, 32 rows 118 / 70; int8 16 rows 57 / 91, 24 rows
+//    61 / 91, 32 rows 80 / 91;
+//  - and calls so small that blocks of up to 16 rows give its CTAs one block, or two tiles, each: there the longer pipeline of the
+//    tcgen05 kernel counts, not its rate.  64 rows over 250 positions (8 kv heads of 128) bf16 13.0 / 16.0 us, e4m3 13.8 / 18.8; 16
+//    rows over 500 e4m3 14.1 / 16.8; 16 rows of 8 heads over 4000 (one kv head) e4m3 19.2 / 25.5.  With five tiles each
+//    instead of two: 64 rows over 1000 e4m3 25.5 / 22.6.
+// The tcgen05 kernel takes everything else.
 struct Shape {
     int nt;  // 8-row column blocks of the few-row kernel; 0: the tcgen05 kernel
     int tb_log, rows_per_block, grid;
-    bool split;  // blocks may be split over CTAs and joined
+    bool split;   // blocks may be split over CTAs and joined
+    bool spread;  // tcgen05 kernel: so few blocks that each has many pieces
 };
 // Sequences that cannot be longer than this are not split by the few-row kernel: a CTA's walk over so few tiles takes
 // no longer than the second launch and its reads (16 sequences of 500 positions: 10.2 us whole, 10.0
 // split and joined; of 250: 6.9 and 9.0).
 constexpr long long kWholePositions = 256;
-Shape shape_of(int head_dim, int dtype, int group, int max_rows, long long max_positions, int num_sms) {
+constexpr int kSmallBlockRows = 16;
+constexpr long long kSpreadPieces = 32;  // pieces per block from which the tcgen05 kernel's join is spread (see there)
+Shape shape_of(const PagedCacheDev& c, const PagedRowsDev& rows, int group, int num_sms) {
     Shape s;
-    const long long r = static_cast<long long>(group) * max_rows;
-    s.nt = r <= (dtype == VERILLM_KV_BF16 ? 24 : 32) ? static_cast<int>((r + 7) / 8) : 0;
+    const long long r = static_cast<long long>(group) * rows.max_rows, positions = static_cast<long long>(rows.table_width) << c.page_shift;
+    auto blocks = [&](int tb_log) {  // at most
+        const long long per_seq = (rows.max_rows + (1LL << tb_log) - 1) >> tb_log;
+        return c.n_kv_heads * std::min(rows.batch * per_seq, (static_cast<long long>(rows.n_rows) >> tb_log) + rows.batch);
+    };
+    s.tb_log = 0;  // tokens per block: a power of two
+    s.nt = 0;
+    if (r <= (c.dtype == VERILLM_KV_BF16 ? 24 : 32)) {
+        s.nt = static_cast<int>((r + 7) / 8);
+        while ((1LL << s.tb_log) < rows.max_rows) ++s.tb_log;  // all of a sequence's
+    } else if (group <= kSmallBlockRows) {
+        int tb_log = 0;
+        while ((2 << tb_log) * group <= kSmallBlockRows) ++tb_log;
+        const int nt = ((group << tb_log) + 7) / 8;
+        const long long ctas = static_cast<long long>(num_sms) * rows_ctas(c.head_dim, c.dtype, nt), n = blocks(tb_log);
+        if (positions <= kWholePositions ? n <= ctas : n * ((positions + PR_TILE - 1) / PR_TILE) <= 2 * ctas) {
+            s.nt = nt;
+            s.tb_log = tb_log;
+        }
+    }
     s.rows_per_block = s.nt ? 8 * s.nt : kPagedTcRows;
-    s.split = s.nt == 0 || max_positions > kWholePositions;
-    s.grid = num_sms * (s.nt == 0 ? 1 : rows_ctas(head_dim, dtype, s.nt));
-    // tokens per block: a power of two; the few-row kernel's single block holds them all
-    s.tb_log = 0;
-    while ((1LL << s.tb_log) < max_rows && (s.nt || (2LL << s.tb_log) * group <= s.rows_per_block)) ++s.tb_log;
+    s.grid = num_sms * (s.nt ? rows_ctas(c.head_dim, c.dtype, s.nt) : 1);
+    if (s.nt == 0)
+        while ((1LL << s.tb_log) < rows.max_rows && (2LL << s.tb_log) * group <= s.rows_per_block) ++s.tb_log;
+    s.split = s.nt == 0 || positions > kWholePositions;
+    s.spread = s.nt == 0 && blocks(s.tb_log) * kSpreadPieces < s.grid;
     return s;
 }
 size_t hdr_bytes(int grid) { return (static_cast<size_t>(2) * grid * sizeof(int4) + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
 
-size_t paged_attention_workspace(int head_dim, int dtype, int group, int max_rows, long long max_positions, int num_sms) {
+size_t paged_attention_workspace(const PagedCacheDev& c, const PagedRowsDev& rows, int group, int num_sms) {
     size_t need = 0;  // that of calls with fewer rows too: the shapes' needs are not quite in their order
-    for (int r = 1;; r = r < 32 && r + 1 < max_rows ? r + 1 : max_rows) {
-        const Shape s = shape_of(head_dim, dtype, group, r < max_rows ? r : max_rows, max_positions, num_sms);
-        const size_t bytes = hdr_bytes(s.grid) + static_cast<size_t>(2) * s.grid * s.rows_per_block * (head_dim + 2) * sizeof(float);
+    PagedRowsDev fewer = rows;
+    for (int r = 1;; r = r < 32 && r + 1 < rows.max_rows ? r + 1 : rows.max_rows) {
+        fewer.max_rows = std::min(r, rows.max_rows);
+        const Shape s = shape_of(c, fewer, group, num_sms);
+        const size_t bytes = hdr_bytes(s.grid) + static_cast<size_t>(2) * s.grid * s.rows_per_block * (c.head_dim + 2) * sizeof(float);
         if (s.split && bytes > need) need = bytes;
-        if (r >= max_rows || s.nt == 0) return need;  // (the tcgen05 kernel needs the most)
+        if (r >= rows.max_rows || s.nt == 0) return need;  // (the tcgen05 kernel needs the most)
     }
 }
 
@@ -797,8 +829,9 @@ cudaError_t paged_attention_init() {
 }
 
 cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_sms, cudaStream_t stream) {
-    const Shape s = shape_of(p.c.head_dim, p.c.dtype, p.group, p.r.max_rows, static_cast<long long>(p.r.table_width) << p.c.page_shift, num_sms);
+    const Shape s = shape_of(p.c, p.r, p.group, num_sms);
     p.tb_log = s.tb_log;
+    p.spread = s.spread ? 1 : 0;
     p.share_log = s.split ? PR_TILE_LOG : 30;
     p.hdr = s.split ? reinterpret_cast<int4*>(workspace) : nullptr;
     p.part = s.split ? reinterpret_cast<float*>(static_cast<char*>(workspace) + hdr_bytes(s.grid)) : nullptr;
@@ -816,11 +849,11 @@ cudaError_t launch_paged_attention(PagedAttnParams p, void* workspace, int num_s
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (rpw == 1)
-        return p.c.head_dim == 64 ? cudaLaunchKernelEx(&cfg, paged_join_kernel<64, 1>, p, s.rows_per_block)
-                                  : cudaLaunchKernelEx(&cfg, paged_join_kernel<128, 1>, p, s.rows_per_block);
-    return p.c.head_dim == 64 ? cudaLaunchKernelEx(&cfg, paged_join_kernel<64, 4>, p, s.rows_per_block)
-                              : cudaLaunchKernelEx(&cfg, paged_join_kernel<128, 4>, p, s.rows_per_block);
+    const bool narrow = p.c.head_dim == 64;
+    void (*join)(PagedAttnParams, int) = s.nt ? (narrow ? paged_join_kernel<64, 1, true> : paged_join_kernel<128, 1, true>)
+                                         : s.spread ? (narrow ? paged_join_kernel<64, 4, true> : paged_join_kernel<128, 4, true>)
+                                                    : (narrow ? paged_join_kernel<64, 4, false> : paged_join_kernel<128, 4, false>);
+    return cudaLaunchKernelEx(&cfg, join, p, s.rows_per_block);
 }
 
 }  // namespace vl

@@ -860,6 +860,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
         BlockWalk k;
         walk_begin(PT_TILE_LOG, p.r, shift, p.tb_log, share, k);
         int4 header = make_int4(0, 0, 0, 0);
+        if (p.spread && lane == 0) first_header(p.hdr, share, k);
         bool more = true;
         for (int n = 0; ok; ++n) {
             const int i = n % PT_PARTS;

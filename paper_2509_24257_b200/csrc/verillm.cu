@@ -439,8 +439,15 @@ int ensure_paged_decode(verillm_model* m) {
         CU_TRY(cudaMemcpy(d.iota, iota.data(), sizeof(int) * c.max_batch, cudaMemcpyHostToDevice));
         // a decode step has one row per sequence; the largest need over the pool types and lengths
         size_t need = 256;
-        for (int t = 0; t < 3; ++t)
-            need = std::max(need, paged_attention_workspace(c.head_dim, t, c.n_heads / c.n_kv_heads, 1, kPagedMaxPositions, m->num_sms));
+        PagedCacheDev cd = {};
+        cd.page_shift = 4;
+        cd.n_kv_heads = c.n_kv_heads;
+        cd.head_dim = c.head_dim;
+        PagedRowsDev rd = {};
+        rd.table_width = static_cast<int>(kPagedMaxPositions / kDecodePage);
+        rd.batch = rd.n_rows = c.max_batch;
+        rd.max_rows = 1;
+        for (cd.dtype = 0; cd.dtype < 3; ++cd.dtype) need = std::max(need, paged_attention_workspace(cd, rd, c.n_heads / c.n_kv_heads, m->num_sms));
         unsigned char* ws = nullptr;
         if ((rc = dev_alloc(&ws, need))) return rc;
         d.attn_ws = ws;
@@ -1262,7 +1269,7 @@ int64_t verillm_op_attention_paged_workspace(const verillm_kv_cache* cache, cons
     PagedRowsDev r;
     int rc = check_paged(cache, rows, &c, &r), sms = 0;
     if (rc || (rc = check_group(cache, n_heads)) || (rc = current_sms(&sms))) return rc;
-    return static_cast<int64_t>(paged_attention_workspace(c.head_dim, c.dtype, n_heads / c.n_kv_heads, r.max_rows, static_cast<long long>(r.table_width) << c.page_shift, sms));
+    return static_cast<int64_t>(paged_attention_workspace(c, r, n_heads / c.n_kv_heads, sms));
 }
 
 int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_rows* rows, const void* q, int64_t q_stride,
@@ -1277,8 +1284,7 @@ int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_r
     if (q == out) return VERILLM_E_INVAL;
     if ((rc = current_sms(&sms))) return rc;
     p.group = n_heads / p.c.n_kv_heads;
-    const int64_t need = static_cast<int64_t>(paged_attention_workspace(p.c.head_dim, p.c.dtype, p.group, p.r.max_rows,
-                                                                        static_cast<long long>(p.r.table_width) << p.c.page_shift, sms));
+    const int64_t need = static_cast<int64_t>(paged_attention_workspace(p.c, p.r, p.group, sms));
     if (need > 0 && !workspace) return VERILLM_E_INVAL;
     if (need > 0 && ((reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < need)) return VERILLM_E_SHAPE;
     if ((rc = ensure_init())) return rc;

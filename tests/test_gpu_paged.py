@@ -581,3 +581,108 @@ def test_two_calls_at_once_and_replayed_chunks():
             for call, w in zip(calls, want):
                 call[1].check()
                 assert torch.equal(call[4], w)
+
+
+# --------------------------------------------------------------------------- edge cases inside large calls
+
+
+class LargeCase(Case):
+    """The sequences of a test followed by so many others that the kernel for many rows takes the call."""
+
+    def __init__(self, dtype, rows, kv, seed, dh=128):
+        super().__init__(dtype, 8, 2, dh, 16, list(rows) + [20] * 150, list(kv) + [40] * 150, seed=seed)
+
+    def device(self):
+        cache, rows = super().device()
+        sms = torch.cuda.get_device_properties(0).multi_processor_count
+        assert vb.attention_paged_workspace(cache, rows, self.n, 8) >= 2 * sms * 256 * (self.dh + 2) * 4
+        return cache, rows
+
+    def verify(self):
+        cache, rows = self.device()
+        lse = torch.zeros(self.n, self.H, device=DEV)
+        got = vb.op_attention_paged(self.dq, cache, rows, lse=lse)
+        rows.check()
+        ref, tol, lref, ltol = self.attention()
+        used = int(self.cu[-1])
+        assert_within(got[:used].reshape(used, self.H, self.dh), ref[:used], tol[:used], "out")
+        assert_within(lse[:used], lref[:used], ltol[:used], "lse")
+        return ref[:used]
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_call_lengths(dtype, dh):
+    LargeCase(dtype, [20, 3, 0, 1, 40, 65, 64, 7], [12, 0, 20, 1, 40, 129, 300, 7], seed=30, dh=dh).verify()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_call_non_finite_entries(dtype):
+    c = LargeCase(dtype, [6, 40], [100, 40], seed=31)
+    k, v = (t.float() if dtype == BF16 else t.float() * s[..., None] for t, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    place = lambda b, p: (int(c.table[b, p // c.ps]), p % c.ps)  # noqa: E731
+    (pg, off), (pg1, off1), (pg2, off2) = place(0, 99), place(1, 38), place(1, 39)
+    v[pg, 0, off, 5] = float("nan")
+    v[pg1, 1, off1, 100] = float("inf")
+    k[pg2, 0, off2, 0] = float("nan")
+    c.set_pools(k.to(BF16), v.to(BF16))
+    ref = c.verify()
+    assert not bool(ref.isfinite().all()) and bool(ref.isfinite().any())
+
+
+@pytest.mark.parametrize("q_size,k_size", [(0.0, 1e-6), (0.0, 0.0), (1e-30, 1e-3), (1e25, 1e-25)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_call_very_small_and_large_queries_and_keys(dtype, q_size, k_size):
+    c = LargeCase(dtype, [6, 40], [300, 140], seed=32)
+    k, v = (t.float() if dtype == BF16 else t.float() * s[..., None] for t, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    c.set_pools((k.nan_to_num(0.0) * k_size).to(BF16), v.to(BF16))
+    c.q.copy_(c.q.float() * q_size)
+    c.verify()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_call_large_scores_and_a_late_maximum(dtype):
+    c = LargeCase(dtype, [2, 20], [700, 400], seed=33)
+    k, v = (t.float() if dtype == BF16 else t.float() * s[..., None] for t, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    for b in range(2):
+        for p in range(c.kv[b]):
+            k[int(c.table[b, p // 16]), :, p % 16] *= 0.02 * p
+    c.set_pools(k.to(BF16), v.to(BF16))
+    c.verify()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_large_call_problems_only_the_device_sees(dtype):
+    c = LargeCase(dtype, [50, 50], [64, 64], seed=34)
+    cache, r = c.device()
+    out = torch.zeros(c.n, 8 * 128, dtype=BF16, device=DEV)
+    ref, tol, _, _ = c.attention()
+    good = r.page_table.clone()
+    for bad in (cache.n_pages, -1, 1 << 30):
+        r.page_table[1, 3] = bad
+        r.status.zero_()
+        vb.op_attention_paged(c.dq, cache, r, out=out)
+        assert int(r.status.item()) == vb.DEV_PAGE_RANGE
+        assert_within(out[:50].reshape(50, 8, 128), ref[:50], tol[:50])
+        assert_within(out[100:c.n - 3].reshape(-1, 8, 128), ref[100:c.n - 3], tol[100:c.n - 3])
+    r.page_table.copy_(good)
+    r.page_table.clamp_(0, cache.n_pages - 1)
+    for length in (-3, 1 << 30):
+        r.kv_len[1] = length
+        r.status.zero_()
+        vb.op_attention_paged(c.dq, cache, r, out=out)
+        assert int(r.status.item()) == vb.DEV_ROWS_RANGE
+        assert_within(out[:50].reshape(50, 8, 128), ref[:50], tol[:50])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_one_block_of_many_rows_over_a_long_context(dtype):
+    """A single block whose tiles lie in most CTAs, and one beside a short sequence: the spread join of large blocks."""
+    for rows, kv in (([16], [16000]), ([30, 1, 7], [9001, 3, 500])):
+        c = Case(dtype, 8, 1, 128, 64, rows, kv, seed=35)
+        cache, r = c.device()
+        got = vb.op_attention_paged(c.dq, cache, r)
+        r.check()
+        ref, tol, _, _ = c.attention()
+        used = int(c.cu[-1])
+        assert_within(got[:used].reshape(used, c.H, c.dh), ref[:used], tol[:used])
