@@ -8,7 +8,7 @@
 // very different lengths and splits a single long sequence over the whole GPU.  A block whose tiles lie in
 // several CTAs leaves fp32 partial results (maximum, sum, unnormalised output), at most one block that began
 // in an earlier CTA ("head" slot) and one that continues in the next ("tail" slot) per CTA; a second kernel joins
-// them in the order of the tiles, so that results do not depend on timing.
+// them in an order that the sizes fix, so that results do not depend on timing.
 #pragma once
 
 #include <cuda_fp16.h>
