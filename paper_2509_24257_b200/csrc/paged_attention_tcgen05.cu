@@ -27,6 +27,10 @@
 // probabilities instead cost the softmax two shared-memory reads and two products per four entries, which it had to wait
 // for: 744 - 840 us for 1024 rows over 32768 positions.)
 //
+// Measured: 512 rows of each of 8 sequences over 4096 positions, 32 query heads on 8 of 128, bf16: 229 us = 986 TFLOP/s at full clock;
+// 1024 rows over 32768, e4m3: 537 us = 1007 TFLOP/s, 570 - 580 at the power limit.  A step of both groups takes 3100 - 3200 cycles; the
+// tensor pipe, the exp2 unit and shared memory need about 2048 of them each.
+//
 // Masked entries: scores are replaced by -inf.  Values behind the sequence's last position are whatever the page
 // holds and become 0.  An infinite or NaN value (or value scale) in a tile that some rows may not see entirely is
 // taken out of the product and put into the results of the rows that see it at the end ("stray").
