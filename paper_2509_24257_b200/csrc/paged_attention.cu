@@ -770,10 +770,12 @@ struct Shape {
     bool split;   // blocks may be split over CTAs and joined
     bool spread;  // tcgen05 kernel: so few blocks that each has many pieces
 };
-// Sequences that cannot be longer than this are not split by the few-row kernel: a CTA's walk over so few tiles takes
-// no longer than the second launch and its reads (16 sequences of 500 positions: 10.2 us whole, 10.0
-// split and joined; of 250: 6.9 and 9.0).
-constexpr long long kWholePositions = 256;
+// Sequences that cannot be longer than this are not split by the few-row kernel: no second launch, no workspace.  A call from
+// a program's loop falls from 20.5 to 15.6 us (one sequence of 500); the kernels' own time is about even (32 query heads on 8
+// of 128, one row, 500 positions, whole / split and joined: one sequence bf16 11.9 / 8.8 us, 16 bf16 13.5 / 15.6, 64 e4m3
+// 22.1 / 29.9; 16 of 250 positions 6.9 / 9.0).
+constexpr long long kWholePositions = 512;
+constexpr long long kWholeSmallBlocks = 256;  // the same for the small calls of many rows (16 rows over 500: 15.0 / 12.9 us)
 constexpr int kSmallBlockRows = 16;
 constexpr long long kSpreadPieces = 32;  // pieces per block from which the tcgen05 kernel's join is spread (see there)
 Shape shape_of(const PagedCacheDev& c, const PagedRowsDev& rows, int group, int num_sms) {
@@ -783,6 +785,7 @@ Shape shape_of(const PagedCacheDev& c, const PagedRowsDev& rows, int group, int 
         const long long per_seq = (rows.max_rows + (1LL << tb_log) - 1) >> tb_log;
         return c.n_kv_heads * std::min(rows.batch * per_seq, (static_cast<long long>(rows.n_rows) >> tb_log) + rows.batch);
     };
+    long long whole = kWholePositions;
     s.tb_log = 0;  // tokens per block: a power of two
     s.nt = 0;
     if (r <= (c.dtype == VERILLM_KV_BF16 ? 24 : 32)) {
@@ -793,16 +796,17 @@ Shape shape_of(const PagedCacheDev& c, const PagedRowsDev& rows, int group, int 
         while ((2 << tb_log) * group <= kSmallBlockRows) ++tb_log;
         const int nt = ((group << tb_log) + 7) / 8;
         const long long ctas = static_cast<long long>(num_sms) * rows_ctas(c.head_dim, c.dtype, nt), n = blocks(tb_log);
-        if (positions <= kWholePositions ? n <= ctas : n * ((positions + PR_TILE - 1) / PR_TILE) <= 2 * ctas) {
+        if (positions <= kWholeSmallBlocks ? n <= ctas : n * ((positions + PR_TILE - 1) / PR_TILE) <= 2 * ctas) {
             s.nt = nt;
             s.tb_log = tb_log;
+            whole = kWholeSmallBlocks;
         }
     }
     s.rows_per_block = s.nt ? 8 * s.nt : kPagedTcRows;
     s.grid = num_sms * (s.nt ? rows_ctas(c.head_dim, c.dtype, s.nt) : 1);
     if (s.nt == 0)
         while ((1LL << s.tb_log) < rows.max_rows && (2LL << s.tb_log) * group <= s.rows_per_block) ++s.tb_log;
-    s.split = s.nt == 0 || positions > kWholePositions;
+    s.split = s.nt == 0 || positions > whole;
     s.spread = s.nt == 0 && blocks(s.tb_log) * kSpreadPieces < s.grid;
     return s;
 }
