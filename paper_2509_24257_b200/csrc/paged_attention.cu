@@ -21,7 +21,7 @@
 // bf16 numbers (16 significant bits), whose second product hides under the loads (114.4 -> 114.8 us for 64 contexts of
 // 2600 on average, and the error of the result falls from 2.3e-3 to the 1.7e-3 of its own rounding).  All else is fp32.
 //
-// Measured, join included: one row of each of 64 contexts of up to 4096, 32 query heads on 8 of 128, bf16: 114 us = 6.05 TB/s, 94 %
+// Measured, join included: one row of each of 64 contexts of up to 4096, 32 query heads on 8 of 128, bf16: 115 us = 6.0 TB/s, 93 %
 // of a copy's rate; two contexts of 131072, 64 query heads, e4m3: 99.5 us = 5.3 TB/s; five drafted rows of 16 contexts of up to
 // 8192, int8: 70 us = 2.7 TB/s, where 24 rows of output and the keys and values in flight take 255 registers and eight
 // warps per SM wait for their own instructions.
@@ -373,10 +373,12 @@ paged_rows_kernel(const PagedAttnParams p) {
                         if (key0 + 2 * t + (e & 1) + 8 * (e >> 1) >= end) v[i][e] = make_uint4(0u, 0u, 0u, 0u);
             }
             // An infinite or NaN value must not reach the rows that may not see its token (their probability 0 times it
-            // would be NaN): such entries are taken out of the product and added row by row.  8-bit pools carry a
-            // non-finite vector in its scale, which is masked with the probability.
+            // would be NaN), nor meet the remainder of a probability, which may be 0 or negative: such entries are taken out of
+            // the product and added row by row.  8-bit pools carry a non-finite vector in its scale, which is masked with
+            // the probability.  (Looking costs 114.4 -> 115.2 us for 64
+            // contexts of up to 4096.)
             bool stray = false;
-            if (L::BF16 && masked) {
+            if (L::BF16) {
                 bool bad = false;
 #pragma unroll
                 for (int i = 0; i < L::VPIECES; ++i)

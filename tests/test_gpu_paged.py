@@ -686,3 +686,20 @@ def test_one_block_of_many_rows_over_a_long_context(dtype):
         ref, tol, _, _ = c.attention()
         used = int(c.cu[-1])
         assert_within(got[:used].reshape(used, c.H, c.dh), ref[:used], tol[:used])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_non_finite_entries_of_joined_contexts(dtype):
+    """Contexts whose pieces are joined, by few CTAs and by many: a NaN key early on, an infinite value among the last."""
+    c = Case(dtype, 8, 2, 128, 16, [1, 3, 2], [3000, 9000, 700], seed=36)
+    k, v = (t.float() if dtype == BF16 else t.float() * s[..., None] for t, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+    for t, b, p, head, value in ((k, 0, 130, 0, float("nan")), (v, 0, 2000, 1, float("inf")), (v, 1, 8998, 0, -float("inf")), (k, 2, 699, 1, float("nan"))):
+        t[int(c.table[b, p // c.ps]), head, p % c.ps, 7] = value
+    c.set_pools(k.to(BF16), v.to(BF16))
+    cache, rows = c.device()
+    got = vb.op_attention_paged(c.dq, cache, rows)
+    rows.check()
+    ref, tol, _, _ = c.attention()
+    used = int(c.cu[-1])
+    assert not bool(ref[:used].isfinite().all()) and bool(ref[:used].isfinite().any())
+    assert_within(got[:used].reshape(used, c.H, c.dh), ref[:used], tol[:used])
