@@ -359,6 +359,8 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  *  workspace DEVICE, 256-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code),
  *            which suffice for smaller calls too.  May be NULL where that is 0.  It holds nothing between calls, but calls
  *            that may overlap (other streams, graphs replayed side by side) need one each.
+ * A cached value that is not finite reaches every row that may see it, however small its weight, and no other: NaN as NaN, an
+ * infinite bf16 value as infinity (in large calls of many rows as NaN where its weight is below 2^-126 of the largest).
  * Keys and values of 8-bit pools enter products in fp16, scaled to its range: rounded to 11 bits in large calls of many
  * rows per sequence, exact in others.  Probabilities are rounded to bf16 (bf16 pools; 16 bits outside such calls) or fp16;
  * sums are fp32.  The rounding and the order of the sums follow from the sizes of the call alone.

@@ -257,6 +257,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 // weight of a partial result with maximum m in one with maximum mx >= m (both may be -inf: nothing to weigh)
 __device__ __forceinline__ float part_weight(float m, float mx) { return m == -INFINITY ? 0.f : exp2_fast(m - mx); }
+// A piece's output times its weight.  An infinite one stays infinite where the weight underflowed to 0, as a NaN does: how the keys
+// were divided into pieces must not decide what is lost.
+__device__ __forceinline__ float weighted(float x, float w) { return w == 0.f && isinf(x) ? x : x * w; }
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);

@@ -110,6 +110,33 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[8], const char* p) {
                  : "l"(p));
 }
 
+// Adds the infinite and NaN values among a warp's keys to the outputs [row][head_dim] (in shared memory, stride ld) of the rows that
+// may see them.
+template <int DH>
+__device__ __forceinline__ void add_stray(const PagedAttnParams& p, const BlockWalk& k, int warp, int lane, int rows, int first_pos, int end, float* out, int ld) {
+    const int shift = p.c.page_shift;
+    __syncwarp();  // the lanes wrote other columns than the ones they look at here
+#pragma unroll 1
+    for (int tile = k.t0; tile < k.t1; ++tile) {
+        const int key0 = tile * PR_TILE + warp * 16;
+        if (key0 >= end) break;
+        const int page = load_page(p.r, shift, p.c.n_pages, k.seq, key0, nullptr);
+        const size_t vec = ((static_cast<size_t>(page) * p.c.n_kv_heads + k.kvh) << shift) + (key0 & ((1 << shift) - 1));
+#pragma unroll 1
+        for (int i = 0; i < 16 && key0 + i < end; ++i) {
+            const unsigned short* v = reinterpret_cast<const unsigned short*>(p.c.v) + (vec + i) * DH;
+#pragma unroll 1
+            for (int col = lane; col < DH; col += 32) {
+                const float x = bf16_bits_to_float(__ldg(v + col));
+                if (isfinite(x)) continue;
+#pragma unroll 1
+                for (int r = 0; r < rows; ++r)
+                    if (key0 + i <= first_pos + r / p.group) out[r * ld + col] += x;
+            }
+        }
+    }
+}
+
 // CTAs per SM, all resident at once: what the registers allow (65536 / 128 threads / CTAs).
 __host__ __device__ constexpr int rows_ctas(int dh, int dtype, int nt) {
     if (dh == 64) return nt <= 2 ? 4 : 2;
@@ -252,6 +279,7 @@ paged_rows_kernel(const PagedAttnParams p) {
             for (int i = 0; i < L::ROW_BYTES; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + i));
         };
         int tile = k.t0;
+        bool stray = false;  // bf16 pools: some value of this warp's was not finite
         size_t vec = 0, vec_next = 0;
         int page2 = 0;
         {
@@ -373,42 +401,24 @@ paged_rows_kernel(const PagedAttnParams p) {
                         if (key0 + 2 * t + (e & 1) + 8 * (e >> 1) >= end) v[i][e] = make_uint4(0u, 0u, 0u, 0u);
             }
             // An infinite or NaN value must not reach the rows that may not see its token (their probability 0 times it
-            // would be NaN), nor meet the remainder of a probability, which may be 0 or negative: such entries are taken out of
-            // the product and added row by row.  8-bit pools carry a non-finite vector in its scale, which is masked with
-            // the probability.  (Looking costs 114.4 -> 115.2 us for 64
-            // contexts of up to 4096.)
-            bool stray = false;
+            // would be NaN), nor meet the remainder of a probability, which may be 0 or negative, nor a probability or factor
+            // that underflowed: such entries are taken out of the product here and put into the results at the end, row by row.
+            // 8-bit pools carry a non-finite vector in its scale, which is masked with the probability and stays NaN
+            // in every product.  (Looking costs 114.4 -> 115.2 us for 64 contexts of up to 4096.)
             if (L::BF16) {
                 bool bad = false;
 #pragma unroll
                 for (int i = 0; i < L::VPIECES; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) bad |= not_finite8(v[i][e]);
-                stray = __any_sync(0xFFFFFFFFu, bad);
-            }
-            auto add_stray = [&](int nt, const float (&e)[4]) {
-#pragma unroll 1
-                for (int kk = 0; kk < 16; ++kk) {
-                    const int src = ((kk & 7) << 2) | t;
-                    const float e0 = __shfl_sync(0xFFFFFFFFu, kk < 8 ? e[0] : e[2], src), e1 = __shfl_sync(0xFFFFFFFFu, kk < 8 ? e[1] : e[3], src);
-                    if (key0 + kk >= end) continue;  // uniform
-                    const char* base = reinterpret_cast<const char*>(c.v) + (vec + kk) * L::ROW_BYTES + g * 16;
+                if (__any_sync(0xFFFFFFFFu, bad)) {
+                    stray = true;
 #pragma unroll
-                    for (int i = 0; i < L::VPIECES; ++i) {
-                        const uint4 x = __ldg(reinterpret_cast<const uint4*>(base + i * 128));
-                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    for (int i = 0; i < L::VPIECES; ++i)
 #pragma unroll
-                        for (int m = 0; m < 4; ++m)
-#pragma unroll
-                            for (int half = 0; half < 2; ++half) {
-                                const float y = half ? bf16_hi(w[m]) : bf16_lo(w[m]);
-                                if (isfinite(y)) continue;
-                                if (key0 + kk <= pos[nt][0]) o[nt][(4 * i + m) % L::MT][2 * half] += e0 * y;
-                                if (key0 + kk <= pos[nt][1]) o[nt][(4 * i + m) % L::MT][2 * half + 1] += e1 * y;
-                            }
-                    }
+                        for (int e = 0; e < 4; ++e) v[i][e] = finite8(v[i][e]);
                 }
-            };
+            }
             uint32_t pb[NT][2], pl[NT][2];  // probabilities for the product; bf16: their roundings' remainders too
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -427,8 +437,6 @@ paged_rows_kernel(const PagedAttnParams p) {
                         e[h] = masked && key0 + g > pos[nt][h] ? 0.f : e[h] * w0;
                         e[2 + h] = masked && key0 + 8 + g > pos[nt][h] ? 0.f : e[2 + h] * w1;
                     }
-                } else if (stray) {
-                    add_stray(nt, e);
                 }
                 const uint32_t p0 = L::BF16 ? pack_bf16(e[0], e[1]) : pack_half(e[0], e[1]), p1 = L::BF16 ? pack_bf16(e[2], e[3]) : pack_half(e[2], e[3]);
                 pb[nt][0] = transpose8(p0);
@@ -437,12 +445,6 @@ paged_rows_kernel(const PagedAttnParams p) {
                     pl[nt][0] = transpose8(pack_bf16(e[0] - bf16_lo(p0), e[1] - bf16_hi(p0)));
                     pl[nt][1] = transpose8(pack_bf16(e[2] - bf16_lo(p1), e[3] - bf16_hi(p1)));
                 }
-            }
-            if (L::BF16 && stray) {
-#pragma unroll
-                for (int i = 0; i < L::VPIECES; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[i][e] = finite8(v[i][e]);
             }
             // ---- O^T += V^T P^T
 #pragma unroll
@@ -503,8 +505,9 @@ paged_rows_kernel(const PagedAttnParams p) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
                     *reinterpret_cast<float2*>(sm_o + (warp * RB + 8 * nt + 2 * t + h) * OLD + L::col(i, g)) =
-                        f[h] == 0.f ? make_float2(0.f, 0.f) : make_float2(o[nt][i][h] * f[h], o[nt][i][2 + h] * f[h]);
+                        make_float2(o[nt][i][h] * f[h], o[nt][i][2 + h] * f[h]);
         }
+        if (L::BF16 && stray) add_stray<DH>(p, k, warp, lane, rows, first_pos, end, sm_o + warp * RB * OLD, OLD);
         __syncthreads();
 
         const bool whole = !p.hdr || (k.t0 == 0 && k.t1 == k.tiles);
@@ -650,9 +653,10 @@ __device__ __forceinline__ void add_pieces(const Pieces<DH>& parts, int n_pieces
             for (int q = 0; q < AHEAD; ++q)
 #pragma unroll
                 for (int j = 0; j < RPW; ++j) {
-                    const float wq = q0 + q < n ? __shfl_sync(0xFFFFFFFFu, w[j], q0 + q) : 0.f;  // (q0 + q is uniform)
+                    const bool one = q0 + q < n;  // uniform; else a repeated read of the last piece
+                    const float wq = one ? __shfl_sync(0xFFFFFFFFu, w[j], q0 + q) : 0.f;
 #pragma unroll
-                    for (int c = 0; c < W; ++c) acc[j][c] += wq == 0.f ? 0.f : x[q][j][c] * wq;
+                    for (int c = 0; c < W; ++c) acc[j][c] += one ? weighted(x[q][j][c], wq) : 0.f;
                 }
         }
     }
@@ -686,7 +690,7 @@ __device__ __forceinline__ void join_spread(const PagedAttnParams& p, int rows_p
                 const float f = part_weight(sm_m[w], top);
                 sum += sm_l[w] * f;
 #pragma unroll
-                for (int c = 0; c < W; ++c) o[c] += f == 0.f ? 0.f : sm_o[w][lane * W + c] * f;
+                for (int c = 0; c < W; ++c) o[c] += weighted(sm_o[w][lane * W + c], f);
             }
             put_row<DH>(p, s, h, r, lane, top, sum, o);
         }
