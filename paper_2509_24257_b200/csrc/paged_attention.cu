@@ -776,12 +776,15 @@ struct Shape {
     bool split;   // blocks may be split over CTAs and joined
     bool spread;  // tcgen05 kernel: so few blocks that each has many pieces
 };
-// Sequences that cannot be longer than this are not split by the few-row kernel: no second launch, no workspace.  A call from
-// a program's loop falls from 20.5 to 15.6 us (one sequence of 500); the kernels' own time is about even (32 query heads on 8
-// of 128, one row, 500 positions, whole / split and joined: one sequence bf16 11.9 / 8.8 us, 16 bf16 13.5 / 15.6, 64 e4m3
-// 22.1 / 29.9; 16 of 250 positions 6.9 / 9.0).
-constexpr long long kWholePositions = 512;
-constexpr long long kWholeSmallBlocks = 256;  // the same for the small calls of many rows (16 rows over 500: 15.0 / 12.9 us)
+// Contexts of at most kWhole positions (by the table's width: the lengths are on the device) are not split by the few-row kernel:
+// four tiles one after the other take as long as a second launch.  Up to kWholeFilled positions, not where the blocks alone keep
+// the CTAs busy: at least one for every second SM, and the last round of them three quarters full where they take several.
+// Device time, whole / split and joined, us: 32 query heads on 8 of 128, one row over 250 positions: 1 sequence bf16 9.0 / 9.0,
+// 16 10.6 / 12.7, 64 e4m3 13.3 / 15.0; over 500: 1 sequence (8 blocks) bf16 12.5 / 9.2, e4m3 13.5 / 10.0; 8 (64 blocks) 12.9 /
+// 12.3 and 13.7 / 12.3; 16 (128) 14.1 / 16.4 and 15.0 / 13.9; 32 16.8 / 19.9 and 16.6 / 17.2; 64 (512 blocks on 444 or 592 CTAs) 36.5 /
+// 33.4 and 18.4 / 26.6; over 1000: 1 18.8 / 10.6, 16 21.7 / 19.0, 64 60.6 / 54.7.  From a Python loop a split call takes 20 us, a whole
+// one 16: a second launch and a workspace.
+constexpr long long kWhole = 256, kWholeFilled = 512;
 constexpr int kSmallBlockRows = 16;
 constexpr long long kSpreadPieces = 32;  // pieces per block from which the tcgen05 kernel's join is spread (see there)
 Shape shape_of(const PagedCacheDev& c, const PagedRowsDev& rows, int group, int num_sms) {
@@ -791,21 +794,22 @@ Shape shape_of(const PagedCacheDev& c, const PagedRowsDev& rows, int group, int 
         const long long per_seq = (rows.max_rows + (1LL << tb_log) - 1) >> tb_log;
         return c.n_kv_heads * std::min(rows.batch * per_seq, (static_cast<long long>(rows.n_rows) >> tb_log) + rows.batch);
     };
-    long long whole = kWholePositions;
+    long long whole = kWhole;
     s.tb_log = 0;  // tokens per block: a power of two
     s.nt = 0;
     if (r <= (c.dtype == VERILLM_KV_BF16 ? 24 : 32)) {
         s.nt = static_cast<int>((r + 7) / 8);
         while ((1LL << s.tb_log) < rows.max_rows) ++s.tb_log;  // all of a sequence's
+        const long long ctas = static_cast<long long>(num_sms) * rows_ctas(c.head_dim, c.dtype, s.nt), n = blocks(s.tb_log), rounds = (n + ctas - 1) / ctas;
+        if (2 * n >= num_sms && (rounds <= 1 || 4 * n >= 3 * rounds * ctas)) whole = kWholeFilled;
     } else if (group <= kSmallBlockRows) {
         int tb_log = 0;
         while ((2 << tb_log) * group <= kSmallBlockRows) ++tb_log;
         const int nt = ((group << tb_log) + 7) / 8;
         const long long ctas = static_cast<long long>(num_sms) * rows_ctas(c.head_dim, c.dtype, nt), n = blocks(tb_log);
-        if (positions <= kWholeSmallBlocks ? n <= ctas : n * ((positions + PR_TILE - 1) / PR_TILE) <= 2 * ctas) {
+        if (positions <= kWhole ? n <= ctas : n * ((positions + PR_TILE - 1) / PR_TILE) <= 2 * ctas) {
             s.nt = nt;
             s.tb_log = tb_log;
-            whole = kWholeSmallBlocks;
         }
     }
     s.rows_per_block = s.nt ? 8 * s.nt : kPagedTcRows;
@@ -821,13 +825,15 @@ size_t hdr_bytes(int grid) { return (static_cast<size_t>(2) * grid * sizeof(int4
 }  // namespace
 
 size_t paged_attention_workspace(const PagedCacheDev& c, const PagedRowsDev& rows, int group, int num_sms) {
-    size_t need = 0;  // that of calls with fewer rows too: the shapes' needs are not quite in their order
+    // That of calls with fewer rows or sequences too: the shapes' needs are not quite in their order, and fewer blocks may be split.
+    size_t need = 0;
     PagedRowsDev fewer = rows;
+    const bool may_split = (static_cast<long long>(rows.table_width) << c.page_shift) > kWhole;
     for (int r = 1;; r = r < 32 && r + 1 < rows.max_rows ? r + 1 : rows.max_rows) {
         fewer.max_rows = std::min(r, rows.max_rows);
         const Shape s = shape_of(c, fewer, group, num_sms);
         const size_t bytes = hdr_bytes(s.grid) + static_cast<size_t>(2) * s.grid * s.rows_per_block * (c.head_dim + 2) * sizeof(float);
-        if (s.split && bytes > need) need = bytes;
+        if ((s.nt == 0 || may_split) && bytes > need) need = bytes;
         if (r >= rows.max_rows || s.nt == 0) return need;  // (the tcgen05 kernel needs the most)
     }
 }
