@@ -336,14 +336,14 @@ class Model:
         status = torch.zeros(1, dtype=torch.int32, device=self.device)
         args = [self._h, tokens.data_ptr(), cu.ctypes.data, batch, int(n_prefill), cs.ctypes.data, cp.ctypes.data, n_check,
                 out.data_ptr(), BF16 if commit_dtype == torch.bfloat16 else F32]
+        name = "verillm_decode_commit" if cache_dtype is None else "verillm_decode_commit_paged"
+        if cache_dtype is not None:
+            args.append(_KV_DTYPES[cache_dtype])
         with torch.cuda.device(self.device):
-            if cache_dtype is None:
-                code = lib().verillm_decode_commit(*args, status.data_ptr(), _stream_ptr(stream))
-            else:
-                code = lib().verillm_decode_commit_paged(*args, _KV_DTYPES[cache_dtype], status.data_ptr(), _stream_ptr(stream))
-        _check(code, "verillm_decode_commit" if cache_dtype is None else "verillm_decode_commit_paged")
+            code = getattr(lib(), name)(*args, status.data_ptr(), _stream_ptr(stream))
+        _check(code, name)
         if int(status.item()) != 0:
-            raise RuntimeError(f"verillm_decode_commit: device status {int(status.item())}")
+            raise RuntimeError(f"{name}: device status {int(status.item())}")
         return out[:, :n_check]
 
     def load_lm_head(self, lm_head: torch.Tensor) -> None:

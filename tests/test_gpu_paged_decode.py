@@ -90,3 +90,12 @@ def test_unknown_cache_types_are_refused(tiny):
     cu = np.asarray(synth.cu_seqlens(wl), dtype=np.int32)
     for dtype in (-1, 3):
         assert vb.lib().verillm_decode_commit_paged(model._h, flat.data_ptr(), cu.ctypes.data, 2, 0, None, None, 0, None, vb.F32, dtype, None, None) == vb.E_INVAL
+
+
+def test_device_problems_are_reported_under_the_entry_that_met_them(tiny):
+    wl, tokens, om, cs, cp, model = tiny
+    flat = torch.from_numpy(tokens.reshape(-1)).to(DEV)
+    flat[5] = wl.shape.vocab  # outside the vocabulary: clamped and reported
+    for cache, name in ((None, "verillm_decode_commit:"), (torch.int8, "verillm_decode_commit_paged:")):
+        with pytest.raises(RuntimeError, match=f"^{name} device status {vb.DEV_TOKEN_RANGE}"):
+            model.decode_commit(flat, synth.cu_seqlens(wl), wl.prompt_len, cs, cp, cache_dtype=cache)
