@@ -243,7 +243,8 @@ def quantised_vectors(x: np.ndarray, kind: str) -> np.ndarray:
     return np.clip(np.rint(y / step) * step, -q, q) * scale
 
 
-def forward_decode_kvcache(m: Model, tokens: np.ndarray, precision: str = "f64", cache: Optional[str] = None) -> np.ndarray:
+def forward_decode_kvcache(m: Model, tokens: np.ndarray, precision: str = "f64", cache: Optional[str] = None,
+                           n_prompt: int = 0) -> np.ndarray:
     """The prover's loop: one position at a time, keys/values of earlier positions taken from a cache.
 
     precision "f64": exact twin of forward_prefill (brute-force check of the paper's equivalence claim).
@@ -251,6 +252,7 @@ def forward_decode_kvcache(m: Model, tokens: np.ndarray, precision: str = "f64",
     attention output and the FFN product are rounded to bf16 where such a stack stores them
     (so the cache holds bf16 keys/values); accumulation and the residual stream stay wide.
     cache "e4m3" / "int8": every key and value vector is stored quantised and attended to as stored.
+    n_prompt: the first positions are a prompt taken in one pass, which attends to its own unquantised keys and values.
     Returns [n_layers, T, d_model] (not rounded; the caller serialises)."""
     keep = (lambda x: x) if cache is None else (lambda x: quantised_vectors(x, cache))
     rnd = (lambda x: x) if precision == "f64" else round_to_bf16
@@ -258,6 +260,7 @@ def forward_decode_kvcache(m: Model, tokens: np.ndarray, precision: str = "f64",
     H, KV, dh = m.n_heads, m.n_kv_heads, m.head_dim
     kc = np.zeros((m.n_layers, T, KV, dh))
     vc = np.zeros((m.n_layers, T, KV, dh))
+    kp, vp = np.zeros((2, m.n_layers, min(n_prompt, T), KV, dh))  # the prompt's, as computed
     states = np.empty((m.n_layers, T, m.d_model), dtype=np.float64)
     for t in range(T):
         h = embed_tokens(m, tokens[t : t + 1])[0]
@@ -266,14 +269,18 @@ def forward_decode_kvcache(m: Model, tokens: np.ndarray, precision: str = "f64",
             w = m.layers[l]
             a = rnd(rmsnorm(h, w["attn_norm"], m.rms_eps))
             q = rnd(rope((w["wq"] @ a).reshape(1, H, dh), p, m.rope_base))[0]
-            kc[l, t] = keep(rnd(rope((w["wk"] @ a).reshape(1, KV, dh), p, m.rope_base))[0])
-            vc[l, t] = keep(rnd((w["wv"] @ a).reshape(KV, dh)))
+            k, v = rnd(rope((w["wk"] @ a).reshape(1, KV, dh), p, m.rope_base))[0], rnd((w["wv"] @ a).reshape(KV, dh))
+            kc[l, t], vc[l, t] = keep(k), keep(v)
+            ka, va = kc[l], vc[l]
+            if t < n_prompt:
+                kp[l, t], vp[l, t] = k, v
+                ka, va = kp[l], vp[l]
             o = np.empty((H, dh))
             for g in range(H):
                 kv = g * KV // H
-                s = kc[l, : t + 1, kv, :] @ q[g] / np.sqrt(float(dh))
+                s = ka[: t + 1, kv, :] @ q[g] / np.sqrt(float(dh))
                 wgt = softmax_rows(s[None, :])[0]
-                o[g] = wgt @ vc[l, : t + 1, kv, :]
+                o[g] = wgt @ va[: t + 1, kv, :]
             u = h + w["wo"] @ rnd(o.reshape(-1))
             f = rnd(rmsnorm(u, w["ffn_norm"], m.rms_eps))
             h = u + w["w_down"] @ rnd(silu(w["w_gate"] @ f) * (w["w_up"] @ f))

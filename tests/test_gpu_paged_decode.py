@@ -99,3 +99,40 @@ def test_device_problems_are_reported_under_the_entry_that_met_them(tiny):
     for cache, name in ((None, "verillm_decode_commit:"), (torch.int8, "verillm_decode_commit_paged:")):
         with pytest.raises(RuntimeError, match=f"^{name} device status {vb.DEV_TOKEN_RANGE}"):
             model.decode_commit(flat, synth.cu_seqlens(wl), wl.prompt_len, cs, cp, cache_dtype=cache)
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "int8"])
+def test_a_prompt_in_one_pass_then_decode_over_an_8_bit_cache_matches_the_oracle(tiny, cache):
+    """What a served prover runs: the prompt attends to its own keys and values, later tokens to what the cache kept of them."""
+    wl, tokens, om, cs, cp, model = tiny
+    both = lambda **kw: np.concatenate([vo.forward_decode_kvcache(om, tokens[b], "bf16", **kw) for b in range(2)], axis=1)  # noqa: E731
+    ref = both(cache=cache, n_prompt=wl.prompt_len)
+    flat = torch.from_numpy(tokens.reshape(-1)).to(DEV)
+    got = model.decode_commit(flat, synth.cu_seqlens(wl), wl.prompt_len, cs, cp, torch.float32, cache_dtype=TYPES[cache])
+    got = got.double().cpu().numpy()
+    rel = H.rel_l2(got, ref)
+    assert rel.max() <= TOL, rel.max()
+    # closer to this than the oracle's other caches are, over the cells where they differ: the prompt unquantised, later tokens not
+    rms = lambda x: np.sqrt((x ** 2).mean())  # noqa: E731
+    for other, cells in ((both(cache=cache), cp < wl.prompt_len), (both(), cp >= wl.prompt_len)):
+        assert rms(rel[:, cells]) < rms(H.rel_l2(other, ref)[:, cells]), cache
+
+
+@pytest.mark.parametrize("cache", [None, "e4m3", "int8"])
+def test_layers_keep_their_own_pages(cache):
+    """Three layers, prompts whose last page is partly filled.  A layer's keys and values differ from the oracle's by the
+    roundings of the layers before it, so a code may be the next one: off by a step where storing it is off by up to half
+    a step.  The states are then off by at most twice what the cache itself changes, on top of a bf16 pass's tolerance."""
+    wl = dataclasses.replace(synth.WORKLOADS["tiny"], batch=2, prompt_len=11, gen_len=23, oracle_weights="bf16")
+    wl = dataclasses.replace(wl, shape=dataclasses.replace(wl.shape, n_layers=3))
+    tokens, om = synth.token_streams(wl), H.oracle_model(wl)
+    cs = np.repeat([0, 1], wl.seq_len).astype(np.int32)
+    cp = np.tile(np.arange(wl.seq_len), 2).astype(np.int32)
+    both = lambda **kw: np.concatenate([vo.forward_decode_kvcache(om, tokens[b], "bf16", **kw) for b in range(2)], axis=1)  # noqa: E731
+    ref, plain = both(cache=cache, n_prompt=wl.prompt_len), both()
+    model = H.gpu_model(wl, len(cs), DEV)
+    flat = torch.from_numpy(tokens.reshape(-1)).to(DEV)
+    got = model.decode_commit(flat, synth.cu_seqlens(wl), wl.prompt_len, cs, cp, torch.float32, cache_dtype=TYPES[cache])
+    model.close()
+    rel = H.rel_l2(got.double().cpu().numpy(), ref)
+    assert rel.max() <= TOL + 2 * H.rel_l2(plain, ref).max(), rel.max()
