@@ -136,3 +136,19 @@ def test_layers_keep_their_own_pages(cache):
     model.close()
     rel = H.rel_l2(got.double().cpu().numpy(), ref)
     assert rel.max() <= TOL + 2 * H.rel_l2(plain, ref).max(), rel.max()
+
+
+def test_calibration_sees_the_attackers_cache():
+    """The attack cells are a trace over the cache named: other statistics than the honest cells', other ones for each type, and
+    further away, most for the coarsest codes."""
+    wl = dataclasses.replace(synth.WORKLOADS["tiny"], check_frac=0.5)
+    away = {}
+    for cache in ("bf16", "int8", "e4m3"):
+        stats, is_attack = calibrate.trace_stats(wl, 8, torch.device(DEV), cache)
+        attack = is_attack.bool()
+        rel = stats[:, vb.STAT_NAMES.index("rel_l2")].double()
+        away["honest"], away[cache] = (x.pow(2).mean().sqrt().item() for x in (rel[~attack], rel[attack]))
+        if cache != "bf16":
+            assert not torch.equal(stats[~attack], stats[attack])
+    # a code is off by up to half a step: 2^-4 of an entry (e4m3) or 2^-8 of the vector's largest (int8)
+    assert away["e4m3"] > away["int8"] > 0 and away["e4m3"] > 1.05 * max(away["honest"], away["bf16"]), away
