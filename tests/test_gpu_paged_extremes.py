@@ -81,3 +81,29 @@ def test_an_infinite_value_of_a_vanishing_weight_in_a_large_call_is_not_lost(nam
         cache, r = c.device()
         got = vb.op_attention_paged(c.dq, cache, r)[:rows[0]].reshape(rows[0], heads, 128).isfinite().cpu()
         assert not bool(got[..., 7].any()) and bool(got[..., :7].all()) and bool(got[..., 8:].all()), (odd, top)
+
+
+@pytest.mark.parametrize("rows,kv", [([3, 2], [200, 40]), ([4, 1], [900, 2000]), ([20] * 160, [90] * 160), ([40, 30], [2000, 1500])])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_later_token_of_great_size_does_not_disturb_the_rows_before_it(dtype, rows, kv):
+    """The last token's key and value are 2^16 times as large as the others'.  Rows that may not see it give what they give
+    without it: 8-bit operands are scaled to the largest of their reach, here 2^18 above the smallest, which leaves a scale
+    within 2^-13 where the tolerance counts 2^-11 for the operand: a quarter more."""
+    c = Case(dtype, 8, 2, 128, 16, rows, kv, seed=43)
+    count = len(rows)
+    if count > 8:
+        c.rows, c.kv = c.rows[:2], c.kv[:2]
+    ref, tol, _, _ = c.attention()
+    c.rows, c.kv = list(rows), list(kv)
+    k, v = _floats(c)
+    for b in range(min(count, 2)):
+        for t in (k, v):
+            page, off = int(c.table[b, (kv[b] - 1) // c.ps]), (kv[b] - 1) % c.ps
+            t[page, :, off] *= 2.0 ** 16
+    c.set_pools(k.to(BF16), v.to(BF16))
+    cache, r = c.device()
+    got = vb.op_attention_paged(c.dq, cache, r)
+    r.check()
+    for b in range(min(count, 2)):
+        at = slice(int(c.cu[b]), int(c.cu[b + 1]) - 1)
+        assert_within(got[at].reshape(-1, c.H, c.dh), ref[at], 1.25 * tol[at], f"sequence {b}")
