@@ -587,7 +587,7 @@ class PagedRows(_Fixed):
         table = page_table.shape
         if len(table) != 2 or kv_len.shape != table[:1] or cu_rows.shape != (table[0] + 1,):
             raise ValueError("page_table is [batch][width], cu_rows [batch + 1], kv_len [batch]")
-        self.__dict__.update(page_table=page_table, cu_rows=cu_rows, kv_len=kv_len, max_rows=int(max_rows), status=status,
+        self.__dict__.update(page_table=page_table, cu_rows=cu_rows, kv_len=kv_len, max_rows=min(int(max_rows), 0x7FFFFFFF), status=status,
                              device=page_table.device, _last=None)
 
     def c_struct(self, n_rows: int) -> KVRowsC:

@@ -45,3 +45,14 @@ def test_workspaces_of_larger_batches_serve_smaller_ones(dtype, rows):
                     ref, tol, _, _ = c.attention()
                     assert_within(got.reshape(c.n, 8, 64), ref, tol)
         assert all(a <= b for a, b in zip(needs, needs[1:])), (kv, needs)
+
+
+def test_any_bound_on_the_rows_is_taken_as_it_is():
+    """A bound beyond 32 bits is a bound: cut off, it would be a small one and the sequences skipped."""
+    c = Case(E4M3, 4, 2, 64, 16, [7, 2], [40, 30], seed=52, pad=0)
+    cache, rows = c.device()
+    want = vb.op_attention_paged(c.dq, cache, rows)
+    for most in (1 << 31, (1 << 32) + 1, 1 << 40):
+        wide = vb.PagedRows(rows.page_table, rows.cu_rows, rows.kv_len, most, rows.status)
+        assert torch.equal(vb.op_attention_paged(c.dq, cache, wide), want)
+        wide.check()
