@@ -363,7 +363,11 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  * infinite bf16 value as infinity (in large calls of many rows as NaN where its weight is below 2^-126 of the largest).
  * Keys and values of 8-bit pools enter products in fp16, scaled to its range: rounded to 11 bits in large calls of many
  * rows per sequence, exact in others.  Probabilities are rounded to bf16 (bf16 pools; 16 bits outside such calls) or fp16;
- * sums are fp32.  The rounding and the order of the sums follow from the sizes of the call alone.
+ * sums are fp32.  These bits hold for vectors whose scale is at least 2^-16 of the largest among the positions that a sequence's
+ * rows attend to, those included that a single row may not see; smaller ones lose them one by one.
+ * The rounding and the order of the sums follow from the sizes of the call and the GPU's number of SMs: head counts, head_dim,
+ * cache type, batch, n_rows, max_rows and table_width * page_size, which stands for the longest context because the lengths are on the
+ * device.  The same contexts under a wider table may be split otherwise and differ in the last bits.
  * status also receives VERILLM_DEV_WAIT_TIMEOUT when a wait inside the kernel gave up; the results are then invalid.
  * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 128 per kv head; workspace too
  * small or not aligned), E_ARCH, E_CUDA. */

@@ -682,7 +682,7 @@ def op_attention_paged(q: torch.Tensor, cache: KVCache, rows: PagedRows, out: Op
     """Causal grouped-query attention of the rows' queries (bf16 [n_rows][n_heads * head_dim], already rotated) over
     the cache -> bf16 [n_rows][n_heads * head_dim].  lse: optional float32 [n_rows][n_heads] that receives the log of
     the sum of exp(scores).  workspace: optional uint8 tensor of `attention_paged_workspace` bytes to use instead of
-    allocating one for the call."""
+    allocating one for the call.  Rows behind the last sequence keep what `out` and `lse` hold; without `out` they are not defined."""
     shape = q.shape
     if len(shape) not in (2, 3):
         raise ValueError("q must be [n_rows][n_heads * head_dim] or [n_rows][n_heads][head_dim]")
@@ -720,7 +720,7 @@ def op_attention_paged(q: torch.Tensor, cache: KVCache, rows: PagedRows, out: Op
 
 
 def attention_paged_workspace(cache: KVCache, rows: PagedRows, n_rows: int, n_heads: int) -> int:
-    """Bytes of workspace that op_attention_paged needs for calls of up to n_rows rows."""
+    """Bytes of workspace that op_attention_paged needs for calls of up to n_rows rows and as many sequences as `rows` has."""
     rc = rows.c_struct(n_rows)
     with torch.cuda.device(cache.device):
         need = lib().verillm_op_attention_paged_workspace(C.byref(cache.c_struct), C.byref(rc), n_heads)

@@ -112,7 +112,7 @@ struct ShareScratch {  // in shared memory
     int seq;
 };
 __device__ __forceinline__ void find_share(int tl, const PagedRowsDev& r, int page_shift, int n_kv_heads, int tb_log, int nthreads,
-                                           int min_per, ShareScratch* sc, WorkShare& w, int* status) {
+                                           ShareScratch* sc, WorkShare& w, int* status) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nwarps = nthreads >> 5;
     int* st0 = blockIdx.x == 0 ? status : nullptr;  // one CTA reports
     auto tiles = [&](int b) -> long long {
@@ -151,8 +151,7 @@ __device__ __forceinline__ void find_share(int tl, const PagedRowsDev& r, int pa
         total = scan(v);
     }
     w.total = total;
-    long long per = short_div(total + gridDim.x - 1, gridDim.x);
-    if (per < min_per) per = min_per;
+    const long long per = short_div(total + gridDim.x - 1, gridDim.x);
     w.per = per;
     w.begin = min(per * blockIdx.x, total);
     w.end = min(w.begin + per, total);

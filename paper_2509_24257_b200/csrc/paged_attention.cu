@@ -162,7 +162,7 @@ paged_rows_kernel(const PagedAttnParams p) {
     const int G = p.group, shift = c.page_shift, ps_mask = (1 << shift) - 1;
 
     WorkShare share;
-    find_share(p.share_log, p.r, shift, c.n_kv_heads, p.tb_log, PR_THREADS, 1, &sm_share, share, p.status);
+    find_share(p.share_log, p.r, shift, c.n_kv_heads, p.tb_log, PR_THREADS, &sm_share, share, p.status);
     pdl_launch_dependents();
     if (share.begin >= share.end) {
         if (tid == 0 && p.hdr) no_headers(p.hdr);
@@ -568,7 +568,9 @@ paged_rows_kernel(const PagedAttnParams p) {
 //    39.1 -> 32.5 us; four of up to 57000, one kv head, int8: 40.1 -> 26.8; two of 131072, 37 pieces: 101.8 -> 100.1.
 //    The tcgen05 kernel's 256-row blocks keep many warps busy as it is; their join is spread where there are fewer than
 //    grid / kSpreadPieces of them (one block of 128 rows over 16000, 125 pieces: 58 -> 20 us; four over 60000, 37 pieces: 77 -> 67;
-//    but with 18 pieces, 64 rows over 32768, 67 would become 77).
+//    but with 18 pieces, 64 rows over 32768, 67 would become 77).  The host sees no lengths: a batch of 16 rows of each of eight sequences on
+//    one kv head, one over 16000 and seven over 100, has eight blocks and is joined by the long one's few warps, 65 us where 20 would do.
+//    Deciding on the device cost the calls that are not spread 59 -> 62 - 65 us (64 rows over 32768) and 592 -> 600 (1024 rows, e4m3).
 constexpr int JOIN_THREADS = 256, JOIN_WARPS = JOIN_THREADS / 32;
 
 // The pieces of one block: piece 0 is its first CTA's tail slot, piece i the head slot of the i-th CTA after it.

@@ -147,8 +147,8 @@ __device__ __forceinline__ void set_registers(bool more) {
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-// The same times a scale given as the sum of two fp16 numbers (both halves of sh, sl): code * sh + code * sl, rounded
-// once to fp16 but for the rounding of the small second product.
+// Four codes times a scale given as the sum of two fp16 numbers (both halves of sh, sl) -> fp16 pairs (0, 1) and (2, 3): code * sh +
+// code * sl, rounded once to fp16 but for the rounding of the small second product.
 template <int DTYPE>
 __device__ __forceinline__ uint2 scaled4(uint32_t w, uint32_t sh, uint32_t sl) {
     const uint2 x = widen4_half<DTYPE>(w);
@@ -289,7 +289,7 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constan
     }
     tc_fence_before();
     WorkShare share;
-    find_share(PT_TILE_LOG, p.r, p.c.page_shift, p.c.n_kv_heads, p.tb_log, PT_THREADS, 1, scratch, share, p.status);
+    find_share(PT_TILE_LOG, p.r, p.c.page_shift, p.c.n_kv_heads, p.tb_log, PT_THREADS, scratch, share, p.status);
     pdl_launch_dependents();
     tc_fence_after();
     if (share.begin >= share.end) {

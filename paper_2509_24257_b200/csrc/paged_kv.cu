@@ -2,10 +2,10 @@
 //
 // One (token, kv head) vector x of head_dim entries is quantised on its own: a = max(max |x_d|, 2^-110),
 // scale = a / Q, code_d = round(x_d * (Q / a)) to the nearest code, ties to even, with Q the largest code (448 for
-// e4m3, 127 for int8); all of it in fp32, so the only rounding of the data is the one to the code.  The floor under
-// a keeps Q / a finite.  A vector with an infinite or NaN entry gets the scale NaN and codes 0: it reads back as
-// NaN throughout, and attention sees NaN exactly in the rows that may see the token.  Reading is code * scale, rounded
-// once to the output type.
+// e4m3, 127 for int8); all of it in fp32: the factor Q / a and the product are each rounded to 24 bits, then the product
+// to the code.  The floor under a keeps Q / a finite.  A vector with an infinite or NaN entry gets the scale NaN and codes
+// 0: it reads back as NaN throughout, and attention sees NaN exactly in the rows that may see the token.  Reading is
+// code * scale in fp32, and that rounded to the output type.
 //
 // Both kernels move every byte once and are bound by HBM (by latency for a decode step's few rows).  head_dim / 16 lanes
 // share a vector of keys and one of values, 16-byte loads and stores, the maximum by shuffles: a lane then finds the row's
