@@ -21,8 +21,8 @@
 // bf16 numbers (16 significant bits), whose second product hides under the loads (114.4 -> 114.8 us for 64 contexts of
 // 2600 on average, and the error of the result falls from 2.3e-3 to the 1.7e-3 of its own rounding).  All else is fp32.
 //
-// Measured, join included: one row of each of 64 contexts of up to 4096, 32 query heads on 8 of 128, bf16: 115 us = 6.0 TB/s, 93 %
-// of a copy's rate; two contexts of 131072, 64 query heads, e4m3: 99.5 us = 5.3 TB/s; five drafted rows of 16 contexts of up to
+// Measured, join included: one row of each of 64 contexts of up to 4096, 32 query heads on 8 of 128, bf16: 116 us = 6.0 TB/s, 92 - 93 %
+// of a copy's rate; two contexts of 131072, 64 query heads, e4m3: 100.5 us = 5.3 TB/s; five drafted rows of 16 contexts of up to
 // 8192, int8: 70 us = 2.7 TB/s, where 24 rows of output and the keys and values in flight take 255 registers and eight
 // warps per SM wait for their own instructions.
 #include <algorithm>
