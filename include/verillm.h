@@ -357,17 +357,19 @@ int verillm_kv_read(const verillm_kv_cache *cache, const verillm_kv_rows *rows, 
  *  out       DEVICE bf16, same form with out_stride, not overlapping q; a row that attends to nothing receives zeros
  *  lse       optional DEVICE float32 [n_rows][n_heads]: log of the sum of exp(scores), -inf for such a row
  *  workspace DEVICE, 256-byte aligned, at least verillm_op_attention_paged_workspace bytes (negative: an error code),
- *            which suffice for smaller calls too.  May be NULL where that is 0.  It holds nothing between calls, but calls
- *            that may overlap (other streams, graphs replayed side by side) need one each.
+ *            which suffice for smaller calls too (fewer rows or sequences).  May be NULL where that is 0.  It holds nothing
+ *            between calls, but calls that may overlap (other streams, graphs replayed side by side) need one each.
  * A cached value that is not finite reaches every row that may see it, however small its weight, and no other: NaN as NaN, an
- * infinite bf16 value as infinity (in large calls of many rows as NaN where its weight is below 2^-126 of the largest).
+ * infinite bf16 value as infinity (NaN where both signs meet, and in large calls of many rows where its weight is below
+ * 2^-126 of the largest).
  * Keys and values of 8-bit pools enter products in fp16, scaled to its range: rounded to 11 bits in large calls of many
  * rows per sequence, exact in others.  Probabilities are rounded to bf16 (bf16 pools; 16 bits outside such calls) or fp16;
  * sums are fp32.  These bits hold for vectors whose scale is at least 2^-16 of the largest among the positions that a sequence's
  * rows attend to, those included that a single row may not see; smaller ones lose them one by one.
- * The rounding and the order of the sums follow from the sizes of the call and the GPU's number of SMs: head counts, head_dim,
- * cache type, batch, n_rows, max_rows and table_width * page_size, which stands for the longest context because the lengths are on the
- * device.  The same contexts under a wider table may be split otherwise and differ in the last bits.
+ * The rounding and the order of the sums follow from the contexts' lengths, the GPU's number of SMs and the sizes of the call: head
+ * counts, head_dim, cache type, batch, n_rows, max_rows and table_width * page_size, by which the host judges the longest
+ * context because the lengths are on the device.  The same contexts under a wider table may be split otherwise and differ
+ * in the last bits.
  * status also receives VERILLM_DEV_WAIT_TIMEOUT when a wait inside the kernel gave up; the results are then invalid.
  * Errors: E_INVAL, E_SHAPE (n_heads not a multiple of n_kv_heads or more than 128 per kv head; workspace too
  * small or not aligned), E_ARCH, E_CUDA. */

@@ -280,13 +280,13 @@ paged_rows_kernel(const PagedAttnParams p) {
         };
         int tile = k.t0;
         bool stray = false;  // bf16 pools: some value of this warp's was not finite
-        size_t vec = 0, vec_next = 0;
+        size_t vec_next = 0;
         int page2 = 0;
         {
             const int key = token_of(tile);
             const int page0 = page_at(key), page1 = L::BF16 ? 0 : page_at(key + PR_TILE);
             if (!L::BF16) page2 = page_at(key + 2 * PR_TILE);
-            vec = vec_in(page0, key);
+            const size_t vec = vec_in(page0, key);
             vec_next = vec_in(page1, key + PR_TILE);
             if (key < end) {
                 load_keys(vec);
@@ -474,7 +474,6 @@ paged_rows_kernel(const PagedAttnParams p) {
                 }
             }
             if (more) load_values(vec_next);
-            vec = vec_next;
             if (!L::BF16) vec_next = vec2;
         }
 
