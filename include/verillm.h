@@ -82,7 +82,9 @@ enum {
     VERILLM_DEV_TOKEN_RANGE = 1, /* token id outside [0, vocab): clamped */
     VERILLM_DEV_WAIT_TIMEOUT = 2, /* a pipeline wait inside a kernel gave up; results are invalid */
     VERILLM_DEV_PAGE_RANGE = 3,   /* a page number outside the pool: not written, read as zeros / as some other page */
-    VERILLM_DEV_ROWS_RANGE = 4    /* cu_rows or kv_len outside what the buffers hold: bounded, or the sequence skipped */
+    VERILLM_DEV_ROWS_RANGE = 4,   /* cu_rows or kv_len outside what the buffers hold: bounded, or the sequence skipped */
+    VERILLM_DEV_LOGITS = 5,       /* a row of logits is no distribution: its sequence ends before it */
+    VERILLM_DEV_NO_PAGES = 6      /* not enough free pages: a sequence did not grow */
 };
 
 enum { VERILLM_BF16 = 0, VERILLM_F32 = 1 };
@@ -377,6 +379,113 @@ int64_t verillm_op_attention_paged_workspace(const verillm_kv_cache *cache, cons
 int verillm_op_attention_paged(const verillm_kv_cache *cache, const verillm_kv_rows *rows, const void *q,
                                int64_t q_stride, int32_t n_heads, void *out, int64_t out_stride, float *lse,
                                void *workspace, int64_t workspace_bytes, int32_t *status, void *cuda_stream);
+
+/* ------------------------------------------------------------------ 4-bit weights
+ * Weights of a prover that keeps them in 4 bits: w[n][k] = (code - 8) * scale, one bf16 scale per group of `group` consecutive inputs of an
+ * output.  codes: uint8 [n][k / 2], the even input in the low half of a byte; scales: bf16 [k / group][n].  All DEVICE, 16-byte aligned. */
+typedef struct {
+    void *codes, *scales;
+    int32_t n, k;  /* outputs (a multiple of 8) and inputs (a multiple of group) */
+    int32_t group; /* 32, 64 or 128 */
+} verillm_w4;
+
+/* Quantises w (DEVICE bf16, n rows of k entries, w_stride entries apart): scale = bf16(max |w| / 7) of the group, code = w / scale to the nearest
+ * whole number, ties to even, within -7 .. 7, plus 8.  A group with an infinite or NaN weight gets the scale NaN and codes 8. */
+int verillm_w4_quantise(const void *w, int64_t w_stride, const verillm_w4 *out, void *cuda_stream);
+/* out[n][k] = (code - 8) * scale, rounded once to out_dtype (VERILLM_BF16 / VERILLM_F32); rows out_stride entries apart. */
+int verillm_w4_dequantise(const verillm_w4 *w, void *out, int64_t out_stride, int32_t out_dtype, void *cuda_stream);
+/* y[rows][n] = x[rows][k] w^T (+ residual): made for the few rows of a decode step or of drafted tokens, right for any number.
+ *  x         DEVICE bf16, 16-byte aligned, x_stride a multiple of 8 entries
+ *  residual  optional DEVICE float32 [rows][residual_stride]; may be y itself (out_dtype F32, same stride)
+ *  y         DEVICE in out_dtype, rows y_stride entries apart, not overlapping x
+ *  status    optional DEVICE word, raised from 0 to VERILLM_DEV_WAIT_TIMEOUT when a wait inside the kernel gave up
+ * Products are exact and sums fp32; the order of the sums follows from n, k, rows and the GPU's number of SMs.  Allocates nothing; make the first call on a device outside
+ * a capture.  Errors: E_INVAL, E_SHAPE (alignment, group, k > 32768, rows > 65536), E_ARCH, E_CUDA. */
+int verillm_op_w4_matvec(const verillm_w4 *w, const void *x, int64_t x_stride, int32_t rows, const float *residual, int64_t residual_stride,
+                         void *y, int64_t y_stride, int32_t out_dtype, int32_t *status, void *cuda_stream);
+
+/* ------------------------------------------------------------------ drafted tokens
+ * A prover that drafts tokens cheaply runs the full model over them in one pass (rows of verillm_op_attention_paged) and keeps those that its own
+ * distribution confirms, so that what it emits is distributed as if it had drafted nothing.
+ *
+ * Sequence b owns the rows cu_rows[b] .. cu_rows[b+1]-1 (n_b of them); row i has the input token tokens[row] and the logits of what follows
+ * it: tokens of rows 1 .. n_b-1 are the drafted ones.  p = softmax(target / T), q = softmax(draft / T) of a row; without draft logits q is one at the
+ * drafted token.  The token x of row i+1 is accepted iff accept_u[i+1] * q(x) < p(x), p and q of row i.  At the first row a where that fails a
+ * token is drawn from max(0, p - q) / sum (from p where that is 0 throughout), if it never fails one from p of the last row: the first v
+ * whose running sum exceeds sample_u[b] times the total (the last v of positive probability if none does).  T = 0: p is one at the largest logit, lowest
+ * index; a token is accepted iff it is that one.  Probabilities below e^-700 of the row's largest count as 0. */
+typedef struct {
+    const void *target;        /* DEVICE [n_rows][vocab] in dtype, rows target_stride entries apart */
+    const void *draft;         /* optional, the same form: row i is what the token of row i + 1 was drawn from; last rows are not read */
+    int64_t target_stride, draft_stride;
+    int32_t dtype;             /* VERILLM_BF16 / VERILLM_F32 */
+    int32_t vocab;             /* at most 2^24 */
+    int32_t batch, n_rows;     /* n_rows: rows that the buffers hold; those behind the last sequence are left as they are */
+    int32_t max_rows;          /* at least every n_b, at most 256; a sequence with more is skipped (VERILLM_DEV_ROWS_RANGE) */
+    const int32_t *cu_rows;    /* DEVICE [batch + 1] */
+    const int32_t *tokens;     /* DEVICE [n_rows] */
+    const int32_t *kv_len;     /* optional DEVICE [batch]: positions cached, these rows among them */
+    const float *temperature;  /* optional DEVICE [batch]: 0 or 2^-100 .. 2^100; NULL: 1 */
+    const float *accept_u;     /* DEVICE [n_rows], uniform in [0, 1); NaN accepts nothing */
+    const float *sample_u;     /* DEVICE [batch], uniform in [0, 1); bounded to [0, 1], NaN counts as 0 */
+} verillm_drafts;
+
+/* Caller-allocated DEVICE outputs */
+typedef struct {
+    int32_t *tokens;    /* [n_rows]: what was emitted: the accepted tokens (rows 0 .. a-1), the drawn one (row a), -1 behind it */
+    int32_t *n_emitted; /* [batch] a + 1 */
+    float *logp;        /* optional [n_rows]: log p of the emitted token (0 for T = 0 and where nothing was emitted) */
+    int32_t *new_len;   /* optional [batch], not kv_len itself: kv_len - n_b + n_emitted, the positions that stay (e.g. for verillm_kv_free) */
+} verillm_draft_report;
+
+/* A row that the walk reaches and that has no distribution (an entry NaN or +inf, in the draft's row too, or all -inf; a temperature out of range)
+ * ends its sequence before it: n_emitted = a, nothing drawn, VERILLM_DEV_LOGITS.  A drafted token outside the vocabulary is rejected
+ * (VERILLM_DEV_TOKEN_RANGE).  Decisions are those of 64-bit arithmetic.
+ *  workspace  DEVICE, 16-byte aligned, verillm_verify_drafts_workspace(n_rows) bytes; holds nothing between calls, but calls that may overlap need one each
+ *  status     optional DEVICE word, raised from 0 to the first problem met, never cleared by the call
+ * Allocates nothing; make the first call on a device outside a capture.  Errors: E_INVAL, E_SHAPE, E_ARCH, E_CUDA. */
+int64_t verillm_verify_drafts_workspace(int32_t n_rows);
+int verillm_verify_drafts(const verillm_drafts *drafts, const verillm_draft_report *report, void *workspace, int64_t workspace_bytes,
+                          int32_t *status, void *cuda_stream);
+
+/* ------------------------------------------------------------------ pages of a paged cache
+ * Who holds which page, kept on the device so that a captured step can grow, shorten and share sequences.  refs[page] counts the table entries
+ * that name it (0: free); sequence b holds the first ceil(kv_len[b] / page_size) entries of its row of the table.  All layers share the table.  The calls change
+ * these arrays and must follow one another (one stream, or events); they give the same result whatever the timing.  Pages that several sequences hold are read
+ * only: verillm_kv_reserve gives a sequence its own copy of a partly filled one before it writes there. */
+typedef struct {
+    const verillm_kv_cache *layers; /* HOST [n_layers], pools of one geometry, at most 128 */
+    int32_t n_layers;
+    int32_t *page_table;            /* DEVICE [batch][table_width] */
+    int32_t *kv_len;                /* DEVICE [batch] */
+    int32_t *refs;                  /* DEVICE [n_pages] */
+    int32_t batch, table_width;     /* table_width * page_size at most 2^26 */
+} verillm_kv_pages;
+
+/* Workspace of the calls below: DEVICE, 16-byte aligned; holds nothing between calls. */
+int64_t verillm_kv_pages_workspace(int32_t batch, int32_t n_pages);
+
+/* Grows every sequence with new_len[b] > kv_len[b] (DEVICE int32 [batch]) to new_len[b]; the others stay.  New pages are the lowest free ones, by sequences
+ * in order, contents as they were.  A sequence whose last page is partly filled and held by others too gets a copy of it first (all layers), also
+ * from the lowest free pages; where all holders of such a page grow, the last of them keeps it.  Sequences are served in order up to the first whose need is not met:
+ * it and all later ones that grow stay as they are (VERILLM_DEV_NO_PAGES).  new_len beyond the table's row: that sequence stays (VERILLM_DEV_ROWS_RANGE). */
+int verillm_kv_reserve(const verillm_kv_pages *pages, const int32_t *new_len, void *workspace, int64_t workspace_bytes, int32_t *status,
+                       void *cuda_stream);
+/* Shortens every sequence with 0 <= new_len[b] < kv_len[b] to new_len[b] (0: all of it): drafts that were rejected, sequences that are done.
+ * A page that nobody names any more is free.  Table entries behind the new end stay as they were and mean nothing. */
+int verillm_kv_free(const verillm_kv_pages *pages, const int32_t *new_len, int32_t *status, void *cuda_stream);
+/* For i < n (at most batch): sequence dst[i], which is empty (kv_len 0), comes to share all that src[i] holds.  src, dst: DEVICE int32 [n]; a src may be
+ * given several times.  A pair whose dst is not empty or was given before, or with an index out of range, does nothing (VERILLM_DEV_ROWS_RANGE). */
+int verillm_kv_fork(const verillm_kv_pages *pages, const int32_t *src, const int32_t *dst, int32_t n, void *workspace, int64_t workspace_bytes,
+                    int32_t *status, void *cuda_stream);
+/* Moves pages so that those in use are 0 .. *n_used - 1 (DEVICE int32): the i-th lowest one numbered n_used or above goes to the i-th lowest free one below.
+ * Contents of all layers, refs and the table follow.  refs has to be right: a page in use that refs calls free would be overwritten. */
+int verillm_kv_compact(const verillm_kv_pages *pages, int32_t *n_used, void *workspace, int64_t workspace_bytes, int32_t *status, void *cuda_stream);
+/* Copies page src_pages[i] of every layer of one set of pools to page dst_pages[i] of another (or of the same one), i < n.  Pools differ at most in
+ * n_pages.  Pairs with a -1 are left out, with other numbers out of range too (VERILLM_DEV_PAGE_RANGE).  Destinations are different pages, and none is a source of
+ * the same call. */
+int verillm_kv_copy(const verillm_kv_cache *src_layers, const verillm_kv_cache *dst_layers, int32_t n_layers, const int32_t *src_pages,
+                    const int32_t *dst_pages, int32_t n, int32_t *status, void *cuda_stream);
 
 /* Per-kernel timing of verify_prefill, for the roofline report (measurement aid, not part of the method).
  * While enabled, every verify_prefill call records one CUDA event after each launch on the caller's

@@ -23,7 +23,7 @@ STAT_NAMES = (
 BF16, F32 = 0, 1
 TOL_BIT_AWARE = 1
 E_INVAL, E_SHAPE, E_RANGE, E_NOMEM, E_CUDA, E_ARCH = -1, -2, -3, -4, -5, -6
-DEV_TOKEN_RANGE, DEV_WAIT_TIMEOUT, DEV_PAGE_RANGE, DEV_ROWS_RANGE = 1, 2, 3, 4
+DEV_TOKEN_RANGE, DEV_WAIT_TIMEOUT, DEV_PAGE_RANGE, DEV_ROWS_RANGE, DEV_LOGITS, DEV_NO_PAGES = 1, 2, 3, 4, 5, 6
 KV_BF16, KV_E4M3, KV_INT8 = 0, 1, 2
 
 EXPORTS = (
@@ -34,6 +34,8 @@ EXPORTS = (
     "verillm_load_lm_head", "verillm_token_match", "verillm_verify_segment", "verillm_spot_check", "verillm_merkle_roots",
     "verillm_threshold_sweep", "verillm_selftest_wait_timeout", "verillm_kv_write", "verillm_kv_read",
     "verillm_op_attention_paged", "verillm_op_attention_paged_workspace", "verillm_decode_commit_paged",
+    "verillm_w4_quantise", "verillm_w4_dequantise", "verillm_op_w4_matvec", "verillm_verify_drafts", "verillm_verify_drafts_workspace",
+    "verillm_kv_pages_workspace", "verillm_kv_reserve", "verillm_kv_free", "verillm_kv_fork", "verillm_kv_compact", "verillm_kv_copy",
 )
 PROF_CLASSES = ("setup", "rmsnorm", "gemm_qkv_rope", "attention", "gemm_o_resid", "gemm_gate_up_swiglu",
                 "gemm_down_resid_compare", "verdict")
@@ -82,6 +84,25 @@ class KVCacheC(C.Structure):
 class KVRowsC(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("page_table", "cu_rows", "kv_len")] + [
         (n, C.c_int32) for n in ("table_width", "batch", "n_rows", "max_rows")]
+
+
+class W4C(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("codes", "scales")] + [(n, C.c_int32) for n in ("n", "k", "group")]
+
+
+class DraftsC(C.Structure):
+    _fields_ = [("target", C.c_void_p), ("draft", C.c_void_p), ("target_stride", C.c_int64), ("draft_stride", C.c_int64)] + [
+        (n, C.c_int32) for n in ("dtype", "vocab", "batch", "n_rows", "max_rows")] + [
+        (n, C.c_void_p) for n in ("cu_rows", "tokens", "kv_len", "temperature", "accept_u", "sample_u")]
+
+
+class DraftReportC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("tokens", "n_emitted", "logp", "new_len")]
+
+
+class KVPagesC(C.Structure):
+    _fields_ = [("layers", C.POINTER(KVCacheC)), ("n_layers", C.c_int32), ("page_table", C.c_void_p), ("kv_len", C.c_void_p),
+                ("refs", C.c_void_p), ("batch", C.c_int32), ("table_width", C.c_int32)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -155,6 +176,23 @@ def lib() -> C.CDLL:
         L.verillm_op_attention_paged.argtypes = [cache_p, rows_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
                                                  C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
         L.verillm_op_attention_paged.restype = C.c_int
+        w4_p, pages_p = C.POINTER(W4C), C.POINTER(KVPagesC)
+        L.verillm_w4_quantise.argtypes = [C.c_void_p, C.c_int64, w4_p, C.c_void_p]
+        L.verillm_w4_dequantise.argtypes = [w4_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]
+        L.verillm_op_w4_matvec.argtypes = [w4_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32,
+                                           C.c_void_p, C.c_void_p]
+        L.verillm_verify_drafts.argtypes = [C.POINTER(DraftsC), C.POINTER(DraftReportC), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.verillm_verify_drafts_workspace.argtypes = [C.c_int32]
+        L.verillm_verify_drafts_workspace.restype = C.c_int64
+        L.verillm_kv_pages_workspace.argtypes = [C.c_int32, C.c_int32]
+        L.verillm_kv_pages_workspace.restype = C.c_int64
+        L.verillm_kv_reserve.argtypes = [pages_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.verillm_kv_free.argtypes = [pages_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.verillm_kv_fork.argtypes = [pages_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.verillm_kv_compact.argtypes = [pages_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.verillm_kv_copy.argtypes = [cache_p, cache_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+        for name in ("w4_quantise", "w4_dequantise", "op_w4_matvec", "verify_drafts", "kv_reserve", "kv_free", "kv_fork", "kv_compact", "kv_copy"):
+            getattr(L, "verillm_" + name).restype = C.c_int
         L.verillm_profile_enable.argtypes = [C.c_void_p, C.c_int32]
         L.verillm_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_int32)]
         L.verillm_profile_enable.restype = C.c_int
@@ -727,3 +765,263 @@ def attention_paged_workspace(cache: KVCache, rows: PagedRows, n_rows: int, n_he
     if need < 0:
         raise VerillmError(int(need), "verillm_op_attention_paged_workspace")
     return int(need)
+
+
+# --------------------------------------------------------------------------- 4-bit weights
+
+
+class W4Weights(_Fixed):
+    """4-bit weights: codes uint8 [n][k / 2] (code + 8, the even input in the low half), scales bf16 [k / group][n].  Wraps the caller's tensors;
+    `w4_quantise` makes them from bf16 weights."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, group: int = 128):
+        shape, dev = codes.shape, codes.get_device()
+        if codes.dtype != torch.uint8 or len(shape) != 2 or scales.dtype != torch.bfloat16 or group not in (32, 64, 128):
+            raise ValueError("codes must be uint8 [n][k / 2], scales bf16 [k / group][n], group 32, 64 or 128")
+        n, k = shape[0], 2 * shape[1]
+        if k % group or scales.shape != (k // group, n):
+            raise ValueError("codes must be uint8 [n][k / 2], scales bf16 [k / group][n], group 32, 64 or 128")
+        if dev < 0 or scales.get_device() != dev or not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("codes and scales must be contiguous and on one CUDA device")
+        self.__dict__.update(codes=codes, scales=scales, group=group, n=n, k=k, device=codes.device,
+                             c_struct=W4C(codes.data_ptr(), scales.data_ptr(), n, k, group))
+
+
+def _strided(t: torch.Tensor, what: str, rows: int, width: int, dtype: torch.dtype, device: torch.device) -> int:
+    """Row stride of a [rows][width] matrix whose rows are contiguous."""
+    if t.dtype != dtype or t.device != device or t.shape != (rows, width) or (t.stride(1) != 1 and width > 1):
+        raise ValueError(f"{what} must be a {dtype} [{rows}][{width}] tensor with contiguous rows on {device}")
+    return t.stride(0) if rows > 1 else width
+
+
+def w4_quantise(w: torch.Tensor, group: int = 128, stream: Optional[torch.cuda.Stream] = None) -> W4Weights:
+    """bf16 [n][k] (rows may be strided) -> 4-bit weights with one scale per `group` inputs."""
+    if w.dim() != 2 or not w.is_cuda or group not in (32, 64, 128) or w.shape[1] % group:
+        raise ValueError("w must be a CUDA matrix whose rows are whole groups of 32, 64 or 128")
+    stride = _strided(w, "w", w.shape[0], w.shape[1], torch.bfloat16, w.device)
+
+    def call(st):
+        out = W4Weights(torch.empty(w.shape[0], w.shape[1] // 2, dtype=torch.uint8, device=w.device),
+                        torch.empty(w.shape[1] // group, w.shape[0], dtype=torch.bfloat16, device=w.device), group)
+        _check(lib().verillm_w4_quantise(w.data_ptr(), stride, C.byref(out.c_struct), st), "verillm_w4_quantise")
+        return out
+
+    return _launch(w.device, stream, call)
+
+
+def w4_dequantise(w: W4Weights, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """[n][k] in bf16 or float32: what the 4-bit weights stand for."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be bf16 or float32")
+
+    def call(st):
+        o = torch.empty(w.n, w.k, dtype=dtype, device=w.device) if out is None else out
+        stride = _strided(o, "out", w.n, w.k, dtype, w.device)
+        _check(lib().verillm_w4_dequantise(C.byref(w.c_struct), o.data_ptr(), stride, F32 if dtype == torch.float32 else BF16, st), "verillm_w4_dequantise")
+        return o
+
+    return _launch(w.device, stream, call)
+
+
+def op_w4_matvec(x: torch.Tensor, w: W4Weights, residual: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
+                 out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """x (bf16 [rows][k], rows may be strided) @ w.T (+ residual, float32 [rows][n]) -> [rows][n] in `dtype` (that of `out`, else bf16).
+    residual may be `out` itself.  status: optional int32 [1] that device problems are reported in."""
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError("x must be [rows][k]")
+    rows, stride = shape[0], _strided(x, "x", shape[0], w.k, torch.bfloat16, w.device)
+    res_stride = 0 if residual is None else _strided(residual, "residual", rows, w.n, torch.float32, w.device)
+    dtype = dtype or (torch.bfloat16 if out is None else out.dtype)
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be bf16 or float32")
+    _check_word(status, w.device)
+
+    def call(st):
+        y = torch.empty(rows, w.n, dtype=dtype, device=w.device) if out is None else out
+        y_stride = w.n if out is None else _strided(y, "out", rows, w.n, dtype, w.device)
+        _check(lib().verillm_op_w4_matvec(C.byref(w.c_struct), x.data_ptr(), stride, rows, _ptr(residual), res_stride, y.data_ptr(), y_stride,
+                                          F32 if dtype == torch.float32 else BF16, _ptr(status), st), "verillm_op_w4_matvec")
+        return y
+
+    return _launch(w.device, stream, call)
+
+
+def _check_word(t: Optional[torch.Tensor], device: torch.device) -> None:
+    if t is not None and (t.dtype != torch.int32 or t.numel() != 1 or t.device != device):
+        raise ValueError(f"status must be an int32 tensor of one entry on {device}")
+
+
+def _vector(t: torch.Tensor, what: str, n: int, dtype: torch.dtype, device: torch.device) -> None:
+    if t.dtype != dtype or t.device != device or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} [{n}] tensor on {device}")
+
+
+# --------------------------------------------------------------------------- drafted tokens
+
+
+class DraftReport:
+    """Device tensors of one check: tokens int32 [n_rows] (what was emitted, -1 behind it), n_emitted int32 [batch], logp float32 [n_rows], new_len
+    int32 [batch] (None without kv_len).  Rows behind the last sequence keep what the tensors held (nothing defined in a fresh report)."""
+
+    def __init__(self, n_rows: int, batch: int, device, with_len: bool):
+        self.tokens = torch.empty(n_rows, dtype=torch.int32, device=device)
+        self.n_emitted = torch.empty(batch, dtype=torch.int32, device=device)
+        self.logp = torch.empty(n_rows, dtype=torch.float32, device=device)
+        self.new_len = torch.empty(batch, dtype=torch.int32, device=device) if with_len else None
+
+
+def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu_rows: torch.Tensor, max_rows: int, accept_u: torch.Tensor, sample_u: torch.Tensor,
+                  draft: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None, kv_len: Optional[torch.Tensor] = None,
+                  report: Optional[DraftReport] = None, workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> DraftReport:
+    """Checks drafted tokens against the target's logits (bf16 or float32 [n_rows][vocab], rows may be strided) with given random numbers: accept_u
+    float32 [n_rows], sample_u float32 [batch].  tokens int32 [n_rows]: every row's input token; those of a sequence's rows behind its first are the
+    drafted ones.  draft: the logits they were drawn from, the same type; without it they count as certain.  temperature float32 [batch], 0 for the
+    largest logit; 1 without it.  kv_len int32 [batch]: gives the report's new_len.  All on one device; the header has the definitions."""
+    if target.dim() != 2 or not target.is_cuda or target.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("target must be a bf16 or float32 CUDA matrix")
+    dev, (n_rows, vocab) = target.device, target.shape
+    batch = cu_rows.shape[0] - 1 if cu_rows.dim() == 1 else 0
+    t_stride = _strided(target, "target", n_rows, vocab, target.dtype, dev)
+    d_stride = 0 if draft is None else _strided(draft, "draft", n_rows, vocab, target.dtype, dev)
+    _vector(cu_rows, "cu_rows", batch + 1, torch.int32, dev)
+    _vector(tokens, "tokens", n_rows, torch.int32, dev)
+    _vector(accept_u, "accept_u", n_rows, torch.float32, dev)
+    _vector(sample_u, "sample_u", batch, torch.float32, dev)
+    if temperature is not None:
+        _vector(temperature, "temperature", batch, torch.float32, dev)
+    if kv_len is not None:
+        _vector(kv_len, "kv_len", batch, torch.int32, dev)
+    _check_word(status, dev)
+    if report is not None:
+        _vector(report.tokens, "report.tokens", n_rows, torch.int32, dev)
+        _vector(report.n_emitted, "report.n_emitted", batch, torch.int32, dev)
+        if report.logp is not None:
+            _vector(report.logp, "report.logp", n_rows, torch.float32, dev)
+        if report.new_len is not None:
+            _vector(report.new_len, "report.new_len", batch, torch.int32, dev)
+            if kv_len is None or report.new_len.data_ptr() == kv_len.data_ptr():
+                raise ValueError("report.new_len needs a kv_len, and one that it is not itself")
+
+    def call(st):
+        rep = report or DraftReport(n_rows, batch, dev, kv_len is not None)
+        ws = workspace
+        if ws is None:
+            ws = torch.empty(max(16, verify_drafts_workspace(n_rows)), dtype=torch.uint8, device=dev)
+        elif ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != dev:
+            raise ValueError("workspace must be a contiguous uint8 tensor on the logits' device")
+        d = DraftsC(target.data_ptr(), _ptr(draft), t_stride, d_stride, F32 if target.dtype == torch.float32 else BF16, vocab, batch, n_rows,
+                    min(int(max_rows), 0x7FFFFFFF), cu_rows.data_ptr(), tokens.data_ptr(), _ptr(kv_len), _ptr(temperature), accept_u.data_ptr(),
+                    sample_u.data_ptr())
+        r = DraftReportC(rep.tokens.data_ptr(), rep.n_emitted.data_ptr(), _ptr(rep.logp), _ptr(rep.new_len))
+        _check(lib().verillm_verify_drafts(C.byref(d), C.byref(r), ws.data_ptr(), ws.numel(), _ptr(status), st), "verillm_verify_drafts")
+        return rep
+
+    return _launch(dev, stream, call)
+
+
+def verify_drafts_workspace(n_rows: int) -> int:
+    """Bytes of workspace that verify_drafts needs for calls of up to n_rows rows."""
+    need = lib().verillm_verify_drafts_workspace(n_rows)
+    if need < 0:
+        raise VerillmError(int(need), "verillm_verify_drafts_workspace")
+    return int(need)
+
+
+# --------------------------------------------------------------------------- pages of a paged cache
+
+
+class KVPages(_Fixed):
+    """Who holds which page of a model's paged cache: caches (one KVCache per layer, one geometry), page_table int32 [batch][width], kv_len int32
+    [batch], refs int32 [n_pages] (table entries that name a page; 0: free).  The calls on it change these tensors and must follow one
+    another.  `alloc` makes an empty one.  Pass `status` (int32 [1], zeroed) to have device problems reported there; `check` reads it."""
+
+    def __init__(self, caches: Sequence[KVCache], page_table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor,
+                 status: Optional[torch.Tensor] = None):
+        caches = tuple(caches)
+        if not caches:
+            raise ValueError("at least one layer's cache")
+        dev = caches[0].device
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.device != dev or not page_table.is_contiguous():
+            raise ValueError(f"page_table must be a contiguous int32 [batch][width] tensor on {dev}")
+        batch, width = page_table.shape
+        _vector(kv_len, "kv_len", batch, torch.int32, dev)
+        _vector(refs, "refs", caches[0].n_pages, torch.int32, dev)
+        if any(c.device != dev for c in caches):
+            raise ValueError("all layers must be on one device")
+        _check_word(status, dev)
+        need = lib().verillm_kv_pages_workspace(batch, caches[0].n_pages)
+        if need < 0:
+            raise VerillmError(int(need), "verillm_kv_pages_workspace")
+        layers = (KVCacheC * len(caches))(*[c.c_struct for c in caches])
+        self.__dict__.update(caches=caches, page_table=page_table, kv_len=kv_len, refs=refs, status=status, device=dev, layers=layers, batch=batch,
+                             workspace=torch.empty(int(need), dtype=torch.uint8, device=dev),
+                             c_struct=KVPagesC(layers, len(caches), page_table.data_ptr(), kv_len.data_ptr(), refs.data_ptr(), batch, width))
+
+    @classmethod
+    def alloc(cls, n_layers: int, batch: int, width: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
+              dtype: torch.dtype = torch.bfloat16, device: str | torch.device = "cuda:0") -> "KVPages":
+        caches = [KVCache.alloc(n_pages, page_size, n_kv_heads, head_dim, dtype, device) for _ in range(n_layers)]
+        return cls(caches, *[torch.zeros(*s, dtype=torch.int32, device=device) for s in ((batch, width), (batch,), (n_pages,), (1,))])
+
+    def rows(self, cu_rows: torch.Tensor, max_rows: int) -> PagedRows:
+        """The rows of a paged call on these sequences."""
+        return PagedRows(self.page_table, cu_rows, self.kv_len, max_rows, self.status)
+
+    def check(self) -> None:
+        """Waits for the device and raises if a call reported a problem."""
+        if self.status is not None and int(self.status.item()) != 0:
+            raise RuntimeError(f"cache pages: device status {int(self.status.item())}")
+
+
+def kv_reserve(pages: KVPages, new_len: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Grows every sequence with new_len[b] > kv_len[b] (int32 [batch]) to new_len[b]: lowest free pages first, a copy of a partly filled page that
+    others hold too.  Where the free pages do not suffice, that sequence and the later ones stay as they are (DEV_NO_PAGES)."""
+    _vector(new_len, "new_len", pages.batch, torch.int32, pages.device)
+    _check(_launch(pages.device, stream, lambda st: lib().verillm_kv_reserve(
+        C.byref(pages.c_struct), new_len.data_ptr(), pages.workspace.data_ptr(), pages.workspace.numel(), _ptr(pages.status), st)), "verillm_kv_reserve")
+
+
+def kv_free(pages: KVPages, new_len: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Shortens every sequence with new_len[b] < kv_len[b] (int32 [batch]) to new_len[b] and lets go of the pages behind."""
+    _vector(new_len, "new_len", pages.batch, torch.int32, pages.device)
+    _check(_launch(pages.device, stream, lambda st: lib().verillm_kv_free(
+        C.byref(pages.c_struct), new_len.data_ptr(), _ptr(pages.status), st)), "verillm_kv_free")
+
+
+def kv_fork(pages: KVPages, src: torch.Tensor, dst: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """The empty sequences dst (int32 [n]) come to share what the sequences src hold."""
+    n = src.shape[0] if src.dim() == 1 else -1
+    _vector(src, "src", n, torch.int32, pages.device)
+    _vector(dst, "dst", n, torch.int32, pages.device)
+    _check(_launch(pages.device, stream, lambda st: lib().verillm_kv_fork(
+        C.byref(pages.c_struct), src.data_ptr(), dst.data_ptr(), n, pages.workspace.data_ptr(), pages.workspace.numel(), _ptr(pages.status), st)),
+        "verillm_kv_fork")
+
+
+def kv_compact(pages: KVPages, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Moves the pages in use to the front of the pools; returns their number (int32 [1], device)."""
+    def call(st):
+        used = torch.empty(1, dtype=torch.int32, device=pages.device)
+        _check(lib().verillm_kv_compact(C.byref(pages.c_struct), used.data_ptr(), pages.workspace.data_ptr(), pages.workspace.numel(),
+                                        _ptr(pages.status), st), "verillm_kv_compact")
+        return used
+
+    return _launch(pages.device, stream, call)
+
+
+def kv_copy(src: Sequence[KVCache], dst: Sequence[KVCache], src_pages: torch.Tensor, dst_pages: torch.Tensor,
+            status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Copies pages src_pages (int32 [n]) of the caches src, one per layer, to pages dst_pages of the caches dst; pairs with a -1 are left out."""
+    dev, n = dst[0].device, src_pages.shape[0] if src_pages.dim() == 1 else -1
+    if len(src) != len(dst) or any(c.device != dev for c in src) or any(c.device != dev for c in dst):
+        raise ValueError("src and dst must have the same number of layers, all on one device")
+    _vector(src_pages, "src_pages", n, torch.int32, dev)
+    _vector(dst_pages, "dst_pages", n, torch.int32, dev)
+    _check_word(status, dev)
+    a, b = [(KVCacheC * len(s))(*[c.c_struct for c in s]) for s in (src, dst)]
+    _check(_launch(dev, stream, lambda st: lib().verillm_kv_copy(a, b, len(a), src_pages.data_ptr(), dst_pages.data_ptr(), n, _ptr(status), st)),
+           "verillm_kv_copy")

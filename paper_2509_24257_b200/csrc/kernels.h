@@ -134,6 +134,67 @@ cudaError_t paged_attention_init();
 cudaError_t launch_paged_attention_tc(const PagedAttnParams& p, int grid, cudaStream_t stream);
 cudaError_t paged_attention_tc_init();
 
+// ------------------------------------------------------------------ 4-bit weights
+struct W4Params {
+    const uint8_t* codes;    // [n][k / 2]
+    const uint16_t* scales;  // bf16 [k / group][n]
+    int n, k, group;
+    const __nv_bfloat16* x;  // [rows][x_stride]
+    long long x_stride;
+    int rows;
+    const float* residual;  // optional [rows][res_stride]
+    long long res_stride;
+    void* y;  // bf16 or fp32 [rows][y_stride]
+    long long y_stride;
+    int out_f32;
+    int* status;
+    // set by the launcher
+    int groups, row_bytes, tiles, kw, ranks;
+};
+constexpr int kW4MaxK = 32768;
+constexpr int kW4MaxRows = 65536;
+cudaError_t launch_w4_matvec(W4Params p, int num_sms, cudaStream_t stream);
+cudaError_t launch_w4_quantise(const void* w, long long w_stride, void* codes, void* scales, int n, int k, int group, int num_sms, cudaStream_t stream);
+cudaError_t launch_w4_dequantise(const void* codes, const void* scales, void* out, long long out_stride, int out_f32, int n, int k, int group,
+                                 int num_sms, cudaStream_t stream);
+
+// ------------------------------------------------------------------ drafted tokens
+struct DraftParams {
+    const void *target, *draft;  // [n_rows] rows of `vocab` logits, bf16 or fp32; draft optional
+    long long target_stride, draft_stride;
+    int bf16_logits, vocab, batch, n_rows, max_rows;
+    const int *cu_rows, *tokens, *kv_len;
+    const float *temperature, *accept_u, *sample_u;  // [batch] (optional), [n_rows], [batch]
+    int *out_tokens, *n_emitted, *new_len;           // [n_rows], [batch], [batch] (optional)
+    float* logp;                                     // optional [n_rows]
+    float4* stats;                                   // [2][n_rows][splits]
+    int* status;
+    int splits, ranks;  // set by the launcher
+};
+constexpr int kDraftMaxRows = 256;  // per sequence
+constexpr int kDraftMaxVocab = 1 << 24;
+size_t draft_workspace(int n_rows);
+cudaError_t launch_verify_drafts(DraftParams p, int num_sms, cudaStream_t stream);
+
+// ------------------------------------------------------------------ pages of a paged cache
+constexpr int kPagesMaxLayers = 128;
+struct PoolSet {  // the pools of all layers
+    char *k[kPagesMaxLayers], *v[kPagesMaxLayers];
+    char *k_scale[kPagesMaxLayers], *v_scale[kPagesMaxLayers];
+};
+struct PagesDev {
+    int *page_table, *kv_len, *refs;
+    int batch, table_width, n_pages, page_shift, n_layers, page_bytes, scale_bytes;  // bytes of one pool's page (scales: 0 for bf16)
+    int* status;
+};
+size_t pages_workspace(int batch, int n_pages);
+cudaError_t launch_kv_reserve(const PagesDev& p, const PoolSet& pools, const int* new_len, int* ws, int num_sms, cudaStream_t stream);
+cudaError_t launch_kv_free(const PagesDev& p, const int* new_len, cudaStream_t stream);
+cudaError_t launch_kv_fork(const PagesDev& p, const int* src, const int* dst, int n, int* ws, cudaStream_t stream);
+cudaError_t launch_kv_compact(const PagesDev& p, const PoolSet& pools, int* n_used, int* ws, int num_sms, cudaStream_t stream);
+cudaError_t launch_kv_copy(const PagesDev& to, const PoolSet& dst_pools, const PoolSet& src_pools, int src_n_pages, const int* src, const int* dst, int n,
+                           int num_sms, cudaStream_t stream);
+
 // ------------------------------------------------------------------ small kernels
 cudaError_t launch_token_maps(const int* cu_seqlens_dev, int batch, int n_tokens, int* pos_of_token,
                               int* seq_of_token, cudaStream_t stream);

@@ -349,26 +349,34 @@ int ensure_decode_state(verillm_model* m, bool paged) {
     return VERILLM_OK;
 }
 
-// Checks a paged cache and the rows of a call and converts them to the kernels' views.
-int check_paged(const verillm_kv_cache* c, const verillm_kv_rows* r, PagedCacheDev* cd, PagedRowsDev* rd) {
-    if (!c || !r || !c->k || !c->v || !r->page_table || !r->cu_rows || !r->kv_len) return VERILLM_E_INVAL;
+// Checks a paged cache and converts it to the kernels' view.
+int check_cache(const verillm_kv_cache* c, PagedCacheDev* cd) {
+    if (!c || !c->k || !c->v) return VERILLM_E_INVAL;
     if (c->dtype != VERILLM_KV_BF16 && c->dtype != VERILLM_KV_E4M3 && c->dtype != VERILLM_KV_INT8) return VERILLM_E_INVAL;
     if (c->dtype != VERILLM_KV_BF16 && (!c->k_scale || !c->v_scale)) return VERILLM_E_INVAL;
-    if (c->n_pages < 1 || c->n_kv_heads < 1 || r->batch < 1 || r->table_width < 1 || r->n_rows < 0 || r->max_rows < 1) return VERILLM_E_INVAL;
+    if (c->n_pages < 1 || c->n_kv_heads < 1) return VERILLM_E_INVAL;
     if (c->head_dim != 64 && c->head_dim != 128) return VERILLM_E_SHAPE;
     int shift = 4;
     while (shift < 8 && (1 << shift) != c->page_size) ++shift;
     if ((1 << shift) != c->page_size) return VERILLM_E_SHAPE;
     // (page, kv head, row in page) is addressed as one 32-bit row number by the tile loads
     if (static_cast<int64_t>(c->n_pages) * c->n_kv_heads * c->page_size > 0x7FFFFFFFLL) return VERILLM_E_SHAPE;
-    // a block's walk over this many positions stays well inside the limit of the kernels' bounded waits
-    if (static_cast<int64_t>(r->table_width) * c->page_size > kPagedMaxPositions) return VERILLM_E_SHAPE;
     if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 31u) return VERILLM_E_SHAPE;  // 32-byte loads
     if (c->dtype != VERILLM_KV_BF16 && ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 15u)) return VERILLM_E_SHAPE;
     cd->k = c->k; cd->v = c->v;
     cd->k_scale = c->dtype == VERILLM_KV_BF16 ? nullptr : c->k_scale;
     cd->v_scale = c->dtype == VERILLM_KV_BF16 ? nullptr : c->v_scale;
     cd->n_pages = c->n_pages; cd->page_shift = shift; cd->n_kv_heads = c->n_kv_heads; cd->head_dim = c->head_dim; cd->dtype = c->dtype;
+    return VERILLM_OK;
+}
+// Checks a paged cache and the rows of a call and converts them to the kernels' views.
+int check_paged(const verillm_kv_cache* c, const verillm_kv_rows* r, PagedCacheDev* cd, PagedRowsDev* rd) {
+    if (!c || !r || !r->page_table || !r->cu_rows || !r->kv_len) return VERILLM_E_INVAL;
+    if (r->batch < 1 || r->table_width < 1 || r->n_rows < 0 || r->max_rows < 1) return VERILLM_E_INVAL;
+    const int rc = check_cache(c, cd);
+    if (rc) return rc;
+    // a block's walk over this many positions stays well inside the limit of the kernels' bounded waits
+    if (static_cast<int64_t>(r->table_width) * c->page_size > kPagedMaxPositions) return VERILLM_E_SHAPE;
     rd->page_table = r->page_table; rd->cu_rows = r->cu_rows; rd->kv_len = r->kv_len;
     rd->table_width = r->table_width; rd->batch = r->batch; rd->n_rows = r->n_rows;
     rd->max_rows = std::min(r->max_rows, std::max(r->n_rows, 1));  // no sequence has more rows than the buffers
@@ -391,6 +399,56 @@ int current_sms(int* num_sms) {
     if (sms[dev] == 0) CU_TRY(cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev));
     *num_sms = sms[dev];
     return VERILLM_OK;
+}
+
+// Checks 4-bit weights; fills n, k, group and the pointers.
+int check_w4(const verillm_w4* w, W4Params* p) {
+    if (!w || !w->codes || !w->scales || w->n < 1 || w->k < 1) return VERILLM_E_INVAL;
+    if (w->group != 32 && w->group != 64 && w->group != 128) return VERILLM_E_SHAPE;
+    if (w->k % w->group || w->n % 8) return VERILLM_E_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(w->codes) & 15u) || (reinterpret_cast<uintptr_t>(w->scales) & 15u)) return VERILLM_E_SHAPE;
+    p->codes = static_cast<const uint8_t*>(w->codes);
+    p->scales = static_cast<const uint16_t*>(w->scales);
+    p->n = w->n; p->k = w->k; p->group = w->group;
+    return VERILLM_OK;
+}
+
+// Checks the layers of a cache (all of one geometry) and converts them to the kernels' view.
+int check_layers(const verillm_kv_cache* layers, int32_t n_layers, PagesDev* d, PoolSet* pools) {
+    if (!layers || n_layers < 1) return VERILLM_E_INVAL;
+    if (n_layers > kPagesMaxLayers) return VERILLM_E_SHAPE;
+    const verillm_kv_cache& a = layers[0];
+    for (int l = 0; l < n_layers; ++l) {
+        const verillm_kv_cache& c = layers[l];
+        PagedCacheDev cd;
+        const int rc = check_cache(&c, &cd);
+        if (rc) return rc;
+        if (c.n_pages != a.n_pages || c.page_size != a.page_size || c.n_kv_heads != a.n_kv_heads || c.head_dim != a.head_dim || c.dtype != a.dtype) return VERILLM_E_SHAPE;
+        pools->k[l] = static_cast<char*>(cd.k);
+        pools->v[l] = static_cast<char*>(cd.v);
+        pools->k_scale[l] = reinterpret_cast<char*>(cd.k_scale);
+        pools->v_scale[l] = reinterpret_cast<char*>(cd.v_scale);
+        d->page_shift = cd.page_shift;
+    }
+    const int64_t vecs = static_cast<int64_t>(a.n_kv_heads) * a.page_size, bytes = vecs * a.head_dim * (a.dtype == VERILLM_KV_BF16 ? 2 : 1);
+    if (bytes > (1LL << 30)) return VERILLM_E_SHAPE;  // a page's bytes are counted in 32 bits
+    d->n_pages = a.n_pages; d->n_layers = n_layers;
+    d->page_bytes = static_cast<int>(bytes);
+    d->scale_bytes = a.dtype == VERILLM_KV_BF16 ? 0 : static_cast<int>(vecs * 4);
+    return VERILLM_OK;
+}
+int check_pages(const verillm_kv_pages* g, PagesDev* d, PoolSet* pools) {
+    if (!g || !g->page_table || !g->kv_len || !g->refs || g->batch < 1 || g->table_width < 1) return VERILLM_E_INVAL;
+    const int rc = check_layers(g->layers, g->n_layers, d, pools);
+    if (rc) return rc;
+    if ((static_cast<int64_t>(g->table_width) << d->page_shift) > kPagedMaxPositions) return VERILLM_E_SHAPE;
+    d->page_table = g->page_table; d->kv_len = g->kv_len; d->refs = g->refs;
+    d->batch = g->batch; d->table_width = g->table_width;
+    return VERILLM_OK;
+}
+int check_pages_workspace(const PagesDev& d, const void* ws, int64_t bytes) {
+    if (!ws) return VERILLM_E_INVAL;
+    return (reinterpret_cast<uintptr_t>(ws) & 15u) || bytes < static_cast<int64_t>(pages_workspace(d.batch, d.n_pages)) ? VERILLM_E_SHAPE : VERILLM_OK;
 }
 
 // The paged cache of one layer of the decode path.
@@ -1290,6 +1348,154 @@ int verillm_op_attention_paged(const verillm_kv_cache* cache, const verillm_kv_r
     if ((rc = ensure_init())) return rc;
     p.q = q; p.q_stride = q_stride; p.out = out; p.out_stride = out_stride; p.lse = lse; p.n_heads = n_heads; p.status = status;
     CU_TRY(launch_paged_attention(p, workspace, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int verillm_w4_quantise(const void* w, int64_t w_stride, const verillm_w4* out, void* cuda_stream) {
+    W4Params p;
+    int rc = check_w4(out, &p), sms = 0;
+    if (rc || (rc = check_rows(w, w_stride, p.k, 8)) || (rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    CU_TRY(launch_w4_quantise(w, w_stride, out->codes, out->scales, p.n, p.k, p.group, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int verillm_w4_dequantise(const verillm_w4* w, void* out, int64_t out_stride, int32_t out_dtype, void* cuda_stream) {
+    W4Params p;
+    int rc = check_w4(w, &p), sms = 0;
+    if (rc) return rc;
+    if (out_dtype != VERILLM_BF16 && out_dtype != VERILLM_F32) return VERILLM_E_INVAL;
+    if ((rc = check_rows(out, out_stride, p.k, 8)) || (rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    CU_TRY(launch_w4_dequantise(p.codes, p.scales, out, out_stride, out_dtype == VERILLM_F32, p.n, p.k, p.group, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int verillm_op_w4_matvec(const verillm_w4* w, const void* x, int64_t x_stride, int32_t rows, const float* residual, int64_t residual_stride,
+                         void* y, int64_t y_stride, int32_t out_dtype, int32_t* status, void* cuda_stream) {
+    W4Params p;
+    std::memset(&p, 0, sizeof(p));
+    int rc = check_w4(w, &p), sms = 0;
+    if (rc) return rc;
+    if (rows < 0 || (out_dtype != VERILLM_BF16 && out_dtype != VERILLM_F32)) return VERILLM_E_INVAL;
+    if (rows == 0) return VERILLM_OK;
+    if (p.k > kW4MaxK || rows > kW4MaxRows) return VERILLM_E_SHAPE;
+    if ((rc = check_rows(x, x_stride, p.k, 8))) return rc;
+    if (!y || y == x) return VERILLM_E_INVAL;
+    if (y_stride < p.n || (residual && residual_stride < p.n)) return VERILLM_E_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(y) & (out_dtype == VERILLM_F32 ? 3u : 1u)) || (reinterpret_cast<uintptr_t>(residual) & 3u)) return VERILLM_E_SHAPE;
+    // the residual may be the output itself, entry by entry
+    if (y == residual && (out_dtype != VERILLM_F32 || y_stride != residual_stride)) return VERILLM_E_INVAL;
+    if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    p.x = static_cast<const bf16*>(x); p.x_stride = x_stride; p.rows = rows;
+    p.residual = residual; p.res_stride = residual_stride;
+    p.y = y; p.y_stride = y_stride; p.out_f32 = out_dtype == VERILLM_F32; p.status = status;
+    CU_TRY(launch_w4_matvec(p, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int64_t verillm_verify_drafts_workspace(int32_t n_rows) {
+    return n_rows < 0 ? VERILLM_E_INVAL : static_cast<int64_t>(draft_workspace(n_rows));
+}
+
+int verillm_verify_drafts(const verillm_drafts* d, const verillm_draft_report* rep, void* workspace, int64_t workspace_bytes, int32_t* status,
+                          void* cuda_stream) {
+    if (!d || !rep || d->batch < 1 || d->n_rows < 0 || d->max_rows < 1 || d->vocab < 1) return VERILLM_E_INVAL;
+    if (d->dtype != VERILLM_BF16 && d->dtype != VERILLM_F32) return VERILLM_E_INVAL;
+    if (!d->cu_rows || !rep->n_emitted || (rep->new_len && !d->kv_len)) return VERILLM_E_INVAL;
+    if (d->max_rows > kDraftMaxRows || d->vocab > kDraftMaxVocab) return VERILLM_E_SHAPE;
+    if (d->n_rows > 0) {
+        if (!d->target || !d->tokens || !d->accept_u || !d->sample_u || !rep->tokens || !workspace) return VERILLM_E_INVAL;
+        const uintptr_t mask = d->dtype == VERILLM_F32 ? 3u : 1u;
+        if (((reinterpret_cast<uintptr_t>(d->target) | reinterpret_cast<uintptr_t>(d->draft)) & mask) || d->target_stride < d->vocab ||
+            (d->draft && d->draft_stride < d->vocab))
+            return VERILLM_E_SHAPE;
+        if ((reinterpret_cast<uintptr_t>(workspace) & 15u) || workspace_bytes < verillm_verify_drafts_workspace(d->n_rows)) return VERILLM_E_SHAPE;
+    }
+    DraftParams p;
+    std::memset(&p, 0, sizeof(p));
+    int rc = ensure_init(), sms = 0;
+    if (rc || (rc = current_sms(&sms))) return rc;
+    p.target = d->target; p.draft = d->draft; p.target_stride = d->target_stride; p.draft_stride = d->draft_stride;
+    p.bf16_logits = d->dtype == VERILLM_BF16; p.vocab = d->vocab; p.batch = d->batch; p.n_rows = d->n_rows; p.max_rows = d->max_rows;
+    p.cu_rows = d->cu_rows; p.tokens = d->tokens; p.kv_len = d->kv_len; p.temperature = d->temperature;
+    p.accept_u = d->accept_u; p.sample_u = d->sample_u;
+    p.out_tokens = rep->tokens; p.n_emitted = rep->n_emitted; p.new_len = rep->new_len; p.logp = rep->logp;
+    p.stats = static_cast<float4*>(workspace); p.status = status;
+    CU_TRY(launch_verify_drafts(p, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int64_t verillm_kv_pages_workspace(int32_t batch, int32_t n_pages) {
+    return batch < 1 || n_pages < 1 ? VERILLM_E_INVAL : static_cast<int64_t>(pages_workspace(batch, n_pages));
+}
+
+int verillm_kv_reserve(const verillm_kv_pages* pages, const int32_t* new_len, void* workspace, int64_t workspace_bytes, int32_t* status,
+                       void* cuda_stream) {
+    PagesDev d;
+    PoolSet pools;
+    int rc = check_pages(pages, &d, &pools), sms = 0;
+    if (rc || (rc = check_pages_workspace(d, workspace, workspace_bytes))) return rc;
+    if (!new_len) return VERILLM_E_INVAL;
+    if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    d.status = status;
+    CU_TRY(launch_kv_reserve(d, pools, new_len, static_cast<int*>(workspace), sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int verillm_kv_free(const verillm_kv_pages* pages, const int32_t* new_len, int32_t* status, void* cuda_stream) {
+    PagesDev d;
+    PoolSet pools;
+    int rc = check_pages(pages, &d, &pools);
+    if (rc) return rc;
+    if (!new_len) return VERILLM_E_INVAL;
+    if ((rc = ensure_init())) return rc;
+    d.status = status;
+    CU_TRY(launch_kv_free(d, new_len, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int verillm_kv_fork(const verillm_kv_pages* pages, const int32_t* src, const int32_t* dst, int32_t n, void* workspace, int64_t workspace_bytes,
+                    int32_t* status, void* cuda_stream) {
+    PagesDev d;
+    PoolSet pools;
+    int rc = check_pages(pages, &d, &pools);
+    if (rc) return rc;
+    if (n < 0) return VERILLM_E_INVAL;
+    if (n == 0) return VERILLM_OK;
+    if (!src || !dst) return VERILLM_E_INVAL;
+    if (n > d.batch) return VERILLM_E_SHAPE;  // destinations are different sequences
+    if ((rc = check_pages_workspace(d, workspace, workspace_bytes)) || (rc = ensure_init())) return rc;
+    d.status = status;
+    CU_TRY(launch_kv_fork(d, src, dst, n, static_cast<int*>(workspace), reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int verillm_kv_compact(const verillm_kv_pages* pages, int32_t* n_used, void* workspace, int64_t workspace_bytes, int32_t* status, void* cuda_stream) {
+    PagesDev d;
+    PoolSet pools;
+    int rc = check_pages(pages, &d, &pools), sms = 0;
+    if (rc || (rc = check_pages_workspace(d, workspace, workspace_bytes))) return rc;
+    if (!n_used) return VERILLM_E_INVAL;
+    if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    d.status = status;
+    CU_TRY(launch_kv_compact(d, pools, n_used, static_cast<int*>(workspace), sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
+    return VERILLM_OK;
+}
+
+int verillm_kv_copy(const verillm_kv_cache* src_layers, const verillm_kv_cache* dst_layers, int32_t n_layers, const int32_t* src_pages,
+                    const int32_t* dst_pages, int32_t n, int32_t* status, void* cuda_stream) {
+    PagesDev s, d;
+    PoolSet from, to;
+    std::memset(&d, 0, sizeof(d));
+    int rc = check_layers(src_layers, n_layers, &s, &from), sms = 0;
+    if (rc || (rc = check_layers(dst_layers, n_layers, &d, &to))) return rc;
+    const verillm_kv_cache &a = src_layers[0], &b = dst_layers[0];
+    if (a.page_size != b.page_size || a.n_kv_heads != b.n_kv_heads || a.head_dim != b.head_dim || a.dtype != b.dtype) return VERILLM_E_SHAPE;
+    if (n < 0) return VERILLM_E_INVAL;
+    if (n == 0) return VERILLM_OK;
+    if (!src_pages || !dst_pages) return VERILLM_E_INVAL;
+    if ((rc = ensure_init()) || (rc = current_sms(&sms))) return rc;
+    d.status = status;
+    CU_TRY(launch_kv_copy(d, to, from, s.n_pages, src_pages, dst_pages, n, sms, reinterpret_cast<cudaStream_t>(cuda_stream)));
     return VERILLM_OK;
 }
 
