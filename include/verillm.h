@@ -400,7 +400,7 @@ int verillm_w4_dequantise(const verillm_w4 *w, void *out, int64_t out_stride, in
  *  y         DEVICE in out_dtype, rows y_stride entries apart, not overlapping x
  *  status    optional DEVICE word, raised from 0 to VERILLM_DEV_WAIT_TIMEOUT when a wait inside the kernel gave up
  * Products are exact and sums fp32; the order of the sums follows from n, k, rows and the GPU's number of SMs.  Allocates nothing; make the first call on a device outside
- * a capture.  Errors: E_INVAL, E_SHAPE (alignment, group, k > 32768, rows > 65536), E_ARCH, E_CUDA. */
+ * a capture.  Errors: E_INVAL, E_SHAPE (alignment, group, rows > 65536), E_ARCH, E_CUDA. */
 int verillm_op_w4_matvec(const verillm_w4 *w, const void *x, int64_t x_stride, int32_t rows, const float *residual, int64_t residual_stride,
                          void *y, int64_t y_stride, int32_t out_dtype, int32_t *status, void *cuda_stream);
 

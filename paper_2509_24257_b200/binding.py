@@ -838,12 +838,13 @@ def op_w4_matvec(x: torch.Tensor, w: W4Weights, residual: Optional[torch.Tensor]
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("dtype must be bf16 or float32")
     _check_word(status, w.device)
+    L = lib()
 
     def call(st):
         y = torch.empty(rows, w.n, dtype=dtype, device=w.device) if out is None else out
         y_stride = w.n if out is None else _strided(y, "out", rows, w.n, dtype, w.device)
-        _check(lib().verillm_op_w4_matvec(C.byref(w.c_struct), x.data_ptr(), stride, rows, _ptr(residual), res_stride, y.data_ptr(), y_stride,
-                                          F32 if dtype == torch.float32 else BF16, _ptr(status), st), "verillm_op_w4_matvec")
+        _check(L.verillm_op_w4_matvec(C.byref(w.c_struct), x.data_ptr(), stride, rows, _ptr(residual), res_stride, y.data_ptr(), y_stride,
+                                      F32 if dtype == torch.float32 else BF16, _ptr(status), st), "verillm_op_w4_matvec")
         return y
 
     return _launch(w.device, stream, call)

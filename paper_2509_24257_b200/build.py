@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libverillm.so")
 SOURCES = ["gemm_tcgen05.cu", "attention_tcgen05.cu", "elementwise.cu", "merkle.cu", "paged_kv.cu", "paged_attention.cu", "paged_attention_tcgen05.cu",
-           "w4.cu", "drafts.cu", "pages.cu", "verillm.cu"]
+           "w4.cu", "w4_tcgen05.cu", "drafts.cu", "pages.cu", "verillm.cu"]
 HEADERS = ["common.cuh", "compare.cuh", "paged.cuh", "kernels.h", os.path.join("..", "..", "include", "verillm.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

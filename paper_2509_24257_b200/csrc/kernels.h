@@ -151,8 +151,12 @@ struct W4Params {
     // set by the launcher
     int groups, row_bytes, tiles, kw, ranks;
 };
-constexpr int kW4MaxK = 32768;
 constexpr int kW4MaxRows = 65536;
+constexpr int kW4FewRows = 8;  // rows of the kernel that keeps x in registers
+// More rows, or longer inputs; called by launch_w4_matvec.
+cudaError_t launch_w4_tc(W4Params p, int num_sms, cudaStream_t stream);
+cudaError_t w4_tc_init();
+cudaError_t w4_init();
 cudaError_t launch_w4_matvec(W4Params p, int num_sms, cudaStream_t stream);
 cudaError_t launch_w4_quantise(const void* w, long long w_stride, void* codes, void* scales, int n, int k, int group, int num_sms, cudaStream_t stream);
 cudaError_t launch_w4_dequantise(const void* codes, const void* scales, void* out, long long out_stride, int out_f32, int n, int k, int group,

@@ -148,6 +148,7 @@ int ensure_init() {
     CU_TRY(attention_tc_init());
     CU_TRY(merkle_init());
     CU_TRY(paged_attention_init());
+    CU_TRY(w4_init());
     done[dev] = true;
     return VERILLM_OK;
 }
@@ -1377,7 +1378,7 @@ int verillm_op_w4_matvec(const verillm_w4* w, const void* x, int64_t x_stride, i
     if (rc) return rc;
     if (rows < 0 || (out_dtype != VERILLM_BF16 && out_dtype != VERILLM_F32)) return VERILLM_E_INVAL;
     if (rows == 0) return VERILLM_OK;
-    if (p.k > kW4MaxK || rows > kW4MaxRows) return VERILLM_E_SHAPE;
+    if (rows > kW4MaxRows) return VERILLM_E_SHAPE;
     if ((rc = check_rows(x, x_stride, p.k, 8))) return rc;
     if (!y || y == x) return VERILLM_E_INVAL;
     if (y_stride < p.n || (residual && residual_stride < p.n)) return VERILLM_E_SHAPE;

@@ -4,12 +4,11 @@
 // Arithmetic: a code is exact in bf16, so the tensor cores form the products x * c of a group exactly and add them in fp32; the
 // group's sum is then multiplied by its scale and added to the running sum, both in fp32.  No weight is rounded again.
 //
-// w4_rows_kernel, up to 8 rows of x: bound by the weights' bytes.  A tile is 16 outputs; a warp takes CH chunks of 128 inputs of
-// it and always the same chunks, so that its part of x stays in registers as operand fragments while weights stream from
-// global memory straight into the other operand (the next tile's are requested before this one's are used).  The order of the inputs inside a
-// product is free as long as both operands agree: a lane takes G / 4 consecutive ones, G / 8 bytes of codes.  A code becomes
-// bf16 by its bits alone (0x4300 | u is 128 + u) and one exact subtraction of 136.  Long inputs are divided over a cluster, whose CTAs leave
-// their sums of a tile in the shared memory of the tile's owner; sums are formed in a fixed order.
+// w4_rows_kernel, up to 8 rows of x: bound by the weights' bytes.  A warp takes 16 outputs and all their inputs, or a part of them; weights stream from
+// global memory straight into one operand of mma.sync, four chunks ahead, x is the other from shared memory, where the CTA laid it out in fragment
+// order.  Warps are independent of one another until their sums meet.  The order of the inputs inside a product is free as long as both operands
+// agree: a lane takes G / 4 consecutive ones, G / 8 bytes of codes.  A code becomes bf16 by its bits alone (0x4300 | u is 128 + u) and one exact
+// subtraction of 136.
 #include "common.cuh"
 #include "kernels.h"
 
@@ -19,8 +18,8 @@ namespace {
 
 typedef __nv_bfloat16 bf16;
 
-constexpr int W4_WARPS = 16;
-constexpr int W4_THREADS = W4_WARPS * 32;
+constexpr int W4_MAX_WARPS = 16;
+constexpr int W4_MAX_SMEM = 224 * 1024;
 constexpr int W4_CHUNK = 128;  // inputs per chunk
 
 __device__ __forceinline__ void mma_bf16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -41,7 +40,7 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t q, int i) {
 
 // WORDS 32-bit words that are read once
 template <int WORDS>
-__device__ __forceinline__ void load_words(const void* p, uint32_t* w) {
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
     if (WORDS == 4)
         asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1 % WORDS]), "=r"(w[2 % WORDS]), "=r"(w[3 % WORDS]) : "l"(p));
     else if (WORDS == 2)
@@ -49,63 +48,11 @@ __device__ __forceinline__ void load_words(const void* p, uint32_t* w) {
     else
         asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
 }
-
-// A warp's share of one tile: codes of rows g and g + 8 and their scales.
-template <int CH, int G>
-struct TileRegs {
-    static constexpr int SB = W4_CHUNK / G, WORDS = G / 32;  // groups per chunk, words per lane and group
-    uint32_t lo[CH][4], hi[CH][4];
-    uint16_t slo[CH][SB], shi[CH][SB];
-
-    __device__ __forceinline__ void load(const W4Params& p, int tile, int chunk0, int lane) {
-        const int g = lane >> 2, t = lane & 3;
-        const int n0 = min(tile * 16 + g, p.n - 1), n1 = min(tile * 16 + g + 8, p.n - 1);  // rows behind the last are computed and not stored
-        const uint8_t* base = p.codes + t * (G / 8);
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-#pragma unroll
-            for (int b = 0; b < SB; ++b) {
-                const int group = (chunk0 + c) * SB + b;
-                const bool in = group < p.groups;
-                if (in) {
-                    const size_t at = static_cast<size_t>(group) * (G / 2);
-                    load_words<WORDS>(base + static_cast<size_t>(n0) * p.row_bytes + at, lo[c] + b * WORDS);
-                    load_words<WORDS>(base + static_cast<size_t>(n1) * p.row_bytes + at, hi[c] + b * WORDS);
-                    slo[c][b] = __ldg(p.scales + static_cast<size_t>(group) * p.n + n0);
-                    shi[c][b] = __ldg(p.scales + static_cast<size_t>(group) * p.n + n1);
-                } else {
-#pragma unroll
-                    for (int w = 0; w < WORDS; ++w) lo[c][b * WORDS + w] = hi[c][b * WORDS + w] = 0x88888888u;
-                    slo[c][b] = shi[c][b] = 0;
-                }
-            }
-        }
-    }
-};
-
-// acc += the share's products; x: operand fragments of the same inputs.
-template <int CH, int G>
-__device__ __forceinline__ void multiply(const TileRegs<CH, G>& w, const uint32_t (&x)[CH][4][4], float (&acc)[4]) {
-    constexpr int SB = TileRegs<CH, G>::SB, WORDS = TileRegs<CH, G>::WORDS;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-#pragma unroll
-        for (int b = 0; b < SB; ++b) {
-            float d[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) {
-                const int k = b * WORDS + i;
-                const uint32_t lo = w.lo[c][k], hi = w.hi[c][k];
-                mma_bf16_16816(d, code_pair(lo, 0), code_pair(hi, 0), code_pair(lo, 1), code_pair(hi, 1), x[c][k][0], x[c][k][1]);
-                mma_bf16_16816(d, code_pair(lo, 2), code_pair(hi, 2), code_pair(lo, 3), code_pair(hi, 3), x[c][k][2], x[c][k][3]);
-            }
-            const float s0 = bf16_bits_to_float(w.slo[c][b]), s1 = bf16_bits_to_float(w.shi[c][b]);
-            acc[0] = fmaf(d[0], s0, acc[0]);
-            acc[1] = fmaf(d[1], s0, acc[1]);
-            acc[2] = fmaf(d[2], s1, acc[2]);
-            acc[3] = fmaf(d[3], s1, acc[3]);
-        }
-    }
+// The bits of a bf16 in a 32-bit register: nothing here waits for them.
+__device__ __forceinline__ uint32_t load_bits16(const uint16_t* p) {
+    uint32_t v;
+    asm volatile("ld.global.nc.u16 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
 }
 
 // One value of the result: the residual added, rounded to the output's type.
@@ -116,135 +63,115 @@ __device__ __forceinline__ void store_y(const W4Params& p, int row, int n, float
     else reinterpret_cast<bf16*>(p.y)[row * p.y_stride + n] = __float2bfloat16_rn(v);
 }
 
-__device__ __forceinline__ void store_cluster(uint32_t addr, const float4& v) {
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
-}
-__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, int* status) {
-    const long long t0 = clock64();
-    while (true) {
-        uint32_t ok;
-        asm volatile(
-            "{\n"
-            ".reg .pred p;\n"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n"
-            "selp.u32 %0, 1, 0, p;\n"
-            "}\n"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity), "r"(kWaitSuspendNs)
-            : "memory");
-        if (ok) return true;
-        if (clock64() - t0 > kWaitLimitCycles) {
-            if (status) atomicCAS(status, 0, VERILLM_DEV_WAIT_TIMEOUT);
-            return false;
-        }
-    }
-}
+// The codes of one chunk of a tile, outputs g and g + 8, and their scales.
+template <int G>
+struct Chunk {
+    static constexpr int SB = W4_CHUNK / G, WORDS = G / 32;  // groups per chunk, words per lane and group
+    uint32_t lo[4], hi[4], slo[SB], shi[SB];
 
-// KW warps share a tile's inputs; the CTA's W4_WARPS / KW groups of warps take neighbouring tiles.  Clusters (of `ranks` CTAs, KW =
-// W4_WARPS) divide longer inputs.  All warps of a cluster make the same number of steps.
-template <int CH, int G>
-__global__ void __launch_bounds__(W4_THREADS) w4_rows_kernel(const W4Params p) {
-    __shared__ float4 part[2][W4_WARPS][32];
-    __shared__ float4 joined[2][8][32];  // [slot][rank][lane] of the tiles that this CTA owns
-    __shared__ uint64_t bars[2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int g = lane >> 2, t = lane & 3;
-    const int kw = p.kw, sub = warp / kw, kidx = warp - sub * kw, per_step = W4_WARPS / kw;
-    const int ranks = p.ranks, rank = ranks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-    const int cluster = blockIdx.x / ranks, n_clusters = gridDim.x / ranks;
-    const int chunk0 = (rank * kw + kidx) * CH;
-    const int row0 = blockIdx.y * 8;
-
-    TileRegs<CH, G> a, b;
-    int step = cluster;
-    a.load(p, min(step * per_step + sub, p.tiles - 1), chunk0, lane);
-
-    // this lane's operand fragments of x: row row0 + g, inputs of its words; pairs (i, i + 4) like the codes'
-    uint32_t x[CH][4][4];
-    constexpr int SB = W4_CHUNK / G, WORDS = G / 32;
+    // code: this lane's bytes of the chunk's first group for output g; hi_bytes, hi_scale: from there to output g + 8
+    __device__ __forceinline__ void load(const W4Params& p, const uint8_t* code, const uint16_t* scale, int group, ptrdiff_t hi_bytes, int hi_scale) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
+        for (int b = 0; b < SB; ++b) {
+            if (SB == 1 || group + b < p.groups) {
+                load_words<WORDS>(code + b * (G / 2), lo + b * WORDS);
+                load_words<WORDS>(code + b * (G / 2) + hi_bytes, hi + b * WORDS);
+                slo[b] = load_bits16(scale + static_cast<size_t>(b) * p.n);
+                shi[b] = load_bits16(scale + static_cast<size_t>(b) * p.n + hi_scale);
+            } else {  // behind the last input: x is zero there
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int group = (chunk0 + c) * SB + k / WORDS;
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (row0 + g < p.rows && group < p.groups)
-                v = __ldg(reinterpret_cast<const uint4*>(p.x + (row0 + g) * p.x_stride + static_cast<size_t>(group) * G + t * (G / 4) + (k % WORDS) * 8));
-            x[c][k][0] = __byte_perm(v.x, v.z, 0x5410);
-            x[c][k][1] = __byte_perm(v.x, v.z, 0x7632);
-            x[c][k][2] = __byte_perm(v.y, v.w, 0x5410);
-            x[c][k][3] = __byte_perm(v.y, v.w, 0x7632);
+                for (int w = 0; w < WORDS; ++w) lo[b * WORDS + w] = hi[b * WORDS + w] = 0x88888888u;
+                slo[b] = shi[b] = 0;
+            }
         }
     }
-    if (ranks > 1) {
-        if (threadIdx.x == 0) {
-            mbar_init(smem_u32(&bars[0]), ranks);
-            mbar_init(smem_u32(&bars[1]), ranks);
-            fence_mbar_init();
+    // acc += the chunk's products; x: the lane's fragments of the same inputs in shared memory, `words` apart
+    __device__ __forceinline__ void multiply(uint32_t x, uint32_t words, float (&acc)[4]) const {
+#pragma unroll
+        for (int b = 0; b < SB; ++b) {
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) {
+                const int k = b * WORDS + i;
+                uint32_t f[4];
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(f[0]), "=r"(f[1]), "=r"(f[2]), "=r"(f[3]) : "r"(x + k * words));
+                mma_bf16_16816(d, code_pair(lo[k], 0), code_pair(hi[k], 0), code_pair(lo[k], 1), code_pair(hi[k], 1), f[0], f[1]);
+                mma_bf16_16816(d, code_pair(lo[k], 2), code_pair(hi[k], 2), code_pair(lo[k], 3), code_pair(hi[k], 3), f[2], f[3]);
+            }
+            const float s0 = bf16_bits_to_float(slo[b]), s1 = bf16_bits_to_float(shi[b]);
+            acc[0] = fmaf(d[0], s0, acc[0]);
+            acc[1] = fmaf(d[1], s0, acc[1]);
+            acc[2] = fmaf(d[2], s1, acc[2]);
+            acc[3] = fmaf(d[3], s1, acc[3]);
         }
-        cluster_arrive();
-        cluster_wait();
     }
+};
 
-    int it = 0, owned = 0;
-    auto one = [&](TileRegs<CH, G>& now, TileRegs<CH, G>& next) {
-        const int tile = step * per_step + sub;
-        step += n_clusters;
-        if (step * per_step < p.tiles) next.load(p, min(step * per_step + sub, p.tiles - 1), chunk0, lane);
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-        multiply<CH, G>(now, x, acc);
-        float4 sum = make_float4(acc[0], acc[1], acc[2], acc[3]);
-        const int buf = it & 1;
-        if (kw > 1) {
-            part[buf][warp][lane] = sum;
-            __syncthreads();
-        }
-        // one warp of each tile adds the shares in order; the others go on (the buffer is written again two steps later, behind a
-        // barrier that this warp has to reach first)
-        if (kidx == it % kw) {
-            if (kw > 1) {
-                sum = part[buf][sub * kw][lane];
-                for (int w = 1; w < kw; ++w) {
-                    const float4 v = part[buf][sub * kw + w][lane];
-                    sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
-                }
-            }
-            bool mine = true;
-            if (ranks > 1) {
-                // the tile's owner gathers the cluster's sums.  A CTA is less than `ranks` steps ahead of another, because it waits for
-                // all of them at each tile that it owns, so two slots suffice.
-                const int owner = it % ranks, slot = (it / ranks) & 1;
-                store_cluster(map_to_cta(smem_u32(&joined[slot][rank][lane]), owner), sum);
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&bars[slot]), owner));
-                mine = owner == rank;
-                if (mine) {
-                    wait_cluster(smem_u32(&bars[slot]), (owned >> 1) & 1, p.status);
-                    sum = joined[slot][0][lane];
-                    for (int r = 1; r < ranks; ++r) {
-                        const float4 v = joined[slot][r][lane];
-                        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
-                    }
-                }
-            }
-            if (mine && tile < p.tiles) {
-                store_y(p, row0 + 2 * t, tile * 16 + g, sum.x);
-                store_y(p, row0 + 2 * t + 1, tile * 16 + g, sum.y);
-                store_y(p, row0 + 2 * t, tile * 16 + g + 8, sum.z);
-                store_y(p, row0 + 2 * t + 1, tile * 16 + g + 8, sum.w);
-            }
-        }
-        if (ranks > 1 && it % ranks == rank) ++owned;
-        ++it;
-    };
-    while (step * per_step < p.tiles) {
-        one(a, b);
-        if (step * per_step >= p.tiles) break;
-        one(b, a);
+// A warp takes every kw-th part of the inputs of one tile of 16 outputs; nothing but the final sum of its kw warps is shared.
+template <int G>
+__global__ void __launch_bounds__(W4_MAX_WARPS * 32) w4_rows_kernel(const W4Params p) {
+    constexpr int SB = Chunk<G>::SB, WORDS = Chunk<G>::WORDS, AHEAD = 4;
+    extern __shared__ __align__(16) uint8_t x_smem[];  // [chunk][word][row][t] pieces of 16 bytes; after them the warps' sums
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int kw = p.kw, sub = warp / kw, kidx = warp - sub * kw, tile = blockIdx.x * (blockDim.x / 32 / kw) + sub;
+    const int chunks = (p.k + W4_CHUNK - 1) / W4_CHUNK;
+    const int c0 = chunks * kidx / kw, c1 = tile < p.tiles ? chunks * (kidx + 1) / kw : c0;
+
+    // (n is a multiple of 8: where a tile has 8 outputs only, they are computed twice)
+    const int n0 = min(tile, p.tiles - 1) * 16 + g;
+    const bool whole = n0 - g + 16 <= p.n;
+    const ptrdiff_t hi_bytes = whole ? 8 * static_cast<ptrdiff_t>(p.row_bytes) : 0;
+    const int hi_scale = whole ? 8 : 0;
+    const uint8_t* code = p.codes + static_cast<size_t>(n0) * p.row_bytes + c0 * 64 + t * (G / 8);
+    const uint16_t* scale = p.scales + static_cast<size_t>(c0) * SB * p.n + n0;
+    Chunk<G> w[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (c0 + i < c1) w[i].load(p, code + i * 64, scale + static_cast<size_t>(i) * SB * p.n, (c0 + i) * SB, hi_bytes, hi_scale);
+
+    // x in the order in which fragments are read, pairs (i, i + 4) like the codes'
+    for (int i = threadIdx.x; i < p.rows * chunks * 16; i += blockDim.x) {
+        const int row = i / (chunks * 16), k8 = i - row * chunks * 16;
+        const int c = k8 >> 4, in = k8 & 15, b = in * 8 / G, rest = in - b * (G / 8);  // chunk, group within it, eighth of the group's inputs
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (k8 * 8 < p.k) v = __ldg(reinterpret_cast<const uint4*>(p.x + row * p.x_stride) + k8);
+        const int at = ((c * 4 + b * WORDS + rest % WORDS) * p.rows + row) * 4 + rest / WORDS;
+        reinterpret_cast<uint4*>(x_smem)[at] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
     }
-    if (ranks > 1) {  // no CTA leaves while another may still write to its shared memory
-        cluster_arrive();
-        cluster_wait();
+    __syncthreads();
+
+    // (rows that do not exist are some other row again: their columns are not stored)
+    const uint32_t words = p.rows * 64, per_chunk = 4 * words;
+    uint32_t x = smem_u32(x_smem) + c0 * per_chunk + (min(g, p.rows - 1) * 4 + t) * 16;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int c = c0; c < c1; c += AHEAD) {
+        code += AHEAD * 64;
+        scale += static_cast<size_t>(AHEAD) * SB * p.n;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (c + i >= c1) break;
+            w[i].multiply(x, words, acc);
+            x += per_chunk;
+            if (c + AHEAD + i < c1) w[i].load(p, code + i * 64, scale + static_cast<size_t>(i) * SB * p.n, (c + AHEAD + i) * SB, hi_bytes, hi_scale);
+        }
+    }
+    float4 sum = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    if (kw > 1) {
+        float4* part = reinterpret_cast<float4*>(x_smem + static_cast<size_t>(chunks) * per_chunk);
+        part[warp * 32 + lane] = sum;
+        __syncthreads();
+        if (kidx != 0) return;
+        for (int i = 1; i < kw; ++i) {  // in the order of the inputs
+            const float4 v = part[(warp + i) * 32 + lane];
+            sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+        }
+    }
+    if (tile >= p.tiles) return;
+    store_y(p, 2 * t, n0, sum.x);
+    store_y(p, 2 * t + 1, n0, sum.y);
+    if (whole) {
+        store_y(p, 2 * t, n0 + 8, sum.z);
+        store_y(p, 2 * t + 1, n0 + 8, sum.w);
     }
 }
 
@@ -310,48 +237,46 @@ __global__ void __launch_bounds__(256) w4_dequantise_kernel(const uint8_t* __res
     }
 }
 
-template <int CH, int G>
-cudaError_t launch_rows(W4Params& p, int num_sms, cudaStream_t stream) {
-    const int per_step = W4_WARPS / p.kw;
-    const int steps = (p.tiles + per_step - 1) / per_step;
-    const int clusters = max(1, min(steps, num_sms / p.ranks));
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(clusters * p.ranks, (p.rows + 7) / 8);
-    cfg.blockDim = dim3(W4_THREADS);
-    cfg.stream = stream;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = p.ranks;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = p.ranks > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, w4_rows_kernel<CH, G>, p);
-}
+// Shared memory of the kernel for few rows: x, and the warps' sums.
+size_t rows_smem(const W4Params& p, int warps) { return static_cast<size_t>((p.k + W4_CHUNK - 1) / W4_CHUNK) * W4_CHUNK * p.rows * 2 + warps * 512; }
 
-template <int CH>
-cudaError_t launch_group(W4Params& p, int num_sms, cudaStream_t stream) {
-    switch (p.group) {
-        case 32: return launch_rows<CH, 32>(p, num_sms, stream);
-        case 64: return launch_rows<CH, 64>(p, num_sms, stream);
-        default: return launch_rows<CH, 128>(p, num_sms, stream);
+template <int G>
+cudaError_t launch_rows(W4Params& p, int num_sms, cudaStream_t stream) {
+    // Small CTAs balance best; as few per SM as x leaves room for, 16 warps in any case.
+    const int per_sm = rows_smem(p, 4) <= 55 * 1024 ? 4 : rows_smem(p, 8) <= 110 * 1024 ? 2 : 1;
+    int warps = 16 / per_sm;
+    // Inputs are divided among a CTA's warps as long as all CTAs run at once, up to 8 ways (16 in one CTA per SM).
+    p.kw = 1;
+    const int chunks = (p.k + W4_CHUNK - 1) / W4_CHUNK;
+    auto ctas = [&](int kw, int w) { return (p.tiles + w / kw - 1) / (w / kw); };
+    while (p.kw < 8 && p.kw * 2 <= chunks && ctas(p.kw * 2, warps < p.kw * 2 ? p.kw * 2 : warps) * (warps < p.kw * 2 ? p.kw * 2 / warps : 1) <= per_sm * num_sms) {
+        p.kw *= 2;
+        if (warps < p.kw) warps = p.kw;
     }
+    w4_rows_kernel<G><<<ctas(p.kw, warps), warps * 32, rows_smem(p, warps), stream>>>(p);
+    return cudaGetLastError();
 }
 
 }  // namespace
+
+cudaError_t w4_init() {
+    cudaError_t e = cudaFuncSetAttribute(w4_rows_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, W4_MAX_SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_rows_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, W4_MAX_SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(w4_rows_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, W4_MAX_SMEM);
+    if (e == cudaSuccess) e = w4_tc_init();
+    return e;
+}
 
 cudaError_t launch_w4_matvec(W4Params p, int num_sms, cudaStream_t stream) {
     p.groups = p.k / p.group;
     p.row_bytes = p.k / 2;
     p.tiles = (p.n + 15) / 16;
-    const int chunks = (p.k + W4_CHUNK - 1) / W4_CHUNK;
-    // one chunk per warp while a CTA's warps suffice, two then, and a cluster for what is longer
-    const int ch = chunks > W4_WARPS ? 2 : 1, warps = (chunks + ch - 1) / ch;
-    p.kw = 1;
-    while (p.kw < warps && p.kw < W4_WARPS) p.kw *= 2;
-    p.ranks = 1;
-    while (p.ranks * p.kw < warps) p.ranks *= 2;
-    if (p.ranks > 8) return cudaErrorInvalidValue;
-    return ch == 1 ? launch_group<1>(p, num_sms, stream) : launch_group<2>(p, num_sms, stream);
+    if (p.rows > kW4FewRows || rows_smem(p, W4_MAX_WARPS) > W4_MAX_SMEM) return launch_w4_tc(p, num_sms, stream);
+    switch (p.group) {
+        case 32: return launch_rows<32>(p, num_sms, stream);
+        case 64: return launch_rows<64>(p, num_sms, stream);
+        default: return launch_rows<128>(p, num_sms, stream);
+    }
 }
 
 cudaError_t launch_w4_quantise(const void* w, long long w_stride, void* codes, void* scales, int n, int k, int group, int num_sms, cudaStream_t stream) {

@@ -46,7 +46,7 @@ def _x(rows, k, seed=1):
 
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("n,k", [(8, 128), (16, 256), (24, 384), (40, 1024), (4096, 128), (1000, 2048), (136, 4096), (2056, 4224), (72, 8192), (264, 14336),
-                                 (24, 28672), (16, 32768)])
+                                 (24, 28672), (16, 32768), (24, 33792), (136, 65664)])
 def test_sizes(n, k, group):
     _, w4 = _weights(n, k, group)
     for rows in (1, 5, 8):
