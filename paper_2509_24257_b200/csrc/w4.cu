@@ -28,14 +28,19 @@ __device__ __forceinline__ void mma_bf16_16816(float (&d)[4], uint32_t a0, uint3
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&r);
+// The same without an addend.
+__device__ __forceinline__ void mma_bf16_16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // Codes i and i + 4 of a word as a pair of bf16.
 __device__ __forceinline__ uint32_t code_pair(uint32_t q, int i) {
-    return sub_bf16x2(((q >> (4 * i)) & 0x000F000Fu) | 0x43004300u, 0x43084308u);
+    uint32_t r;  // (the compiler makes two instructions of an and and an or with constants)
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(q >> (4 * i)), "r"(0x000F000Fu), "r"(0x43004300u));
+    asm("sub.rn.bf16x2 %0, %0, %1;" : "+r"(r) : "r"(0x43084308u));
+    return r;
 }
 
 // WORDS 32-bit words that are read once
@@ -69,15 +74,15 @@ struct Chunk {
     static constexpr int SB = W4_CHUNK / G, WORDS = G / 32;  // groups per chunk, words per lane and group
     uint32_t lo[4], hi[4], slo[SB], shi[SB];
 
-    // code: this lane's bytes of the chunk's first group for output g; hi_bytes, hi_scale: from there to output g + 8
-    __device__ __forceinline__ void load(const W4Params& p, const uint8_t* code, const uint16_t* scale, int group, ptrdiff_t hi_bytes, int hi_scale) {
+    // code: this lane's bytes of the chunk's first group for output g, code_hi for output g + 8; scale, scale_hi likewise
+    __device__ __forceinline__ void load(const W4Params& p, const uint8_t* code, const uint8_t* code_hi, const uint16_t* scale, const uint16_t* scale_hi, int group) {
 #pragma unroll
         for (int b = 0; b < SB; ++b) {
             if (SB == 1 || group + b < p.groups) {
                 load_words<WORDS>(code + b * (G / 2), lo + b * WORDS);
-                load_words<WORDS>(code + b * (G / 2) + hi_bytes, hi + b * WORDS);
+                load_words<WORDS>(code_hi + b * (G / 2), hi + b * WORDS);
                 slo[b] = load_bits16(scale + static_cast<size_t>(b) * p.n);
-                shi[b] = load_bits16(scale + static_cast<size_t>(b) * p.n + hi_scale);
+                shi[b] = load_bits16(scale_hi + static_cast<size_t>(b) * p.n);
             } else {  // behind the last input: x is zero there
 #pragma unroll
                 for (int w = 0; w < WORDS; ++w) lo[b * WORDS + w] = hi[b * WORDS + w] = 0x88888888u;
@@ -89,13 +94,14 @@ struct Chunk {
     __device__ __forceinline__ void multiply(uint32_t x, uint32_t words, float (&acc)[4]) const {
 #pragma unroll
         for (int b = 0; b < SB; ++b) {
-            float d[4] = {0.f, 0.f, 0.f, 0.f};
+            float d[4];
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) {
                 const int k = b * WORDS + i;
                 uint32_t f[4];
                 asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(f[0]), "=r"(f[1]), "=r"(f[2]), "=r"(f[3]) : "r"(x + k * words));
-                mma_bf16_16816(d, code_pair(lo[k], 0), code_pair(hi[k], 0), code_pair(lo[k], 1), code_pair(hi[k], 1), f[0], f[1]);
+                if (i == 0) mma_bf16_16816_first(d, code_pair(lo[k], 0), code_pair(hi[k], 0), code_pair(lo[k], 1), code_pair(hi[k], 1), f[0], f[1]);
+                else mma_bf16_16816(d, code_pair(lo[k], 0), code_pair(hi[k], 0), code_pair(lo[k], 1), code_pair(hi[k], 1), f[0], f[1]);
                 mma_bf16_16816(d, code_pair(lo[k], 2), code_pair(hi[k], 2), code_pair(lo[k], 3), code_pair(hi[k], 3), f[2], f[3]);
             }
             const float s0 = bf16_bits_to_float(slo[b]), s1 = bf16_bits_to_float(shi[b]);
@@ -120,23 +126,43 @@ __global__ void __launch_bounds__(W4_MAX_WARPS * 32) w4_rows_kernel(const W4Para
     // (n is a multiple of 8: where a tile has 8 outputs only, they are computed twice)
     const int n0 = min(tile, p.tiles - 1) * 16 + g;
     const bool whole = n0 - g + 16 <= p.n;
-    const ptrdiff_t hi_bytes = whole ? 8 * static_cast<ptrdiff_t>(p.row_bytes) : 0;
-    const int hi_scale = whole ? 8 : 0;
-    const uint8_t* code = p.codes + static_cast<size_t>(n0) * p.row_bytes + c0 * 64 + t * (G / 8);
-    const uint16_t* scale = p.scales + static_cast<size_t>(c0) * SB * p.n + n0;
+    const uint8_t *code = p.codes + static_cast<size_t>(n0) * p.row_bytes + c0 * 64 + t * (G / 8), *code_hi = code + (whole ? 8 * static_cast<ptrdiff_t>(p.row_bytes) : 0);
+    const uint16_t *scale = p.scales + static_cast<size_t>(c0) * SB * p.n + n0, *scale_hi = scale + (whole ? 8 : 0);
+    const ptrdiff_t scale_step = static_cast<ptrdiff_t>(SB) * p.n;
     Chunk<G> w[AHEAD];
+    auto load = [&](int i, int c) {  // the next chunk, number c, into stage i
+        w[i].load(p, code, code_hi, scale, scale_hi, c * SB);
+        code += 64;
+        code_hi += 64;
+        scale += scale_step;
+        scale_hi += scale_step;
+    };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
-        if (c0 + i < c1) w[i].load(p, code + i * 64, scale + static_cast<size_t>(i) * SB * p.n, (c0 + i) * SB, hi_bytes, hi_scale);
+        if (c0 + i < c1) load(i, c0 + i);
 
     // x in the order in which fragments are read, pairs (i, i + 4) like the codes'
-    for (int i = threadIdx.x; i < p.rows * chunks * 16; i += blockDim.x) {
-        const int row = i / (chunks * 16), k8 = i - row * chunks * 16;
-        const int c = k8 >> 4, in = k8 & 15, b = in * 8 / G, rest = in - b * (G / 8);  // chunk, group within it, eighth of the group's inputs
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (k8 * 8 < p.k) v = __ldg(reinterpret_cast<const uint4*>(p.x + row * p.x_stride) + k8);
-        const int at = ((c * 4 + b * WORDS + rest % WORDS) * p.rows + row) * 4 + rest / WORDS;
-        reinterpret_cast<uint4*>(x_smem)[at] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+    {
+        constexpr int U = 4;  // loads in flight
+        const unsigned per_row = chunks * 16, total = p.rows * per_row;
+        for (unsigned i0 = threadIdx.x; i0 < total; i0 += U * blockDim.x) {
+            uint4 v[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const unsigned i = i0 + j * blockDim.x, row = i / per_row, k8 = i - row * per_row;
+                v[j] = make_uint4(0u, 0u, 0u, 0u);
+                if (i < total && k8 * 8 < p.k) v[j] = __ldg(reinterpret_cast<const uint4*>(p.x + row * p.x_stride) + k8);
+            }
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const unsigned i = i0 + j * blockDim.x, row = i / per_row, k8 = i - row * per_row;
+                if (i >= total) break;
+                const int c = k8 >> 4, in = k8 & 15, b = in * 8 / G, rest = in - b * (G / 8);  // chunk, group within it, eighth of the group's inputs
+                const int at = ((c * 4 + b * WORDS + rest % WORDS) * p.rows + row) * 4 + rest / WORDS;
+                reinterpret_cast<uint4*>(x_smem)[at] = make_uint4(__byte_perm(v[j].x, v[j].z, 0x5410), __byte_perm(v[j].x, v[j].z, 0x7632),
+                                                                  __byte_perm(v[j].y, v[j].w, 0x5410), __byte_perm(v[j].y, v[j].w, 0x7632));
+            }
+        }
     }
     __syncthreads();
 
@@ -145,14 +171,12 @@ __global__ void __launch_bounds__(W4_MAX_WARPS * 32) w4_rows_kernel(const W4Para
     uint32_t x = smem_u32(x_smem) + c0 * per_chunk + (min(g, p.rows - 1) * 4 + t) * 16;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
     for (int c = c0; c < c1; c += AHEAD) {
-        code += AHEAD * 64;
-        scale += static_cast<size_t>(AHEAD) * SB * p.n;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             if (c + i >= c1) break;
             w[i].multiply(x, words, acc);
             x += per_chunk;
-            if (c + AHEAD + i < c1) w[i].load(p, code + i * 64, scale + static_cast<size_t>(i) * SB * p.n, (c + AHEAD + i) * SB, hi_bytes, hi_scale);
+            if (c + AHEAD + i < c1) load(i, c + AHEAD + i);
         }
     }
     float4 sum = make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -242,16 +266,20 @@ size_t rows_smem(const W4Params& p, int warps) { return static_cast<size_t>((p.k
 
 template <int G>
 cudaError_t launch_rows(W4Params& p, int num_sms, cudaStream_t stream) {
-    // Small CTAs balance best; as few per SM as x leaves room for, 16 warps in any case.
-    const int per_sm = rows_smem(p, 4) <= 55 * 1024 ? 4 : rows_smem(p, 8) <= 110 * 1024 ? 2 : 1;
-    int warps = 16 / per_sm;
-    // Inputs are divided among a CTA's warps as long as all CTAs run at once, up to 8 ways (16 in one CTA per SM).
-    p.kw = 1;
+    // Small CTAs balance best as long as laying out x costs each little (4 warps, four CTAs per SM); with more of x one CTA of 16 warps per SM.
+    // Measured, 8 rows x 28672 x 4096: 19 us with 16 warps, 41 with 4; one row x 57344 x 8192: 63 and 57.
+    const bool small = rows_smem(p, 4) <= 20 * 1024;
+    int warps = small ? 4 : 16;
+    // A tile's inputs are divided among kw of a CTA's warps while all CTAs run at once and a warp keeps four chunks (eight ways: half as many
+    // CTAs per SM, for long inputs only).  One row x 4096 x 14336: 10.6 us eight ways, 12.3 four, 34.8 undivided.
     const int chunks = (p.k + W4_CHUNK - 1) / W4_CHUNK;
     auto ctas = [&](int kw, int w) { return (p.tiles + w / kw - 1) / (w / kw); };
-    while (p.kw < 8 && p.kw * 2 <= chunks && ctas(p.kw * 2, warps < p.kw * 2 ? p.kw * 2 : warps) * (warps < p.kw * 2 ? p.kw * 2 / warps : 1) <= per_sm * num_sms) {
-        p.kw *= 2;
-        if (warps < p.kw) warps = p.kw;
+    p.kw = 1;
+    while (p.kw < 8) {
+        const int kw = 2 * p.kw, w = kw > warps ? kw : warps;
+        if (chunks < (small && kw == 8 ? 64 : 4 * kw) || ctas(kw, w) > num_sms * (16 / w)) break;
+        p.kw = kw;
+        warps = w;
     }
     w4_rows_kernel<G><<<ctas(p.kw, warps), warps * 32, rows_smem(p, warps), stream>>>(p);
     return cudaGetLastError();

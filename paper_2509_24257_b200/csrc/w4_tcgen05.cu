@@ -91,10 +91,9 @@ __device__ __forceinline__ void widen(uint32_t q, uint32_t* r) {
     const uint32_t t = q >> 4;
     const uint32_t m[4] = {__byte_perm(q, t, 0x4400), __byte_perm(q, t, 0x5511), __byte_perm(q, t, 0x6622), __byte_perm(q, t, 0x7733)};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t v = (m[i] & 0x000F000Fu) | 0x43004300u, s = 0x43084308u;
-        const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&s));
-        r[i] = *reinterpret_cast<const uint32_t*>(&d);
+    for (int i = 0; i < 4; ++i) {  // (the compiler makes two instructions of an and and an or with constants)
+        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r[i]) : "r"(m[i]), "r"(0x000F000Fu), "r"(0x43004300u));
+        asm("sub.rn.bf16x2 %0, %0, %1;" : "+r"(r[i]) : "r"(0x43084308u));
     }
 }
 
