@@ -38,18 +38,22 @@ struct Row {
         off = static_cast<int>((reinterpret_cast<uintptr_t>(base) & 15u) / sizeof(T));
         blocks = (v + off + E - 1) / E;
     }
-    // Entries [j0, j0 + E), -inf outside the row.
-    __device__ __forceinline__ void load(int j0, float (&f)[E]) const {
-        if (j0 >= 0 && j0 + E <= vocab && (reinterpret_cast<uintptr_t>(base + j0) & 15u) == 0) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(base + j0));
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    // Entries [j0, j0 + E) as they lie in memory, -inf outside the row.
+    __device__ __forceinline__ uint4 load(int j0) const {
+        if (j0 >= 0 && j0 + E <= vocab && (reinterpret_cast<uintptr_t>(base + j0) & 15u) == 0) return __ldg(reinterpret_cast<const uint4*>(base + j0));
+        uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < E; ++i)
-                f[i] = sizeof(T) == 4 ? __uint_as_float(w[i % 4]) : i & 1 ? bf16_hi(w[i / 2 % 4]) : bf16_lo(w[i / 2 % 4]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i) f[i] = j0 + i >= 0 && j0 + i < vocab ? entry(j0 + i) : -INFINITY;
+        for (int i = 0; i < 4; ++i) {
+            if (sizeof(T) == 4) w[i] = __float_as_uint(in(j0 + i) ? entry(j0 + i) : -INFINITY);
+            else w[i] = (__float_as_uint(in(j0 + 2 * i) ? entry(j0 + 2 * i) : -INFINITY) >> 16) | __float_as_uint(in(j0 + 2 * i + 1) ? entry(j0 + 2 * i + 1) : -INFINITY);
         }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ bool in(int j) const { return j >= 0 && j < vocab; }
+    // Entry i of what load gave
+    __device__ static __forceinline__ float get(const uint4& v, int i) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        return sizeof(T) == 4 ? __uint_as_float(w[i % 4]) : i & 1 ? bf16_hi(w[i / 2 % 4]) : bf16_lo(w[i / 2 % 4]);
     }
     __device__ __forceinline__ float entry(int j) const {
         if (sizeof(T) == 4) return __ldg(reinterpret_cast<const float*>(base) + j);
@@ -61,6 +65,24 @@ __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// Pairs of fp32 operations
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 
 __device__ __forceinline__ bool temp_valid(float t) { return t == 0.f || (t >= kMinTemp && t <= kMaxTemp); }
@@ -98,16 +120,12 @@ __global__ void __launch_bounds__(DR_THREADS) draft_rows_kernel(const DraftParam
     const int b0 = blockIdx.y * per, b1 = min(b0 + per, r.blocks);
 
     // the first blocks are on their way while the row's sequence is looked up
-    float f[DR_UNROLL][E];
+    uint4 raw[DR_UNROLL];
+    constexpr uint32_t kNothing = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;  // -inf
     auto fetch = [&](int b) {
 #pragma unroll
         for (int u = 0; u < DR_UNROLL; ++u) {
-            if (b + u * DR_THREADS < b1) {
-                r.load((b + u * DR_THREADS) * E - r.off, f[u]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < E; ++i) f[u][i] = -INFINITY;
-            }
+            raw[u] = b + u * DR_THREADS < b1 ? r.load((b + u * DR_THREADS) * E - r.off) : make_uint4(kNothing, kNothing, kNothing, kNothing);
         }
     };
     fetch(b0 + tid);
@@ -129,13 +147,16 @@ __global__ void __launch_bounds__(DR_THREADS) draft_rows_kernel(const DraftParam
     float m = -INFINITY, s = 0.f;
     int at = 0x7FFFFFFF;
     for (int b = b0 + tid; b < b1; b += DR_THREADS * DR_UNROLL) {
-        if (b != b0 + tid) fetch(b);
+        uint4 now[DR_UNROLL];
+#pragma unroll
+        for (int u = 0; u < DR_UNROLL; ++u) now[u] = raw[u];
+        fetch(b + DR_THREADS * DR_UNROLL);  // the next blocks are on their way under these
         if (greedy) {
 #pragma unroll
             for (int u = 0; u < DR_UNROLL; ++u)
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    const float v = f[u][i];
+                    const float v = r.get(now[u], i);
                     if (v > m) {
                         m = v;
                         at = (b + u * DR_THREADS) * E - r.off + i;
@@ -148,19 +169,22 @@ __global__ void __launch_bounds__(DR_THREADS) draft_rows_kernel(const DraftParam
 #pragma unroll
         for (int u = 0; u < DR_UNROLL; ++u)
 #pragma unroll
-            for (int i = 0; i < E; ++i) top = fmaxf(top, f[u][i]);
+            for (int i = 0; i < E; ++i) top = fmaxf(top, r.get(now[u], i));
         // an entry of -inf with nothing finite before it: any finite reference does
         const float ref = top == -INFINITY ? 0.f : top;
-        float add[DR_UNROLL];
+        const uint64_t less = pack2(-ref, -ref), c2 = pack2(c, c);
+        uint64_t add[2] = {0, 0};
 #pragma unroll
-        for (int u = 0; u < DR_UNROLL; ++u) {
-            add[u] = 0.f;
+        for (int u = 0; u < DR_UNROLL; ++u)
 #pragma unroll
-            for (int i = 0; i < E; ++i) add[u] += exp2_approx((f[u][i] - ref) * c);
-        }
-        s = m == -INFINITY ? s : s * exp2_approx((m - ref) * c);
-#pragma unroll
-        for (int u = 0; u < DR_UNROLL; ++u) s += add[u];
+            for (int i = 0; i < E; i += 2) {
+                float x, y;
+                unpack2(mul2(add2(pack2(r.get(now[u], i), r.get(now[u], i + 1)), less), c2), x, y);
+                add[i / 2 & 1] = add2(add[i / 2 & 1], pack2(exp2_approx(x), exp2_approx(y)));
+            }
+        float s0, s1;
+        unpack2(add2(add[0], add[1]), s0, s1);
+        s = (m == -INFINITY ? s : s * exp2_approx((m - ref) * c)) + (s0 + s1);
         m = top;
     }
     // join: (m, s) pairs by their larger maximum, in a fixed order
@@ -190,33 +214,38 @@ __global__ void __launch_bounds__(DR_THREADS) draft_rows_kernel(const DraftParam
     }
 }
 
-// exp(d / T) for d <= 0 in 64 bits: 2^(j/64) from a table and a polynomial of degree 4 for the rest, |r| <= ln 2 / 128 (a table-driven
-// exponential after P. T. P. Tang, 1989), relative error below 1e-13.
+// exp((l - top) / T) for l <= top in 64 bits: 2^n times a polynomial for the rest, |r| <= 1/2, degree 8 through the nine Chebyshev points, relative error
+// below 2e-12; a factor that all entries of a row share may differ more (top / T is rounded once).  No table: reads of one in shared memory
+// conflict (a draw of 64 sequences: 134 us with one of 256 entries).
 struct Exp64 {
-    const double* table;  // 2^(j / 64), shared memory
-    double inv_t, scale;  // 1 / T, 64 / (T ln 2)
-    float floor;          // d below this: 0
-    __device__ __forceinline__ double operator()(float l, float top) const {
-        const float df = l - top;
-        if (!(df > floor)) return 0.0;
-        const double d = static_cast<double>(l) - static_cast<double>(top);
-        const double big = fma(d, scale, 6755399441055744.0);  // 1.5 2^52: the nearest integer in the low bits
-        const int n = __double2loint(big);
-        const double r = fma(big - 6755399441055744.0, -kLn2 / 64.0, d * inv_t);
-        double e = fma(r, 1.0 / 24.0, 1.0 / 6.0);
-        e = fma(r, e, 0.5);
+    double scale;  // log2 e / T
+    float floor;   // differences of logits below this: 0
+    __device__ __forceinline__ double shift(float top) const { return -static_cast<double>(top) * scale; }
+    __device__ __forceinline__ double operator()(float l, float top, double shift) const {
+        // the float as a double by its bits: a conversion instruction costs as much as four additions (no subnormals, infinities or NaN matter here)
+        const int bits = __float_as_int(l);
+        const double d = __hiloint2double(((bits >> 3) & 0x8FFFFFFF) + 0x38000000, bits << 29);
+        const double x = fma(d, scale, shift), big = x + 6755399441055744.0;  // 1.5 2^52: the nearest integer in the low bits
+        const double r = x - (big - 6755399441055744.0);
+        double e = fma(r, 1.3255224878668817e-06, 1.5310079402249296e-05);
+        e = fma(r, e, 0.00015403455852453838);
+        e = fma(r, e, 0.0013333450568000645);
+        e = fma(r, e, 0.009618129159402558);
+        e = fma(r, e, 0.05550410941205933);
+        e = fma(r, e, 0.2402265069581299);
+        e = fma(r, e, 0.6931471805459335);
         e = fma(r, e, 1.0);
-        e = fma(r, e, 1.0);
-        e *= table[n & 63];
-        return __hiloint2double(__double2hiint(e) + ((n >> 6) << 20), __double2loint(e));
+        e = __hiloint2double(__double2hiint(e) + (__double2loint(big) << 20), __double2loint(e));
+        return l - top > floor ? e : 0.0;
     }
 };
 
-// What the running sums are made of.
+// What is drawn from: weights of a row's entries.
 struct Weights {
     int kind;       // 0: p; 1: p without token x; 2: max(0, p - q)
     int x;
     float pm, qm;   // the rows' maxima
+    double ps, qs;  // their shifts
     double a, b;    // kind 2: a e_p - b e_q, a = sum e_q, b = sum e_p
 };
 
@@ -234,35 +263,32 @@ __device__ __forceinline__ double load_cluster64(uint32_t addr) {
 template <typename T>
 __device__ __forceinline__ void weights_of(const Row<T>& rp, const Row<T>& rq, const Exp64& ex, const Weights& w, int j0, double (&v)[Row<T>::E]) {
     constexpr int E = Row<T>::E;
-    float f[E];
-    rp.load(j0, f);
+    const uint4 f = rp.load(j0);
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = ex(f[i], w.pm);
+    for (int i = 0; i < E; ++i) v[i] = ex(rp.get(f, i), w.pm, w.ps);
     if (w.kind == 1) {
 #pragma unroll
         for (int i = 0; i < E; ++i)
             if (j0 + i == w.x) v[i] = 0.0;
     } else if (w.kind == 2) {
-        rq.load(j0, f);
+        const uint4 g = rq.load(j0);
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = fmax(0.0, __dsub_rn(__dmul_rn(w.a, v[i]), __dmul_rn(w.b, ex(f[i], w.qm))));  // (no fma: 0 where p = q)
+        for (int i = 0; i < E; ++i) v[i] = fmax(0.0, __dsub_rn(__dmul_rn(w.a, v[i]), __dmul_rn(w.b, ex(rq.get(g, i), w.qm, w.qs))));  // (no fma: 0 where p = q)
     }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftParams p) {
     constexpr int E = Row<T>::E;
-    __shared__ double table[64];
-    __shared__ double warp_tot[2][DV_WARPS];
-    __shared__ double cta_tot[4];  // two pairs, used in turn
-    __shared__ float sm_pm[kDraftMaxRows], sm_ps[kDraftMaxRows], sm_qm[kDraftMaxRows];
+    __shared__ double warp_tot[4][DV_WARPS];
+    __shared__ double cta_tot[2][4];  // used in turn
+    __shared__ float sm_pm[kDraftMaxRows], sm_ps[kDraftMaxRows], sm_qm[kDraftMaxRows], sm_qs[kDraftMaxRows];
     __shared__ int sm_code[kDraftMaxRows], sm_arg[kDraftMaxRows];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ranks = p.ranks, rank = ranks > 1 ? static_cast<int>(cluster_ctarank()) : 0, b = blockIdx.x / ranks;
     const SeqRows s = seq_rows(p, b);
     const float temp = temp_of(p, b);
     const bool greedy = temp == 0.f;
-    if (tid < 64) table[tid] = exp2(tid / 64.0);
     pdl_wait();
     if (s.bad && tid == 0 && rank == 0) raise(p.status, VERILLM_DEV_ROWS_RANGE);
     if (s.bad || s.n == 0 || !temp_valid(temp)) {  // (the whole cluster)
@@ -280,11 +306,8 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
         return;
     }
     const float c = greedy ? 0.f : static_cast<float>(kLog2e / static_cast<double>(temp));
-    const double inv_t = greedy ? 1.0 : 1.0 / static_cast<double>(temp);
     Exp64 ex;
-    ex.table = table;
-    ex.inv_t = inv_t;
-    ex.scale = inv_t * (64.0 / kLn2);
+    ex.scale = greedy ? 1.0 : kLog2e / static_cast<double>(temp);
     ex.floor = fmaxf(-700.f * temp, -3.0e38f);
 
     // ---- every row: its statistics and what fp32 says of the token that follows it
@@ -357,6 +380,7 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
             sm_pm[i] = pm;
             sm_ps[i] = ps;
             sm_qm[i] = qm;
+            sm_qs[i] = qs;
         }
     }
     __syncthreads();
@@ -367,72 +391,108 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     const int wb0 = rank * per_cta + warp * per_warp;
     const int wb1 = min(min(wb0 + per_warp, (rank + 1) * per_cta), blocks);
     int turn = 0;
-    // totals of two running sums over the cluster; before[k]: of the CTAs before this one
-    auto cluster_totals = [&](double v0, double v1, double (&total)[2], double (&mine)[2]) {
-        v0 = warp_sum64(v0);
-        v1 = warp_sum64(v1);
-        if (lane == 0) {
-            warp_tot[0][warp] = v0;
-            warp_tot[1][warp] = v1;
+    // One pass over row i in 64 bits.  Per warp, per CTA and over the cluster: 0 = sum of e_p (without token x for kind 1); for kind 2 that and 1 = sum of e_q
+    // over the entries with p <= q, 2 and 3 the same over those with p > q, as fp32 sees it (it errs only where p and q agree to 10^-6, which changes the sum of
+    // max(0, p - q) by less than 10^-12).
+    Weights w;
+    double total[4];  // of the row: 0 sum of e_p, 1 of e_q, 2 and 3 over p > q
+    double cta_part = 0.0;  // lane 4 r + i: sum i of CTA r
+    auto pass = [&](int i, int kind, int x) {
+        const Row<T> rp(p.target, p.target_stride, s.row0 + i, p.vocab), rq(p.draft ? p.draft : p.target, p.draft ? p.draft_stride : p.target_stride, s.row0 + i, p.vocab);
+        w.kind = kind;
+        w.x = x;
+        w.pm = sm_pm[i];
+        w.qm = sm_qm[i];
+        w.ps = ex.shift(w.pm);
+        w.qs = ex.shift(w.qm);
+        const float kp = -w.pm * c - log2f(sm_ps[i]), kq = -w.qm * c - log2f(sm_qs[i]);
+        double v[4] = {0.0, 0.0, 0.0, 0.0};
+        // blocks are fetched two steps ahead
+        auto fetch = [&](int k, uint4& f, uint4& g) {
+            const int j0 = k < wb1 ? k * E - rp.off : p.vocab;
+            f = rp.load(j0);
+            if (kind == 2) g = rq.load(j0);
+        };
+        uint4 f0, f1, g0 = make_uint4(0u, 0u, 0u, 0u), g1 = g0;
+        fetch(wb0 + lane, f0, g0);
+        fetch(wb0 + lane + 32, f1, g1);
+        for (int k = wb0 + lane; k - lane < wb1; k += 32) {
+            const uint4 f = f0, g = g0;
+            f0 = f1;
+            g0 = g1;
+            fetch(k + 64, f1, g1);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float lp = rp.get(f, e);
+                double ep = ex(lp, w.pm, w.ps);
+                if (kind == 1 && k * E - rp.off + e == x) ep = 0.0;
+                if (kind == 2) {
+                    const float lq = rq.get(g, e);
+                    const double eq = ex(lq, w.qm, w.qs);
+                    if (fmaf(lp, c, kp) > fmaf(lq, c, kq)) {
+                        v[2] += ep;
+                        v[3] += eq;
+                    } else {
+                        v[0] += ep;
+                        v[1] += eq;
+                    }
+                } else {
+                    v[0] += ep;
+                }
+            }
+        }
+        __syncthreads();  // the sums of an earlier pass have been read
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const double sum = warp_sum64(v[q]);
+            if (lane == 0) warp_tot[q][warp] = sum;
         }
         __syncthreads();
-        mine[0] = mine[1] = 0.0;
-        for (int w = 0; w < DV_WARPS; ++w) {
-            mine[0] += warp_tot[0][w];
-            mine[1] += warp_tot[1][w];
-        }
-        if (tid == 0) {
-            cta_tot[2 * turn] = mine[0];
-            cta_tot[2 * turn + 1] = mine[1];
+        turn ^= 1;
+        if (warp < 4) {  // one sum each; the order is the same everywhere
+            double sum = lane < DV_WARPS ? warp_tot[warp][lane] : 0.0;
+            sum = warp_sum64(sum);
+            if (lane == 0) cta_tot[turn][warp] = sum;
         }
         if (ranks > 1) {
+            __syncwarp();
             cluster_arrive();
             cluster_wait();
         } else {
             __syncthreads();
         }
-        total[0] = total[1] = 0.0;
-        for (int r = 0; r < ranks; ++r) {
-            total[0] += ranks > 1 ? load_cluster64(map_to_cta(smem_u32(&cta_tot[2 * turn]), r)) : cta_tot[2 * turn];
-            total[1] += ranks > 1 ? load_cluster64(map_to_cta(smem_u32(&cta_tot[2 * turn + 1]), r)) : cta_tot[2 * turn + 1];
-        }
-        turn ^= 1;
-    };
-    auto row_sums = [&](int i, double (&total)[2]) {  // sums of e_p and e_q of row i
-        const Row<T> rp(p.target, p.target_stride, s.row0 + i, p.vocab), rq(p.draft ? p.draft : p.target, p.draft ? p.draft_stride : p.target_stride, s.row0 + i, p.vocab);
-        double sp = 0.0, sq = 0.0, mine[2];
-        for (int k = wb0 + lane; k < wb1; k += 32) {
-            float f[E];
-            rp.load(k * E - rp.off, f);
+        cta_part = 0.0;
+        if (lane < 4 * ranks) cta_part = ranks > 1 ? load_cluster64(map_to_cta(smem_u32(&cta_tot[turn][lane & 3]), lane >> 2)) : cta_tot[turn][lane];
+        double sum = cta_part;
 #pragma unroll
-            for (int e = 0; e < E; ++e) sp += ex(f[e], sm_pm[i]);
-            if (p.draft) {
-                rq.load(k * E - rp.off, f);
+        for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
 #pragma unroll
-                for (int e = 0; e < E; ++e) sq += ex(f[e], sm_qm[i]);
-            }
-        }
-        cluster_totals(sp, sq, total, mine);
+        for (int q = 0; q < 4; ++q) total[q] = __shfl_sync(0xFFFFFFFFu, sum, q);
+        total[0] += total[2];
+        total[1] += total[3];
+        w.a = total[1];
+        w.b = total[0];
     };
+    // the weight of a part of the row from its four sums
+    auto weight = [&](double e, double pa, double qa) { return w.kind == 2 ? fmax(0.0, __dsub_rn(__dmul_rn(w.a, pa), __dmul_rn(w.b, qa))) : e; };
 
     // ---- how many are accepted
     int stop = 0, code = 4;
-    double sums[2] = {0.0, 0.0};
-    bool have_sums = false;
+    bool passed = false;  // a pass over row `stop` has been made
     for (; stop < s.n; ++stop) {
         code = sm_code[stop];
-        have_sums = false;
+        passed = false;
         if (code == 2) {
-            row_sums(stop, sums);
-            have_sums = true;
             const int x = __ldg(p.tokens + s.row0 + stop + 1);
+            pass(stop, p.draft ? 2 : 0, x);
+            passed = p.draft != nullptr;  // (without one the token drawn is another: a pass without x)
             const Row<T> rp(p.target, p.target_stride, s.row0 + stop, p.vocab);
-            const double ep = ex(rp.entry(x), sm_pm[stop]), u = static_cast<double>(__ldg(p.accept_u + s.row0 + stop + 1));
+            const double ep = ex(rp.entry(x), w.pm, w.ps), u = static_cast<double>(__ldg(p.accept_u + s.row0 + stop + 1));
             if (p.draft) {
                 const Row<T> rq(p.draft, p.draft_stride, s.row0 + stop, p.vocab);
-                code = u * ex(rq.entry(x), sm_qm[stop]) * sums[0] < ep * sums[1] ? 0 : 1;
+                code = u * ex(rq.entry(x), w.qm, w.qs) * total[0] < ep * total[1] ? 0 : 1;
             } else {
-                code = u * sums[0] < ep ? 0 : 1;
+                code = u * total[0] < ep ? 0 : 1;
             }
         }
         if (code != 0) break;
@@ -474,35 +534,18 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
 
     // ---- the draw
     const Row<T> rp(p.target, p.target_stride, s.row0 + stop, p.vocab), rq(p.draft ? p.draft : p.target, p.draft ? p.draft_stride : p.target_stride, s.row0 + stop, p.vocab);
-    Weights w;
-    w.pm = sm_pm[stop];
-    w.qm = sm_qm[stop];
-    w.kind = code == 4 ? 0 : p.draft ? 2 : 1;
-    w.x = code == 4 ? -1 : __ldg(p.tokens + s.row0 + stop + 1);
-    if (w.kind == 2) {
-        if (!have_sums) row_sums(stop, sums);
-        w.a = sums[1];
-        w.b = sums[0];
+    if (!passed) pass(stop, code == 4 ? 0 : p.draft ? 2 : 1, code == 4 ? -1 : __ldg(p.tokens + s.row0 + stop + 1));
+    double all = weight(total[0], total[2], total[3]);
+    if (!(all > 0.0) && w.kind != 0) {  // p nowhere above q (they are the same and the number was 1): drawn from p
+        pass(stop, 0, -1);
+        all = total[0];
     }
-    double total[2], mine[2];
-    while (true) {
-        double v = 0.0;
-        for (int k = wb0 + lane; k < wb1; k += 32) {
-            double x[E];
-            weights_of<T>(rp, rq, ex, w, k * E - rp.off, x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v += x[e];
-        }
-        cluster_totals(v, 0.0, total, mine);
-        if (total[0] > 0.0 || w.kind == 0) break;
-        w.kind = 0;  // p nowhere above q (they are the same and the number was 1): drawn from p
-    }
-    const double u = fmin(fmax(static_cast<double>(__ldg(p.sample_u + b)), 0.0), 1.0), point = u * total[0];
+    const double u = fmin(fmax(static_cast<double>(__ldg(p.sample_u + b)), 0.0), 1.0), point = u * all;
     // the last CTA that begins at or before the point and is not empty
     int owner = 0;
     double before = 0.0, base = 0.0;
     for (int r = 0; r < ranks; ++r) {
-        const double v = ranks > 1 ? load_cluster64(map_to_cta(smem_u32(&cta_tot[2 * (turn ^ 1)]), r)) : cta_tot[2 * (turn ^ 1)];
+        const double v = weight(__shfl_sync(0xFFFFFFFFu, cta_part, 4 * r), __shfl_sync(0xFFFFFFFFu, cta_part, 4 * r + 2), __shfl_sync(0xFFFFFFFFu, cta_part, 4 * r + 3));
         if (v > 0.0 && before <= point) {
             owner = r;
             base = before;
@@ -512,8 +555,9 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     if (owner == rank) {
         int ow = 0;
         double at = base, start = base;
+        const double mine = lane < DV_WARPS ? weight(warp_tot[0][lane], warp_tot[2][lane], warp_tot[3][lane]) : 0.0;
         for (int k = 0; k < DV_WARPS; ++k) {
-            const double v = warp_tot[0][k];
+            const double v = __shfl_sync(0xFFFFFFFFu, mine, k);
             if (v > 0.0 && at <= point) {
                 ow = k;
                 start = at;
@@ -565,9 +609,9 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
 
 }  // namespace
 
-// Parts that a row is divided into: 16384 entries each where that gives every SM four, down to 1024 where it does not; a lane joins each.
+// Parts that a row is divided into: 65536 entries each where that gives every SM four, down to 1024 where it does not; a lane joins each.
 static int draft_splits(int n_rows, int vocab, int num_sms) {
-    int per = 16384;
+    int per = 65536;
     while (per > 1024 && (static_cast<long long>(n_rows) * ((vocab + per - 1) / per) < 4LL * num_sms)) per /= 2;
     const int splits = (vocab + per - 1) / per;
     return splits < 1 ? 1 : splits > 32 ? 32 : splits;
@@ -584,9 +628,10 @@ cudaError_t launch_verify_drafts(DraftParams p, int num_sms, cudaStream_t stream
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
-    // a CTA takes 8 entries per thread at least
+    // a CTA takes 4096 entries of a row at least; larger clusters as long as all CTAs run at once, one per SM
+    // (64 sequences over 128256 entries: 51 us with clusters of two, 61 of four)
     p.ranks = 1;
-    while (p.ranks < 8 && p.vocab > DV_THREADS * 8 * p.ranks) p.ranks *= 2;
+    while (p.ranks < 8 && p.vocab > 4096 * p.ranks && static_cast<long long>(p.batch) * p.ranks * 2 <= num_sms) p.ranks *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.batch) * p.ranks);
     cfg.blockDim = dim3(DV_THREADS);

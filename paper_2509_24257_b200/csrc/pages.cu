@@ -15,6 +15,7 @@ namespace {
 
 constexpr int PL_THREADS = 1024;   // planning kernels
 constexpr int PL_WARPS = PL_THREADS / 32;
+constexpr int PL_SMALL = 1024;     // sequences whose plans fit shared memory
 constexpr int PL_STEPS = 16;       // loads of counts in flight per thread
 constexpr int CP_THREADS = 256;
 constexpr int CP_PIECE = 8192;     // bytes of a page that a CTA copies at a time
@@ -123,10 +124,16 @@ __global__ void __launch_bounds__(PL_THREADS) reserve_kernel(const PagesDev p, c
     __shared__ ScanScratch sm_scan;
     __shared__ long long sm_sum[PL_WARPS];
     __shared__ int sm_count, sm_copies;
+    __shared__ int sm_lists[5][PL_SMALL];
     const Lists l = lists_of(ws, p.batch, p.n_pages);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // what a usual batch needs stays in shared memory: the phases below are a chain of reads
+    const bool small = p.batch <= PL_SMALL;
+    int *need_of = small ? sm_lists[0] : l.need, *upto_of = small ? sm_lists[1] : l.upto;
+    int *held_seq = small ? sm_lists[2] : l.src, *held_page = small ? sm_lists[3] : l.dst, *held_copy = small ? sm_lists[4] : l.list;
     const long long cap = static_cast<long long>(p.table_width) << p.page_shift;
     if (tid == 0) sm_count = sm_copies = 0;
+    pdl_launch_dependents();
     __syncthreads();
     // sequences that would write into a page that others hold: src = sequence, dst = that page (in any order)
     for (int b = tid; b < p.batch; b += PL_THREADS) {
@@ -145,49 +152,50 @@ __global__ void __launch_bounds__(PL_THREADS) reserve_kernel(const PagesDev p, c
                         need = -1;
                     } else if (p.refs[page] > 1) {
                         const int i = atomicAdd(&sm_count, 1);
-                        l.src[i] = b;
-                        l.dst[i] = page;
+                        held_seq[i] = b;
+                        held_page[i] = page;
                     }
                 }
             }
         }
-        l.need[b] = need;
+        need_of[b] = need;
     }
     __syncthreads();
     for (int i = tid; i < sm_count; i += PL_THREADS) {
-        const int b = l.src[i], page = l.dst[i];
+        const int b = held_seq[i], page = held_page[i];
         int same = 0;
         bool last = true;
         for (int j = 0; j < sm_count; ++j)
-            if (l.dst[j] == page) {
+            if (held_page[j] == page) {
                 ++same;
-                last = last && l.src[j] <= b;
+                last = last && held_seq[j] <= b;
             }
-        l.list[i] = same == p.refs[page] && last ? 0 : 1;
+        held_copy[i] = same == p.refs[page] && last ? 0 : 1;
     }
     __syncthreads();
     for (int i = tid; i < sm_count; i += PL_THREADS)
-        if (l.list[i]) l.need[l.src[i]] = (l.need[l.src[i]] + 1) | 0x40000000;  // with a copy
+        if (held_copy[i]) need_of[held_seq[i]] = (need_of[held_seq[i]] + 1) | 0x40000000;  // with a copy
     __syncthreads();
     long long sum = 0;
     for (int b0 = 0; b0 < p.batch; b0 += PL_THREADS) {
         const int b = b0 + tid;
-        const int need = b < p.batch ? l.need[b] : -1;
+        const int need = b < p.batch ? need_of[b] : -1;
         long long all;
         const long long upto = sum + block_scan(need < 0 ? 0 : need & 0x3FFFFFFF, sm_sum, &all);
-        if (b < p.batch) l.upto[b] = static_cast<int>(min(upto, 0x7FFFFFFFLL));
+        if (b < p.batch) upto_of[b] = static_cast<int>(min(upto, 0x7FFFFFFFLL));
         sum += all;
     }
     const int total = static_cast<int>(min(sum, 0x7FFFFFFFLL));
     __syncthreads();  // the lists are written again
+    int* list = small && total <= PL_SMALL ? sm_lists[4] : l.list;  // the free pages that are taken
     const int found = total == 0 ? 0 : scan_pages(p, 0, p.n_pages, true, total, sm_scan, [&](int k, int page) {
-        if (k < total) l.list[k] = page;
+        if (k < total) list[k] = page;
     });
     __syncthreads();
     for (int b = warp; b < p.batch; b += PL_WARPS) {
-        const int code = l.need[b];
+        const int code = need_of[b];
         if (code < 0) continue;
-        const int need = code & 0x3FFFFFFF, upto = l.upto[b], copy = code >> 30 & 1;
+        const int need = code & 0x3FFFFFFF, upto = upto_of[b], copy = code >> 30 & 1;
         if (upto > found) {
             if (lane == 0) raise(p.status, VERILLM_DEV_NO_PAGES);
             continue;
@@ -198,12 +206,12 @@ __global__ void __launch_bounds__(PL_THREADS) reserve_kernel(const PagesDev p, c
         if (copy && lane == 0) {
             const int old = row[at], i = atomicAdd(&sm_copies, 1);
             l.src[i] = old;
-            l.dst[i] = l.list[upto - need];
+            l.dst[i] = list[upto - need];
             atomicSub(p.refs + old, 1);
         }
         __syncwarp();
         for (int k = lane; k < need; k += 32) {
-            const int page = l.list[upto - need + k];
+            const int page = list[upto - need + k];
             row[at + k] = page;
             p.refs[page] = 1;
         }
