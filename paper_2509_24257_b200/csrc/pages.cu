@@ -46,31 +46,43 @@ __device__ __forceinline__ long long block_scan(long long v, long long* sm, long
     __syncthreads();
     if (lane == 31) sm[warp] = v;
     __syncthreads();
-    long long before = 0, all = 0;
-    for (int w = 0; w < PL_WARPS; ++w) {
-        before += w < warp ? sm[w] : 0;
-        all += sm[w];
+    long long all = sm[lane];  // (every warp adds up the warps' sums for itself)
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xFFFFFFFFu, all, o);
+        if (lane >= o) all += u;
     }
-    *total = all;
-    return v + before;
+    *total = __shfl_sync(0xFFFFFFFFu, all, 31);
+    const long long before = __shfl_sync(0xFFFFFFFFu, all, warp > 0 ? warp - 1 : 0);
+    return v + (warp > 0 ? before : 0);
 }
+static_assert(PL_WARPS == 32, "a lane per warp in block_scan");
 
 // Calls found(index among those found, page) for the pages of [first, last) whose being free equals `free`, in order, until at least `most` were
 // found; returns how many.  A step looks at PL_STEPS runs of PL_THREADS pages, whose counts are read together.
 struct ScanScratch {
     int count[PL_STEPS][PL_WARPS], run[PL_STEPS];
 };
+// early: the counts of the first step where they have been read already, or null.
+__device__ __forceinline__ void read_counts(const PagesDev& p, long long base, int last, bool free, int (&refs)[PL_STEPS]) {
+#pragma unroll
+    for (int u = 0; u < PL_STEPS; ++u) {
+        const long long page = base + u * PL_THREADS + threadIdx.x;
+        refs[u] = page < last ? p.refs[page] : free ? 1 : 0;
+    }
+}
 template <typename F>
-__device__ __forceinline__ int scan_pages(const PagesDev& p, int first, int last, bool free, int most, ScanScratch& sm, F found) {
+__device__ __forceinline__ int scan_pages(const PagesDev& p, int first, int last, bool free, int most, ScanScratch& sm, const int (*early)[PL_STEPS], F found) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int count = 0;
     for (long long base = first; base < last && count < most; base += PL_STEPS * PL_THREADS) {
         int refs[PL_STEPS];
         unsigned who[PL_STEPS];
+        if (early && base == first) {
 #pragma unroll
-        for (int u = 0; u < PL_STEPS; ++u) {
-            const long long page = base + u * PL_THREADS + tid;
-            refs[u] = page < last ? p.refs[page] : free ? 1 : 0;
+            for (int u = 0; u < PL_STEPS; ++u) refs[u] = (*early)[u];
+        } else {
+            read_counts(p, base, last, free, refs);
         }
 #pragma unroll
         for (int u = 0; u < PL_STEPS; ++u) {
@@ -124,7 +136,7 @@ __global__ void __launch_bounds__(PL_THREADS) reserve_kernel(const PagesDev p, c
     __shared__ ScanScratch sm_scan;
     __shared__ long long sm_sum[PL_WARPS];
     __shared__ int sm_count, sm_copies;
-    __shared__ int sm_lists[5][PL_SMALL];
+    __shared__ int sm_lists[7][PL_SMALL];
     const Lists l = lists_of(ws, p.batch, p.n_pages);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // what a usual batch needs stays in shared memory: the phases below are a chain of reads
@@ -132,6 +144,8 @@ __global__ void __launch_bounds__(PL_THREADS) reserve_kernel(const PagesDev p, c
     int *need_of = small ? sm_lists[0] : l.need, *upto_of = small ? sm_lists[1] : l.upto;
     int *held_seq = small ? sm_lists[2] : l.src, *held_page = small ? sm_lists[3] : l.dst, *held_copy = small ? sm_lists[4] : l.list;
     const long long cap = static_cast<long long>(p.table_width) << p.page_shift;
+    int early[PL_STEPS];  // read under the first phases, written only in the last
+    read_counts(p, 0, p.n_pages, true, early);
     if (tid == 0) sm_count = sm_copies = 0;
     pdl_launch_dependents();
     __syncthreads();
@@ -159,18 +173,23 @@ __global__ void __launch_bounds__(PL_THREADS) reserve_kernel(const PagesDev p, c
             }
         }
         need_of[b] = need;
+        if (small) {
+            sm_lists[5][b] = len;
+            sm_lists[6][b] = want;
+        }
     }
     __syncthreads();
-    for (int i = tid; i < sm_count; i += PL_THREADS) {
+    for (int i = warp; i < sm_count; i += PL_WARPS) {
         const int b = held_seq[i], page = held_page[i];
-        int same = 0;
-        bool last = true;
-        for (int j = 0; j < sm_count; ++j)
+        int same = 0, later = 0;
+        for (int j = lane; j < sm_count; j += 32)
             if (held_page[j] == page) {
                 ++same;
-                last = last && held_seq[j] <= b;
+                later |= held_seq[j] > b;
             }
-        held_copy[i] = same == p.refs[page] && last ? 0 : 1;
+        same = __reduce_add_sync(0xFFFFFFFFu, same);
+        later = __reduce_or_sync(0xFFFFFFFFu, later);
+        if (lane == 0) held_copy[i] = same == p.refs[page] && !later ? 0 : 1;
     }
     __syncthreads();
     for (int i = tid; i < sm_count; i += PL_THREADS)
@@ -188,7 +207,7 @@ __global__ void __launch_bounds__(PL_THREADS) reserve_kernel(const PagesDev p, c
     const int total = static_cast<int>(min(sum, 0x7FFFFFFFLL));
     __syncthreads();  // the lists are written again
     int* list = small && total <= PL_SMALL ? sm_lists[4] : l.list;  // the free pages that are taken
-    const int found = total == 0 ? 0 : scan_pages(p, 0, p.n_pages, true, total, sm_scan, [&](int k, int page) {
+    const int found = total == 0 ? 0 : scan_pages(p, 0, p.n_pages, true, total, sm_scan, &early, [&](int k, int page) {
         if (k < total) list[k] = page;
     });
     __syncthreads();
@@ -200,9 +219,9 @@ __global__ void __launch_bounds__(PL_THREADS) reserve_kernel(const PagesDev p, c
             if (lane == 0) raise(p.status, VERILLM_DEV_NO_PAGES);
             continue;
         }
-        const int len = p.kv_len[b], want = new_len[b];  // (len was in range: a bounded one does not grow past the table)
+        const int len = small ? sm_lists[5][b] : max(p.kv_len[b], 0), want = small ? sm_lists[6][b] : new_len[b];  // (a length that was bounded does not grow)
         int* row = p.page_table + static_cast<size_t>(b) * p.table_width;
-        const int at = pages_of(len < 0 ? 0 : len, p.page_shift) - copy;
+        const int at = pages_of(len, p.page_shift) - copy;
         if (copy && lane == 0) {
             const int old = row[at], i = atomicAdd(&sm_copies, 1);
             l.src[i] = old;
@@ -283,11 +302,11 @@ __global__ void __launch_bounds__(256) fork_len_kernel(const PagesDev p, const i
 __global__ void __launch_bounds__(PL_THREADS) compact_kernel(const PagesDev p, int* n_used, int* ws) {
     __shared__ ScanScratch sm_scan;
     const Lists l = lists_of(ws, p.batch, p.n_pages);
-    const int used = scan_pages(p, 0, p.n_pages, false, 0x7FFFFFFF, sm_scan, [](int, int) {});
-    const int holes = scan_pages(p, 0, used, true, 0x7FFFFFFF, sm_scan, [&](int k, int page) { l.dst[k] = page; });
+    const int used = scan_pages(p, 0, p.n_pages, false, 0x7FFFFFFF, sm_scan, nullptr, [](int, int) {});
+    const int holes = scan_pages(p, 0, used, true, 0x7FFFFFFF, sm_scan, nullptr, [&](int k, int page) { l.dst[k] = page; });
     __syncthreads();
     if (holes > 0) {
-        scan_pages(p, used, p.n_pages, false, 0x7FFFFFFF, sm_scan, [&](int k, int page) { l.src[k] = page; });
+        scan_pages(p, used, p.n_pages, false, 0x7FFFFFFF, sm_scan, nullptr, [&](int k, int page) { l.src[k] = page; });
         __syncthreads();
         for (int i = threadIdx.x; i < holes; i += PL_THREADS) {
             const int s = l.src[i], d = l.dst[i];
