@@ -34,7 +34,7 @@ EXPORTS = (
     "verillm_load_lm_head", "verillm_token_match", "verillm_verify_segment", "verillm_spot_check", "verillm_merkle_roots",
     "verillm_threshold_sweep", "verillm_selftest_wait_timeout", "verillm_kv_write", "verillm_kv_read",
     "verillm_op_attention_paged", "verillm_op_attention_paged_workspace", "verillm_decode_commit_paged",
-    "verillm_w4_quantise", "verillm_w4_dequantise", "verillm_op_w4_matvec", "verillm_verify_drafts", "verillm_verify_drafts_workspace",
+    "verillm_quantise_w4", "verillm_decode_commit_w4", "verillm_w4_quantise", "verillm_w4_dequantise", "verillm_op_w4_matvec", "verillm_verify_drafts", "verillm_verify_drafts_workspace",
     "verillm_kv_pages_workspace", "verillm_kv_reserve", "verillm_kv_free", "verillm_kv_fork", "verillm_kv_compact", "verillm_kv_copy",
 )
 PROF_CLASSES = ("setup", "rmsnorm", "gemm_qkv_rope", "attention", "gemm_o_resid", "gemm_gate_up_swiglu",
@@ -166,6 +166,9 @@ def lib() -> C.CDLL:
         L.verillm_op_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
         L.verillm_decode_commit_paged.argtypes = L.verillm_decode_commit.argtypes[:10] + [C.c_int32, C.c_void_p, C.c_void_p]
         L.verillm_decode_commit_paged.restype = C.c_int
+        L.verillm_decode_commit_w4.argtypes = L.verillm_decode_commit_paged.argtypes
+        L.verillm_quantise_w4.argtypes = [C.c_void_p, C.c_int32, C.c_void_p]
+        L.verillm_decode_commit_w4.restype = L.verillm_quantise_w4.restype = C.c_int
         cache_p, rows_p = C.POINTER(KVCacheC), C.POINTER(KVRowsC)
         L.verillm_kv_write.argtypes = [cache_p, rows_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
         L.verillm_kv_write.restype = C.c_int
@@ -363,8 +366,9 @@ class Model:
 
     def decode_commit(self, tokens: torch.Tensor, cu_seqlens: Sequence[int], n_prefill: int, check_seq: Sequence[int],
                       check_pos: Sequence[int], commit_dtype: torch.dtype = torch.bfloat16,
-                      stream: Optional[torch.cuda.Stream] = None, cache_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
-        """cache_dtype: bf16, float8_e4m3fn or int8 decodes over a paged cache of that type; None over the contiguous bf16 one."""
+                      stream: Optional[torch.cuda.Stream] = None, cache_dtype: Optional[torch.dtype] = None, w4: bool = False) -> torch.Tensor:
+        """cache_dtype: bf16, float8_e4m3fn or int8 decodes over a paged cache of that type; None over the contiguous bf16 one.  w4: on the
+        4-bit weights that `quantise_w4` made."""
         cu = _i32(cu_seqlens)
         cs, cp = _i32(check_seq), _i32(check_pos)
         n_check, batch = int(cs.shape[0]), int(cu.shape[0]) - 1
@@ -374,15 +378,20 @@ class Model:
         status = torch.zeros(1, dtype=torch.int32, device=self.device)
         args = [self._h, tokens.data_ptr(), cu.ctypes.data, batch, int(n_prefill), cs.ctypes.data, cp.ctypes.data, n_check,
                 out.data_ptr(), BF16 if commit_dtype == torch.bfloat16 else F32]
-        name = "verillm_decode_commit" if cache_dtype is None else "verillm_decode_commit_paged"
-        if cache_dtype is not None:
-            args.append(_KV_DTYPES[cache_dtype])
+        name = "verillm_decode_commit_w4" if w4 else "verillm_decode_commit" if cache_dtype is None else "verillm_decode_commit_paged"
+        if cache_dtype is not None or w4:
+            args.append(-1 if cache_dtype is None else _KV_DTYPES[cache_dtype])
         with torch.cuda.device(self.device):
             code = getattr(lib(), name)(*args, status.data_ptr(), _stream_ptr(stream))
         _check(code, name)
         if int(status.item()) != 0:
             raise RuntimeError(f"{name}: device status {int(status.item())}")
         return out[:, :n_check]
+
+    def quantise_w4(self, group: int = 128, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Makes 4-bit copies of the projections, one scale per `group` inputs, for decode_commit(w4=True)."""
+        with torch.cuda.device(self.device):
+            _check(lib().verillm_quantise_w4(self._h, int(group), _stream_ptr(stream)), "verillm_quantise_w4")
 
     def load_lm_head(self, lm_head: torch.Tensor) -> None:
         if lm_head.dtype != torch.bfloat16 or not lm_head.is_contiguous():

@@ -1,13 +1,13 @@
 """Threshold sensitivity of the bit-aware tests on honest and quantised-prover traces.
 
-    python -m paper_2509_24257_b200.calibrate [--workload small] [--bits 8 | --cache e4m3] [--check-frac 0.25]
+    python -m paper_2509_24257_b200.calibrate [--workload small] [--bits 8 | --cache e4m3 | --w4 128] [--check-frac 0.25]
 
 Follows the paper's "Threshold Sensitivity Analysis": each of the four thresholds (P_e, |e|, P_m, P_w) is
 varied while the others stay at their selected values, and FPR / FNR / TPR / TNR are read off cells of
 honest traces and of attack traces.  Here the honest prover is the library's bf16 KV-cache decode, the
 attacker is the same decode on fake-quantised weights (synth.fake_quantise), the verifier recomputes with
 the true weights.  With --cache the attacker keeps the true weights and serves with a quantised key/value cache instead
-(the paged cache of decode_commit).  Every step runs in the library's kernels (decode_commit, verify_prefill,
+(the paged cache of decode_commit), with --w4 it decodes on 4-bit weights with a scale per that many inputs.  Every step runs in the library's kernels (decode_commit, verify_prefill,
 threshold_sweep), this module only arranges the calls and prints the table.
 """
 from __future__ import annotations
@@ -48,21 +48,23 @@ def variants(selected: Dict[str, float] = SELECTED, grid: Dict[str, Sequence[flo
 CACHES = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}
 
 
-def trace_stats(wl: synth.Workload, bits: int, device: torch.device, cache: Optional[str] = None):
+def trace_stats(wl: synth.Workload, bits: int, device: torch.device, cache: Optional[str] = None, w4: Optional[int] = None):
     """Statistics [n_cells][NSTAT] (device) of honest cells followed by attack cells, and the class flags.  cache: the
-    attacker's key/value cache type; None: the attacker quantises its weights to `bits` instead."""
+    attacker's key/value cache type; w4: the group size of its 4-bit weights; neither: the attacker quantises its weights to `bits` per output instead."""
     w = synth.model_weights(wl, device)
     cs, cp = synth.check_positions(wl)
     cu = synth.cu_seqlens(wl)
     flat = torch.from_numpy(synth.token_streams(wl).reshape(-1)).to(device)
     verifier = vb.Model.from_weights(wl.shape, w, wl.n_tokens, len(cs), wl.batch, device)
     attacker = verifier
-    if cache is None:
+    if cache is None and w4 is None:
         attacker = vb.Model.from_weights(wl.shape, synth.quantised_model_weights(w, bits), wl.n_tokens, len(cs), wl.batch, device)
+    if w4 is not None:
+        attacker.quantise_w4(w4)
     tol = vb.default_tol()
     parts = []
-    for prover, cache_dtype in ((verifier, None), (attacker, CACHES[cache] if cache else None)):
-        committed = prover.decode_commit(flat, cu, wl.prompt_len, cs, cp, torch.bfloat16, cache_dtype=cache_dtype).contiguous()
+    for prover, cache_dtype, low in ((verifier, None, False), (attacker, CACHES[cache] if cache else None, w4 is not None)):
+        committed = prover.decode_commit(flat, cu, wl.prompt_len, cs, cp, torch.bfloat16, cache_dtype=cache_dtype, w4=low).contiguous()
         rep = verifier.verify_prefill(flat, cu, committed, cs, cp, tol)
         parts.append(rep.stats.reshape(-1, vb.NSTAT).clone())
     if attacker is not verifier:
@@ -90,12 +92,13 @@ def main() -> None:
     ap.add_argument("--workload", default="small")
     ap.add_argument("--bits", type=int, default=8)
     ap.add_argument("--cache", choices=sorted(CACHES), help="the attacker quantises its key/value cache, not its weights")
+    ap.add_argument("--w4", type=int, choices=(32, 64, 128), help="the attacker decodes on 4-bit weights with a scale per that many inputs")
     ap.add_argument("--check-frac", type=float, default=0.25)
     args = ap.parse_args()
     wl = dataclasses.replace(synth.WORKLOADS[args.workload], check_frac=args.check_frac)
-    stats, is_attack = trace_stats(wl, args.bits, torch.device("cuda", 0), args.cache)
+    stats, is_attack = trace_stats(wl, args.bits, torch.device("cuda", 0), args.cache, args.w4)
     print(f"{wl.name}: {int((is_attack == 0).sum())} honest and {int(is_attack.sum())} "
-          f"{args.cache + ' cache' if args.cache else 'int' + str(args.bits)} attack cells")
+          f"{', '.join(([f'4-bit weights (groups of {args.w4})'] if args.w4 else []) + ([args.cache + ' cache'] if args.cache else [])) or 'int' + str(args.bits)} attack cells")
     print(f"{'threshold':>22} {'FPR':>8} {'FNR':>8} {'TPR':>8} {'TNR':>8}")
     for name, val, fpr, fnr, tpr, tnr in sensitivity_rows(stats, is_attack):
         mark = " (selected)" if SELECTED[name] == val else ""

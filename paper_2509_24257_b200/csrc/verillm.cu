@@ -44,6 +44,11 @@ struct LayerDev {
     CUtensorMap t_wqkv_h, t_wo_h, t_wgu_h, t_wd_h;  // boxes of 128 weight rows (one half per CTA of a pair)
 };
 
+// 4-bit copies of a layer's projections, laid out like the bf16 ones.
+struct LayerW4 {
+    verillm_w4 wqkv, wo, wgu, wd;
+};
+
 struct DecodeState {
     bool ready = false;
     bf16* kv_cache = nullptr;   // [n_layers][max_tokens][2 * KV * dh]
@@ -120,6 +125,10 @@ struct verillm_model {
     int* tm_claimed = nullptr;
     int n_tiles_v = 0;
     CUtensorMap t_lm, t_lm_h, t_tm_y;
+    // 4-bit weights (allocated by verillm_quantise_w4): every layer's, and one layer's as bf16 for passes over prompts
+    std::vector<LayerW4> w4;
+    unsigned char* w4_mem = nullptr;
+    LayerDev w4_layer;
     DecodeState dec;
     Profile prof;
     int last_launches = 0;
@@ -239,6 +248,7 @@ struct LayerRun {
     int next_layer;               // layer whose attention norm follows this block's output, -1 if none
     bool norm_ready;              // in/out: xn / sumsq already hold the input of this layer's attention norm
     size_t split_cursor = 0;  // next free slot of the K-part counter arena
+    const LayerDev* weights = nullptr;  // used in place of the handle's, if set
 };
 constexpr int kSplitInts = 80;  // one counter per tile of a last round (at most 73 with 74 pairs of SMs)
 
@@ -251,7 +261,7 @@ int split_reset(verillm_model* m, LayerRun& r, cudaStream_t st) {
 
 int run_layer(verillm_model* m, int l, LayerRun& r, int* status, cudaStream_t st, int* launches) {
     const verillm_config& c = m->cfg;
-    const LayerDev& w = m->layers[l];
+    const LayerDev& w = r.weights ? *r.weights : m->layers[l];
     GemmParams p;
     std::memset(&p, 0, sizeof(p));
     p.status = status;
@@ -558,6 +568,8 @@ void verillm_free(verillm_model* m) {
     cudaFree(d.kv_cache); cudaFree(d.hidden_tmp); cudaFree(d.resid); cudaFree(d.qkv); cudaFree(d.gu);
     cudaFree(d.xn); cudaFree(d.q); cudaFree(d.attn); cudaFree(d.mid); cudaFree(d.ints);
     cudaFree(d.pool); cudaFree(d.pool_scale); cudaFree(d.kv_row); cudaFree(d.iota); cudaFree(d.attn_ws);
+    cudaFree(m->w4_mem);
+    cudaFree(m->w4_layer.wqkv); cudaFree(m->w4_layer.wo); cudaFree(m->w4_layer.wgu); cudaFree(m->w4_layer.wd);
     for (cudaEvent_t e : m->prof.ev) cudaEventDestroy(e);
     delete m;
 }
@@ -1020,8 +1032,9 @@ int verillm_merkle_roots(const float* states, int32_t n_vec, int32_t d_model, ui
 // cache_dtype: -1 for the contiguous bf16 cache, else VERILLM_KV_* for the paged one.
 static int decode_impl(verillm_model* m, const int32_t* tokens, const int32_t* cu_seqlens, int32_t batch, int32_t n_prefill,
                        const int32_t* check_seq, const int32_t* check_pos, int32_t n_check, void* committed_out, int32_t commit_dtype,
-                       int32_t cache_dtype, int32_t* status, void* cuda_stream) {
+                       int32_t cache_dtype, bool w4, int32_t* status, void* cuda_stream) {
     if (!m || !tokens || n_prefill < 0) return VERILLM_E_INVAL;
+    if (w4 && m->w4.empty()) return VERILLM_E_INVAL;  // verillm_quantise_w4 first
     if (commit_dtype != VERILLM_BF16 && commit_dtype != VERILLM_F32) return VERILLM_E_INVAL;
     if (n_check > 0 && !committed_out) return VERILLM_E_INVAL;
     int M = 0, max_len = 0, rc;
@@ -1112,6 +1125,17 @@ static int decode_impl(verillm_model* m, const int32_t* tokens, const int32_t* c
         for (int l = 0; l < c.n_layers; ++l) {
             run.next_layer = l + 1 < c.n_layers ? l + 1 : -1;
             cl.hidden_out = d.hidden_tmp + static_cast<size_t>(l) * n_check * c.d_model;
+            if (w4) {
+                // the pass over the prompts runs on this layer's 4-bit weights as bf16
+                LayerDev& q = m->w4_layer;
+                q.attn_norm = m->layers[l].attn_norm;
+                q.ffn_norm = m->layers[l].ffn_norm;
+                const verillm_w4* from[4] = {&m->w4[l].wqkv, &m->w4[l].wo, &m->w4[l].wgu, &m->w4[l].wd};
+                bf16* to[4] = {q.wqkv, q.wo, q.wgu, q.wd};
+                for (int i = 0; i < 4; ++i)
+                    CU_TRY(launch_w4_dequantise(from[i]->codes, from[i]->scales, to[i], from[i]->k, 0, from[i]->n, from[i]->k, from[i]->group, m->num_sms, st));
+                run.weights = &q;
+            }
             if ((rc = run_layer(m, l, run, dev_status, st, &launches))) return rc;
             // run_layer leaves this layer's rotated keys and values in qkv: append them to the cache
             if (paged) {
@@ -1181,11 +1205,24 @@ static int decode_impl(verillm_model* m, const int32_t* tokens, const int32_t* c
             const int s0 = slots_first[t - t_begin], n_slots = slots_first[t - t_begin + 1] - s0;
             CU_TRY(launch_gather_tokens(tokens, i_row_tok + r0, rows, i_tok, st));
             CU_TRY(launch_embed(i_tok, m->embed, rows, c.d_model, c.vocab, d.resid, dev_status, st));
+            // out = x w^T, or out += x w^T
+            auto project = [&](const bf16* x, const bf16* w, const verillm_w4* q, float* out, int n, int k, int accumulate) -> cudaError_t {
+                if (!w4) return launch_skinny_gemm(x, w, out, rows, n, k, accumulate, st);
+                W4Params p;
+                std::memset(&p, 0, sizeof(p));
+                p.codes = static_cast<const uint8_t*>(q->codes); p.scales = static_cast<const uint16_t*>(q->scales);
+                p.n = n; p.k = k; p.group = q->group;
+                p.x = x; p.x_stride = k; p.rows = rows;
+                p.residual = accumulate ? out : nullptr; p.res_stride = n;
+                p.y = out; p.y_stride = n; p.out_f32 = 1; p.status = dev_status;
+                return launch_w4_matvec(p, m->num_sms, st);
+            };
             for (int l = 0; l < c.n_layers; ++l) {
                 const LayerDev& w = m->layers[l];
+                const LayerW4* q4 = w4 ? &m->w4[l] : nullptr;
                 bf16* cache_l = paged ? d.kv_row : d.kv_cache + static_cast<size_t>(l) * T * 2 * m->d_kv;
                 CU_TRY(launch_rmsnorm(d.resid, w.attn_norm, d.xn, rows, c.d_model, c.rms_eps, st));
-                CU_TRY(launch_skinny_gemm(d.xn, w.wqkv, d.qkv, rows, m->n_qkv, c.d_model, 0, st));
+                CU_TRY(project(d.xn, w.wqkv, q4 ? &q4->wqkv : nullptr, d.qkv, m->n_qkv, c.d_model, 0));
                 CU_TRY(launch_decode_rope_append(d.qkv, paged ? d.iota : i_row_tok + r0, i_row_pos + r0, rows, c.n_heads, c.n_kv_heads,
                                                  c.head_dim, m->rope_cs, d.q, cache_l, st));
                 if (paged) {
@@ -1200,11 +1237,11 @@ static int decode_impl(verillm_model* m, const int32_t* tokens, const int32_t* c
                     CU_TRY(launch_decode_attention(d.q, cache_l, i_row_start + r0, i_row_pos + r0, rows, c.n_heads,
                                                    c.n_kv_heads, c.head_dim, t + 1, d.attn, st));
                 }
-                CU_TRY(launch_skinny_gemm(d.attn, w.wo, d.resid, rows, c.d_model, m->d_q, 1, st));
+                CU_TRY(project(d.attn, w.wo, q4 ? &q4->wo : nullptr, d.resid, c.d_model, m->d_q, 1));
                 CU_TRY(launch_rmsnorm(d.resid, w.ffn_norm, d.xn, rows, c.d_model, c.rms_eps, st));
-                CU_TRY(launch_skinny_gemm(d.xn, w.wgu, d.gu, rows, 2 * c.d_ffn, c.d_model, 0, st));
+                CU_TRY(project(d.xn, w.wgu, q4 ? &q4->wgu : nullptr, d.gu, 2 * c.d_ffn, c.d_model, 0));
                 CU_TRY(launch_swiglu_rows(d.gu, d.mid, rows, c.d_ffn, st));
-                CU_TRY(launch_skinny_gemm(d.mid, w.wd, d.resid, rows, c.d_model, c.d_ffn, 1, st));
+                CU_TRY(project(d.mid, w.wd, q4 ? &q4->wd : nullptr, d.resid, c.d_model, c.d_ffn, 1));
                 if (n_slots > 0)
                     CU_TRY(launch_gather_rows(d.resid, i_slot_row + s0, i_slot_id + s0, n_slots, c.d_model,
                                               d.hidden_tmp + static_cast<size_t>(l) * n_check * c.d_model, st));
@@ -1221,7 +1258,7 @@ static int decode_impl(verillm_model* m, const int32_t* tokens, const int32_t* c
 int verillm_decode_commit(verillm_model* m, const int32_t* tokens, const int32_t* cu_seqlens, int32_t batch,
                           int32_t n_prefill, const int32_t* check_seq, const int32_t* check_pos, int32_t n_check,
                           void* committed_out, int32_t commit_dtype, int32_t* status, void* cuda_stream) try {
-    return decode_impl(m, tokens, cu_seqlens, batch, n_prefill, check_seq, check_pos, n_check, committed_out, commit_dtype, -1, status,
+    return decode_impl(m, tokens, cu_seqlens, batch, n_prefill, check_seq, check_pos, n_check, committed_out, commit_dtype, -1, false, status,
                        cuda_stream);
 } catch (const std::bad_alloc&) {  // host index tables
     return VERILLM_E_NOMEM;
@@ -1232,6 +1269,74 @@ int verillm_decode_commit_paged(verillm_model* m, const int32_t* tokens, const i
                                 int32_t commit_dtype, int32_t cache_dtype, int32_t* status, void* cuda_stream) try {
     if (cache_dtype != VERILLM_KV_BF16 && cache_dtype != VERILLM_KV_E4M3 && cache_dtype != VERILLM_KV_INT8) return VERILLM_E_INVAL;
     return decode_impl(m, tokens, cu_seqlens, batch, n_prefill, check_seq, check_pos, n_check, committed_out, commit_dtype, cache_dtype,
+                       false, status, cuda_stream);
+} catch (const std::bad_alloc&) {
+    return VERILLM_E_NOMEM;
+}
+
+// 4-bit copies of all projections, one allocation; the norms, the embedding and the output head stay as they are.
+int verillm_quantise_w4(verillm_model* m, int32_t group, void* cuda_stream) try {
+    if (!m) return VERILLM_E_INVAL;
+    if (group != 32 && group != 64 && group != 128) return VERILLM_E_SHAPE;
+    const verillm_config& c = m->cfg;
+    const int dims[4][2] = {{m->n_qkv, c.d_model}, {c.d_model, m->d_q}, {2 * c.d_ffn, c.d_model}, {c.d_model, c.d_ffn}};  // outputs, inputs
+    size_t at[5] = {0}, codes[4];
+    for (int i = 0; i < 4; ++i) {
+        if (dims[i][1] % group || dims[i][0] % 8) return VERILLM_E_SHAPE;
+        const size_t n = dims[i][0], k = dims[i][1];
+        codes[i] = n * k / 2;
+        at[i + 1] = at[i] + ((codes[i] + n * (k / group) * 2 + 255) & ~static_cast<size_t>(255));
+    }
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    int rc;
+    LayerDev& q = m->w4_layer;
+    if (!q.wd) {
+        if (!q.wqkv && (rc = dev_alloc(&q.wqkv, static_cast<size_t>(m->n_qkv) * c.d_model))) return rc;
+        if (!q.wo && (rc = dev_alloc(&q.wo, static_cast<size_t>(c.d_model) * m->d_q))) return rc;
+        if (!q.wgu && (rc = dev_alloc(&q.wgu, static_cast<size_t>(2) * c.d_ffn * c.d_model))) return rc;
+        if ((rc = dev_alloc(&q.wd, static_cast<size_t>(c.d_model) * c.d_ffn))) return rc;
+        bool ok = true;
+        for (int half = 0; half < 2; ++half) {
+            const uint32_t box = half ? 128 : kGemmBN;
+            ok = ok && make_tmap_bf16_2d(half ? &q.t_wqkv_h : &q.t_wqkv, q.wqkv, m->n_qkv, c.d_model, c.d_model, box) == 0;
+            ok = ok && make_tmap_bf16_2d(half ? &q.t_wo_h : &q.t_wo, q.wo, c.d_model, m->d_q, m->d_q, box) == 0;
+            ok = ok && make_tmap_bf16_2d(half ? &q.t_wgu_h : &q.t_wgu, q.wgu, 2 * static_cast<uint64_t>(c.d_ffn), c.d_model, c.d_model, box) == 0;
+            ok = ok && make_tmap_bf16_2d(half ? &q.t_wd_h : &q.t_wd, q.wd, c.d_model, c.d_ffn, c.d_ffn, box) == 0;
+        }
+        if (!ok) return VERILLM_E_CUDA;
+    }
+    if (!m->w4.empty() && m->w4[0].wqkv.group != group) {  // other sizes
+        CU_TRY(cudaDeviceSynchronize());
+        cudaFree(m->w4_mem);
+        m->w4_mem = nullptr;
+        m->w4.clear();
+    }
+    if (!m->w4_mem && (rc = dev_alloc(&m->w4_mem, at[4] * c.n_layers))) return rc;
+    std::vector<LayerW4> made(c.n_layers);
+    for (int l = 0; l < c.n_layers; ++l) {
+        const LayerDev& w = m->layers[l];
+        const bf16* from[4] = {w.wqkv, w.wo, w.wgu, w.wd};
+        verillm_w4* to[4] = {&made[l].wqkv, &made[l].wo, &made[l].wgu, &made[l].wd};
+        for (int i = 0; i < 4; ++i) {
+            unsigned char* base = m->w4_mem + at[4] * l + at[i];
+            to[i]->codes = base;
+            to[i]->scales = base + codes[i];
+            to[i]->n = dims[i][0]; to[i]->k = dims[i][1]; to[i]->group = group;
+            if ((rc = verillm_w4_quantise(from[i], dims[i][1], to[i], cuda_stream))) return rc;
+        }
+    }
+    CU_TRY(cudaStreamSynchronize(st));
+    m->w4.swap(made);
+    return VERILLM_OK;
+} catch (const std::bad_alloc&) {
+    return VERILLM_E_NOMEM;
+}
+
+int verillm_decode_commit_w4(verillm_model* m, const int32_t* tokens, const int32_t* cu_seqlens, int32_t batch, int32_t n_prefill,
+                             const int32_t* check_seq, const int32_t* check_pos, int32_t n_check, void* committed_out, int32_t commit_dtype,
+                             int32_t cache_dtype, int32_t* status, void* cuda_stream) try {
+    if (cache_dtype < -1 || cache_dtype > VERILLM_KV_INT8) return VERILLM_E_INVAL;
+    return decode_impl(m, tokens, cu_seqlens, batch, n_prefill, check_seq, check_pos, n_check, committed_out, commit_dtype, cache_dtype, true,
                        status, cuda_stream);
 } catch (const std::bad_alloc&) {
     return VERILLM_E_NOMEM;
