@@ -610,6 +610,10 @@ class KVCache(_Fixed):
             k=k, v=v, k_scale=k_scale, v_scale=v_scale, device=k.device, n_pages=n_pages, n_kv_heads=n_kv_heads, page_size=page_size, head_dim=head_dim,
             c_struct=KVCacheC(k.data_ptr(), v.data_ptr(), _ptr(k_scale), _ptr(v_scale), n_pages, page_size, n_kv_heads, head_dim, dtype))
 
+    @property
+    def raw(self) -> bytes:
+        return bytes(self.c_struct)
+
     @classmethod
     def alloc(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16,
               device: str | torch.device = "cuda:0") -> "KVCache":
@@ -798,9 +802,12 @@ class W4Weights(_Fixed):
 
 def _strided(t: torch.Tensor, what: str, rows: int, width: int, dtype: torch.dtype, device: torch.device) -> int:
     """Row stride of a [rows][width] matrix whose rows are contiguous."""
-    if t.dtype != dtype or t.device != device or t.shape != (rows, width) or (t.stride(1) != 1 and width > 1):
+    if t.dtype is not dtype or t.get_device() != device.index or t.shape != (rows, width):
         raise ValueError(f"{what} must be a {dtype} [{rows}][{width}] tensor with contiguous rows on {device}")
-    return t.stride(0) if rows > 1 else width
+    strides = t.stride()
+    if strides[1] != 1 and width > 1:
+        raise ValueError(f"{what} must be a {dtype} [{rows}][{width}] tensor with contiguous rows on {device}")
+    return strides[0] if rows > 1 else width
 
 
 def w4_quantise(w: torch.Tensor, group: int = 128, stream: Optional[torch.cuda.Stream] = None) -> W4Weights:
@@ -864,9 +871,19 @@ def _check_word(t: Optional[torch.Tensor], device: torch.device) -> None:
         raise ValueError(f"status must be an int32 tensor of one entry on {device}")
 
 
-def _vector(t: torch.Tensor, what: str, n: int, dtype: torch.dtype, device: torch.device) -> None:
-    if t.dtype != dtype or t.device != device or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} [{n}] tensor on {device}")
+def _vector(t: torch.Tensor, what: str, n: int, dtype: torch.dtype, index: int) -> None:
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} [{n}] tensor on cuda:{index}")
+
+
+def _call(what: str, device: torch.device, stream: Optional[torch.cuda.Stream], fn, *args) -> None:
+    """fn(*args, stream pointer) as `_launch` makes it, and its answer checked; for calls that allocate nothing themselves."""
+    if stream is None and _raw_stream is not None and torch.cuda.current_device() == device.index:
+        code = fn(*args, _raw_stream(device.index))
+    else:
+        code = _launch(device, stream, lambda st: fn(*args, st))
+    if code != 0:
+        raise VerillmError(code, what)
 
 
 # --------------------------------------------------------------------------- drafted tokens
@@ -893,41 +910,42 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu_rows: torch.Ten
     largest logit; 1 without it.  kv_len int32 [batch]: gives the report's new_len.  All on one device; the header has the definitions."""
     if target.dim() != 2 or not target.is_cuda or target.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("target must be a bf16 or float32 CUDA matrix")
-    dev, (n_rows, vocab) = target.device, target.shape
+    dev, (n_rows, vocab), at = target.device, target.shape, target.get_device()
     batch = cu_rows.shape[0] - 1 if cu_rows.dim() == 1 else 0
     t_stride = _strided(target, "target", n_rows, vocab, target.dtype, dev)
     d_stride = 0 if draft is None else _strided(draft, "draft", n_rows, vocab, target.dtype, dev)
-    _vector(cu_rows, "cu_rows", batch + 1, torch.int32, dev)
-    _vector(tokens, "tokens", n_rows, torch.int32, dev)
-    _vector(accept_u, "accept_u", n_rows, torch.float32, dev)
-    _vector(sample_u, "sample_u", batch, torch.float32, dev)
+    _vector(cu_rows, "cu_rows", batch + 1, torch.int32, at)
+    _vector(tokens, "tokens", n_rows, torch.int32, at)
+    _vector(accept_u, "accept_u", n_rows, torch.float32, at)
+    _vector(sample_u, "sample_u", batch, torch.float32, at)
     if temperature is not None:
-        _vector(temperature, "temperature", batch, torch.float32, dev)
+        _vector(temperature, "temperature", batch, torch.float32, at)
     if kv_len is not None:
-        _vector(kv_len, "kv_len", batch, torch.int32, dev)
+        _vector(kv_len, "kv_len", batch, torch.int32, at)
     _check_word(status, dev)
     if report is not None:
-        _vector(report.tokens, "report.tokens", n_rows, torch.int32, dev)
-        _vector(report.n_emitted, "report.n_emitted", batch, torch.int32, dev)
+        _vector(report.tokens, "report.tokens", n_rows, torch.int32, at)
+        _vector(report.n_emitted, "report.n_emitted", batch, torch.int32, at)
         if report.logp is not None:
-            _vector(report.logp, "report.logp", n_rows, torch.float32, dev)
+            _vector(report.logp, "report.logp", n_rows, torch.float32, at)
         if report.new_len is not None:
-            _vector(report.new_len, "report.new_len", batch, torch.int32, dev)
+            _vector(report.new_len, "report.new_len", batch, torch.int32, at)
             if kv_len is None or report.new_len.data_ptr() == kv_len.data_ptr():
                 raise ValueError("report.new_len needs a kv_len, and one that it is not itself")
+    L = lib()
 
     def call(st):
         rep = report or DraftReport(n_rows, batch, dev, kv_len is not None)
         ws = workspace
         if ws is None:
-            ws = torch.empty(max(16, verify_drafts_workspace(n_rows)), dtype=torch.uint8, device=dev)
+            ws = torch.empty(max(16, L.verillm_verify_drafts_workspace(n_rows)), dtype=torch.uint8, device=dev)
         elif ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != dev:
             raise ValueError("workspace must be a contiguous uint8 tensor on the logits' device")
         d = DraftsC(target.data_ptr(), _ptr(draft), t_stride, d_stride, F32 if target.dtype == torch.float32 else BF16, vocab, batch, n_rows,
                     min(int(max_rows), 0x7FFFFFFF), cu_rows.data_ptr(), tokens.data_ptr(), _ptr(kv_len), _ptr(temperature), accept_u.data_ptr(),
                     sample_u.data_ptr())
         r = DraftReportC(rep.tokens.data_ptr(), rep.n_emitted.data_ptr(), _ptr(rep.logp), _ptr(rep.new_len))
-        _check(lib().verillm_verify_drafts(C.byref(d), C.byref(r), ws.data_ptr(), ws.numel(), _ptr(status), st), "verillm_verify_drafts")
+        _check(L.verillm_verify_drafts(C.byref(d), C.byref(r), ws.data_ptr(), ws.numel(), _ptr(status), st), "verillm_verify_drafts")
         return rep
 
     return _launch(dev, stream, call)
@@ -944,6 +962,11 @@ def verify_drafts_workspace(n_rows: int) -> int:
 # --------------------------------------------------------------------------- pages of a paged cache
 
 
+def _layers(caches: Sequence[KVCache]):
+    """The caches' descriptions as a C array."""
+    return (KVCacheC * len(caches)).from_buffer_copy(b"".join([c.raw for c in caches]))
+
+
 class KVPages(_Fixed):
     """Who holds which page of a model's paged cache: caches (one KVCache per layer, one geometry), page_table int32 [batch][width], kv_len int32
     [batch], refs int32 [n_pages] (table entries that name a page; 0: free).  The calls on it change these tensors and must follow one
@@ -958,18 +981,19 @@ class KVPages(_Fixed):
         if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.device != dev or not page_table.is_contiguous():
             raise ValueError(f"page_table must be a contiguous int32 [batch][width] tensor on {dev}")
         batch, width = page_table.shape
-        _vector(kv_len, "kv_len", batch, torch.int32, dev)
-        _vector(refs, "refs", caches[0].n_pages, torch.int32, dev)
+        _vector(kv_len, "kv_len", batch, torch.int32, dev.index)
+        _vector(refs, "refs", caches[0].n_pages, torch.int32, dev.index)
         if any(c.device != dev for c in caches):
             raise ValueError("all layers must be on one device")
         _check_word(status, dev)
         need = lib().verillm_kv_pages_workspace(batch, caches[0].n_pages)
         if need < 0:
             raise VerillmError(int(need), "verillm_kv_pages_workspace")
-        layers = (KVCacheC * len(caches))(*[c.c_struct for c in caches])
+        layers = _layers(caches)
+        workspace = torch.empty(int(need), dtype=torch.uint8, device=dev)
+        c_struct = KVPagesC(layers, len(caches), page_table.data_ptr(), kv_len.data_ptr(), refs.data_ptr(), batch, width)
         self.__dict__.update(caches=caches, page_table=page_table, kv_len=kv_len, refs=refs, status=status, device=dev, layers=layers, batch=batch,
-                             workspace=torch.empty(int(need), dtype=torch.uint8, device=dev),
-                             c_struct=KVPagesC(layers, len(caches), page_table.data_ptr(), kv_len.data_ptr(), refs.data_ptr(), batch, width))
+                             workspace=workspace, c_struct=c_struct, _ref=C.byref(c_struct), _ws=workspace.data_ptr(), _ws_bytes=int(need), _status=_ptr(status))
 
     @classmethod
     def alloc(cls, n_layers: int, batch: int, width: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
@@ -990,34 +1014,30 @@ class KVPages(_Fixed):
 def kv_reserve(pages: KVPages, new_len: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Grows every sequence with new_len[b] > kv_len[b] (int32 [batch]) to new_len[b]: lowest free pages first, a copy of a partly filled page that
     others hold too.  Where the free pages do not suffice, that sequence and the later ones stay as they are (DEV_NO_PAGES)."""
-    _vector(new_len, "new_len", pages.batch, torch.int32, pages.device)
-    _check(_launch(pages.device, stream, lambda st: lib().verillm_kv_reserve(
-        C.byref(pages.c_struct), new_len.data_ptr(), pages.workspace.data_ptr(), pages.workspace.numel(), _ptr(pages.status), st)), "verillm_kv_reserve")
+    _vector(new_len, "new_len", pages.batch, torch.int32, pages.device.index)
+    _call("verillm_kv_reserve", pages.device, stream, lib().verillm_kv_reserve, pages._ref, new_len.data_ptr(), pages._ws, pages._ws_bytes, pages._status)
 
 
 def kv_free(pages: KVPages, new_len: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Shortens every sequence with new_len[b] < kv_len[b] (int32 [batch]) to new_len[b] and lets go of the pages behind."""
-    _vector(new_len, "new_len", pages.batch, torch.int32, pages.device)
-    _check(_launch(pages.device, stream, lambda st: lib().verillm_kv_free(
-        C.byref(pages.c_struct), new_len.data_ptr(), _ptr(pages.status), st)), "verillm_kv_free")
+    _vector(new_len, "new_len", pages.batch, torch.int32, pages.device.index)
+    _call("verillm_kv_free", pages.device, stream, lib().verillm_kv_free, pages._ref, new_len.data_ptr(), pages._status)
 
 
 def kv_fork(pages: KVPages, src: torch.Tensor, dst: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """The empty sequences dst (int32 [n]) come to share what the sequences src hold."""
     n = src.shape[0] if src.dim() == 1 else -1
-    _vector(src, "src", n, torch.int32, pages.device)
-    _vector(dst, "dst", n, torch.int32, pages.device)
-    _check(_launch(pages.device, stream, lambda st: lib().verillm_kv_fork(
-        C.byref(pages.c_struct), src.data_ptr(), dst.data_ptr(), n, pages.workspace.data_ptr(), pages.workspace.numel(), _ptr(pages.status), st)),
-        "verillm_kv_fork")
+    _vector(src, "src", n, torch.int32, pages.device.index)
+    _vector(dst, "dst", n, torch.int32, pages.device.index)
+    _call("verillm_kv_fork", pages.device, stream, lib().verillm_kv_fork, pages._ref, src.data_ptr(), dst.data_ptr(), n, pages._ws, pages._ws_bytes,
+          pages._status)
 
 
 def kv_compact(pages: KVPages, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Moves the pages in use to the front of the pools; returns their number (int32 [1], device)."""
     def call(st):
         used = torch.empty(1, dtype=torch.int32, device=pages.device)
-        _check(lib().verillm_kv_compact(C.byref(pages.c_struct), used.data_ptr(), pages.workspace.data_ptr(), pages.workspace.numel(),
-                                        _ptr(pages.status), st), "verillm_kv_compact")
+        _check(lib().verillm_kv_compact(pages._ref, used.data_ptr(), pages._ws, pages._ws_bytes, pages._status, st), "verillm_kv_compact")
         return used
 
     return _launch(pages.device, stream, call)
@@ -1029,9 +1049,7 @@ def kv_copy(src: Sequence[KVCache], dst: Sequence[KVCache], src_pages: torch.Ten
     dev, n = dst[0].device, src_pages.shape[0] if src_pages.dim() == 1 else -1
     if len(src) != len(dst) or any(c.device != dev for c in src) or any(c.device != dev for c in dst):
         raise ValueError("src and dst must have the same number of layers, all on one device")
-    _vector(src_pages, "src_pages", n, torch.int32, dev)
-    _vector(dst_pages, "dst_pages", n, torch.int32, dev)
+    _vector(src_pages, "src_pages", n, torch.int32, dev.index)
+    _vector(dst_pages, "dst_pages", n, torch.int32, dev.index)
     _check_word(status, dev)
-    a, b = [(KVCacheC * len(s))(*[c.c_struct for c in s]) for s in (src, dst)]
-    _check(_launch(dev, stream, lambda st: lib().verillm_kv_copy(a, b, len(a), src_pages.data_ptr(), dst_pages.data_ptr(), n, _ptr(status), st)),
-           "verillm_kv_copy")
+    _call("verillm_kv_copy", dev, stream, lib().verillm_kv_copy, _layers(src), _layers(dst), len(dst), src_pages.data_ptr(), dst_pages.data_ptr(), n, _ptr(status))
