@@ -5,6 +5,14 @@
 // first operand, lane = output; x comes by TMA as the second.  tcgen05 products of one scale group go to one of two accumulators in tensor memory;
 // another warp group reads each, multiplies by its output's scale and adds to fp32 sums in registers.  So products are exact, scales are
 // applied in fp32, and no weight is rounded again.  Slices of one tile are joined through the cluster's shared memory in the order of the inputs.
+//
+// What bounds it: the hand-overs.  A unit passes four roles (widened, multiplied, read out, its buffers free again), each 100 - 250 cycles behind the
+// one before; a CTA keeps two units under way and takes about 860 cycles for each with the work itself left out, 1500 with it, and two CTAs share an SM.
+// 64 rows x 28672 x 4096: 34.5 us = 435 TFLOP/s (floor 9.4 us, the codes' bytes); 16 rows 27.5 us; 64 rows x 4096 x 14336 in groups of 64 22 us.
+// Tried: operands handed over by halves of units, twice as many under way (64 rows 0.3 us less, 16 rows 1.4 more), one CTA per SM over an equal share
+// of all units with partial tiles in global memory (46 us and 6 for the join), tiles beginning at different inputs and scales prefetched into L2
+// (no change), one issuing warp (no change).  What the outputs' stores and the slices' join cost counts too: with y written row by row behind each
+// row's residual, and a join that only a part of the threads took part in, the first of these took 39 us and 64 rows x 9472 x 4096 33.5 instead of 20.
 #include "common.cuh"
 #include "kernels.h"
 
@@ -97,11 +105,34 @@ __device__ __forceinline__ void widen(uint32_t q, uint32_t* r) {
     }
 }
 
-__device__ __forceinline__ void tc_store_y(const W4Params& p, int row, int n, float v) {
-    if (row >= p.rows || n >= p.n) return;
-    if (p.residual) v += p.residual[row * p.res_stride + n];
-    if (p.out_f32) reinterpret_cast<float*>(p.y)[row * p.y_stride + n] = v;
-    else reinterpret_cast<bf16*>(p.y)[row * p.y_stride + n] = __float2bfloat16_rn(v);
+// Stores COUNT neighbours of y from (row, n) on, along a row or down a column, of which `live` exist.  What is added is read first: the reads wait
+// together, and for no store.
+template <int COUNT>
+__device__ __forceinline__ void tc_store_y(const W4Params& p, int row, int n, bool along, const float* v, int live) {
+    float r[COUNT];
+    const long long ys = along ? 1 : p.y_stride;
+    if (p.residual) {
+        const float* res = p.residual + row * p.res_stride + n;
+        const long long rs = along ? 1 : p.res_stride;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) r[i] = i < live ? res[i * rs] : 0.f;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) r[i] += v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) r[i] = v[i];
+    }
+    if (p.out_f32) {
+        float* y = reinterpret_cast<float*>(p.y) + row * p.y_stride + n;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i)
+            if (i < live) y[i * ys] = r[i];
+    } else {
+        bf16* y = reinterpret_cast<bf16*>(p.y) + row * p.y_stride + n;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i)
+            if (i < live) y[i * ys] = __float2bfloat16_rn(r[i]);
+    }
 }
 
 template <int N, int G>
@@ -116,13 +147,10 @@ __global__ void __launch_bounds__(T_THREADS, 2) w4_tc_kernel(const __grid_consta
 
     const int ranks = p.ranks, rank = ranks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
     const int n0 = blockIdx.x / ranks * T_TILE, row0 = blockIdx.y * N;
-    // Units go in pairs, a stage of codes each; what lies behind the last input is read as zeros and scaled by 0.  Every tile begins at another
-    // pair of its slice: tiles that walk the same columns in step read from the same few memory channels at a time (28672 x 4096: 32 us that way).
+    // Units go in pairs, a stage of codes each; what lies behind the last input is read as zeros and scaled by 0.
     const int pairs_all = (p.k + 2 * T_UNIT - 1) / (2 * T_UNIT);
-    const int q_first = pairs_all * rank / ranks, pairs = pairs_all * (rank + 1) / ranks - q_first, q_end = q_first + pairs;
-    const int q_begin = q_first + static_cast<int>(blockIdx.x / ranks) % pairs;
-    const int units = 2 * pairs, groups = units * SB;
-    auto next_pair = [&](int& q) { q = q + 1 == q_end ? q_first : q + 1; };
+    const int q_first = pairs_all * rank / ranks, pairs = pairs_all * (rank + 1) / ranks - q_first;
+    const int units = 2 * pairs, groups = units * SB, g_first = q_first * (2 * SB);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < T_WSTAGES; ++i) {
@@ -191,16 +219,14 @@ __global__ void __launch_bounds__(T_THREADS, 2) w4_tc_kernel(const __grid_consta
         // scales are fetched AHEAD groups early; the bits are converted where they are used, because a conversion waits for the load
         constexpr int AHEAD = 4;
         uint32_t s[AHEAD];
-        int q_next = q_begin, g_in = 0;  // the group whose scale is fetched next: pair, and within it
+        int g_next = g_first;  // the group whose scale is fetched next
+        sc += static_cast<size_t>(g_first) * p.n;
         auto fetch = [&](uint32_t& to) {
-            const int g = q_next * (2 * SB) + g_in;
             // (16 bits into a 32-bit register: nothing here waits for them)
             asm volatile("{\n.reg .pred in;\nsetp.ne.u32 in, %2, 0;\nmov.u32 %0, 0;\n@in ld.global.nc.u16 %0, [%1];\n}\n"
-                         : "=r"(to) : "l"(sc + static_cast<size_t>(g) * p.n), "r"(g < p.groups ? 1 : 0));
-            if (++g_in == 2 * SB) {
-                g_in = 0;
-                next_pair(q_next);
-            }
+                         : "=r"(to) : "l"(sc), "r"(g_next < p.groups ? 1 : 0));
+            ++g_next;
+            sc += p.n;
         };
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
@@ -235,7 +261,7 @@ __global__ void __launch_bounds__(T_THREADS, 2) w4_tc_kernel(const __grid_consta
         }
         if (ranks == 1) {
 #pragma unroll
-            for (int r = 0; r < N; ++r) tc_store_y(p, row0 + r, n, acc[r]);
+            for (int r = 0; r < N; r += 16) tc_store_y<16>(p, row0 + r, n, false, acc + r, n < p.n ? p.rows - row0 - r : 0);
         } else {
             // the slices' sums side by side in each CTA's shared memory: the stages of codes are idle once the last product is complete and every
             // copy has landed
@@ -277,30 +303,29 @@ __global__ void __launch_bounds__(T_THREADS, 2) w4_tc_kernel(const __grid_consta
             warp_wait(bar(L::DRAIN), 0, p.status);
         } else if (warp == 13) {  // ---------------- x
             if (leader) tma_prefetch_desc(&map_x);
-            int u = 0, q = q_begin;
+            int u = 0;
             Ring<T_XSTAGES> x;
             for (; u < units; ++u, x.next()) {
                 if (u >= T_XSTAGES && !unit_done(u - T_XSTAGES)) break;
                 if (leader) {
-                    const int k = q * (2 * T_UNIT) + (u & 1) * T_UNIT;
+                    const int k = q_first * (2 * T_UNIT) + u * T_UNIT;
                     mbar_arrive_expect_tx(bar(L::U_FULL + x.at), L::XBYTES);
                     tma_load_2d(base + L::X0 + x.at * L::XBYTES, &map_x, k, row0, bar(L::U_FULL + x.at));
                     tma_load_2d(base + L::X0 + x.at * L::XBYTES + L::XHALF, &map_x, k + 64, row0, bar(L::U_FULL + x.at));
                 }
-                if (u & 1) next_pair(q);
                 __syncwarp();
             }
             // copies that are under way land before the CTA ends
             for (int j = max(0, u - T_XSTAGES); j < u; ++j) warp_wait(bar(L::U_FULL + j % T_XSTAGES), (j / T_XSTAGES) & 1, p.status);
         } else if (warp == 14) {  // ---------------- codes
             if (leader) tma_prefetch_desc(&map_w);
-            int j = 0, q = q_begin;
+            int j = 0;
             Ring<T_WSTAGES> w;
-            for (; j < pairs; ++j, w.next(), next_pair(q)) {
+            for (; j < pairs; ++j, w.next()) {
                 if (j >= T_WSTAGES && !warp_wait(bar(L::W_EMPTY + w.at), w.phase ^ 1u, p.status)) break;
                 if (leader) {
                     mbar_arrive_expect_tx(bar(L::W_FULL + w.at), T_WBYTES);
-                    tma_load_2d(base + w.at * T_WBYTES, &map_w, q * (T_UNIT / 2), n0, bar(L::W_FULL + w.at));
+                    tma_load_2d(base + w.at * T_WBYTES, &map_w, (q_first + j) * (T_UNIT / 2), n0, bar(L::W_FULL + w.at));
                 }
                 __syncwarp();
             }
@@ -317,17 +342,19 @@ __global__ void __launch_bounds__(T_THREADS, 2) w4_tc_kernel(const __grid_consta
     // rows dealt over the cluster
     cluster_arrive();
     cluster_wait();
-    const int rows = min(p.rows - row0, N);
-    for (int i = threadIdx.x; i < rows * T_TILE; i += T_THREADS) {
-        const int r = i / T_TILE, c = i % T_TILE;
-        if (r % ranks != rank) continue;
-        float v = 0.f;
+    const int mine = (min(p.rows - row0, N) - rank + ranks - 1) / ranks;  // rows of this CTA: rank, rank + ranks, ..
+    for (int i = threadIdx.x; i < mine * (T_TILE / 4); i += T_THREADS) {
+        const int r = rank + ranks * (i / (T_TILE / 4)), c = i % (T_TILE / 4) * 4;
+        float v[4] = {};
+#pragma unroll 2
         for (int q = 0; q < ranks; ++q) {
-            float f;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(map_to_cta(base + 4u * i, q)) : "memory");
-            v += f;
+            float f[4];
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]) : "r"(map_to_cta(base + 4u * (r * T_TILE + c), q)) : "memory");
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += f[e];
         }
-        tc_store_y(p, row0 + r, n0 + c, v);
+        tc_store_y<4>(p, row0 + r, n0 + c, true, v, p.n - n0 - c);
     }
     cluster_arrive();  // no CTA leaves while another still reads its sums
     cluster_wait();
