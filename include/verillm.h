@@ -452,7 +452,8 @@ typedef struct {
 
 /* A row that the walk reaches and that has no distribution (an entry NaN or +inf, in the draft's row too, or all -inf; a temperature out of range)
  * ends its sequence before it: n_emitted = a, nothing drawn, VERILLM_DEV_LOGITS.  A drafted token outside the vocabulary is rejected
- * (VERILLM_DEV_TOKEN_RANGE).  Decisions are those of 64-bit arithmetic.
+ * (VERILLM_DEV_TOKEN_RANGE).  Decisions are those of 64-bit arithmetic (T below 2^-60: with
+ * zero logits taken for 2^-127).
  *  workspace  DEVICE, 16-byte aligned, verillm_verify_drafts_workspace(n_rows) bytes; holds nothing between calls, but calls that may overlap need one each
  *  status     optional DEVICE word, raised from 0 to the first problem met, never cleared by the call
  * Allocates nothing; make the first call on a device outside a capture.  Errors: E_INVAL, E_SHAPE, E_ARCH, E_CUDA. */

@@ -215,18 +215,19 @@ __global__ void __launch_bounds__(DR_THREADS) draft_rows_kernel(const DraftParam
 }
 
 // exp((l - top) / T) for l <= top in 64 bits: 2^n times a polynomial for the rest, |r| <= 1/2, degree 8 through the nine Chebyshev points, relative error
-// below 2e-12; a factor that all entries of a row share may differ more (top / T is rounded once).  No table: reads of one in shared memory
-// conflict (a draw of 64 sequences: 134 us with one of 256 entries).
+// below 2e-12.  No table: reads of one in shared memory conflict (a draw of 64 sequences: 134 us with one of 256 entries).
 struct Exp64 {
     double scale;  // log2 e / T
     float floor;   // differences of logits below this: 0
-    __device__ __forceinline__ double shift(float top) const { return -static_cast<double>(top) * scale; }
-    __device__ __forceinline__ double operator()(float l, float top, double shift) const {
-        // the float as a double by its bits: a conversion instruction costs as much as four additions (no subnormals, infinities or NaN matter here)
+    // less: -top
+    __device__ __forceinline__ double operator()(float l, float top, double less) const {
+        // the float as a double by its bits: a conversion instruction costs as much as four additions (subnormals become
+        // 2^-127 or so, infinities and NaN do not matter here)
         const int bits = __float_as_int(l);
         const double d = __hiloint2double(((bits >> 3) & 0x8FFFFFFF) + 0x38000000, bits << 29);
-        const double x = fma(d, scale, shift), big = x + 6755399441055744.0;  // 1.5 2^52: the nearest integer in the low bits
-        const double r = x - (big - 6755399441055744.0);
+        // the difference first: both may be far larger than it, and scale is as large as 2^100
+        const double x = d + less, big = fma(x, scale, 6755399441055744.0);  // 1.5 2^52: the nearest integer in the low bits
+        const double r = fma(x, scale, -(big - 6755399441055744.0));
         double e = fma(r, 1.3255224878668817e-06, 1.5310079402249296e-05);
         e = fma(r, e, 0.00015403455852453838);
         e = fma(r, e, 0.0013333450568000645);
@@ -245,7 +246,7 @@ struct Weights {
     int kind;       // 0: p; 1: p without token x; 2: max(0, p - q)
     int x;
     float pm, qm;   // the rows' maxima
-    double ps, qs;  // their shifts
+    double ps, qs;  // and -1 times these
     double a, b;    // kind 2: a e_p - b e_q, a = sum e_q, b = sum e_p
 };
 
@@ -392,8 +393,8 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     const int wb1 = min(min(wb0 + per_warp, (rank + 1) * per_cta), blocks);
     int turn = 0;
     // One pass over row i in 64 bits.  Per warp, per CTA and over the cluster: 0 = sum of e_p (without token x for kind 1); for kind 2 that and 1 = sum of e_q
-    // over the entries with p <= q, 2 and 3 the same over those with p > q, as fp32 sees it (it errs only where p and q agree to 10^-6, which changes the sum of
-    // max(0, p - q) by less than 10^-12).
+    // over the entries with p <= q, 2 and 3 the same over those with p > q, as fp32 sees it (from differences to the largest logits: it errs only where p and q
+    // agree to about 10^-6 times 1 - log p).
     Weights w;
     double total[4];  // of the row: 0 sum of e_p, 1 of e_q, 2 and 3 over p > q
     double cta_part = 0.0;  // lane 4 r + i: sum i of CTA r
@@ -403,9 +404,9 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
         w.x = x;
         w.pm = sm_pm[i];
         w.qm = sm_qm[i];
-        w.ps = ex.shift(w.pm);
-        w.qs = ex.shift(w.qm);
-        const float kp = -w.pm * c - log2f(sm_ps[i]), kq = -w.qm * c - log2f(sm_qs[i]);
+        w.ps = -static_cast<double>(w.pm);
+        w.qs = -static_cast<double>(w.qm);
+        const float kp = -log2f(sm_ps[i]), kq = -log2f(sm_qs[i]);
         double v[4] = {0.0, 0.0, 0.0, 0.0};
         // blocks are fetched two steps ahead
         auto fetch = [&](int k, uint4& f, uint4& g) {
@@ -429,7 +430,7 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
                 if (kind == 2) {
                     const float lq = rq.get(g, e);
                     const double eq = ex(lq, w.qm, w.qs);
-                    if (fmaf(lp, c, kp) > fmaf(lq, c, kq)) {
+                    if (fmaf(lp - w.pm, c, kp) > fmaf(lq - w.qm, c, kq)) {
                         v[2] += ep;
                         v[3] += eq;
                     } else {
@@ -566,34 +567,38 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
         }
         if (warp == ow) {
             int token = -1;
-            double run = start;
-            for (int k0 = wb0; k0 < wb1; k0 += 32) {
-                const int k = k0 + lane;
-                double x[E], sum = 0.0;
-#pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = 0.0;
-                if (k < wb1) weights_of<T>(rp, rq, ex, w, k * E - rp.off, x);
-#pragma unroll
-                for (int e = 0; e < E; ++e) sum += x[e];
-                double incl = sum;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const double v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                    if (lane >= o) incl += v;
-                }
-                const double begin = run + (incl - sum);
-                const unsigned who = __ballot_sync(0xFFFFFFFFu, sum > 0.0 && begin <= point);
-                if (who) {
-                    int tok = -1;
-                    double r = begin;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        if (x[e] > 0.0 && r <= point) tok = k * E - rp.off + e;
-                        r += x[e];
+            // a warp's sums can come out above 0 by rounding where its entries are all 0 (p = q there to 10^-16): then one of p's
+            for (int again = 0; again < 2 && token < 0; ++again) {
+                if (again) w.kind = 0;
+                double run = start;
+                for (int k0 = wb0; k0 < wb1; k0 += 32) {
+                    const int k = k0 + lane;
+                    double x[E], sum = 0.0;
+    #pragma unroll
+                    for (int e = 0; e < E; ++e) x[e] = 0.0;
+                    if (k < wb1) weights_of<T>(rp, rq, ex, w, k * E - rp.off, x);
+    #pragma unroll
+                    for (int e = 0; e < E; ++e) sum += x[e];
+                    double incl = sum;
+    #pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const double v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+                        if (lane >= o) incl += v;
                     }
-                    token = __shfl_sync(0xFFFFFFFFu, tok, 31 - __clz(who));
+                    const double begin = run + (incl - sum);
+                    const unsigned who = __ballot_sync(0xFFFFFFFFu, sum > 0.0 && begin <= point);
+                    if (who) {
+                        int tok = -1;
+                        double r = begin;
+    #pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            if (x[e] > 0.0 && r <= point) tok = k * E - rp.off + e;
+                            r += x[e];
+                        }
+                        token = __shfl_sync(0xFFFFFFFFu, tok, 31 - __clz(who));
+                    }
+                    run += __shfl_sync(0xFFFFFFFFu, incl, 31);
                 }
-                run += __shfl_sync(0xFFFFFFFFu, incl, 31);
             }
             if (lane == 0) {
                 p.out_tokens[s.row0 + stop] = token;
@@ -637,9 +642,12 @@ cudaError_t launch_verify_drafts(DraftParams p, int num_sms, cudaStream_t stream
     cfg.blockDim = dim3(DV_THREADS);
     cfg.stream = stream;
     cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // its start under the first kernel's end
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    int n = 1;
+    int n = 0;
+    if (p.n_rows > 0) {  // its start under the first kernel's end
+        at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
     if (p.ranks > 1) {
         at[n].id = cudaLaunchAttributeClusterDimension;
         at[n].val.clusterDim.x = p.ranks;

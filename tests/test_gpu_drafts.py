@@ -136,6 +136,28 @@ def test_far_temperatures_and_peaked_rows(vocab):
     _check(m)
 
 
+@pytest.mark.parametrize("vocab", [900, 30000])
+def test_ties_of_large_logits_at_small_temperatures(vocab):
+    m = _make([5] * 8, vocab, torch.float32, True, [2.0 ** -100, 2.0 ** -60, 1e-9, 1e-4] * 2)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for name in ("target", "draft"):
+        m[name] = torch.where(torch.rand(40, vocab, generator=g, device=DEV) < 0.3, 12345.678, m[name])
+    m["tokens"] = m["draft"].roll(1, 0).argmax(-1).to(torch.int32)
+    _check(m)
+    _check(dict(m, draft=None))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_drafts_close_to_the_target_far_from_zero(dtype):
+    """Logits near 500 at T = 0.01: log p is a difference of numbers near 72000."""
+    m = _make([3] * 40, 2000, torch.float32, True, [0.01] * 40, spread=0.02)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    m["target"] = (m["target"] + (500 if dtype == torch.float32 else 0)).to(dtype)
+    m["draft"] = (m["target"].float() + 0.002 * torch.randn(120, 2000, generator=g, device=DEV)).to(dtype)
+    m["ua"] = 0.9 + 0.1 * m["ua"]
+    _check(m)
+
+
 def test_numbers_next_to_the_border_are_decided_in_64_bits():
     """accept_u set to p / q rounded to fp32 and its two neighbours: fp32 sums of 3000 terms cannot tell them apart."""
     m = _make([9] * 30, 3000, torch.float32, True, [0.9] * 30, spread=0.8)
