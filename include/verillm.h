@@ -442,7 +442,7 @@ typedef struct {
     const float *sample_u;     /* DEVICE [batch], uniform in [0, 1); bounded to [0, 1], NaN counts as 0 */
 } verillm_drafts;
 
-/* Caller-allocated DEVICE outputs */
+/* Caller-allocated DEVICE outputs, not overlapping the inputs */
 typedef struct {
     int32_t *tokens;    /* [n_rows]: what was emitted: the accepted tokens (rows 0 .. a-1), the drawn one (row a), -1 behind it */
     int32_t *n_emitted; /* [batch] a + 1 */

@@ -1046,6 +1046,8 @@ def kv_compact(pages: KVPages, stream: Optional[torch.cuda.Stream] = None) -> to
 def kv_copy(src: Sequence[KVCache], dst: Sequence[KVCache], src_pages: torch.Tensor, dst_pages: torch.Tensor,
             status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Copies pages src_pages (int32 [n]) of the caches src, one per layer, to pages dst_pages of the caches dst; pairs with a -1 are left out."""
+    if not dst:
+        raise ValueError("at least one layer's cache")
     dev, n = dst[0].device, src_pages.shape[0] if src_pages.dim() == 1 else -1
     if len(src) != len(dst) or any(c.device != dev for c in src) or any(c.device != dev for c in dst):
         raise ValueError("src and dst must have the same number of layers, all on one device")

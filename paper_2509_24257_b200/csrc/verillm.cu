@@ -1303,7 +1303,11 @@ int verillm_quantise_w4(verillm_model* m, int32_t group, void* cuda_stream) try 
             ok = ok && make_tmap_bf16_2d(half ? &q.t_wgu_h : &q.t_wgu, q.wgu, 2 * static_cast<uint64_t>(c.d_ffn), c.d_model, c.d_model, box) == 0;
             ok = ok && make_tmap_bf16_2d(half ? &q.t_wd_h : &q.t_wd, q.wd, c.d_model, c.d_ffn, c.d_ffn, box) == 0;
         }
-        if (!ok) return VERILLM_E_CUDA;
+        if (!ok) {  // (wd stands for all of it being there)
+            cudaFree(q.wd);
+            q.wd = nullptr;
+            return VERILLM_E_CUDA;
+        }
     }
     if (!m->w4.empty() && m->w4[0].wqkv.group != group) {  // other sizes
         CU_TRY(cudaDeviceSynchronize());
@@ -1515,6 +1519,8 @@ int verillm_verify_drafts(const verillm_drafts* d, const verillm_draft_report* r
             (d->draft && d->draft_stride < d->vocab))
             return VERILLM_E_SHAPE;
         if ((reinterpret_cast<uintptr_t>(workspace) & 15u) || workspace_bytes < verillm_verify_drafts_workspace(d->n_rows)) return VERILLM_E_SHAPE;
+        // what one CTA writes others may still read
+        if (rep->tokens == d->tokens || static_cast<const void*>(rep->logp) == d->accept_u) return VERILLM_E_INVAL;
     }
     DraftParams p;
     std::memset(&p, 0, sizeof(p));

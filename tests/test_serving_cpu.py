@@ -88,6 +88,18 @@ def test_bad_reports_and_workspaces_are_refused(library):
     assert library.verillm_verify_drafts_workspace(-1) == vb.E_INVAL
 
 
+def test_reports_over_their_inputs_are_refused(library):
+    call = library.verillm_verify_drafts
+    apart = dict(tokens=PTR + (1 << 20), logp=PTR + (2 << 20))
+    for kw in (dict(tokens=PTR), dict(logp=PTR)):
+        assert call(C.byref(_drafts()), C.byref(_report(**dict(apart, **kw))), PTR, 1 << 30, None, None) == vb.E_INVAL
+
+
+def test_no_layers_to_copy():
+    with pytest.raises(ValueError):
+        vb.kv_copy([], [], None, None)
+
+
 def _layers(n=2, **kw):
     f = dict(k=PTR, v=PTR, k_scale=PTR, v_scale=PTR, n_pages=10, page_size=16, n_kv_heads=2, head_dim=64, dtype=vb.KV_E4M3)
     a = [dict(f) for _ in range(n)]
