@@ -10,7 +10,7 @@
 // draft_rows_kernel, bound by HBM and by the instructions per entry: maximum and sum of exp2 in fp32 of every row that counts, divided over the vocabulary, one
 // pass (64 sequences of 6 rows x 128256 bf16 entries, target and draft: about 45 us for 180 MB, 62 % of the copy rate).
 // draft_verify_kernel, a cluster per sequence, bound by the fp64 pipe where it draws (the same call: about 50 us), by latency for small calls: joins these, accepts what is clear at fp32's error, decides the rows next to the border from
-// sums in 64 bits, and draws by sums in 64 bits: over CTAs, warps, steps of a warp, lanes and entries, at each level the last part that begins at or before
+// sums in 64 bits, and draws by sums in 64 bits: over CTAs, warps, parts of a warp's share, steps, lanes and entries, at each level the last part that begins at or before
 // the drawn point and is not empty.
 #include "common.cuh"
 #include "kernels.h"
@@ -284,6 +284,7 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     constexpr int E = Row<T>::E;
     __shared__ double warp_tot[4][DV_WARPS];
     __shared__ double cta_tot[2][4];  // used in turn
+    __shared__ double part_tot[DV_WARPS];
     __shared__ float sm_pm[kDraftMaxRows], sm_ps[kDraftMaxRows], sm_qm[kDraftMaxRows], sm_qs[kDraftMaxRows];
     __shared__ int sm_code[kDraftMaxRows], sm_arg[kDraftMaxRows];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -566,22 +567,46 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
             }
             at += v;
         }
-        if (warp == ow) {
-            int token = -1;
-            // a warp's sums can come out above 0 by rounding where its entries are all 0 (p = q there to 10^-16): then one of p's
-            for (int again = 0; again < 2 && token < 0; ++again) {
-                if (again) w.kind = 0;
-                double run = start;
-                for (int k0 = wb0; k0 < wb1; k0 += 32) {
+        // that warp's blocks again, dealt over all warps in whole steps of 32, and the one with the point
+        const int o0 = rank * per_cta + ow * per_warp, o1 = min(min(o0 + per_warp, (rank + 1) * per_cta), blocks);
+        const int per_part = (o1 - o0 + DV_WARPS * 32 - 1) / (DV_WARPS * 32) * 32, k_first = o0 + warp * per_part, k_last = min(k_first + per_part, o1);
+        // a warp's sums can come out above 0 by rounding where its entries are all 0 (p = q there to 10^-16): then one of p's
+        for (int again = 0; again < 2; ++again) {
+            if (again) w.kind = 0;
+            double x[E], sum = 0.0;
+            auto step = [&](int k) {  // x = the weights of block k
+                double v = 0.0;
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] = 0.0;
+                if (k < k_last) weights_of<T>(rp, rq, ex, w, k * E - rp.off, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) v += x[e];
+                return v;
+            };
+            for (int k0 = k_first; k0 < k_last; k0 += 32) sum += step(k0 + lane);
+            const double part = warp_sum64(sum);
+            if (again) __syncthreads();  // (the sums of the first try have been read)
+            if (lane == 0) part_tot[warp] = part;
+            __syncthreads();
+            int op = -1;
+            double at = start, run = start;
+            const double mine = lane < DV_WARPS ? part_tot[lane] : 0.0;
+            for (int k = 0; k < DV_WARPS; ++k) {
+                const double v = __shfl_sync(0xFFFFFFFFu, mine, k);
+                if (v > 0.0 && at <= point) {
+                    op = k;
+                    run = at;
+                }
+                at += v;
+            }
+            if (op < 0) continue;
+            if (warp == op) {
+                int token = -1;
+                for (int k0 = k_first; k0 < k_last; k0 += 32) {
                     const int k = k0 + lane;
-                    double x[E], sum = 0.0;
-    #pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = 0.0;
-                    if (k < wb1) weights_of<T>(rp, rq, ex, w, k * E - rp.off, x);
-    #pragma unroll
-                    for (int e = 0; e < E; ++e) sum += x[e];
+                    if (per_part > 32) sum = step(k);  // (else it is still there)
                     double incl = sum;
-    #pragma unroll
+#pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
                         const double v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
                         if (lane >= o) incl += v;
@@ -591,7 +616,7 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
                     if (who) {
                         int tok = -1;
                         double r = begin;
-    #pragma unroll
+#pragma unroll
                         for (int e = 0; e < E; ++e) {
                             if (x[e] > 0.0 && r <= point) tok = k * E - rp.off + e;
                             r += x[e];
@@ -600,11 +625,12 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
                     }
                     run += __shfl_sync(0xFFFFFFFFu, incl, 31);
                 }
+                if (lane == 0) {
+                    p.out_tokens[s.row0 + stop] = token;
+                    if (p.logp) p.logp[s.row0 + stop] = token < 0 ? 0.f : static_cast<float>(kLn2) * ((rp.entry(token) - w.pm) * c - log2f(sm_ps[stop]));
+                }
             }
-            if (lane == 0) {
-                p.out_tokens[s.row0 + stop] = token;
-                if (p.logp) p.logp[s.row0 + stop] = token < 0 ? 0.f : static_cast<float>(kLn2) * ((rp.entry(token) - w.pm) * c - log2f(sm_ps[stop]));
-            }
+            break;
         }
     }
     if (ranks > 1) {
