@@ -8,8 +8,9 @@
 // often enough.  Two kernels:
 //
 // draft_rows_kernel, bound by HBM and by the instructions per entry: maximum and sum of exp2 in fp32 of every row that counts, divided over the vocabulary, one
-// pass (64 sequences of 6 rows x 128256 bf16 entries, target and draft: about 45 us for 180 MB, 62 % of the copy rate).
-// draft_verify_kernel, a cluster per sequence, bound by the fp64 pipe where it draws (the same call: about 50 us), by latency for small calls: joins these, accepts what is clear at fp32's error, decides the rows next to the border from
+// pass (64 sequences of up to 6 rows x 128256 bf16 entries, target and draft: 37 us for 146 MB, 61 % of the copy rate).
+// draft_verify_kernel, a cluster per sequence, bound by issue and the fp64 pipe where it draws (the same call: 42 us, fp64 pipe a third busy, 1.95 of 4
+// instructions a clock), by a chain of reads and barriers for small calls (9 us): joins these, accepts what is clear at fp32's error, decides the rows next to the border from
 // sums in 64 bits, and draws by sums in 64 bits: over CTAs, warps, parts of a warp's share, steps, lanes and entries, at each level the last part that begins at or before
 // the drawn point and is not empty.
 #include "common.cuh"
@@ -661,7 +662,7 @@ cudaError_t launch_verify_drafts(DraftParams p, int num_sms, cudaStream_t stream
         if (e != cudaSuccess) return e;
     }
     // a CTA takes 4096 entries of a row at least; larger clusters as long as all CTAs run at once, one per SM
-    // (64 sequences over 128256 entries: 51 us with clusters of two, 61 of four)
+    // (64 sequences over 128256 entries: two waves of clusters of four take 10 us longer than clusters of two)
     p.ranks = 1;
     while (p.ranks < 8 && p.vocab > 4096 * p.ranks && static_cast<long long>(p.batch) * p.ranks * 2 <= num_sms) p.ranks *= 2;
     cudaLaunchConfig_t cfg = {};

@@ -4,9 +4,10 @@
 // of n positions holds the first ceil(n / page_size) entries of its row of the table.  Every operation gives the same result whatever the timing: free pages are taken lowest
 // first, by sequences in order.
 //
-// Planning is one CTA's work over a few thousand integers, bound by latency (64 sequences growing and shrinking, 9000 pages: 15.4 us for both calls; 21.9 with
-// counts read phase by phase and holders compared by single threads).  Copies are HBM-bound and spread over the GPU in pieces of 8 KB: the number of copies is only known
-// on the device, so a fixed grid walks them (24 sequences of 6000 positions, 4 layers, out, compacted and in: 186 us for 896 MB, 75 % of the copy rate).
+// Planning is one CTA's work over a few thousand integers, bound by latency (64 sequences growing and shrinking, 9000 pages: 14.2 us for both calls; 21.9 with
+// counts read phase by phase and holders compared by single threads).  Copies are HBM-bound and spread over the GPU in pieces of 32 KB: the number of copies is only known
+// on the device, so a fixed grid walks them (24 sequences of 6000 positions, 4 layers, some in, the rest compacted: 156 us for 896 MB with the planning, 89 % of the
+// copy rate).
 #include "common.cuh"
 #include "kernels.h"
 
@@ -19,7 +20,8 @@ constexpr int PL_WARPS = PL_THREADS / 32;
 constexpr int PL_SMALL = 1024;     // sequences whose plans fit shared memory
 constexpr int PL_STEPS = 16;       // loads of counts in flight per thread
 constexpr int CP_THREADS = 256;
-constexpr int CP_PIECE = 8192;     // bytes of a page that a CTA copies at a time
+constexpr int CP_LOADS = 8;        // 16-byte loads in flight per thread (the two copies of the header's example 175 us with 2, 170 with 4, 156 with 8)
+constexpr int CP_PIECE = CP_THREADS * 16 * CP_LOADS;  // bytes of a page that a CTA copies at a time
 constexpr int WS_HEADER = 32;      // ints: [0] number of copies, [1] first page behind those in use
 
 __device__ __forceinline__ void raise(int* status, int code) {
@@ -335,37 +337,62 @@ struct CopyJob {
     int batch, table_width, page_shift;
 };
 
+// Pieces are counted by (pair, layer, piece of a page), the last running fastest; a CTA takes every gridDim.x-th, by additions with carries: a division of
+// 64-bit numbers in every thread costs more than the copy.  Where a piece lies is looked up while the one before it is on its way.
 __device__ __forceinline__ void copy_pages(const CopyJob& job, const PoolSet& from, const PoolSet& to) {
     const int n = job.count ? __ldcg(job.count) : job.n;
-    const int page_pieces = (job.page_bytes + CP_PIECE - 1) / CP_PIECE, scale_pieces = (job.scale_bytes + CP_PIECE - 1) / CP_PIECE;
-    const int pieces = 2 * (page_pieces + scale_pieces);
-    const long long total = static_cast<long long>(n) * job.n_layers * pieces;
-    for (long long u = blockIdx.x; u < total; u += gridDim.x) {
-        const long long q = u / pieces;
-        int piece = static_cast<int>(u - q * pieces);
-        const int layer = static_cast<int>(q % job.n_layers), i = static_cast<int>(q / job.n_layers);
-        const int s = __ldcg(job.src + i), d = __ldcg(job.dst + i);
-        if (s == -1 || d == -1) continue;
+    const unsigned page_pieces = (job.page_bytes + CP_PIECE - 1) / CP_PIECE, scale_pieces = (job.scale_bytes + CP_PIECE - 1) / CP_PIECE;
+    const unsigned pieces = 2 * (page_pieces + scale_pieces), layers = job.n_layers;
+    const unsigned step_piece = gridDim.x % pieces, step_layer = gridDim.x / pieces % layers, step_pair = gridDim.x / pieces / layers;
+    unsigned piece = blockIdx.x % pieces, layer = blockIdx.x / pieces % layers;
+    long long pair = blockIdx.x / pieces / layers;
+
+    struct Place {
+        const char* x;
+        char* y;
+        int bytes;  // 0: nothing to copy
+    };
+    auto place = [&] {
+        Place at = {nullptr, nullptr, 0};
+        if (pair >= n) return at;
+        const int s = __ldcg(job.src + pair), d = __ldcg(job.dst + pair);
+        if (s == -1 || d == -1) return at;
         if (static_cast<unsigned>(s) >= static_cast<unsigned>(job.src_n_pages) || static_cast<unsigned>(d) >= static_cast<unsigned>(job.dst_n_pages)) {
             if (threadIdx.x == 0) raise(job.status, VERILLM_DEV_PAGE_RANGE);
-            continue;
+            return at;
         }
-        const bool value = piece >= page_pieces + scale_pieces;
-        if (value) piece -= page_pieces + scale_pieces;
-        const bool scale = piece >= page_pieces;
-        if (scale) piece -= page_pieces;
+        unsigned k = piece;
+        const bool value = k >= page_pieces + scale_pieces;
+        if (value) k -= page_pieces + scale_pieces;
+        const bool scale = k >= page_pieces;
+        if (scale) k -= page_pieces;
         const char* a = scale ? (value ? from.v_scale[layer] : from.k_scale[layer]) : (value ? from.v[layer] : from.k[layer]);
         char* b = scale ? (value ? to.v_scale[layer] : to.k_scale[layer]) : (value ? to.v[layer] : to.k[layer]);
-        const int bytes = scale ? job.scale_bytes : job.page_bytes;
-        const int begin = piece * CP_PIECE, end = min(begin + CP_PIECE, bytes);
-        const char* x = a + static_cast<size_t>(s) * bytes;
-        char* y = b + static_cast<size_t>(d) * bytes;
-        const int o = begin + threadIdx.x * 16;
-        uint4 v0, v1;
-        if (o < end) v0 = *reinterpret_cast<const uint4*>(x + o);
-        if (o + CP_THREADS * 16 < end) v1 = *reinterpret_cast<const uint4*>(x + o + CP_THREADS * 16);
-        if (o < end) *reinterpret_cast<uint4*>(y + o) = v0;
-        if (o + CP_THREADS * 16 < end) *reinterpret_cast<uint4*>(y + o + CP_THREADS * 16) = v1;
+        const int bytes = scale ? job.scale_bytes : job.page_bytes, begin = static_cast<int>(k) * CP_PIECE;
+        at.x = a + static_cast<size_t>(s) * bytes + begin;
+        at.y = b + static_cast<size_t>(d) * bytes + begin;
+        at.bytes = min(CP_PIECE, bytes - begin);
+        return at;
+    };
+    const int o = threadIdx.x * 16;
+    Place next = place();
+    while (pair < n) {
+        const Place at = next;
+        uint4 v[CP_LOADS];
+#pragma unroll
+        for (int i = 0; i < CP_LOADS; ++i)
+            if (o + i * CP_THREADS * 16 < at.bytes) v[i] = *reinterpret_cast<const uint4*>(at.x + o + i * CP_THREADS * 16);
+        piece += step_piece;
+        unsigned carry = piece >= pieces ? 1 : 0;
+        if (carry) piece -= pieces;
+        layer += step_layer + carry;
+        carry = layer >= layers ? 1 : 0;
+        if (carry) layer -= layers;
+        pair += step_pair + carry;
+        next = place();
+#pragma unroll
+        for (int i = 0; i < CP_LOADS; ++i)
+            if (o + i * CP_THREADS * 16 < at.bytes) *reinterpret_cast<uint4*>(at.y + o + i * CP_THREADS * 16) = v[i];
     }
 }
 
@@ -400,7 +427,7 @@ CopyJob job_of(const PagesDev& p) {
 }
 unsigned copy_grid(const CopyJob& j, long long most, int num_sms) {
     const long long units = most * j.n_layers * 2 * ((j.page_bytes + CP_PIECE - 1) / CP_PIECE + (j.scale_bytes + CP_PIECE - 1) / CP_PIECE);
-    return static_cast<unsigned>(units < 1 ? 1 : units < 8LL * num_sms ? units : 8LL * num_sms);
+    return static_cast<unsigned>(units < 1 ? 1 : units < 16LL * num_sms ? units : 16LL * num_sms);
 }
 // `kernel` after the one before it in the stream, its start under that one's end.
 template <typename... A>
