@@ -118,6 +118,12 @@ def test_large_vocabulary(dtype):
     _check(_make([4, 3], 128256, dtype, False, [1.0, 0.0]))
 
 
+@pytest.mark.parametrize("vocab,dtype", [(50257, torch.float32), (100003, torch.bfloat16)])
+def test_large_vocabulary_of_more_sequences_than_clusters_fit(vocab, dtype):
+    _check(_make([2, 1] * 40, vocab, dtype, True, [0.9, 1.1] * 40))
+    _check(_make([2, 1] * 40, vocab, dtype, False, [0.9, 1.1] * 40))
+
+
 @pytest.mark.parametrize("rows", [[1], [0], [0, 0, 3], [1] * 40, [17, 0, 1], [64], [256], [3, 200, 2]])
 def test_rows(rows):
     _check(_make(rows, 500, torch.float32, True, [0.8] * len(rows), spread=0.3))

@@ -289,6 +289,21 @@ def test_copy_between_pools(dtype, ps, heads, dim):
     assert all(torch.equal(x[0], x[1]) for c in a.caches for x in _raw(c))
 
 
+@pytest.mark.parametrize("layers,dtype", [(1, torch.bfloat16), (3, torch.int8), (7, torch.float8_e4m3fn)])
+def test_more_pages_to_copy_than_run_at_once(layers, dtype):
+    a, _ = _pages(1, 1, 3000, 16, layers, 1, 64, dtype, 1)
+    b, _ = _pages(1, 1, 3500, 16, layers, 1, 64, dtype, 2)
+    g = torch.Generator().manual_seed(5)
+    src, dst = torch.randint(-1, 3000, (3400,), generator=g, dtype=torch.int32), torch.randperm(3500, generator=g)[:3400].to(torch.int32)
+    want = [[w.clone() for w in _raw(c)] for c in b.caches]
+    ok = src >= 0
+    for ca, ws in zip(a.caches, want):
+        for w, x in zip(ws, _raw(ca)):
+            w[dst[ok].long().to(DEV)] = x[src[ok].long().to(DEV)]
+    vb.kv_copy(a.caches, b.caches, src.to(DEV), dst.to(DEV))
+    assert all(torch.equal(x, y) for c, ws in zip(b.caches, want) for x, y in zip(_raw(c), ws))
+
+
 def test_pools_beyond_four_gigabytes():
     ps, heads, dim, n = 256, 8, 128, 9000  # 4.7 GB per pool
     k = torch.zeros(n, heads, ps, dim, dtype=torch.bfloat16, device=DEV)
