@@ -12,9 +12,14 @@
 // draft_verify_kernel, a cluster per sequence, bound by issue and the fp64 pipe where it draws (the same call: 42 us, fp64 pipe a third busy, 1.95 of 4
 // instructions a clock), by a chain of reads and barriers for small calls (9 us): joins these, accepts what is clear at fp32's error, decides the rows next to the border from
 // sums in 64 bits, and draws by sums in 64 bits: over CTAs, warps, parts of a warp's share, steps, lanes and entries, at each level the last part that begins at or before
-// the drawn point and is not empty.
+// the drawn point and is not empty.  max(0, p - q) needs both rows' totals, which the pass over them yields only at its end: it adds up p and q over the entries
+// with p > q as fp32 sees it, and beside them a bound of what the entries near p = q may be worth.  Where the drawn point is not farther than that from the
+// borders of its token, a second pass adds up max(0, p - q) itself (logits of 128256 entries, the draft's 0.6 away: no draw of 2560, 0.1 away: 6 in fp32, 0.01
+// away: 300, within 0.001: all).
 #include "common.cuh"
 #include "kernels.h"
+
+#include <type_traits>
 
 namespace vl {
 
@@ -245,11 +250,11 @@ struct Exp64 {
 
 // What is drawn from: weights of a row's entries.
 struct Weights {
-    int kind;       // 0: p; 1: p without token x; 2: max(0, p - q)
+    int kind;       // 0: p; 1: p without token x; 2: max(0, p - q); 3: the same, from the totals of a pass of kind 2
     int x;
     float pm, qm;   // the rows' maxima
     double ps, qs;  // and -1 times these
-    double a, b;    // kind 2: a e_p - b e_q, a = sum e_q, b = sum e_p
+    double a, b;    // kinds 2 and 3: a e_p - b e_q, a = sum e_q, b = sum e_p
 };
 
 __device__ __forceinline__ double warp_sum64(double v) {
@@ -263,6 +268,12 @@ __device__ __forceinline__ double load_cluster64(uint32_t addr) {
     return v;
 }
 
+__device__ __forceinline__ float load_cluster32(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
 template <typename T>
 __device__ __forceinline__ void weights_of(const Row<T>& rp, const Row<T>& rq, const Exp64& ex, const Weights& w, int j0, double (&v)[Row<T>::E]) {
     constexpr int E = Row<T>::E;
@@ -273,7 +284,7 @@ __device__ __forceinline__ void weights_of(const Row<T>& rp, const Row<T>& rq, c
 #pragma unroll
         for (int i = 0; i < E; ++i)
             if (j0 + i == w.x) v[i] = 0.0;
-    } else if (w.kind == 2) {
+    } else if (w.kind >= 2) {
         const uint4 g = rq.load(j0);
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = fmax(0.0, __dsub_rn(__dmul_rn(w.a, v[i]), __dmul_rn(w.b, ex(rq.get(g, i), w.qm, w.qs))));  // (no fma: 0 where p = q)
@@ -285,6 +296,8 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     constexpr int E = Row<T>::E;
     __shared__ double warp_tot[4][DV_WARPS];
     __shared__ double cta_tot[2][4];  // used in turn
+    __shared__ float warp_near[DV_WARPS], cta_near[2];
+    __shared__ float sm_sure;  // not 0: the token drawn is the right one
     __shared__ double part_tot[DV_WARPS];
     __shared__ float sm_pm[kDraftMaxRows], sm_ps[kDraftMaxRows], sm_qm[kDraftMaxRows], sm_qs[kDraftMaxRows];
     __shared__ int sm_code[kDraftMaxRows], sm_arg[kDraftMaxRows];
@@ -389,6 +402,8 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     }
     __syncthreads();
 
+    int stop = 0;  // row that is drawn from, once it is known
+
     // ---- sums in 64 bits over the cluster
     const int blocks = (p.vocab + E - 1) / E + 1;  // of any row, whatever its alignment
     const int per_cta = (blocks + ranks - 1) / ranks, per_warp = (per_cta + DV_WARPS - 1) / DV_WARPS;
@@ -396,12 +411,61 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     const int wb1 = min(min(wb0 + per_warp, (rank + 1) * per_cta), blocks);
     int turn = 0;
     // One pass over row i in 64 bits.  Per warp, per CTA and over the cluster: 0 = sum of e_p (without token x for kind 1); for kind 2 that and 1 = sum of e_q
-    // over the entries with p <= q, 2 and 3 the same over those with p > q, as fp32 sees it (from differences to the largest logits: it errs only where p and q
-    // agree to about 10^-6 times 1 - log p).
+    // over the entries with p <= q, 2 and 3 the same over those with p > q, as fp32 sees it (from differences to the largest logits).
+    //
+    // `err` bounds what that may be wrong by, of all parts together.  log2 p = (l - max) c - log2(sum): the difference, the product and the logarithm
+    // are each rounded by at most 2^-23 of log2 p (c's own error is common to p and q), those of p and q together by less than 6e-7 |log2 p|; with both sums right
+    // to 2.5e-6 of their ratio, which the pass itself shows, an entry is on the wrong side only where fp32 sees p and q within 4e-6 + 6e-7 |log2 p| of one another, and |p - q| is
+    // at most that times p.
     Weights w;
     double total[4];  // of the row: 0 sum of e_p, 1 of e_q, 2 and 3 over p > q
     double cta_part = 0.0;  // lane 4 r + i: sum i of CTA r
-    auto pass = [&](int i, int kind, int x) {
+    double err = 0.0;
+    // joins the threads' sums v; bounded: and near, the sum of p times its distance from q, into err
+    auto join = [&](const double (&v)[4], bool bounded, float near) {
+        __syncthreads();  // the sums of an earlier pass have been read
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const double sum = warp_sum64(v[q]);
+            if (lane == 0) warp_tot[q][warp] = sum;
+        }
+        if (bounded) {
+            near = warp_sum(near);
+            if (lane == 0) warp_near[warp] = near;
+        }
+        __syncthreads();
+        turn ^= 1;
+        if (warp < 4) {  // one sum each; the order is the same everywhere
+            double sum = lane < DV_WARPS ? warp_tot[warp][lane] : 0.0;
+            sum = warp_sum64(sum);
+            if (lane == 0) cta_tot[turn][warp] = sum;
+        } else if (warp == 4 && bounded) {
+            const float sum = warp_sum(lane < DV_WARPS ? warp_near[lane] : 0.f);
+            if (lane == 0) cta_near[turn] = sum;
+        }
+        if (ranks > 1) {
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+        cta_part = 0.0;
+        if (lane < 4 * ranks) cta_part = ranks > 1 ? load_cluster64(map_to_cta(smem_u32(&cta_tot[turn][lane & 3]), lane >> 2)) : cta_tot[turn][lane];
+        float of_cta = 0.f;
+        if (bounded && lane < ranks) of_cta = ranks > 1 ? load_cluster32(map_to_cta(smem_u32(&cta_near[turn]), lane)) : cta_near[turn];
+        err = bounded ? warp_sum(of_cta) : 0.f;
+        double sum = cta_part;
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) total[q] = __shfl_sync(0xFFFFFFFFu, sum, q);
+        total[0] += total[2];
+        total[1] += total[3];
+    };
+    // TWO: kind 2, whose loop is compiled by itself (64 sequences over 128256 entries: 74 us for the call, 83 with one loop for all kinds).
+    auto pass_as = [&](auto two, int i, int kind, int x) {
+        constexpr bool TWO = decltype(two)::value;
         const Row<T> rp(p.target, p.target_stride, s.row0 + i, p.vocab), rq(p.draft ? p.draft : p.target, p.draft ? p.draft_stride : p.target_stride, s.row0 + i, p.vocab);
         w.kind = kind;
         w.x = x;
@@ -410,12 +474,12 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
         w.ps = -static_cast<double>(w.pm);
         w.qs = -static_cast<double>(w.qm);
         const float kp = -log2f(sm_ps[i]), kq = -log2f(sm_qs[i]);
-        double v[4] = {0.0, 0.0, 0.0, 0.0};
+        double v[4] = {0.0, 0.0, 0.0, 0.0}, near = 0.0;
         // blocks are fetched two steps ahead
         auto fetch = [&](int k, uint4& f, uint4& g) {
             const int j0 = k < wb1 ? k * E - rp.off : p.vocab;
             f = rp.load(j0);
-            if (kind == 2) g = rq.load(j0);
+            if (TWO) g = rq.load(j0);
         };
         uint4 f0, f1, g0 = make_uint4(0u, 0u, 0u, 0u), g1 = g0;
         fetch(wb0 + lane, f0, g0);
@@ -429,11 +493,13 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
             for (int e = 0; e < E; ++e) {
                 const float lp = rp.get(f, e);
                 double ep = ex(lp, w.pm, w.ps);
-                if (kind == 1 && k * E - rp.off + e == x) ep = 0.0;
-                if (kind == 2) {
+                if (!TWO && kind == 1 && k * E - rp.off + e == x) ep = 0.0;
+                if (TWO) {
                     const float lq = rq.get(g, e);
                     const double eq = ex(lq, w.qm, w.qs);
-                    if (fmaf(lp - w.pm, c, kp) > fmaf(lq - w.qm, c, kq)) {
+                    const float log_p = fmaf(lp - w.pm, c, kp), diff = log_p - fmaf(lq - w.qm, c, kq), eps = fmaf(-6e-7f, log_p, 4e-6f);
+                    if (fabsf(diff) < eps) near += ep * static_cast<double>(eps);
+                    if (diff > 0.f) {
                         v[2] += ep;
                         v[3] += eq;
                     } else {
@@ -445,43 +511,38 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
                 }
             }
         }
-        __syncthreads();  // the sums of an earlier pass have been read
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const double sum = warp_sum64(v[q]);
-            if (lane == 0) warp_tot[q][warp] = sum;
-        }
-        __syncthreads();
-        turn ^= 1;
-        if (warp < 4) {  // one sum each; the order is the same everywhere
-            double sum = lane < DV_WARPS ? warp_tot[warp][lane] : 0.0;
-            sum = warp_sum64(sum);
-            if (lane == 0) cta_tot[turn][warp] = sum;
-        }
-        if (ranks > 1) {
-            __syncwarp();
-            cluster_arrive();
-            cluster_wait();
-        } else {
-            __syncthreads();
-        }
-        cta_part = 0.0;
-        if (lane < 4 * ranks) cta_part = ranks > 1 ? load_cluster64(map_to_cta(smem_u32(&cta_tot[turn][lane & 3]), lane >> 2)) : cta_tot[turn][lane];
-        double sum = cta_part;
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) total[q] = __shfl_sync(0xFFFFFFFFu, sum, q);
-        total[0] += total[2];
-        total[1] += total[3];
+        // (up to float, and not to 0 from above it)
+        join(v, TWO, near > 0.0 ? fmaxf(__double2float_ru(near), 1e-37f) : 0.f);
         w.a = total[1];
         w.b = total[0];
+        if (TWO) {
+            // (a p in units of a e_p; 2^x - 1 is less than 0.75 x up to x = 0.2, and where 4e-6 + 6e-7 |log2 p| is more e_p is 0)
+            const double of_p = total[1] * static_cast<double>(sm_ps[i]), of_q = total[0] * static_cast<double>(sm_qs[i]);
+            err = fabs(of_p - of_q) <= 2.5e-6 * of_q ? 0.75 * total[1] * err : INFINITY;
+        }
+    };
+    auto pass = [&](int i, int kind, int x) {
+        if (kind == 2) pass_as(std::true_type(), i, 2, x);
+        else pass_as(std::false_type(), i, kind, x);
+    };
+    // After a pass of kind 2: the sums of max(0, p - q), entry by entry from its totals.
+    auto exact_pass = [&] {
+        const Row<T> rp(p.target, p.target_stride, s.row0 + stop, p.vocab), rq(p.draft, p.draft_stride, s.row0 + stop, p.vocab);
+        w.kind = 3;
+        double v[4] = {0.0, 0.0, 0.0, 0.0};
+        for (int k = wb0 + lane; k < wb1; k += 32) {
+            double x[E];
+            weights_of<T>(rp, rq, ex, w, k * E - rp.off, x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[0] += x[e];
+        }
+        join(v, false, 0.f);
     };
     // the weight of a part of the row from its four sums
     auto weight = [&](double e, double pa, double qa) { return w.kind == 2 ? fmax(0.0, __dsub_rn(__dmul_rn(w.a, pa), __dmul_rn(w.b, qa))) : e; };
 
     // ---- how many are accepted
-    int stop = 0, code = 4;
+    int code = 4;
     bool passed = false;  // a pass over row `stop` has been made
     for (; stop < s.n; ++stop) {
         code = sm_code[stop];
@@ -540,40 +601,43 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     const Row<T> rp(p.target, p.target_stride, s.row0 + stop, p.vocab), rq(p.draft ? p.draft : p.target, p.draft ? p.draft_stride : p.target_stride, s.row0 + stop, p.vocab);
     if (!passed) pass(stop, code == 4 ? 0 : p.draft ? 2 : 1, code == 4 ? -1 : __ldg(p.tokens + s.row0 + stop + 1));
     double all = weight(total[0], total[2], total[3]);
+    if (err > 0.0 && !(all > 2.0 * p.vocab * err)) {  // as good as every point would be too near a border
+        exact_pass();
+        all = total[0];
+    }
     if (!(all > 0.0) && w.kind != 0) {  // p nowhere above q (they are the same and the number was 1): drawn from p
         pass(stop, 0, -1);
         all = total[0];
     }
-    const double u = fmin(fmax(static_cast<double>(__ldg(p.sample_u + b)), 0.0), 1.0), point = u * all;
-    // the last CTA that begins at or before the point and is not empty
-    int owner = 0;
-    double before = 0.0, base = 0.0;
-    for (int r = 0; r < ranks; ++r) {
-        const double v = weight(__shfl_sync(0xFFFFFFFFu, cta_part, 4 * r), __shfl_sync(0xFFFFFFFFu, cta_part, 4 * r + 2), __shfl_sync(0xFFFFFFFFu, cta_part, 4 * r + 3));
-        if (v > 0.0 && before <= point) {
-            owner = r;
-            base = before;
-        }
-        before += v;
-    }
-    if (owner == rank) {
-        int ow = 0;
-        double at = base, start = base;
-        const double mine = lane < DV_WARPS ? weight(warp_tot[0][lane], warp_tot[2][lane], warp_tot[3][lane]) : 0.0;
-        for (int k = 0; k < DV_WARPS; ++k) {
-            const double v = __shfl_sync(0xFFFFFFFFu, mine, k);
-            if (v > 0.0 && at <= point) {
-                ow = k;
-                start = at;
+    const double u = fmin(fmax(static_cast<double>(__ldg(p.sample_u + b)), 0.0), 1.0);
+    for (;;) {  // a second time where the first is not sure
+        const double point = u * all;
+        // the last CTA that begins at or before the point and is not empty
+        int owner = 0;
+        double before = 0.0, base = 0.0;
+        for (int r = 0; r < ranks; ++r) {
+            const double v = weight(__shfl_sync(0xFFFFFFFFu, cta_part, 4 * r), __shfl_sync(0xFFFFFFFFu, cta_part, 4 * r + 2), __shfl_sync(0xFFFFFFFFu, cta_part, 4 * r + 3));
+            if (v > 0.0 && before <= point) {
+                owner = r;
+                base = before;
             }
-            at += v;
+            before += v;
         }
-        // that warp's blocks again, dealt over all warps in whole steps of 32, and the one with the point
-        const int o0 = rank * per_cta + ow * per_warp, o1 = min(min(o0 + per_warp, (rank + 1) * per_cta), blocks);
-        const int per_part = (o1 - o0 + DV_WARPS * 32 - 1) / (DV_WARPS * 32) * 32, k_first = o0 + warp * per_part, k_last = min(k_first + per_part, o1);
-        // a warp's sums can come out above 0 by rounding where its entries are all 0 (p = q there to 10^-16): then one of p's
-        for (int again = 0; again < 2; ++again) {
-            if (again) w.kind = 0;
+        if (owner == rank) {
+            int ow = 0;
+            double at = base, start = base;
+            const double mine = lane < DV_WARPS ? weight(warp_tot[0][lane], warp_tot[2][lane], warp_tot[3][lane]) : 0.0;
+            for (int k = 0; k < DV_WARPS; ++k) {
+                const double v = __shfl_sync(0xFFFFFFFFu, mine, k);
+                if (v > 0.0 && at <= point) {
+                    ow = k;
+                    start = at;
+                }
+                at += v;
+            }
+            // that warp's blocks again, dealt over all warps in whole steps of 32, and the one with the point
+            const int o0 = rank * per_cta + ow * per_warp, o1 = min(min(o0 + per_warp, (rank + 1) * per_cta), blocks);
+            const int per_part = (o1 - o0 + DV_WARPS * 32 - 1) / (DV_WARPS * 32) * 32, k_first = o0 + warp * per_part, k_last = min(k_first + per_part, o1);
             double x[E], sum = 0.0;
             auto step = [&](int k) {  // x = the weights of block k
                 double v = 0.0;
@@ -586,23 +650,25 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
             };
             for (int k0 = k_first; k0 < k_last; k0 += 32) sum += step(k0 + lane);
             const double part = warp_sum64(sum);
-            if (again) __syncthreads();  // (the sums of the first try have been read)
             if (lane == 0) part_tot[warp] = part;
+            if (tid == 0) sm_sure = 0.f;
             __syncthreads();
+            // (none where the warp's share came out above 0 by what fp32 mistook: then it is not sure)
             int op = -1;
-            double at = start, run = start;
-            const double mine = lane < DV_WARPS ? part_tot[lane] : 0.0;
+            double run = start;
+            at = start;
+            const double parts = lane < DV_WARPS ? part_tot[lane] : 0.0;
             for (int k = 0; k < DV_WARPS; ++k) {
-                const double v = __shfl_sync(0xFFFFFFFFu, mine, k);
+                const double v = __shfl_sync(0xFFFFFFFFu, parts, k);
                 if (v > 0.0 && at <= point) {
                     op = k;
                     run = at;
                 }
                 at += v;
             }
-            if (op < 0) continue;
             if (warp == op) {
                 int token = -1;
+                double begin_of = 0.0, size_of = 0.0;
                 for (int k0 = k_first; k0 < k_last; k0 += 32) {
                     const int k = k0 + lane;
                     if (per_part > 32) sum = step(k);  // (else it is still there)
@@ -616,25 +682,49 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
                     const unsigned who = __ballot_sync(0xFFFFFFFFu, sum > 0.0 && begin <= point);
                     if (who) {
                         int tok = -1;
-                        double r = begin;
+                        double r = begin, at_tok = 0.0, of_tok = 0.0;
 #pragma unroll
                         for (int e = 0; e < E; ++e) {
-                            if (x[e] > 0.0 && r <= point) tok = k * E - rp.off + e;
+                            if (x[e] > 0.0 && r <= point) {
+                                tok = k * E - rp.off + e;
+                                at_tok = r;
+                                of_tok = x[e];
+                            }
                             r += x[e];
                         }
-                        token = __shfl_sync(0xFFFFFFFFu, tok, 31 - __clz(who));
+                        const int from = 31 - __clz(who);
+                        token = __shfl_sync(0xFFFFFFFFu, tok, from);
+                        begin_of = __shfl_sync(0xFFFFFFFFu, at_tok, from);
+                        size_of = __shfl_sync(0xFFFFFFFFu, of_tok, from);
                     }
                     run += __shfl_sync(0xFFFFFFFFu, incl, 31);
                 }
-                if (lane == 0) {
+                // the point and where the token begins are off by at most err each
+                const bool sure = err == 0.0 || (begin_of + 2.0 * err <= point && point + 2.0 * err < begin_of + size_of);
+                if (lane == 0 && sure) {
+                    sm_sure = 1.f;
                     p.out_tokens[s.row0 + stop] = token;
                     if (p.logp) p.logp[s.row0 + stop] = token < 0 ? 0.f : static_cast<float>(kLn2) * ((rp.entry(token) - w.pm) * c - log2f(sm_ps[stop]));
                 }
             }
-            break;
         }
+        if (err == 0.0) break;
+        __syncwarp();
+        bool sure;
+        if (ranks > 1) {
+            cluster_arrive();
+            cluster_wait();
+            sure = load_cluster32(map_to_cta(smem_u32(&sm_sure), owner)) != 0.f;
+        } else {
+            __syncthreads();
+            sure = sm_sure != 0.f;
+        }
+        if (sure) break;
+        exact_pass();
+        all = total[0];
     }
     if (ranks > 1) {
+        __syncwarp();
         cluster_arrive();
         cluster_wait();
     }
