@@ -212,10 +212,12 @@ int verillm_decode_commit_paged(verillm_model *model, const int32_t *tokens, con
 
 /* The trace of a prover that keeps its projections in 4 bits.
  *  verillm_quantise_w4: makes 4-bit copies of the handle's projections with one scale per `group` inputs (32, 64 or 128; verillm_w4_quantise), beside
- *    the bf16 ones that the verifier uses, and one layer's worth of bf16 scratch; to be called again after weights were loaded anew.  Synchronises the stream.
+ *    the bf16 ones that the verifier uses, and one layer's worth of bf16 scratch; to be called again after weights were loaded anew, which drops the copies, as a call does that
+ *    fails on the device.  Synchronises the stream.
  *    E_SHAPE where a projection's inputs are no multiple of group.
  *  verillm_decode_commit_w4: verillm_decode_commit (cache_dtype -1) or verillm_decode_commit_paged (VERILLM_KV_*) on them.  Decoded tokens multiply by the
- *    4-bit weights themselves (verillm_op_w4_matvec), the pass over the prompts by what they stand for, rounded to bf16. */
+ *    4-bit weights themselves (verillm_op_w4_matvec), the pass over the prompts by what they stand for, rounded to bf16.  E_INVAL without 4-bit copies of the
+ *    weights that are loaded. */
 int verillm_quantise_w4(verillm_model *model, int32_t group, void *cuda_stream);
 int verillm_decode_commit_w4(verillm_model *model, const int32_t *tokens, const int32_t *cu_seqlens, int32_t batch,
                              int32_t n_prefill, const int32_t *check_seq, const int32_t *check_pos, int32_t n_check,

@@ -125,9 +125,11 @@ struct verillm_model {
     int* tm_claimed = nullptr;
     int n_tiles_v = 0;
     CUtensorMap t_lm, t_lm_h, t_tm_y;
-    // 4-bit weights (allocated by verillm_quantise_w4): every layer's, and one layer's as bf16 for passes over prompts
+    // 4-bit weights (allocated by verillm_quantise_w4): every layer's, empty unless they are those of the weights now loaded; and one layer's as
+    // bf16 for passes over prompts
     std::vector<LayerW4> w4;
     unsigned char* w4_mem = nullptr;
+    int w4_group = 0;  // what w4_mem is laid out for
     LayerDev w4_layer;
     DecodeState dec;
     Profile prof;
@@ -613,6 +615,7 @@ int verillm_load_layer(verillm_model* m, int32_t layer, const verillm_layer_weig
     LayerDev& L = m->layers[layer];
     const size_t d = c.d_model, e = sizeof(bf16);
     int rc;
+    m->w4.clear();  // 4-bit copies of other weights
     if ((rc = copy_in(L.attn_norm, w->attn_norm, d * e, on_device))) return rc;
     if ((rc = copy_in(L.ffn_norm, w->ffn_norm, d * e, on_device))) return rc;
     if ((rc = copy_in(L.wqkv, w->wq, m->d_q * d * e, on_device))) return rc;
@@ -1309,14 +1312,15 @@ int verillm_quantise_w4(verillm_model* m, int32_t group, void* cuda_stream) try 
             return VERILLM_E_CUDA;
         }
     }
-    if (!m->w4.empty() && m->w4[0].wqkv.group != group) {  // other sizes
+    std::vector<LayerW4> made(c.n_layers);
+    m->w4.clear();  // none, until all of them are made
+    if (m->w4_mem && m->w4_group != group) {  // other sizes
         CU_TRY(cudaDeviceSynchronize());
         cudaFree(m->w4_mem);
         m->w4_mem = nullptr;
-        m->w4.clear();
     }
     if (!m->w4_mem && (rc = dev_alloc(&m->w4_mem, at[4] * c.n_layers))) return rc;
-    std::vector<LayerW4> made(c.n_layers);
+    m->w4_group = group;
     for (int l = 0; l < c.n_layers; ++l) {
         const LayerDev& w = m->layers[l];
         const bf16* from[4] = {w.wqkv, w.wo, w.wgu, w.wd};
