@@ -970,7 +970,8 @@ def _layers(caches: Sequence[KVCache]):
 class KVPages(_Fixed):
     """Who holds which page of a model's paged cache: caches (one KVCache per layer, one geometry), page_table int32 [batch][width], kv_len int32
     [batch], refs int32 [n_pages] (table entries that name a page; 0: free).  The calls on it change these tensors and must follow one
-    another.  `alloc` makes an empty one.  Pass `status` (int32 [1], zeroed) to have device problems reported there; `check` reads it."""
+    another.  `alloc` makes an empty one.  Pass `status` (int32 [1], zeroed) to have device problems reported there; `check` reads it.  Only the tensors
+    passed in have to outlive the calls' work on the device (and captured graphs), the holder itself need not."""
 
     def __init__(self, caches: Sequence[KVCache], page_table: torch.Tensor, kv_len: torch.Tensor, refs: torch.Tensor,
                  status: Optional[torch.Tensor] = None):
@@ -993,7 +994,8 @@ class KVPages(_Fixed):
         workspace = torch.empty(int(need), dtype=torch.uint8, device=dev)
         c_struct = KVPagesC(layers, len(caches), page_table.data_ptr(), kv_len.data_ptr(), refs.data_ptr(), batch, width)
         self.__dict__.update(caches=caches, page_table=page_table, kv_len=kv_len, refs=refs, status=status, device=dev, layers=layers, batch=batch,
-                             workspace=workspace, c_struct=c_struct, _ref=C.byref(c_struct), _ws=workspace.data_ptr(), _ws_bytes=int(need), _status=_ptr(status))
+                             workspace=workspace, c_struct=c_struct, _ref=C.byref(c_struct), _ws=workspace.data_ptr(), _ws_bytes=int(need), _status=_ptr(status),
+                             _ws_stream=_raw_stream(dev.index) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream)
 
     @classmethod
     def alloc(cls, n_layers: int, batch: int, width: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
@@ -1011,11 +1013,29 @@ class KVPages(_Fixed):
             raise RuntimeError(f"cache pages: device status {int(self.status.item())}")
 
 
+def _pages_call(what: str, pages: KVPages, stream: Optional[torch.cuda.Stream], fn, *args) -> None:
+    """fn(pages, *args, workspace, its bytes, status, stream pointer).  The holder's workspace belongs to the stream it was made on and goes with the
+    holder: calls on another stream, and captured ones, allocate theirs."""
+    if stream is None and _raw_stream is not None and torch.cuda.current_device() == pages.device.index:
+        st = _raw_stream(pages.device.index)
+        if st == pages._ws_stream and (st == 0 or not torch.cuda.is_current_stream_capturing()):  # (the default stream is never captured)
+            code = fn(pages._ref, *args, pages._ws, pages._ws_bytes, pages._status, st)
+            if code != 0:
+                raise VerillmError(code, what)
+            return
+
+    def call(st):
+        ws = torch.empty(pages._ws_bytes, dtype=torch.uint8, device=pages.device)
+        return fn(pages._ref, *args, ws.data_ptr(), pages._ws_bytes, pages._status, st)
+
+    _check(_launch(pages.device, stream, call), what)
+
+
 def kv_reserve(pages: KVPages, new_len: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Grows every sequence with new_len[b] > kv_len[b] (int32 [batch]) to new_len[b]: lowest free pages first, a copy of a partly filled page that
     others hold too.  Where the free pages do not suffice, that sequence and the later ones stay as they are (DEV_NO_PAGES)."""
     _vector(new_len, "new_len", pages.batch, torch.int32, pages.device.index)
-    _call("verillm_kv_reserve", pages.device, stream, lib().verillm_kv_reserve, pages._ref, new_len.data_ptr(), pages._ws, pages._ws_bytes, pages._status)
+    _pages_call("verillm_kv_reserve", pages, stream, lib().verillm_kv_reserve, new_len.data_ptr())
 
 
 def kv_free(pages: KVPages, new_len: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -1029,18 +1049,17 @@ def kv_fork(pages: KVPages, src: torch.Tensor, dst: torch.Tensor, stream: Option
     n = src.shape[0] if src.dim() == 1 else -1
     _vector(src, "src", n, torch.int32, pages.device.index)
     _vector(dst, "dst", n, torch.int32, pages.device.index)
-    _call("verillm_kv_fork", pages.device, stream, lib().verillm_kv_fork, pages._ref, src.data_ptr(), dst.data_ptr(), n, pages._ws, pages._ws_bytes,
-          pages._status)
+    _pages_call("verillm_kv_fork", pages, stream, lib().verillm_kv_fork, src.data_ptr(), dst.data_ptr(), n)
 
 
 def kv_compact(pages: KVPages, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Moves the pages in use to the front of the pools; returns their number (int32 [1], device)."""
-    def call(st):
-        used = torch.empty(1, dtype=torch.int32, device=pages.device)
-        _check(lib().verillm_kv_compact(pages._ref, used.data_ptr(), pages._ws, pages._ws_bytes, pages._status, st), "verillm_kv_compact")
-        return used
+    def make(st=None):
+        return torch.empty(1, dtype=torch.int32, device=pages.device)
 
-    return _launch(pages.device, stream, call)
+    used = make() if stream is None else _launch(pages.device, stream, make)
+    _pages_call("verillm_kv_compact", pages, stream, lib().verillm_kv_compact, used.data_ptr())
+    return used
 
 
 def kv_copy(src: Sequence[KVCache], dst: Sequence[KVCache], src_pages: torch.Tensor, dst_pages: torch.Tensor,
