@@ -326,8 +326,8 @@ __global__ void __launch_bounds__(PL_THREADS) compact_kernel(const PagesDev p, i
 }
 
 struct CopyJob {
-    const int *src, *dst, *count;  // count: on the device, or null
-    int n;                         // (count null) number of pairs
+    const int *src, *dst, *count;  // count: number of pairs, on the device, or null
+    int n;                         // number of pairs, with `count` what the lists hold at most
     int src_n_pages, dst_n_pages;
     int n_layers, page_bytes, scale_bytes;
     int* status;
@@ -340,7 +340,7 @@ struct CopyJob {
 // Pieces are counted by (pair, layer, piece of a page), the last running fastest; a CTA takes every gridDim.x-th, by additions with carries: a division of
 // 64-bit numbers in every thread costs more than the copy.  Where a piece lies is looked up while the one before it is on its way.
 __device__ __forceinline__ void copy_pages(const CopyJob& job, const PoolSet& from, const PoolSet& to) {
-    const int n = job.count ? __ldcg(job.count) : job.n;
+    const int n = job.count ? min(__ldcg(job.count), job.n) : job.n;
     const unsigned page_pieces = (job.page_bytes + CP_PIECE - 1) / CP_PIECE, scale_pieces = (job.scale_bytes + CP_PIECE - 1) / CP_PIECE;
     const unsigned pieces = 2 * (page_pieces + scale_pieces), layers = job.n_layers;
     const unsigned step_piece = gridDim.x % pieces, step_layer = gridDim.x / pieces % layers, step_pair = gridDim.x / pieces / layers;
@@ -460,7 +460,8 @@ cudaError_t launch_kv_reserve(const PagesDev& p, const PoolSet& pools, const int
     j.src = l.src;
     j.dst = l.dst;
     j.count = l.header;
-    return launch_after(move_pages_kernel, copy_grid(j, p.batch, num_sms), CP_THREADS, stream, j, pools);
+    j.n = p.batch;  // (a copy per sequence at most)
+    return launch_after(move_pages_kernel, copy_grid(j, j.n, num_sms), CP_THREADS, stream, j, pools);
 }
 
 cudaError_t launch_kv_free(const PagesDev& p, const int* new_len, cudaStream_t stream) {
@@ -485,6 +486,7 @@ cudaError_t launch_kv_compact(const PagesDev& p, const PoolSet& pools, int* n_us
     j.src = l.src;
     j.dst = l.dst;
     j.count = l.header;
+    j.n = p.n_pages;
     j.first = l.header + 1;
     j.rename = l.list;
     j.page_table = p.page_table;
@@ -492,7 +494,7 @@ cudaError_t launch_kv_compact(const PagesDev& p, const PoolSet& pools, int* n_us
     j.batch = p.batch;
     j.table_width = p.table_width;
     j.page_shift = p.page_shift;
-    return launch_after(move_pages_kernel, copy_grid(j, p.n_pages, num_sms), CP_THREADS, stream, j, pools);
+    return launch_after(move_pages_kernel, copy_grid(j, j.n, num_sms), CP_THREADS, stream, j, pools);
 }
 
 cudaError_t launch_kv_copy(const PagesDev& to, const PoolSet& dst_pools, const PoolSet& src_pools, int src_n_pages, const int* src, const int* dst, int n,
