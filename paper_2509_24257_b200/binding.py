@@ -995,7 +995,7 @@ class KVPages(_Fixed):
         c_struct = KVPagesC(layers, len(caches), page_table.data_ptr(), kv_len.data_ptr(), refs.data_ptr(), batch, width)
         self.__dict__.update(caches=caches, page_table=page_table, kv_len=kv_len, refs=refs, status=status, device=dev, layers=layers, batch=batch,
                              workspace=workspace, c_struct=c_struct, _ref=C.byref(c_struct), _ws=workspace.data_ptr(), _ws_bytes=int(need), _status=_ptr(status),
-                             _ws_stream=_raw_stream(dev.index) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream)
+                             _index=dev.index, _ws_stream=_raw_stream(dev.index) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream)
 
     @classmethod
     def alloc(cls, n_layers: int, batch: int, width: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
@@ -1016,11 +1016,12 @@ class KVPages(_Fixed):
 def _pages_call(what: str, pages: KVPages, stream: Optional[torch.cuda.Stream], fn, *args) -> None:
     """fn(pages, *args, workspace, its bytes, status, stream pointer).  The holder's workspace belongs to the stream it was made on and goes with the
     holder: calls on another stream, and captured ones, allocate theirs."""
-    if stream is None and _raw_stream is not None and torch.cuda.current_device() == pages.device.index:
-        st = _raw_stream(pages.device.index)
+    index = pages._index
+    if stream is None and _raw_stream is not None and torch.cuda.current_device() == index:
+        st = _raw_stream(index)
         if st == pages._ws_stream and (st == 0 or not torch.cuda.is_current_stream_capturing()):  # (the default stream is never captured)
             code = fn(pages._ref, *args, pages._ws, pages._ws_bytes, pages._status, st)
-            if code != 0:
+            if code:
                 raise VerillmError(code, what)
             return
 
@@ -1054,10 +1055,10 @@ def kv_fork(pages: KVPages, src: torch.Tensor, dst: torch.Tensor, stream: Option
 
 def kv_compact(pages: KVPages, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Moves the pages in use to the front of the pools; returns their number (int32 [1], device)."""
-    def make(st=None):
-        return torch.empty(1, dtype=torch.int32, device=pages.device)
-
-    used = make() if stream is None else _launch(pages.device, stream, make)
+    if stream is None:
+        used = torch.empty(1, dtype=torch.int32, device=pages.device)
+    else:
+        used = _launch(pages.device, stream, lambda st: torch.empty(1, dtype=torch.int32, device=pages.device))
     _pages_call("verillm_kv_compact", pages, stream, lib().verillm_kv_compact, used.data_ptr())
     return used
 
