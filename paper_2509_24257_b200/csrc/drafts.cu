@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(DR_THREADS) draft_rows_kernel(const DraftParam
     const int per = (r.blocks + splits - 1) / splits;
     const int b0 = blockIdx.y * per, b1 = min(b0 + per, r.blocks);
 
-    // the first blocks are on their way while the row's sequence is looked up
+    // the target's first blocks are on their way while the row's sequence is looked up; a draft row that nothing follows need not be there to be read
     uint4 raw[DR_UNROLL];
     constexpr uint32_t kNothing = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;  // -inf
     auto fetch = [&](int b) {
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(DR_THREADS) draft_rows_kernel(const DraftParam
             raw[u] = b + u * DR_THREADS < b1 ? r.load((b + u * DR_THREADS) * E - r.off) : make_uint4(kNothing, kNothing, kNothing, kNothing);
         }
     };
-    fetch(b0 + tid);
+    if (!draft) fetch(b0 + tid);
     pdl_launch_dependents();
     if (tid == 0) sm_seq = -1;
     __syncthreads();
@@ -149,6 +149,7 @@ __global__ void __launch_bounds__(DR_THREADS) draft_rows_kernel(const DraftParam
     const float temp = temp_of(p, seq);
     const bool greedy = temp == 0.f;
     if (!temp_valid(temp) || (greedy && draft)) return;
+    if (draft) fetch(b0 + tid);
     const float c = greedy ? 0.f : static_cast<float>(kLog2e / static_cast<double>(temp));
 
     float m = -INFINITY, s = 0.f;
