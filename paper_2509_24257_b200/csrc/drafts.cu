@@ -592,6 +592,7 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     }
     if (code == 3 || greedy) {
         if (ranks > 1) {  // another CTA may still read this one's sums
+            __syncwarp();  // (whole warps arrive)
             cluster_arrive();
             cluster_wait();
         }

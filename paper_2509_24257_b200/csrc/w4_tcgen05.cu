@@ -356,6 +356,7 @@ __global__ void __launch_bounds__(T_THREADS, 2) w4_tc_kernel(const __grid_consta
         }
         tc_store_y<4>(p, row0 + r, n0 + c, true, v, p.n - n0 - c);
     }
+    __syncwarp();  // (whole warps arrive)
     cluster_arrive();  // no CTA leaves while another still reads its sums
     cluster_wait();
 }
