@@ -9,17 +9,15 @@
 //
 // draft_rows_kernel, bound by HBM and by the instructions per entry: maximum and sum of exp2 in fp32 of every row that counts, divided over the vocabulary, one
 // pass (64 sequences of up to 6 rows x 128256 bf16 entries, target and draft: 37 us for 146 MB, 61 % of the copy rate).
-// draft_verify_kernel, a cluster per sequence, bound by issue and the fp64 pipe where it draws (the same call: 42 us, fp64 pipe a third busy, 1.95 of 4
+// draft_verify_kernel, a cluster per sequence, bound by issue and the fp64 pipe where it draws (the same call: 34 us, fp64 pipe a third busy, 2 of 4
 // instructions a clock), by a chain of reads and barriers for small calls (9 us): joins these, accepts what is clear at fp32's error, decides the rows next to the border from
 // sums in 64 bits, and draws by sums in 64 bits: over CTAs, warps, parts of a warp's share, steps, lanes and entries, at each level the last part that begins at or before
 // the drawn point and is not empty.  max(0, p - q) needs both rows' totals, which the pass over them yields only at its end: it adds up p and q over the entries
 // with p > q as fp32 sees it, and beside them a bound of what the entries near p = q may be worth.  Where the drawn point is not farther than that from the
 // borders of its token, a second pass adds up max(0, p - q) itself (logits of 128256 entries, the draft's 0.6 away: no draw of 2560, 0.1 away: 6 in fp32, 0.01
-// away: 300, within 0.001: all).
+// away: 300, within 0.001: all; 64 of them, one row each, 60 us without it, 91 - 96 with it).
 #include "common.cuh"
 #include "kernels.h"
-
-#include <type_traits>
 
 namespace vl {
 
@@ -275,20 +273,19 @@ __device__ __forceinline__ float load_cluster32(uint32_t addr) {
     return v;
 }
 
+// The weights of block f of a row that begins at entry j0, g: the draft's (kinds 2 and 3).
 template <typename T>
-__device__ __forceinline__ void weights_of(const Row<T>& rp, const Row<T>& rq, const Exp64& ex, const Weights& w, int j0, double (&v)[Row<T>::E]) {
+__device__ __forceinline__ void weights_of(const uint4& f, const uint4& g, const Exp64& ex, const Weights& w, int j0, double (&v)[Row<T>::E]) {
     constexpr int E = Row<T>::E;
-    const uint4 f = rp.load(j0);
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = ex(rp.get(f, i), w.pm, w.ps);
+    for (int i = 0; i < E; ++i) v[i] = ex(Row<T>::get(f, i), w.pm, w.ps);
     if (w.kind == 1) {
 #pragma unroll
         for (int i = 0; i < E; ++i)
             if (j0 + i == w.x) v[i] = 0.0;
     } else if (w.kind >= 2) {
-        const uint4 g = rq.load(j0);
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = fmax(0.0, __dsub_rn(__dmul_rn(w.a, v[i]), __dmul_rn(w.b, ex(rq.get(g, i), w.qm, w.qs))));  // (no fma: 0 where p = q)
+        for (int i = 0; i < E; ++i) v[i] = fmax(0.0, __dsub_rn(__dmul_rn(w.a, v[i]), __dmul_rn(w.b, ex(Row<T>::get(g, i), w.qm, w.qs))));  // (no fma: 0 where p = q)
     }
 }
 
@@ -411,8 +408,8 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
     const int wb0 = rank * per_cta + warp * per_warp;
     const int wb1 = min(min(wb0 + per_warp, (rank + 1) * per_cta), blocks);
     int turn = 0;
-    // One pass over row i in 64 bits.  Per warp, per CTA and over the cluster: 0 = sum of e_p (without token x for kind 1); for kind 2 that and 1 = sum of e_q
-    // over the entries with p <= q, 2 and 3 the same over those with p > q, as fp32 sees it (from differences to the largest logits).
+    // One pass over a row in 64 bits.  Per warp, per CTA and over the cluster: 0 = sum of e_p (without token x for kind 1); for kind 2 that and 1 = sum of e_q
+    // over the entries with p <= q, 2 and 3 the same over those with p > q, as fp32 sees it (from differences to the largest logits); for kind 3 the sum of max(0, p - q).
     //
     // `err` bounds what that may be wrong by, of all parts together.  log2 p = (l - max) c - log2(sum): the difference, the product and the logarithm
     // are each rounded by at most 2^-23 of log2 p (c's own error is common to p and q), those of p and q together by less than 6e-7 |log2 p|; with both sums right
@@ -464,40 +461,37 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
         total[0] += total[2];
         total[1] += total[3];
     };
-    // TWO: kind 2, whose loop is compiled by itself (64 sequences over 128256 entries: 74 us for the call, 83 with one loop for all kinds).
-    auto pass_as = [&](auto two, int i, int kind, int x) {
-        constexpr bool TWO = decltype(two)::value;
-        const Row<T> rp(p.target, p.target_stride, s.row0 + i, p.vocab), rq(p.draft ? p.draft : p.target, p.draft ? p.draft_stride : p.target_stride, s.row0 + i, p.vocab);
+    // A pass over row `stop`; one of kind 3 follows one of kind 2 over the same row.
+    auto pass = [&](int kind, int x) {
+        const Row<T> rp(p.target, p.target_stride, s.row0 + stop, p.vocab), rq(p.draft ? p.draft : p.target, p.draft ? p.draft_stride : p.target_stride, s.row0 + stop, p.vocab);
         w.kind = kind;
         w.x = x;
-        w.pm = sm_pm[i];
-        w.qm = sm_qm[i];
+        w.pm = sm_pm[stop];
+        w.qm = sm_qm[stop];
         w.ps = -static_cast<double>(w.pm);
         w.qs = -static_cast<double>(w.qm);
-        const float kp = -log2f(sm_ps[i]), kq = -log2f(sm_qs[i]);
         double v[4] = {0.0, 0.0, 0.0, 0.0}, near = 0.0;
         // blocks are fetched two steps ahead
         auto fetch = [&](int k, uint4& f, uint4& g) {
             const int j0 = k < wb1 ? k * E - rp.off : p.vocab;
             f = rp.load(j0);
-            if (TWO) g = rq.load(j0);
+            if (kind >= 2) g = rq.load(j0);
         };
         uint4 f0, f1, g0 = make_uint4(0u, 0u, 0u, 0u), g1 = g0;
         fetch(wb0 + lane, f0, g0);
         fetch(wb0 + lane + 32, f1, g1);
-        for (int k = wb0 + lane; k - lane < wb1; k += 32) {
-            const uint4 f = f0, g = g0;
-            f0 = f1;
-            g0 = g1;
-            fetch(k + 64, f1, g1);
+        // (a loop for kind 2 alone: 64 sequences over 128256 entries took 83 us with one for all kinds, 74 then)
+        if (kind == 2) {
+            const float kp = -log2f(sm_ps[stop]), kq = -log2f(sm_qs[stop]);
+            for (int k = wb0 + lane; k - lane < wb1; k += 32) {
+                const uint4 f = f0, g = g0;
+                f0 = f1;
+                g0 = g1;
+                fetch(k + 64, f1, g1);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float lp = rp.get(f, e);
-                double ep = ex(lp, w.pm, w.ps);
-                if (!TWO && kind == 1 && k * E - rp.off + e == x) ep = 0.0;
-                if (TWO) {
-                    const float lq = rq.get(g, e);
-                    const double eq = ex(lq, w.qm, w.qs);
+                for (int e = 0; e < E; ++e) {
+                    const float lp = rp.get(f, e), lq = rq.get(g, e);
+                    const double ep = ex(lp, w.pm, w.ps), eq = ex(lq, w.qm, w.qs);
                     const float log_p = fmaf(lp - w.pm, c, kp), diff = log_p - fmaf(lq - w.qm, c, kq), eps = fmaf(-6e-7f, log_p, 4e-6f);
                     if (fabsf(diff) < eps) near += ep * static_cast<double>(eps);
                     if (diff > 0.f) {
@@ -507,112 +501,106 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
                         v[0] += ep;
                         v[1] += eq;
                     }
-                } else {
-                    v[0] += ep;
                 }
+            }
+        } else {
+            for (int k = wb0 + lane; k - lane < wb1; k += 32) {
+                const uint4 f = f0, g = g0;
+                f0 = f1;
+                g0 = g1;
+                fetch(k + 64, f1, g1);
+                double x[E];
+                weights_of<T>(f, g, ex, w, k * E - rp.off, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[0] += x[e];
             }
         }
         // (up to float, and not to 0 from above it)
-        join(v, TWO, near > 0.0 ? fmaxf(__double2float_ru(near), 1e-37f) : 0.f);
-        w.a = total[1];
-        w.b = total[0];
-        if (TWO) {
+        join(v, kind == 2, near > 0.0 ? fmaxf(__double2float_ru(near), 1e-37f) : 0.f);
+        if (kind == 2) {
+            w.a = total[1];
+            w.b = total[0];
             // (a p in units of a e_p; 2^x - 1 is less than 0.75 x up to x = 0.2, and where 4e-6 + 6e-7 |log2 p| is more e_p is 0)
-            const double of_p = total[1] * static_cast<double>(sm_ps[i]), of_q = total[0] * static_cast<double>(sm_qs[i]);
+            const double of_p = total[1] * static_cast<double>(sm_ps[stop]), of_q = total[0] * static_cast<double>(sm_qs[stop]);
             err = fabs(of_p - of_q) <= 2.5e-6 * of_q ? 0.75 * total[1] * err : INFINITY;
         }
-    };
-    auto pass = [&](int i, int kind, int x) {
-        if (kind == 2) pass_as(std::true_type(), i, 2, x);
-        else pass_as(std::false_type(), i, kind, x);
-    };
-    // After a pass of kind 2: the sums of max(0, p - q), entry by entry from its totals.
-    auto exact_pass = [&] {
-        const Row<T> rp(p.target, p.target_stride, s.row0 + stop, p.vocab), rq(p.draft, p.draft_stride, s.row0 + stop, p.vocab);
-        w.kind = 3;
-        double v[4] = {0.0, 0.0, 0.0, 0.0};
-        for (int k = wb0 + lane; k < wb1; k += 32) {
-            double x[E];
-            weights_of<T>(rp, rq, ex, w, k * E - rp.off, x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[0] += x[e];
-        }
-        join(v, false, 0.f);
     };
     // the weight of a part of the row from its four sums
     auto weight = [&](double e, double pa, double qa) { return w.kind == 2 ? fmax(0.0, __dsub_rn(__dmul_rn(w.a, pa), __dmul_rn(w.b, qa))) : e; };
 
-    // ---- how many are accepted
-    int code = 4;
-    bool passed = false;  // a pass over row `stop` has been made
-    for (; stop < s.n; ++stop) {
+    // ---- how many are accepted, and the draw behind them.  There is one place for all passes, because calls find the code cold between others: one sequence
+    // after 1 ms of other kernels takes 16 - 18 us, 22 - 26 with the pass compiled where it is called.
+    int code, kind, drafted;
+    auto walk = [&] {  // to the first row that is not clearly accepted (the last one's code is never 0), and the pass that it takes
+        while (sm_code[stop] == 0) ++stop;
         code = sm_code[stop];
-        passed = false;
-        if (code == 2) {
-            const int x = __ldg(p.tokens + s.row0 + stop + 1);
-            pass(stop, p.draft ? 2 : 0, x);
-            passed = p.draft != nullptr;  // (without one the token drawn is another: a pass without x)
-            const Row<T> rp(p.target, p.target_stride, s.row0 + stop, p.vocab);
-            const double ep = ex(rp.entry(x), w.pm, w.ps), u = static_cast<double>(__ldg(p.accept_u + s.row0 + stop + 1));
-            if (p.draft) {
-                const Row<T> rq(p.draft, p.draft_stride, s.row0 + stop, p.vocab);
-                code = u * ex(rq.entry(x), w.qm, w.qs) * total[0] < ep * total[1] ? 0 : 1;
-            } else {
-                code = u * total[0] < ep ? 0 : 1;
-            }
-        }
-        if (code != 0) break;
-    }
-    // (the last row's code is never 0: stop < n)
-
-    if (rank == 0) {
-        for (int i = tid; i < s.n; i += DV_THREADS) {
-            const int row = s.row0 + i;
-            int tok = -1;
-            float lp = 0.f;
-            if (i < stop) {
-                tok = __ldg(p.tokens + row + 1);
-                if (!greedy) {
-                    const Row<T> rp(p.target, p.target_stride, row, p.vocab);
-                    lp = static_cast<float>(kLn2) * ((rp.entry(tok) - sm_pm[i]) * c - log2f(sm_ps[i]));
-                }
-            } else if (i == stop) {
-                if (code != 3 && !greedy) continue;  // written by whoever draws it
-                if (code != 3) tok = sm_arg[i];
-            }
-            p.out_tokens[row] = tok;
-            if (p.logp) p.logp[row] = lp;
-        }
-        if (tid == 0) {
-            const int emitted = code == 3 ? stop : stop + 1;
-            if (code == 3) raise(p.status, VERILLM_DEV_LOGITS);
-            p.n_emitted[b] = emitted;
-            if (p.new_len) p.new_len[b] = p.kv_len[b] - s.n + emitted;
-        }
-    }
-    if (code == 3 || greedy) {
-        if (ranks > 1) {  // another CTA may still read this one's sums
-            __syncwarp();  // (whole warps arrive)
-            cluster_arrive();
-            cluster_wait();
-        }
-        return;
-    }
-
-    // ---- the draw
-    const Row<T> rp(p.target, p.target_stride, s.row0 + stop, p.vocab), rq(p.draft ? p.draft : p.target, p.draft ? p.draft_stride : p.target_stride, s.row0 + stop, p.vocab);
-    if (!passed) pass(stop, code == 4 ? 0 : p.draft ? 2 : 1, code == 4 ? -1 : __ldg(p.tokens + s.row0 + stop + 1));
-    double all = weight(total[0], total[2], total[3]);
-    if (err > 0.0 && !(all > 2.0 * p.vocab * err)) {  // as good as every point would be too near a border
-        exact_pass();
-        all = total[0];
-    }
-    if (!(all > 0.0) && w.kind != 0) {  // p nowhere above q (they are the same and the number was 1): drawn from p
-        pass(stop, 0, -1);
-        all = total[0];
-    }
+        drafted = code == 1 || code == 2 ? __ldg(p.tokens + s.row0 + stop + 1) : -1;
+        kind = code == 4 ? 0 : p.draft ? 2 : code == 2 ? 0 : 1;
+    };
+    walk();
+    bool written = false, made = false;  // made: there is a pass to draw from already
     const double u = fmin(fmax(static_cast<double>(__ldg(p.sample_u + b)), 0.0), 1.0);
-    for (;;) {  // a second time where the first is not sure
+    for (;;) {
+        if (code != 2 && !written) {
+            written = true;
+            if (rank == 0) {
+                for (int i = tid; i < s.n; i += DV_THREADS) {
+                    const int row = s.row0 + i;
+                    int tok = -1;
+                    float lp = 0.f;
+                    if (i < stop) {
+                        tok = __ldg(p.tokens + row + 1);
+                        if (!greedy) {
+                            const Row<T> rp(p.target, p.target_stride, row, p.vocab);
+                            lp = static_cast<float>(kLn2) * ((rp.entry(tok) - sm_pm[i]) * c - log2f(sm_ps[i]));
+                        }
+                    } else if (i == stop) {
+                        if (code != 3 && !greedy) continue;  // written by whoever draws it
+                        if (code != 3) tok = sm_arg[i];
+                    }
+                    p.out_tokens[row] = tok;
+                    if (p.logp) p.logp[row] = lp;
+                }
+                if (tid == 0) {
+                    const int emitted = code == 3 ? stop : stop + 1;
+                    if (code == 3) raise(p.status, VERILLM_DEV_LOGITS);
+                    p.n_emitted[b] = emitted;
+                    if (p.new_len) p.new_len[b] = p.kv_len[b] - s.n + emitted;
+                }
+            }
+            if (code == 3 || greedy) {
+                if (ranks > 1) {  // another CTA may still read this one's sums
+                    __syncwarp();  // (whole warps arrive)
+                    cluster_arrive();
+                    cluster_wait();
+                }
+                return;
+            }
+        }
+        if (!made) pass(kind, drafted);
+        made = false;
+        const Row<T> rp(p.target, p.target_stride, s.row0 + stop, p.vocab), rq(p.draft ? p.draft : p.target, p.draft ? p.draft_stride : p.target_stride, s.row0 + stop, p.vocab);
+        if (code == 2) {  // decided from sums in 64 bits
+            const double ep = ex(rp.entry(drafted), w.pm, w.ps), au = static_cast<double>(__ldg(p.accept_u + s.row0 + stop + 1));
+            if (p.draft ? au * ex(rq.entry(drafted), w.qm, w.qs) * total[0] < ep * total[1] : au * total[0] < ep) {
+                ++stop;
+                walk();
+            } else {
+                code = 1;
+                if (p.draft) made = true;
+                else kind = 1;
+            }
+            continue;
+        }
+        const double all = weight(total[0], total[2], total[3]);
+        if (err > 0.0 && !(all > 2.0 * p.vocab * err)) {  // as good as every point would be too near a border
+            kind = 3;
+            continue;
+        }
+        if (!(all > 0.0) && kind != 0) {  // p nowhere above q (they are the same and the number was 1): drawn from p
+            kind = 0;
+            continue;
+        }
         const double point = u * all;
         // the last CTA that begins at or before the point and is not empty
         int owner = 0;
@@ -645,7 +633,8 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
                 double v = 0.0;
 #pragma unroll
                 for (int e = 0; e < E; ++e) x[e] = 0.0;
-                if (k < k_last) weights_of<T>(rp, rq, ex, w, k * E - rp.off, x);
+                const int j0 = k * E - rp.off;
+                if (k < k_last) weights_of<T>(rp.load(j0), kind >= 2 ? rq.load(j0) : make_uint4(0u, 0u, 0u, 0u), ex, w, j0, x);
 #pragma unroll
                 for (int e = 0; e < E; ++e) v += x[e];
                 return v;
@@ -722,8 +711,7 @@ __global__ void __launch_bounds__(DV_THREADS) draft_verify_kernel(const DraftPar
             sure = sm_sure != 0.f;
         }
         if (sure) break;
-        exact_pass();
-        all = total[0];
+        kind = 3;
     }
     if (ranks > 1) {
         __syncwarp();
