@@ -413,8 +413,8 @@ int verillm_w4_dequantise(const verillm_w4 *w, void *out, int64_t out_stride, in
  *  residual  optional DEVICE float32 [rows][residual_stride]; may be y itself (out_dtype F32, same stride)
  *  y         DEVICE in out_dtype, rows y_stride entries apart, not overlapping x
  *  status    optional DEVICE word, raised from 0 to VERILLM_DEV_WAIT_TIMEOUT when a wait inside the kernel gave up
- * Products are exact and sums fp32; the order of the sums follows from n, k, rows and the GPU's number of SMs.  Allocates nothing; make the first call on a device outside
- * a capture.  Errors: E_INVAL, E_SHAPE (alignment, group, rows > 65536), E_ARCH, E_CUDA. */
+ * Products are exact and sums fp32; the order of the sums follows from n, k, rows and the GPU's number of SMs.  A group's sum is formed before its scale
+ * is applied and has to be finite itself: with |x| below 1e35 it is.  Allocates nothing; make the first call on a device outside a capture.  Errors: E_INVAL, E_SHAPE (alignment, group, rows > 65536), E_ARCH, E_CUDA. */
 int verillm_op_w4_matvec(const verillm_w4 *w, const void *x, int64_t x_stride, int32_t rows, const float *residual, int64_t residual_stride,
                          void *y, int64_t y_stride, int32_t out_dtype, int32_t *status, void *cuda_stream);
 
@@ -448,14 +448,15 @@ typedef struct {
 typedef struct {
     int32_t *tokens;    /* [n_rows]: what was emitted: the accepted tokens (rows 0 .. a-1), the drawn one (row a), -1 behind it */
     int32_t *n_emitted; /* [batch] a + 1 */
-    float *logp;        /* optional [n_rows]: log p of the emitted token (0 for T = 0 and where nothing was emitted) */
+    float *logp;        /* optional [n_rows]: log p of the emitted token, of fp32 sums (within 2^-20 (1 + |log p|) + 5e-6; 0 for T = 0 and where nothing was
+                           emitted) */
     int32_t *new_len;   /* optional [batch], not kv_len itself: kv_len - n_b + n_emitted, the positions that stay (e.g. for verillm_kv_free) */
 } verillm_draft_report;
 
 /* A row that the walk reaches and that has no distribution (an entry NaN or +inf, in the draft's row too, or all -inf; a temperature out of range)
  * ends its sequence before it: n_emitted = a, nothing drawn, VERILLM_DEV_LOGITS.  A drafted token outside the vocabulary is rejected
- * (VERILLM_DEV_TOKEN_RANGE).  Decisions are those of 64-bit arithmetic (T below 2^-60: with
- * zero logits taken for 2^-127).
+ * (VERILLM_DEV_TOKEN_RANGE).  Decisions, draws from max(0, p - q) where p and q nearly agree among them, are those of 64-bit arithmetic with
+ * exponentials right to 2^-38 (T below 2^-60: with zero logits taken for 2^-127).
  *  workspace  DEVICE, 16-byte aligned, verillm_verify_drafts_workspace(n_rows) bytes; holds nothing between calls, but calls that may overlap need one each
  *  status     optional DEVICE word, raised from 0 to the first problem met, never cleared by the call
  * Allocates nothing; make the first call on a device outside a capture.  Errors: E_INVAL, E_SHAPE, E_ARCH, E_CUDA. */

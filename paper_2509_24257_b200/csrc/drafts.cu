@@ -9,7 +9,7 @@
 //
 // draft_rows_kernel, bound by HBM and by the instructions per entry: maximum and sum of exp2 in fp32 of every row that counts, divided over the vocabulary, one
 // pass (64 sequences of up to 6 rows x 128256 bf16 entries, target and draft: 37 us for 146 MB, 61 % of the copy rate).
-// draft_verify_kernel, a cluster per sequence, bound by issue and the fp64 pipe where it draws (the same call: 34 us, fp64 pipe a third busy, 2 of 4
+// draft_verify_kernel, a cluster per sequence, bound by issue and the fp64 pipe where it draws (the same call: 34 us, fp64 pipe 40 % busy, 2.1 of 4
 // instructions a clock), by a chain of reads and barriers for small calls (9 us): joins these, accepts what is clear at fp32's error, decides the rows next to the border from
 // sums in 64 bits, and draws by sums in 64 bits: over CTAs, warps, parts of a warp's share, steps, lanes and entries, at each level the last part that begins at or before
 // the drawn point and is not empty.  max(0, p - q) needs both rows' totals, which the pass over them yields only at its end: it adds up p and q over the entries
