@@ -33,3 +33,18 @@ def test_draft_logits_end_before_the_last_row(rows, vocab, dtype):
     assert vb.lib().verillm_verify_drafts(C.byref(d), C.byref(r), ws.data_ptr(), ws.numel(), status.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
     want, counts, _ = _reference(m["target"], m["tokens"].tolist(), cu, m["ua"].tolist(), m["us"].tolist(), m["draft"], temp.tolist())
     assert tokens.tolist() == want and count.tolist() == counts and int(status.item()) == 0
+
+
+@pytest.mark.parametrize("with_draft", [True, False])
+@pytest.mark.parametrize("temp", [0.0, 1.0])
+def test_a_last_row_without_a_distribution(with_draft, temp):
+    """Everything is accepted up to the buffers' last row, which nothing follows and nothing can be drawn from."""
+    m = _make([1, 4], 50000, torch.float32, with_draft, [temp] * 2)
+    m["target"][[0, 4]] = float("nan")
+    m["tokens"][2:] = m["target"][1:4].argmax(-1).to(torch.int32)
+    m["ua"].zero_()
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    rep = vb.verify_drafts(m["target"], m["tokens"], torch.tensor(m["cu"], dtype=torch.int32, device=DEV), 4, m["ua"], m["us"], draft=m["draft"],
+                           temperature=torch.full((2,), temp, device=DEV), status=status)
+    assert rep.tokens.tolist() == [-1] + m["tokens"].tolist()[2:] + [-1] and rep.n_emitted.tolist() == [0, 3]
+    assert int(status.item()) == vb.DEV_LOGITS
